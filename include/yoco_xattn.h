@@ -71,6 +71,8 @@ extern "C" {
 #define YOCO_ERR_CUDA                 (-4)  /* a CUDA call failed; see yoco_xattn_last_cuda_error */
 #define YOCO_ERR_TIMEOUT              (-5)  /* a bounded device-side wait expired               */
 #define YOCO_ERR_STATIC_SCRATCH_EXCEEDED (-6) /* yoco_xattn_decode_static: problem too large    */
+#define YOCO_ERR_BAD_PAGE             (-7)  /* a page table entry is not a page of the pool     */
+#define YOCO_ERR_HOST_MEMORY          (-8)  /* the host could not allocate a call's tables      */
 
 #define YOCO_MODE_DECODE 0   /* split-KV kernel, G*T <= 16 query rows per KV head        */
 #define YOCO_MODE_CHUNK  1   /* tensor-core (tcgen05) kernel, any T >= 1                 */
@@ -341,14 +343,114 @@ int32_t yoco_kv_append_fp8(const yoco_kv_append_shape* shape, const void* X, con
                            void* K8, void* V8, const float* k_scale_host, const float* v_scale_host,
                            const int32_t* cu_kv_host, const int32_t* kv_len_host, void* stream);
 
-/* (No counterpart in the paper.)  Synchronises `stream`; returns YOCO_OK or YOCO_ERR_TIMEOUT if an
- * append kernel on the current device gave up a wait since the last call of this function (which
+/* ---- Paged cache ----------------------------------------------------------------------------
+ * (No counterpart in the paper, whose Section 2.2 writes one K^, V^ per sequence; the rotation is the RoPE whose
+ * base its length-extension table gives per context length.)  A pool holds pages of P tokens; the rows of one page
+ * are head-major, [Hkv, P, d], and a device table names the pages of every sequence:
+ *     row(page, c, slot) = page * page_rows + c * P + slot
+ *     key j of sequence i, head c:  row(page_table[i * table_stride + j / P], c, j % P)
+ * Sequences grow by appending page numbers, and may share pages of a common prefix.  Two element formats:
+ *   bf16   K_pages, V_pages: d bf16 a row (d = 64 or 128)
+ *   4-bit  K4, V4: d/2 bytes a row, channel 2e in the low nibble of byte e, 2e + 1 in the high one (d = 128);
+ *          K_scale, V_scale: d/32 fp16 a row.  The value of a channel is (code - 8) * scale of its 32 channels,
+ *          codes 1 .. 15 (0 reads as -8).  4.5 bits a value.  A V scale must stay below 448 in magnitude (append
+ *          writes no larger one).
+ * Pools start on 16-byte boundaries (scales too).  Pool, table, Q and O are device memory of the current device.
+ *
+ * Table entries are read on the device, only those that hold a key of the call.  One outside [0, num_pages) is
+ * never followed: attention and gather read zeros in its place, append stores nothing for it, and the call's status
+ * (yoco_xattn_status of its workspace; yoco_kv_append_status for append and gather) becomes
+ * YOCO_ERR_BAD_PAGE, wait class YOCO_STATUS_BAD_PAGE.  Results of other sequences are not affected. */
+typedef struct yoco_paged_layout {
+    int32_t page_size;       /* P: 16, 32, 64, 128 or 256                                  */
+    int32_t num_pages;       /* pages in each pool                                         */
+    int32_t table_stride;    /* table entries per sequence, >= ceil(N_i / P)               */
+    int32_t rope_pairs;      /* 0: channels (c, c + d/2) turn together, 1: (2c, 2c + 1)    */
+    int64_t page_rows;       /* rows between two pages: >= Hkv * P, a multiple of 16; 0 -> Hkv * P.
+                                2 * Hkv * P describes a pool with K and V pages side by side.
+                                num_pages * page_rows must stay below 2^31                 */
+    const float* cos_sin;    /* device [max_pos, d] fp32, 16-byte aligned: d/2 cosines, then d/2 sines, of the angles
+                                of every position; NULL = rows are stored as given        */
+    int32_t max_pos;         /* positions in cos_sin                                       */
+} yoco_paged_layout;
+
+typedef struct yoco_paged_append_shape {
+    int32_t B;               /* sequences (<= 512)                                        */
+    int32_t Hkv;             /* KV heads                                                  */
+    int32_t d;               /* head dimension: 64 or 128 (4-bit rows: 128)               */
+    int32_t T;               /* new tokens per sequence when new_len_host is NULL         */
+    int64_t src_stride;      /* elements between two tokens of K_new (and V_new); a multiple of 8; 0 -> Hkv * d */
+} yoco_paged_append_shape;
+
+/* Stores the rows of the new tokens at positions [N_i - n_i, N_i) of every sequence, n_i = new_len_host[i] (host [B],
+ * may be 0) or shape->T.  K_new, V_new: bf16, the tokens of all sequences one after the other (no padding between
+ * sequences), heads consecutive inside a token: usually two slices of one projection's output.  With layout->cos_sin
+ * every key is first turned by the angles a of its position: a pair becomes (x1 cos a - x2 sin a, x2 cos a + x1 sin a),
+ * each of the three operations rounded to fp32.  bf16 rows are rounded once, from that.  kv_len_host: host
+ * [B], N_i including the new tokens.  Other rows of the pools are not touched.  Two tokens of one call must
+ * not land in the same slot. */
+int32_t yoco_paged_append(const yoco_paged_append_shape* shape, const yoco_paged_layout* layout, const void* K_new,
+                          const void* V_new, void* K_pages, void* V_pages, const int32_t* page_table,
+                          const int32_t* new_len_host, const int32_t* kv_len_host, void* stream);
+/* The same into 4-bit pages.  Per 32 channels of a row (a key after its rotation, in fp32):
+ *     scale = fp16(min(max|x| * fp32(1/7), 448)),  code = 8 + clamp(rint(x * fp32(1 / scale)), -7, 7)
+ * and code 8 throughout where the scale is 0.  Rows should be finite: an infinity is stored as +-7 * 448, a NaN
+ * as the code 1. */
+int32_t yoco_paged_append_q4(const yoco_paged_append_shape* shape, const yoco_paged_layout* layout, const void* K_new,
+                             const void* V_new, void* K4, void* K_scale, void* V4, void* V_scale,
+                             const int32_t* page_table, const int32_t* new_len_host, const int32_t* kv_len_host,
+                             void* stream);
+
+/* Reads positions [begin_i, end_i) (host [B] each) of every sequence back as a packed, tight, head-major bf16 cache
+ * ([Hkv, end_i - begin_i, d] per sequence): what the calls over packed caches take, or what a 4-bit cache stands for
+ * (each value rounded to bf16 once).  shape: B, Hkv, d are read.  Rows are stored as they are in the pages: rotated
+ * keys stay rotated. */
+int32_t yoco_paged_gather(const yoco_paged_append_shape* shape, const yoco_paged_layout* layout, const void* K_pages,
+                          const void* V_pages, const int32_t* page_table, const int32_t* begin_host,
+                          const int32_t* end_host, void* K, void* V, void* stream);
+int32_t yoco_paged_gather_q4(const yoco_paged_append_shape* shape, const yoco_paged_layout* layout, const void* K4,
+                             const void* K_scale, const void* V4, const void* V_scale, const int32_t* page_table,
+                             const int32_t* begin_host, const int32_t* end_host, void* K, void* V, void* stream);
+
+/* Queries of one layer turned by the angles of their rows' positions N_i - T + t (the counterpart of the append's
+ * rotation; a row at a negative position, which sees no key, is copied).  Q, Q_rot [B, Hq, T, d] bf16, may be the
+ * same buffer; B <= 512. */
+int32_t yoco_rope_q(const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
+                    const int32_t* kv_len_host, void* Q_rot, void* stream);
+
+/* Attention over a paged cache.  Q, O, lse, workspace, lengths, window and the result are as for yoco_xattn_decode
+ * (G*T <= 16) and yoco_xattn_chunk (any T); shape->kv_head_stride must be 0.  Q is taken as given (see yoco_rope_q).
+ * The _q4 forms read 4-bit pages; Q is widened to fp16 for the products, |Q| < 65504.
+ * The workspace is sized by yoco_xattn_workspace_size_paged (mode: YOCO_MODE_DECODE or YOCO_MODE_CHUNK; q4: 0 or 1).
+ * A call recorded into a CUDA graph keeps kv_len as it was; the page table is read at every replay. */
+int32_t yoco_xattn_workspace_size_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout,
+                                        const int32_t* kv_len_host, int32_t sm_count, int32_t mode, int32_t q4,
+                                        size_t* bytes);
+int32_t yoco_xattn_decode_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
+                                const void* K_pages, const void* V_pages, const int32_t* page_table,
+                                const int32_t* kv_len_host, void* O, float* lse, void* workspace,
+                                size_t workspace_bytes, void* stream);
+int32_t yoco_xattn_decode_paged_q4(const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
+                                   const void* K4, const void* K_scale, const void* V4, const void* V_scale,
+                                   const int32_t* page_table, const int32_t* kv_len_host, void* O, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+int32_t yoco_xattn_chunk_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
+                               const void* K_pages, const void* V_pages, const int32_t* page_table,
+                               const int32_t* kv_len_host, void* O, float* lse, void* workspace,
+                               size_t workspace_bytes, void* stream);
+int32_t yoco_xattn_chunk_paged_q4(const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
+                                  const void* K4, const void* K_scale, const void* V4, const void* V_scale,
+                                  const int32_t* page_table, const int32_t* kv_len_host, void* O, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* (No counterpart in the paper.)  Synchronises `stream`; returns YOCO_OK, or YOCO_ERR_TIMEOUT if an
+ * append kernel on the current device gave up a wait (YOCO_ERR_BAD_PAGE: a paged append or gather met a bad page) since the last call of this function (which
  * clears the record).  The _detail form also reports which wait and which CTA (see below). */
 int32_t yoco_kv_append_status(void* stream);
 int32_t yoco_kv_append_status_detail(void* stream, int32_t* wait_class, int32_t* cta);
 
 /* (No counterpart in the paper.)  Synchronises `stream`, reads the status word that the last
- * decode/chunk call using `workspace` left, returns YOCO_OK or YOCO_ERR_TIMEOUT.  workspace = NULL
+ * decode/chunk call using `workspace` left, returns YOCO_OK, YOCO_ERR_TIMEOUT or YOCO_ERR_BAD_PAGE.  workspace = NULL
  * reads the word of the built-in buffer of yoco_xattn_decode_static on the current device. */
 int32_t yoco_xattn_status(const void* workspace, void* stream);
 
@@ -356,13 +458,14 @@ int32_t yoco_xattn_status(const void* workspace, void* stream);
  * out: the kind of wait (YOCO_WAIT_*) and the linear index of the CTA.  yoco_xattn_status_detail
  * reads the word like yoco_xattn_status and decodes it (either output may be NULL; wait_class 0
  * and cta -1 when nothing happened); yoco_xattn_decode_status_word decodes a word the caller holds
- * (pure host).  Both return YOCO_OK or YOCO_ERR_TIMEOUT. */
+ * (pure host).  Both return YOCO_OK, YOCO_ERR_TIMEOUT or YOCO_ERR_BAD_PAGE. */
 #define YOCO_WAIT_ITEM_QUEUE 1  /* decode: hand-over of the next work item inside a CTA            */
 #define YOCO_WAIT_RING_FULL  2  /* a consumer waiting for a tile copy to land                      */
 #define YOCO_WAIT_RING_EMPTY 3  /* the producer waiting for a stage to be released                 */
 #define YOCO_WAIT_TENSOR     4  /* tensor-core hand-over: scores ready, P written, product done    */
 #define YOCO_WAIT_DRAIN      5  /* on the way out: something already started did not finish        */
 #define YOCO_WAIT_MISALIGNED 6  /* shared memory not 1 KB aligned; the kernel did nothing          */
+#define YOCO_STATUS_BAD_PAGE 7  /* no wait: a page table entry outside the pool (YOCO_ERR_BAD_PAGE) */
 int32_t yoco_xattn_status_detail(const void* workspace, void* stream, int32_t* wait_class, int32_t* cta);
 int32_t yoco_xattn_decode_status_word(int32_t word, int32_t* wait_class, int32_t* cta);
 

@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libyoco_xattn.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE_TOO_SMALL, ERR_CUDA, ERR_TIMEOUT = 0, -1, -2, -3, -4, -5
 ERR_STATIC_SCRATCH_EXCEEDED = -6
+ERR_BAD_PAGE, ERR_HOST_MEMORY = -7, -8
 MODE_DECODE, MODE_CHUNK = 0, 1
 
 
@@ -29,6 +30,17 @@ class Shape(ctypes.Structure):
 class KvAppendShape(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32), ("T", ctypes.c_int32),
                 ("d_model", ctypes.c_int32), ("eps", ctypes.c_float), ("kv_head_stride", ctypes.c_int64)]
+
+
+class PagedLayout(ctypes.Structure):
+    _fields_ = [("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("table_stride", ctypes.c_int32),
+                ("rope_pairs", ctypes.c_int32), ("page_rows", ctypes.c_int64), ("cos_sin", ctypes.c_void_p),
+                ("max_pos", ctypes.c_int32)]
+
+
+class PagedAppendShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32), ("T", ctypes.c_int32),
+                ("src_stride", ctypes.c_int64)]
 
 
 class Segment(ctypes.Structure):
@@ -105,6 +117,20 @@ def lib() -> ctypes.CDLL:
         for name in ("yoco_xattn_status_detail", "yoco_xattn_decode_status_word", "yoco_kv_append_status_detail",
                      "yoco_xattn_selftest_wait_expiry"):
             getattr(L, name).restype = i32
+        lay = ctypes.POINTER(PagedLayout)
+        rows = [ctypes.POINTER(PagedAppendShape), lay]
+        L.yoco_xattn_workspace_size_paged.argtypes = [ctypes.POINTER(Shape), lay, vp, i32, i32, i32, ctypes.POINTER(sz)]
+        attend, attend_q4 = [vp] * 7 + [vp, sz, vp], [vp] * 9 + [vp, sz, vp]
+        for name, args in (("yoco_xattn_decode_paged", [ctypes.POINTER(Shape), lay] + attend),
+                           ("yoco_xattn_chunk_paged", [ctypes.POINTER(Shape), lay] + attend),
+                           ("yoco_xattn_decode_paged_q4", [ctypes.POINTER(Shape), lay] + attend_q4),
+                           ("yoco_xattn_chunk_paged_q4", [ctypes.POINTER(Shape), lay] + attend_q4),
+                           ("yoco_paged_append", rows + [vp] * 8), ("yoco_paged_append_q4", rows + [vp] * 10),
+                           ("yoco_paged_gather", rows + [vp] * 8), ("yoco_paged_gather_q4", rows + [vp] * 10),
+                           ("yoco_rope_q", [ctypes.POINTER(Shape), lay] + [vp] * 4)):
+            getattr(L, name).argtypes = args
+            getattr(L, name).restype = i32
+        L.yoco_xattn_workspace_size_paged.restype = i32
         L.yoco_xattn_profile_enable.argtypes = [i32]
         L.yoco_xattn_profile_collect.argtypes = [vp, i32, vp]
         L.yoco_xattn_strerror.argtypes = [i32]
@@ -371,6 +397,7 @@ def yoco_xattn_status(workspace, stream=None) -> int:
     return int(lib().yoco_xattn_status(_ptr(workspace), _stream_ptr(stream)))
 
 
+STATUS_BAD_PAGE = 7
 WAIT_ITEM_QUEUE, WAIT_RING_FULL, WAIT_RING_EMPTY, WAIT_TENSOR, WAIT_DRAIN, WAIT_MISALIGNED = 1, 2, 3, 4, 5, 6
 
 
@@ -421,6 +448,175 @@ def yoco_xattn_selftest_wait_expiry_fp8(shape: Shape, Q, K8, V8, k_scale, v_scal
                                                    _stream_ptr(stream))
     if rc != OK:
         raise YocoError(rc, "yoco_xattn_selftest_wait_expiry_fp8")
+
+
+# ---- paged cache -----------------------------------------------------------------------------------
+def make_paged_layout(page_size, num_pages, table_stride, page_rows=0, cos_sin=None, rope_pairs=0) -> PagedLayout:
+    """``cos_sin``: fp32 CUDA tensor [positions, d] (d/2 cosines, then d/2 sines) or None; it is kept alive by the layout."""
+    if cos_sin is not None and (str(cos_sin.dtype) != "torch.float32" or cos_sin.dim() != 2 or not cos_sin.is_contiguous()):
+        raise ValueError("cos_sin must be a contiguous fp32 tensor [positions, d]")
+    layout = PagedLayout(int(page_size), int(num_pages), int(table_stride), int(rope_pairs), int(page_rows),
+                         None if cos_sin is None else cos_sin.data_ptr(), 0 if cos_sin is None else cos_sin.shape[0])
+    layout.tensor = cos_sin
+    return layout
+
+
+# What each argument after (shape, layout) is: "q" bf16 rows [B, Hq, T, d], "g" bf16 output of a gather, "x" bf16 rows of
+# the new tokens (strided between tokens), "k" bf16 pool, "c" pool of 4-bit codes, "s" pool of their scales, "i" device
+# table of pages, "n" host int32 array or None, "l" fp32 [B, Hq, T] or None, "w" workspace bytes.
+_PAGED_ARGS = {
+    "yoco_xattn_decode_paged": "qkkinqlw", "yoco_xattn_chunk_paged": "qkkinqlw",
+    "yoco_xattn_decode_paged_q4": "qcscsinqlw", "yoco_xattn_chunk_paged_q4": "qcscsinqlw",
+    "yoco_paged_append": "xxkkinn", "yoco_paged_append_q4": "xxcscsinn",
+    "yoco_paged_gather": "kkinngg", "yoco_paged_gather_q4": "cscsinngg",
+    "yoco_rope_q": "qnq",
+}
+_PAGED_TYPES = {"q": "torch.bfloat16", "g": "torch.bfloat16", "x": "torch.bfloat16", "k": "torch.bfloat16", "c": "torch.uint8",
+                "s": "torch.float16", "i": "torch.int32", "l": "torch.float32"}
+
+
+class PreparedPagedCall:
+    """A call of one of the paged-cache functions whose arguments are checked and marshalled once; run() only
+    enqueues.  The tensors and host arrays are kept alive; host int32 arrays are read at every run(), so a serving
+    loop may advance its lengths in place."""
+
+    def __init__(self, fn_name, shape, layout, *args, stream=None):
+        import torch
+        kinds = _PAGED_ARGS[fn_name]
+        if len(args) != len(kinds):
+            raise TypeError(f"{fn_name} takes {len(kinds)} arguments after the layout, got {len(args)}")
+        self._keep = [shape, layout, stream]
+        out, device, host = [ctypes.byref(shape), ctypes.byref(layout)], torch.cuda.current_device(), []
+        for n, (kind, a) in enumerate(zip(kinds, args)):
+            if kind == "n":
+                keep, p = _host_i32(a)
+                if keep is not None and keep.size < shape.B:
+                    raise ValueError(f"{fn_name}: host array {n} has {keep.size} entries for {shape.B} sequences")
+                self._keep.append(keep)
+                host.append(keep)
+                out.append(p)
+                continue
+            if a is None and kind == "l":
+                out.append(None)
+                continue
+            if not a.is_cuda or a.device.index != device:
+                raise ValueError(f"{fn_name}: tensor {n} is on {a.device}, the current device is cuda:{device}")
+            if str(a.dtype) != _PAGED_TYPES.get(kind, str(a.dtype)):
+                raise ValueError(f"{fn_name}: tensor {n} has type {a.dtype}, not {_PAGED_TYPES[kind]}")
+            if kind not in "xkcs" and not a.is_contiguous():
+                raise ValueError(f"{fn_name}: tensor {n} must be contiguous")
+            self._keep.append(a)
+            out.append(_ptr(a))
+            if kind == "w":
+                out.append(ctypes.c_size_t(a.numel() * a.element_size()))
+        self._check_sizes(fn_name, kinds, shape, layout, args, host)
+        out.append(_stream_ptr(stream))
+        self._name, self._fn, self._args = fn_name, getattr(lib(), fn_name), tuple(out)
+
+    @staticmethod
+    def _check_sizes(fn_name, kinds, shape, layout, args, host):
+        """Every tensor holds what the call may touch (elements from its first one to the end of its storage)."""
+        P, B = layout.page_size, shape.B
+        rows = (layout.num_pages - 1) * (layout.page_rows or shape.Hkv * P) + shape.Hkv * P
+        need = {"i": B * layout.table_stride, "k": rows * shape.d, "c": rows * (shape.d // 2), "s": rows * (shape.d // 32)}
+        if "q" in kinds:
+            need["l"] = B * shape.Hq * shape.T
+            need["q"] = need["l"] * shape.d
+        elif "x" in kinds:
+            tokens = int(host[0][:B].sum()) if host[0] is not None else B * shape.T
+            need["x"] = max(0, tokens - 1) * (shape.src_stride or shape.Hkv * shape.d) + shape.Hkv * shape.d if tokens else 0
+        elif host[0] is not None and host[1] is not None:
+            need["g"] = int((host[1][:B].astype(np.int64) - host[0][:B]).sum()) * shape.Hkv * shape.d
+        cos_sin = getattr(layout, "tensor", None)
+        if cos_sin is not None and (cos_sin.shape[1] != shape.d or not cos_sin.is_cuda):
+            raise ValueError(f"{fn_name}: cos_sin is {tuple(cos_sin.shape)} on {cos_sin.device} for head dimension {shape.d}")
+        for n, (kind, a) in enumerate(zip(kinds, args)):
+            if a is not None and kind in need:
+                have = a.untyped_storage().nbytes() // a.element_size() - a.storage_offset()
+                if have < need[kind]:
+                    raise ValueError(f"{fn_name}: tensor {n} holds {have} elements, the call needs {need[kind]}")
+
+    def run(self) -> None:
+        rc = self._fn(*self._args)
+        if rc != OK:
+            raise YocoError(rc, self._name)
+
+
+def prepare_paged(fn_name, shape, layout, *args, stream=None) -> PreparedPagedCall:
+    """``fn_name(shape, layout, *args)`` with its arguments marshalled once; call .run() to enqueue it."""
+    return PreparedPagedCall(fn_name, shape, layout, *args, stream=stream)
+
+
+def yoco_xattn_workspace_size_paged(shape: Shape, layout: PagedLayout, kv_len, mode: int, q4: bool = False,
+                                    sm_count: int = 0) -> int:
+    keep, p_len = _host_i32(kv_len)
+    out = ctypes.c_size_t(0)
+    rc = lib().yoco_xattn_workspace_size_paged(ctypes.byref(shape), ctypes.byref(layout), p_len, sm_count, mode, int(q4),
+                                               ctypes.byref(out))
+    if rc != OK:
+        raise YocoError(rc, "yoco_xattn_workspace_size_paged")
+    return int(out.value)
+
+
+def yoco_xattn_decode_paged(shape: Shape, layout: PagedLayout, Q, K_pages, V_pages, page_table, kv_len, O, lse, workspace,
+                            stream=None) -> None:
+    """Enqueue attention of a few query rows (G*T <= 16) over a paged bf16 cache."""
+    prepare_paged("yoco_xattn_decode_paged", shape, layout, Q, K_pages, V_pages, page_table, kv_len, O, lse, workspace,
+                  stream=stream).run()
+
+
+def yoco_xattn_decode_paged_q4(shape: Shape, layout: PagedLayout, Q, K4, K_scale, V4, V_scale, page_table, kv_len, O, lse,
+                               workspace, stream=None) -> None:
+    """The same over 4-bit pages (codes [pages, Hkv, P, d/2] bytes, scales [pages, Hkv, P, d/32] fp16)."""
+    prepare_paged("yoco_xattn_decode_paged_q4", shape, layout, Q, K4, K_scale, V4, V_scale, page_table, kv_len, O, lse,
+                  workspace, stream=stream).run()
+
+
+def yoco_xattn_chunk_paged(shape: Shape, layout: PagedLayout, Q, K_pages, V_pages, page_table, kv_len, O, lse, workspace,
+                           stream=None) -> None:
+    """Enqueue the multi-token (tcgen05) attention over a paged bf16 cache; any T."""
+    prepare_paged("yoco_xattn_chunk_paged", shape, layout, Q, K_pages, V_pages, page_table, kv_len, O, lse, workspace,
+                  stream=stream).run()
+
+
+def yoco_xattn_chunk_paged_q4(shape: Shape, layout: PagedLayout, Q, K4, K_scale, V4, V_scale, page_table, kv_len, O, lse,
+                              workspace, stream=None) -> None:
+    """The multi-token attention over 4-bit pages; any T."""
+    prepare_paged("yoco_xattn_chunk_paged_q4", shape, layout, Q, K4, K_scale, V4, V_scale, page_table, kv_len, O, lse,
+                  workspace, stream=stream).run()
+
+
+def yoco_paged_append(shape: PagedAppendShape, layout: PagedLayout, K_new, V_new, K_pages, V_pages, page_table, new_len,
+                      kv_len, stream=None) -> None:
+    """Store the new tokens' rows (keys turned by their positions when the layout has a table) in the last
+    ``new_len[i]`` (None: T) positions of every sequence."""
+    prepare_paged("yoco_paged_append", shape, layout, K_new, V_new, K_pages, V_pages, page_table, new_len, kv_len,
+                  stream=stream).run()
+
+
+def yoco_paged_append_q4(shape: PagedAppendShape, layout: PagedLayout, K_new, V_new, K4, K_scale, V4, V_scale, page_table,
+                         new_len, kv_len, stream=None) -> None:
+    """The same into 4-bit pages."""
+    prepare_paged("yoco_paged_append_q4", shape, layout, K_new, V_new, K4, K_scale, V4, V_scale, page_table, new_len,
+                  kv_len, stream=stream).run()
+
+
+def yoco_paged_gather(shape: PagedAppendShape, layout: PagedLayout, K_pages, V_pages, page_table, begin, end, K, V,
+                      stream=None) -> None:
+    """Read positions [begin[i], end[i]) back as a packed head-major bf16 cache."""
+    prepare_paged("yoco_paged_gather", shape, layout, K_pages, V_pages, page_table, begin, end, K, V, stream=stream).run()
+
+
+def yoco_paged_gather_q4(shape: PagedAppendShape, layout: PagedLayout, K4, K_scale, V4, V_scale, page_table, begin, end, K,
+                         V, stream=None) -> None:
+    """The same from 4-bit pages: the values they stand for, rounded to bf16."""
+    prepare_paged("yoco_paged_gather_q4", shape, layout, K4, K_scale, V4, V_scale, page_table, begin, end, K, V,
+                  stream=stream).run()
+
+
+def yoco_rope_q(shape: Shape, layout: PagedLayout, Q, kv_len, Q_rot, stream=None) -> None:
+    """Turn the queries [B, Hq, T, d] by the angles of their rows' positions N_i - T + t."""
+    prepare_paged("yoco_rope_q", shape, layout, Q, kv_len, Q_rot, stream=stream).run()
 
 
 def yoco_xattn_profile_enable(max_records: int) -> None:

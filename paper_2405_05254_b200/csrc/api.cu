@@ -2,11 +2,14 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
+#include <climits>
 #include <cmath>
 #include <cstring>
 #include <list>
 #include <memory>
 #include <mutex>
+#include <new>
 
 #include "kernels.h"
 #include "plan.h"
@@ -16,6 +19,11 @@ namespace yoco {
 namespace {
 
 thread_local int32_t g_last_cuda_error = 0;
+
+// what a status word of the device means to the caller
+int32_t status_code(int32_t word) {
+    return word == kStatusOk ? YOCO_OK : (word & 0xFF) == kBadPage ? YOCO_ERR_BAD_PAGE : YOCO_ERR_TIMEOUT;
+}
 
 int32_t cuda_fail(cudaError_t e) {
     g_last_cuda_error = (int32_t)e;
@@ -32,6 +40,7 @@ constexpr int kMaxDevices = 64;
 struct DeviceState {
     bool ready = false;
     int sm_count = 0;
+    int32_t* append_status = nullptr;    // status word of the kernels that take no workspace
 };
 std::mutex g_mutex;
 DeviceState g_dev[kMaxDevices];
@@ -52,6 +61,8 @@ int32_t device_state(DeviceState** out) {
         YOCO_CUDA_TRY(chunk_pair_kernel_setup());
         YOCO_CUDA_TRY(kv_append_kernel_setup());
         YOCO_CUDA_TRY(decode_fp8_kernel_setup());
+        YOCO_CUDA_TRY(decode_q4_kernel_setup());
+        YOCO_CUDA_TRY(kv_append_status_address(&st.append_status));
         st.ready = true;
     }
     *out = &st;
@@ -61,11 +72,12 @@ int32_t device_state(DeviceState** out) {
 // ---- plan cache ---------------------------------------------------------------------------
 struct PlanKey {
     yoco_xattn_shape shape;
-    int32_t sm_count, mode, max_sub, eight_bit;
+    int32_t sm_count, mode, max_sub;
+    CacheForm form;
     std::vector<int32_t> lens, cu, key_off, totals;
     bool operator==(const PlanKey& o) const {
         return std::memcmp(&shape, &o.shape, sizeof shape) == 0 && sm_count == o.sm_count &&
-               mode == o.mode && max_sub == o.max_sub && eight_bit == o.eight_bit && lens == o.lens && cu == o.cu &&
+               mode == o.mode && max_sub == o.max_sub && form == o.form && lens == o.lens && cu == o.cu &&
                key_off == o.key_off && totals == o.totals;
     }
 };
@@ -91,14 +103,15 @@ std::vector<std::shared_ptr<const ReadyPlan>> g_captured_plans;
 // alive for the caller even if another thread evicts it from the cache meanwhile.
 int32_t cached_plan(const yoco_xattn_shape& s, const int32_t* cu, const int32_t* lens, int32_t sm_count,
                     int32_t mode, int32_t max_sub, std::shared_ptr<const ReadyPlan>& out,
-                    const int32_t* key_off = nullptr, const int32_t* totals = nullptr, bool eight_bit = false) {
+                    const int32_t* key_off = nullptr, const int32_t* totals = nullptr,
+                    const CacheForm& form = kBf16Cache) {
     PlanKey key;
     std::memset(&key.shape, 0, sizeof key.shape);
     key.shape = s;
     key.sm_count = sm_count;
     key.mode = mode;
     key.max_sub = max_sub;
-    key.eight_bit = eight_bit ? 1 : 0;
+    key.form = form;
     if (lens) key.lens.assign(lens, lens + s.B);
     if (cu) key.cu.assign(cu, cu + s.B + 1);
     if (key_off) key.key_off.assign(key_off, key_off + s.B);
@@ -113,7 +126,7 @@ int32_t cached_plan(const yoco_xattn_shape& s, const int32_t* cu, const int32_t*
             }
     }
     auto ready = std::make_shared<ReadyPlan>();
-    int32_t rc = make_plan(s, cu, lens, sm_count, mode, ready->plan, max_sub, key_off, totals, eight_bit);
+    int32_t rc = make_plan(s, cu, lens, sm_count, mode, ready->plan, max_sub, key_off, totals, form);
     if (rc != YOCO_OK) return rc;
     const Plan& plan = ready->plan;
     ready->blob.assign(kWorkspaceHeaderBytes / 4 + plan.table.size(), 0);
@@ -166,13 +179,14 @@ int32_t get_encoder(EncodeTiledFn* fn) {
 struct MapKey {
     const void* base;
     int64_t rows;
-    int32_t d, box_rows, u8;
+    int32_t row_bytes, box_rows, box_bytes, bf16;
     bool operator==(const MapKey& o) const {
-        return base == o.base && rows == o.rows && d == o.d && box_rows == o.box_rows && u8 == o.u8;
+        return base == o.base && rows == o.rows && row_bytes == o.row_bytes && box_rows == o.box_rows &&
+               box_bytes == o.box_bytes && bf16 == o.bf16;
     }
 };
 struct MapCache {
-    static constexpr int kEntries = 8;
+    static constexpr int kEntries = 16;
     MapKey key[kEntries];
     CUtensorMap map[kEntries];
     int used = 0, next = 0;
@@ -193,42 +207,48 @@ struct MapCache {
 };
 thread_local MapCache g_maps;
 
-// 2-D bf16 map over a row-major [rows, d] matrix, box {64 channels, box_rows}, 128-byte swizzle.
-int32_t make_map_2d(CUtensorMap* map, const void* base, int64_t rows, int32_t d, int32_t box_rows) {
-    const MapKey mk{base, rows, d, box_rows, 0};
+// 2-D map over a row-major matrix of `rows` rows of row_bytes bytes, as bf16 or bytes; box {box_bytes, box_rows},
+// swizzled by the box's width (128 or 64 bytes) or not at all.
+int32_t make_map(CUtensorMap* map, const void* base, int64_t rows, int32_t row_bytes, int32_t box_bytes,
+                 int32_t box_rows, bool bf16, CUtensorMapSwizzle swizzle) {
+    const MapKey mk{base, rows, row_bytes, box_rows, box_bytes, bf16 ? 1 : 0};
     if (g_maps.find(mk, map)) return YOCO_OK;
     EncodeTiledFn enc;
     int32_t rc = get_encoder(&enc);
     if (rc != YOCO_OK) return rc;
-    cuuint64_t gdim[2] = {(cuuint64_t)d, (cuuint64_t)rows};
-    cuuint64_t gstride[1] = {(cuuint64_t)d * 2};
-    cuuint32_t box[2] = {64u, (cuuint32_t)box_rows};
+    const int32_t elem = bf16 ? 2 : 1;
+    cuuint64_t gdim[2] = {(cuuint64_t)(row_bytes / elem), (cuuint64_t)rows};
+    cuuint64_t gstride[1] = {(cuuint64_t)row_bytes};
+    cuuint32_t box[2] = {(cuuint32_t)(box_bytes / elem), (cuuint32_t)box_rows};
     cuuint32_t estr[2] = {1u, 1u};
-    CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), gdim, gstride,
-                     box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    CUresult r = enc(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2,
+                     const_cast<void*>(base), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue);
     g_maps.put(mk, *map);
     return YOCO_OK;
 }
 
-// 2-D byte map over a row-major [rows, 128] matrix of FP8 values, box {128, box_rows}, 128-byte swizzle.
+// bf16 [rows, d], box {64 channels, box_rows}, 128-byte swizzle
+int32_t make_map_2d(CUtensorMap* map, const void* base, int64_t rows, int32_t d, int32_t box_rows) {
+    return make_map(map, base, rows, d * 2, 128, box_rows, true, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+// FP8 bytes [rows, 128], box {128, box_rows}, 128-byte swizzle
 int32_t make_map_2d_u8(CUtensorMap* map, const void* base, int64_t rows, int32_t box_rows) {
-    const MapKey mk{base, rows, 128, box_rows, 1};
-    if (g_maps.find(mk, map)) return YOCO_OK;
-    EncodeTiledFn enc;
-    int32_t rc = get_encoder(&enc);
-    if (rc != YOCO_OK) return rc;
-    cuuint64_t gdim[2] = {128u, (cuuint64_t)rows};
-    cuuint64_t gstride[1] = {128u};
-    cuuint32_t box[2] = {128u, (cuuint32_t)box_rows};
-    cuuint32_t estr[2] = {1u, 1u};
-    CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), gdim, gstride, box, estr,
-                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue);
-    g_maps.put(mk, *map);
-    return YOCO_OK;
+    return make_map(map, base, rows, 128, 128, box_rows, false, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+// the four maps of a 4-bit pool pair, for tiles of `tile` keys
+int32_t make_q4_maps(PagedQ4Maps* m, const void* K, const void* k_scale, const void* V, const void* v_scale,
+                     const PageMap& pages, int32_t tile) {
+    const int32_t box = std::min(1 << pages.page_shift, tile);
+    int32_t rc;
+    if ((rc = make_map(&m->k, K, pages.rows, 64, 64, box, false, CU_TENSOR_MAP_SWIZZLE_64B)) != YOCO_OK) return rc;
+    if ((rc = make_map(&m->v, V, pages.rows, 64, 64, box, false, CU_TENSOR_MAP_SWIZZLE_64B)) != YOCO_OK) return rc;
+    if ((rc = make_map(&m->k_scale, k_scale, pages.rows / 16, 128, 128, box / 16, false, CU_TENSOR_MAP_SWIZZLE_NONE)) != YOCO_OK)
+        return rc;
+    return make_map(&m->v_scale, v_scale, pages.rows / 16, 128, 128, box / 16, false, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 // per-head scales of an 8-bit cache (host pointers)
@@ -262,6 +282,13 @@ bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) &
 struct SelfTest {
     int64_t wait_limit_ns;
 };
+// a paged cache: where its rows are, and the scales of 4-bit rows (null: bf16 rows)
+struct PagedCall {
+    PageMap pages;
+    const void* k_scale;
+    const void* v_scale;
+    CacheForm form() const { return k_scale ? kPagedQ4Cache : kPagedCache; }
+};
 // where the keys of this call sit in the whole sequences (one shard of a key-range-sharded cache)
 struct ShardPos {
     const int32_t* key_offset;   // host [B]
@@ -272,7 +299,7 @@ int32_t run(const yoco_xattn_shape* shape, int32_t mode, const void* Q, const vo
             const int32_t* cu_kv_host, const int32_t* kv_len_host, void* O, float* lse,
             void* workspace, size_t workspace_bytes, void* stream_v, float* part_out = nullptr,
             const Fp8Scales* fp8 = nullptr, int32_t max_sub = kMaxSubItems, const SelfTest* selftest = nullptr,
-            const ShardPos* shard = nullptr) {
+            const ShardPos* shard = nullptr, const PagedCall* paged = nullptr) {
     // part_out != null: the result is a partial one (fp32 rows + their LSE in `lse`, no bf16 O)
     if (!shape) return YOCO_ERR_INVALID_ARG;
     int32_t rc = validate_shape(*shape, mode);
@@ -291,7 +318,7 @@ int32_t run(const yoco_xattn_shape* shape, int32_t mode, const void* Q, const vo
     std::shared_ptr<const ReadyPlan> ready;
     if ((rc = cached_plan(*shape, cu_kv_host, kv_len_host, dev->sm_count, mode, max_sub, ready,
                           shard ? shard->key_offset : nullptr, shard ? shard->kv_total : nullptr,
-                          fp8 != nullptr)) != YOCO_OK)
+                          paged ? paged->form() : fp8 ? kFp8Cache : kBf16Cache)) != YOCO_OK)
         return rc;
     const Plan& plan = ready->plan;
     if ((int64_t)workspace_bytes < plan.info.workspace_bytes) return YOCO_ERR_WORKSPACE_TOO_SMALL;
@@ -333,7 +360,16 @@ int32_t run(const yoco_xattn_shape* shape, int32_t mode, const void* Q, const vo
         timed = prof;
         if (mode == YOCO_MODE_DECODE) {
             CUtensorMap tmK, tmV;
-            if (fp8) {
+            PagedQ4Maps q4;
+            const bool four_bit = paged && paged->k_scale;
+            if (four_bit) {
+                if ((rc = make_q4_maps(&q4, K, paged->k_scale, V, paged->v_scale, paged->pages, kDecodeTileN)) != YOCO_OK)
+                    return rc;
+            } else if (paged) {
+                const int32_t box = std::min(1 << paged->pages.page_shift, kDecodeTileN);
+                if ((rc = make_map_2d(&tmK, K, paged->pages.rows, shape->d, box)) != YOCO_OK) return rc;
+                if ((rc = make_map_2d(&tmV, V, paged->pages.rows, shape->d, box)) != YOCO_OK) return rc;
+            } else if (fp8) {
                 if ((rc = make_map_2d_u8(&tmK, K, plan.kv_rows_extent, kDecodeTileN)) != YOCO_OK) return rc;
                 if ((rc = make_map_2d_u8(&tmV, V, plan.kv_rows_extent, kDecodeTileN)) != YOCO_OK) return rc;
             } else {
@@ -357,11 +393,15 @@ int32_t run(const yoco_xattn_shape* shape, int32_t mode, const void* Q, const vo
             p.force_partial = part_out ? 1 : 0;
             p.sub_items = plan.sub_items;
             p.work_counter = reinterpret_cast<int32_t*>(ws + kWorkCounterOffset);
+            if (paged) p.pages = paged->pages;
             if (selftest) {
                 p.wait_limit_ns = selftest->wait_limit_ns;
                 p.selftest_skip_loads = 1;
             }
-            if (fp8) {
+            if (four_bit) {
+                YOCO_CUDA_TRY(launch_decode_q4(p, q4, plan.info.num_groups, stream,
+                                               inline_tables ? &ready->decode_tab : nullptr));
+            } else if (fp8) {
                 DecodeFp8Params p8{};
                 p8.base = p;
                 p8.Hkv = shape->Hkv;
@@ -373,9 +413,10 @@ int32_t run(const yoco_xattn_shape* shape, int32_t mode, const void* Q, const vo
                                                 inline_tables ? &ready->decode_tab : nullptr));
             } else {
                 YOCO_CUDA_TRY(launch_decode(p, tmK, tmV, plan.info.num_groups, stream,
-                                            inline_tables ? &ready->decode_tab : nullptr));
+                                            inline_tables ? &ready->decode_tab : nullptr, paged != nullptr));
             }
         } else {
+            if (paged) return YOCO_ERR_UNSUPPORTED;
             CUtensorMap tmQ, tmK, tmV;
             const int64_t q_rows = (int64_t)shape->B * shape->Hq * shape->T;
             if ((rc = make_map_2d(&tmQ, Q, q_rows, shape->d, kChunkTileM)) != YOCO_OK) return rc;
@@ -467,6 +508,163 @@ int32_t static_scratch_address(void** out) {
     }
     *out = g_static_scratch_addr[dev];
     return YOCO_OK;
+}
+
+// ---- paged cache ---------------------------------------------------------------------------
+// Runs a call that allocates host memory (plans, tables) without letting an exception through the C boundary.
+template <class F>
+int32_t no_throw(F f) {
+    try {
+        return f();
+    } catch (const std::bad_alloc&) {
+        return YOCO_ERR_HOST_MEMORY;
+    } catch (...) {
+        return YOCO_ERR_INVALID_ARG;
+    }
+}
+
+bool valid_page_size(int32_t P) { return P == 16 || P == 32 || P == 64 || P == 128 || P == 256; }
+
+// Checks the layout against the lengths of a call (kv_len_host null: every N_i = max_kv_len) and fills the map.
+int32_t page_map(const yoco_paged_layout* layout, int32_t B, int32_t Hkv, const int32_t* kv_len_host, int32_t max_kv_len,
+                 const int32_t* page_table, PageMap* out) {
+    if (!layout) return YOCO_ERR_INVALID_ARG;
+    const yoco_paged_layout& L = *layout;
+    if (L.num_pages <= 0 || L.table_stride < 0 || L.page_rows < 0 || (L.rope_pairs != 0 && L.rope_pairs != 1) || Hkv <= 0 || B < 0)
+        return YOCO_ERR_INVALID_ARG;
+    if (!valid_page_size(L.page_size)) return YOCO_ERR_UNSUPPORTED;
+    const int64_t tight = (int64_t)Hkv * L.page_size;
+    const int64_t page_rows = L.page_rows ? L.page_rows : tight;
+    if (page_rows < tight) return YOCO_ERR_INVALID_ARG;
+    // row numbers are 32-bit, and the scale rows of a 4-bit pool are read sixteen at a time
+    if (page_rows % 16 != 0 || page_rows > (1ll << 31) / L.num_pages - 1) return YOCO_ERR_UNSUPPORTED;
+    if (!page_table || !aligned(page_table, 4)) return YOCO_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < B; ++i) {
+        const int64_t n = kv_len_host ? kv_len_host[i] : max_kv_len;
+        if (n < 0 || (n + L.page_size - 1) / L.page_size > L.table_stride) return YOCO_ERR_INVALID_ARG;
+    }
+    int shift = 4;
+    while ((1 << shift) < L.page_size) ++shift;
+    *out = PageMap{page_table, L.table_stride, shift, L.num_pages, (int32_t)page_rows, Hkv,
+                   (int32_t)((int64_t)(L.num_pages - 1) * page_rows + tight)};
+    return YOCO_OK;
+}
+
+int32_t attend_paged(int32_t mode, const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
+                     const void* K, const void* k_scale, const void* V, const void* v_scale, bool q4,
+                     const int32_t* page_table, const int32_t* kv_len_host, void* O, float* lse, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+    return no_throw([&]() -> int32_t {
+        if (!shape) return YOCO_ERR_INVALID_ARG;
+        int32_t rc = validate_shape(*shape, mode);
+        if (rc != YOCO_OK) return rc;
+        if (shape->kv_head_stride != 0) return YOCO_ERR_INVALID_ARG;
+        if (q4 && shape->d != 128) return YOCO_ERR_UNSUPPORTED;
+        if (shape->B == 0) return YOCO_OK;
+        PagedCall pc{};
+        if ((rc = page_map(layout, shape->B, shape->Hkv, kv_len_host, shape->max_kv_len, page_table, &pc.pages)) != YOCO_OK)
+            return rc;
+        if (q4 && (!k_scale || !v_scale || !aligned(k_scale, 16) || !aligned(v_scale, 16))) return YOCO_ERR_INVALID_ARG;
+        pc.k_scale = q4 ? k_scale : nullptr;
+        pc.v_scale = q4 ? v_scale : nullptr;
+        return run(shape, mode, Q, K, V, nullptr, kv_len_host, O, lse, workspace, workspace_bytes, stream, nullptr,
+                   nullptr, kMaxSubItems, nullptr, nullptr, &pc);
+    });
+}
+
+// What append, gather and rope_q share: first positions and tokens of every sequence.  begin/end: positions of
+// sequence i are [begin(i), end(i)).
+template <class Begin, class End>
+int32_t sequence_table(int32_t B, Begin begin, End end, SeqTable* tab, int64_t* tokens, int32_t* per_seq) {
+    if (B > kAppendMaxSequences) return YOCO_ERR_UNSUPPORTED;
+    std::memset(tab, 0, sizeof *tab);
+    *tokens = 0;
+    *per_seq = B > 0 ? end(0) - begin(0) : 0;
+    for (int32_t i = 0; i < B; ++i) {
+        const int64_t lo = begin(i), hi = end(i);
+        if (lo < 0 || hi < lo) return YOCO_ERR_INVALID_ARG;
+        tab->pos0[i] = (int32_t)lo;
+        tab->tok0[i] = (int32_t)*tokens;
+        *tokens += hi - lo;
+        if (*tokens >= (1ll << 31)) return YOCO_ERR_UNSUPPORTED;
+        if (hi - lo != *per_seq) *per_seq = 0;
+    }
+    tab->tok0[B] = (int32_t)*tokens;
+    return YOCO_OK;
+}
+
+int32_t check_rotation(const yoco_paged_layout& L, int64_t max_len, Rotation* rot) {
+    if (L.cos_sin) {
+        if (!aligned(L.cos_sin, 16) || L.max_pos < max_len) return YOCO_ERR_INVALID_ARG;
+        *rot = Rotation{L.cos_sin, L.rope_pairs};
+    } else {
+        *rot = Rotation{nullptr, 0};
+    }
+    return YOCO_OK;
+}
+
+int32_t paged_rows(const yoco_paged_append_shape* shape, const yoco_paged_layout* layout, bool append, bool q4,
+                   const void* k_new, const void* v_new, const void* K, const void* k_scale, const void* V,
+                   const void* v_scale, const int32_t* page_table, const int32_t* begin_host, const int32_t* end_host,
+                   const int32_t* new_len_host, void* k_out, void* v_out, void* stream) {
+    return no_throw([&]() -> int32_t {
+        if (!shape) return YOCO_ERR_INVALID_ARG;
+        const yoco_paged_append_shape& s = *shape;
+        if (s.B < 0 || s.Hkv <= 0 || s.d <= 0 || s.T < 0 || s.src_stride < 0) return YOCO_ERR_INVALID_ARG;
+        if ((s.d != 64 && s.d != 128) || (q4 && s.d != 128) || s.B > kAppendMaxSequences) return YOCO_ERR_UNSUPPORTED;
+        if (s.B == 0) return YOCO_OK;
+        if (!end_host || (!append && !begin_host)) return YOCO_ERR_INVALID_ARG;
+        PagedRowsParams p{};
+        int32_t rc = page_map(layout, s.B, s.Hkv, end_host, 0, page_table, &p.pages);
+        if (rc != YOCO_OK) return rc;
+        if (!K || !V || !aligned(K, 16) || !aligned(V, 16)) return YOCO_ERR_INVALID_ARG;
+        if (q4 && (!k_scale || !v_scale || !aligned(k_scale, 16) || !aligned(v_scale, 16))) return YOCO_ERR_INVALID_ARG;
+        if (append) {
+            if (!k_new || !v_new || !aligned(k_new, 16) || !aligned(v_new, 16)) return YOCO_ERR_INVALID_ARG;
+            p.src_stride = s.src_stride ? s.src_stride : (int64_t)s.Hkv * s.d;
+            if (p.src_stride < (int64_t)s.Hkv * s.d) return YOCO_ERR_INVALID_ARG;
+            if (p.src_stride % 8 != 0) return YOCO_ERR_UNSUPPORTED;
+            if (new_len_host)
+                for (int32_t i = 0; i < s.B; ++i)
+                    if (new_len_host[i] < 0) return YOCO_ERR_INVALID_ARG;
+        } else if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16)) {
+            return YOCO_ERR_INVALID_ARG;
+        }
+        SeqTable tab;
+        int64_t tokens = 0;
+        rc = sequence_table(
+            s.B,
+            [&](int32_t i) -> int64_t {
+                return append ? (int64_t)end_host[i] - (new_len_host ? new_len_host[i] : s.T) : begin_host[i];
+            },
+            [&](int32_t i) -> int64_t { return end_host[i]; }, &tab, &tokens, &p.tokens_per_seq);
+        if (rc != YOCO_OK) return rc;
+        // grids are counted in 32 bits
+        if (tokens * s.Hkv * (s.d / 8) >= (1ll << 37)) return YOCO_ERR_UNSUPPORTED;
+        if (append) {
+            int64_t max_len = 0;
+            for (int32_t i = 0; i < s.B; ++i) max_len = std::max<int64_t>(max_len, end_host[i]);
+            if ((rc = check_rotation(*layout, max_len, &p.rot)) != YOCO_OK) return rc;
+        }
+        if (tokens == 0) return YOCO_OK;
+        DeviceState* dev = nullptr;
+        if ((rc = device_state(&dev)) != YOCO_OK) return rc;
+        p.k_src = static_cast<const __nv_bfloat16*>(k_new);
+        p.v_src = static_cast<const __nv_bfloat16*>(v_new);
+        p.k_pool = const_cast<void*>(K);
+        p.v_pool = const_cast<void*>(V);
+        p.k_scale = static_cast<__half*>(const_cast<void*>(k_scale));
+        p.v_scale = static_cast<__half*>(const_cast<void*>(v_scale));
+        p.k_out = static_cast<__nv_bfloat16*>(k_out);
+        p.v_out = static_cast<__nv_bfloat16*>(v_out);
+        p.status = dev->append_status;
+        p.B = s.B;
+        p.d = s.d;
+        p.tokens = (int32_t)tokens;
+        cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+        YOCO_CUDA_TRY(append ? launch_paged_append(p, tab, q4, st) : launch_paged_gather(p, tab, q4, st));
+        return YOCO_OK;
+    });
 }
 
 }  // namespace
@@ -681,7 +879,7 @@ int32_t yoco_xattn_workspace_size_chunk_fp8(const yoco_xattn_shape* shape, const
     }
     Plan plan;
     int32_t rc = make_plan(*shape, nullptr, kv_len_host, sm_count, YOCO_MODE_CHUNK, plan, kMaxSubItems, nullptr, nullptr,
-                           true);
+                           kFp8Cache);
     if (rc != YOCO_OK) return rc;
     *bytes = (size_t)plan.info.workspace_bytes;
     return YOCO_OK;
@@ -778,10 +976,123 @@ int32_t yoco_kv_append_fp8(const yoco_kv_append_shape* shape, const void* X, con
                           stream);
 }
 
+int32_t yoco_xattn_workspace_size_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout,
+                                        const int32_t* kv_len_host, int32_t sm_count, int32_t mode, int32_t q4,
+                                        size_t* bytes) {
+    return no_throw([&]() -> int32_t {
+        if (!shape || !layout || !bytes || sm_count < 0) return YOCO_ERR_INVALID_ARG;
+        int32_t rc = validate_shape(*shape, mode);
+        if (rc != YOCO_OK) return rc;
+        if (shape->kv_head_stride != 0) return YOCO_ERR_INVALID_ARG;
+        if ((q4 && shape->d != 128) || !valid_page_size(layout->page_size)) return YOCO_ERR_UNSUPPORTED;
+        if (sm_count == 0) {
+            DeviceState* dev = nullptr;
+            if ((rc = device_state(&dev)) != YOCO_OK) return rc;
+            sm_count = dev->sm_count;
+        }
+        Plan plan;
+        rc = make_plan(*shape, nullptr, kv_len_host, sm_count, mode, plan, kMaxSubItems, nullptr, nullptr,
+                       q4 ? kPagedQ4Cache : kPagedCache);
+        if (rc != YOCO_OK) return rc;
+        *bytes = (size_t)plan.info.workspace_bytes;
+        return YOCO_OK;
+    });
+}
+
+int32_t yoco_xattn_decode_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
+                                const void* K_pages, const void* V_pages, const int32_t* page_table,
+                                const int32_t* kv_len_host, void* O, float* lse, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+    return attend_paged(YOCO_MODE_DECODE, shape, layout, Q, K_pages, nullptr, V_pages, nullptr, false, page_table,
+                        kv_len_host, O, lse, workspace, workspace_bytes, stream);
+}
+
+int32_t yoco_xattn_decode_paged_q4(const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
+                                   const void* K4, const void* K_scale, const void* V4, const void* V_scale,
+                                   const int32_t* page_table, const int32_t* kv_len_host, void* O, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+    return attend_paged(YOCO_MODE_DECODE, shape, layout, Q, K4, K_scale, V4, V_scale, true, page_table, kv_len_host, O,
+                        lse, workspace, workspace_bytes, stream);
+}
+
+int32_t yoco_xattn_chunk_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
+                               const void* K_pages, const void* V_pages, const int32_t* page_table,
+                               const int32_t* kv_len_host, void* O, float* lse, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+    return attend_paged(YOCO_MODE_CHUNK, shape, layout, Q, K_pages, nullptr, V_pages, nullptr, false, page_table,
+                        kv_len_host, O, lse, workspace, workspace_bytes, stream);
+}
+
+int32_t yoco_xattn_chunk_paged_q4(const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
+                                  const void* K4, const void* K_scale, const void* V4, const void* V_scale,
+                                  const int32_t* page_table, const int32_t* kv_len_host, void* O, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+    return attend_paged(YOCO_MODE_CHUNK, shape, layout, Q, K4, K_scale, V4, V_scale, true, page_table, kv_len_host, O,
+                        lse, workspace, workspace_bytes, stream);
+}
+
+int32_t yoco_paged_append(const yoco_paged_append_shape* shape, const yoco_paged_layout* layout, const void* K_new,
+                          const void* V_new, void* K_pages, void* V_pages, const int32_t* page_table,
+                          const int32_t* new_len_host, const int32_t* kv_len_host, void* stream) {
+    return paged_rows(shape, layout, true, false, K_new, V_new, K_pages, nullptr, V_pages, nullptr, page_table, nullptr,
+                      kv_len_host, new_len_host, nullptr, nullptr, stream);
+}
+
+int32_t yoco_paged_append_q4(const yoco_paged_append_shape* shape, const yoco_paged_layout* layout, const void* K_new,
+                             const void* V_new, void* K4, void* K_scale, void* V4, void* V_scale,
+                             const int32_t* page_table, const int32_t* new_len_host, const int32_t* kv_len_host,
+                             void* stream) {
+    return paged_rows(shape, layout, true, true, K_new, V_new, K4, K_scale, V4, V_scale, page_table, nullptr,
+                      kv_len_host, new_len_host, nullptr, nullptr, stream);
+}
+
+int32_t yoco_paged_gather(const yoco_paged_append_shape* shape, const yoco_paged_layout* layout, const void* K_pages,
+                          const void* V_pages, const int32_t* page_table, const int32_t* begin_host,
+                          const int32_t* end_host, void* K, void* V, void* stream) {
+    return paged_rows(shape, layout, false, false, nullptr, nullptr, K_pages, nullptr, V_pages, nullptr, page_table,
+                      begin_host, end_host, nullptr, K, V, stream);
+}
+
+int32_t yoco_paged_gather_q4(const yoco_paged_append_shape* shape, const yoco_paged_layout* layout, const void* K4,
+                             const void* K_scale, const void* V4, const void* V_scale, const int32_t* page_table,
+                             const int32_t* begin_host, const int32_t* end_host, void* K, void* V, void* stream) {
+    return paged_rows(shape, layout, false, true, nullptr, nullptr, K4, K_scale, V4, V_scale, page_table, begin_host,
+                      end_host, nullptr, K, V, stream);
+}
+
+int32_t yoco_rope_q(const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
+                    const int32_t* kv_len_host, void* Q_rot, void* stream) {
+    return no_throw([&]() -> int32_t {
+        if (!shape || !layout) return YOCO_ERR_INVALID_ARG;
+        int32_t rc = validate_shape(*shape, YOCO_MODE_CHUNK);
+        if (rc != YOCO_OK) return rc;
+        if (shape->B == 0) return YOCO_OK;
+        if (shape->B > kAppendMaxSequences) return YOCO_ERR_UNSUPPORTED;
+        if (!Q || !Q_rot || !aligned(Q, 16) || !aligned(Q_rot, 16) || !layout->cos_sin || (layout->rope_pairs & ~1))
+            return YOCO_ERR_INVALID_ARG;
+        SeqTable tab;
+        std::memset(&tab, 0, sizeof tab);
+        int64_t max_len = 0;
+        for (int32_t i = 0; i < shape->B; ++i) {
+            const int32_t n = kv_len_host ? kv_len_host[i] : shape->max_kv_len;
+            if (n < 0) return YOCO_ERR_INVALID_ARG;
+            tab.pos0[i] = (int32_t)std::max<int64_t>((int64_t)n - shape->T, INT32_MIN);   // may be negative
+            max_len = std::max<int64_t>(max_len, n);
+        }
+        Rotation rot;
+        if ((rc = check_rotation(*layout, max_len, &rot)) != YOCO_OK) return rc;
+        DeviceState* dev = nullptr;
+        if ((rc = device_state(&dev)) != YOCO_OK) return rc;
+        YOCO_CUDA_TRY(launch_rope_q(static_cast<const __nv_bfloat16*>(Q), static_cast<__nv_bfloat16*>(Q_rot), shape->B,
+                                    shape->Hq, shape->T, shape->d, rot, tab, reinterpret_cast<cudaStream_t>(stream)));
+        return YOCO_OK;
+    });
+}
+
 int32_t yoco_kv_append_status(void* stream) {
     int32_t word = 0;
     YOCO_CUDA_TRY(read_and_clear_kv_append_status(&word, reinterpret_cast<cudaStream_t>(stream)));
-    return word == kStatusOk ? YOCO_OK : YOCO_ERR_TIMEOUT;
+    return status_code(word);
 }
 
 int32_t yoco_kv_append_status_detail(void* stream, int32_t* wait_class, int32_t* cta) {
@@ -810,7 +1121,7 @@ int32_t yoco_xattn_status(const void* workspace, void* stream) {
     int32_t word = 0;
     int32_t rc = read_status_word(workspace, stream, &word);
     if (rc != YOCO_OK) return rc;
-    return word == kStatusOk ? YOCO_OK : YOCO_ERR_TIMEOUT;
+    return status_code(word);
 }
 
 int32_t yoco_xattn_status_detail(const void* workspace, void* stream, int32_t* wait_class, int32_t* cta) {
@@ -823,7 +1134,7 @@ int32_t yoco_xattn_status_detail(const void* workspace, void* stream, int32_t* w
 int32_t yoco_xattn_decode_status_word(int32_t word, int32_t* wait_class, int32_t* cta) {
     if (wait_class) *wait_class = word & 0xFF;
     if (cta) *cta = (int32_t)((uint32_t)word >> 8) - 1;
-    return word == kStatusOk ? YOCO_OK : YOCO_ERR_TIMEOUT;
+    return status_code(word);
 }
 
 int32_t yoco_xattn_selftest_wait_expiry(const yoco_xattn_shape* shape, const void* Q, const void* K, const void* V,
@@ -882,6 +1193,8 @@ const char* yoco_xattn_strerror(int32_t code) {
         case YOCO_ERR_WORKSPACE_TOO_SMALL: return "workspace too small";
         case YOCO_ERR_CUDA: return "CUDA call failed (see yoco_xattn_last_cuda_error)";
         case YOCO_ERR_TIMEOUT: return "a bounded device-side wait expired";
+        case YOCO_ERR_HOST_MEMORY: return "host memory allocation failed";
+        case YOCO_ERR_BAD_PAGE: return "a page table entry is not a page of the pool";
         case YOCO_ERR_STATIC_SCRATCH_EXCEEDED:
             return "problem needs more scratch than the built-in static buffer holds; "
                    "use yoco_xattn_decode with a caller-provided workspace";

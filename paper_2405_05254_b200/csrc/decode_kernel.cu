@@ -17,7 +17,12 @@
 // warps through a two-entry queue in shared memory, so the tile ring never drains between
 // items.  Fast SMs thereby take more pieces than slow ones; what a piece computes and where
 // its partial result goes is fixed by the plan.
+//
+// PAGED = true finds the rows of a tile through a page table: a page holds P consecutive keys of
+// every KV head, so a 64-key tile is one box of a page (P >= 64) or 64 / P boxes of as many pages.
+// Only the producer knows; its page numbers are read two tiles ahead of the copies that use them.
 #include "kernels.h"
+#include "page_map.cuh"
 #include "ptx.cuh"
 
 namespace yoco {
@@ -50,7 +55,7 @@ __device__ __forceinline__ uint32_t ld_global_u32(const __nv_bfloat16* p) {
     return *reinterpret_cast<const uint32_t*>(p);
 }
 
-template <int D, int ROWS>
+template <int D, int ROWS, bool PAGED>
 __device__ __forceinline__ void decode_body(const CUtensorMap& tmK, const CUtensorMap& tmV,
                                             const DecodeParams& p) {
     using C = Cfg<D, ROWS>;
@@ -129,6 +134,8 @@ __device__ __forceinline__ void decode_body(const CUtensorMap& tmK, const CUtens
                     if (s_lo >= s_hi) continue;
                     const int k_lo = seg.k_begin + s_lo * TILE_N;
                     const int k_hi = min(seg.k_begin + s_hi * TILE_N, seg.k_end);
+                    PageCursor<TILE_N> pc;
+                    if (PAGED) pc.start(p.pages, seg.stream, k_lo, k_hi);
                     for (int k0 = k_lo; k0 < k_hi; k0 += TILE_N, ++it) {
                         const uint32_t stage = it % STAGES, round = it / STAGES;
                         // self-test of the give-up path: nothing is armed, so no stage is needed either
@@ -140,6 +147,18 @@ __device__ __forceinline__ void decode_body(const CUtensorMap& tmK, const CUtens
                         }
                         uint8_t* kdst = stage_mem + stage * C::STAGE_BYTES;
                         uint8_t* vdst = kdst + C::TENSOR_BYTES;
+                        if (PAGED) {
+                            mbar_expect_tx(&full_bar[stage], pc.rows() * (D * 2 * 2));
+                            pc.for_each_box(ab.status, [&](int dst_row, int row) {
+#pragma unroll
+                                for (int h = 0; h < C::HALVES; ++h) {
+                                    tma_load_2d(kdst + h * HALF_BYTES + dst_row * 128, &tmK, h * 64, row, &full_bar[stage]);
+                                    tma_load_2d(vdst + h * HALF_BYTES + dst_row * 128, &tmV, h * 64, row, &full_bar[stage]);
+                                }
+                            });
+                            pc.next();
+                            continue;
+                        }
                         mbar_expect_tx(&full_bar[stage], C::STAGE_BYTES);
                         const int row = seg.kv_row0 + (k0 - seg.k_begin);
 #pragma unroll
@@ -418,41 +437,41 @@ __device__ __forceinline__ void decode_body(const CUtensorMap& tmK, const CUtens
 }
 
 // work tables in global memory (the workspace)
-template <int D, int ROWS>
+template <int D, int ROWS, bool PAGED>
 __global__ void __launch_bounds__(kThreads, 2)
 decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
               const DecodeParams p) {
-    decode_body<D, ROWS>(tmK, tmV, p);
+    decode_body<D, ROWS, PAGED>(tmK, tmV, p);
 }
 
 // work tables as kernel parameters
-template <int D, int ROWS>
+template <int D, int ROWS, bool PAGED>
 __global__ void __launch_bounds__(kThreads, 2)
 decode_kernel_inline(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                      const DecodeParams p0, const __grid_constant__ DecodeInlineTables tab) {
     DecodeParams p = p0;
     p.segments = tab.seg;
     p.group_begin = tab.group_begin;
-    decode_body<D, ROWS>(tmK, tmV, p);
+    decode_body<D, ROWS, PAGED>(tmK, tmV, p);
 }
 
-template <int D, int ROWS>
+template <int D, int ROWS, bool PAGED>
 cudaError_t launch_one(const DecodeParams& p, const CUtensorMap& tmK, const CUtensorMap& tmV,
                        int num_groups, cudaStream_t stream, const DecodeInlineTables* inline_tab) {
     using C = Cfg<D, ROWS>;
     if (inline_tab)
-        decode_kernel_inline<D, ROWS><<<num_groups, kThreads, C::SMEM_BYTES, stream>>>(tmK, tmV, p, *inline_tab);
+        decode_kernel_inline<D, ROWS, PAGED><<<num_groups, kThreads, C::SMEM_BYTES, stream>>>(tmK, tmV, p, *inline_tab);
     else
-        decode_kernel<D, ROWS><<<num_groups, kThreads, C::SMEM_BYTES, stream>>>(tmK, tmV, p);
+        decode_kernel<D, ROWS, PAGED><<<num_groups, kThreads, C::SMEM_BYTES, stream>>>(tmK, tmV, p);
     return cudaGetLastError();
 }
 
-template <int D, int ROWS>
+template <int D, int ROWS, bool PAGED>
 cudaError_t setup_one() {
-    cudaError_t e = cudaFuncSetAttribute(decode_kernel<D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    cudaError_t e = cudaFuncSetAttribute(decode_kernel<D, ROWS, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          Cfg<D, ROWS>::SMEM_BYTES);
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(decode_kernel_inline<D, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    return cudaFuncSetAttribute(decode_kernel_inline<D, ROWS, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 Cfg<D, ROWS>::SMEM_BYTES);
 }
 
@@ -460,21 +479,34 @@ cudaError_t setup_one() {
 
 cudaError_t decode_kernel_setup() {
     cudaError_t e;
-    if ((e = setup_one<128, 8>()) != cudaSuccess) return e;
-    if ((e = setup_one<128, 16>()) != cudaSuccess) return e;
-    if ((e = setup_one<64, 8>()) != cudaSuccess) return e;
-    return setup_one<64, 16>();
+    if ((e = setup_one<128, 8, false>()) != cudaSuccess) return e;
+    if ((e = setup_one<128, 16, false>()) != cudaSuccess) return e;
+    if ((e = setup_one<64, 8, false>()) != cudaSuccess) return e;
+    if ((e = setup_one<64, 16, false>()) != cudaSuccess) return e;
+    if ((e = setup_one<128, 8, true>()) != cudaSuccess) return e;
+    if ((e = setup_one<128, 16, true>()) != cudaSuccess) return e;
+    if ((e = setup_one<64, 8, true>()) != cudaSuccess) return e;
+    return setup_one<64, 16, true>();
 }
 
-cudaError_t launch_decode(const DecodeParams& p, const CUtensorMap& tmK, const CUtensorMap& tmV,
-                          int num_groups, cudaStream_t stream, const DecodeInlineTables* tab) {
-    if (num_groups <= 0) return cudaSuccess;
+namespace {
+template <bool PAGED>
+cudaError_t launch_any(const DecodeParams& p, const CUtensorMap& tmK, const CUtensorMap& tmV, int num_groups,
+                       cudaStream_t stream, const DecodeInlineTables* tab) {
     const bool wide = p.rows_per_stream > 8;
     if (p.d == 128)
-        return wide ? launch_one<128, 16>(p, tmK, tmV, num_groups, stream, tab)
-                    : launch_one<128, 8>(p, tmK, tmV, num_groups, stream, tab);
-    return wide ? launch_one<64, 16>(p, tmK, tmV, num_groups, stream, tab)
-                : launch_one<64, 8>(p, tmK, tmV, num_groups, stream, tab);
+        return wide ? launch_one<128, 16, PAGED>(p, tmK, tmV, num_groups, stream, tab)
+                    : launch_one<128, 8, PAGED>(p, tmK, tmV, num_groups, stream, tab);
+    return wide ? launch_one<64, 16, PAGED>(p, tmK, tmV, num_groups, stream, tab)
+                : launch_one<64, 8, PAGED>(p, tmK, tmV, num_groups, stream, tab);
+}
+}  // namespace
+
+cudaError_t launch_decode(const DecodeParams& p, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                          int num_groups, cudaStream_t stream, const DecodeInlineTables* tab, bool paged) {
+    if (num_groups <= 0) return cudaSuccess;
+    return paged ? launch_any<true>(p, tmK, tmV, num_groups, stream, tab)
+                 : launch_any<false>(p, tmK, tmV, num_groups, stream, tab);
 }
 
 }  // namespace yoco

@@ -3,6 +3,7 @@
 
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
 
@@ -22,6 +23,7 @@ enum WaitClass : int32_t {
     kWaitTensor = 4,      // a tensor-core hand-over: scores ready, P written, product finished
     kWaitDrain = 5,       // leaving: a copy or product that had been started did not finish in time
     kWaitMisaligned = 6,  // dynamic shared memory not 1 KB aligned (no wait involved; nothing ran)
+    kBadPage = 7,         // a page table entry outside the pool (no wait involved; its rows read as zeros / are not written)
 };
 __host__ __device__ constexpr int32_t status_word(int32_t wait_class, int32_t cta) {
     return wait_class | ((cta + 1) << 8);
@@ -71,6 +73,17 @@ struct CombineParams {
 cudaError_t launch_combine(const CombineParams& p, cudaStream_t stream,
                            const CombineInlineTables* inline_tab = nullptr, bool after_attention = false);
 
+// Where the rows of a paged cache are: row(page, head c, slot) = page * page_rows + c * P + slot, P = 1 << page_shift.
+struct PageMap {
+    const int32_t* table;       // device [B, table_stride]: page that holds keys [j P, (j + 1) P) of sequence b
+    int32_t table_stride;
+    int32_t page_shift;
+    int32_t num_pages;
+    int32_t page_rows;
+    int32_t Hkv;
+    int32_t rows;               // rows of the pool: a row number no load can reach
+};
+
 struct DecodeParams {
     const __nv_bfloat16* Q;     // [B*Hq*T, d]
     __nv_bfloat16* O;           // [B*Hq*T, d]
@@ -91,13 +104,16 @@ struct DecodeParams {
     int64_t wait_limit_ns;      // 0 = the default limit of a bounded wait
     int32_t selftest_skip_loads;// self-test of the give-up path: the producer arms no copy, so the first
                                 // consumer wait runs out (with nothing in flight) and the kernel returns
+    PageMap pages;              // paged cache only
 };
 // tmK / tmV: 2-D tensor maps over the [rows, d] view of K and V, box {64, kDecodeTileN},
 // 128-byte swizzle.
 // inline_tab (host, may be null): segments and group offsets passed as kernel parameters instead
 // of p.segments / p.group_begin.
+// paged: rows are found through p.pages; the maps' boxes are {64, min(P, kDecodeTileN)}.
 cudaError_t launch_decode(const DecodeParams& p, const CUtensorMap& tmK, const CUtensorMap& tmV,
-                          int num_groups, cudaStream_t stream, const DecodeInlineTables* inline_tab = nullptr);
+                          int num_groups, cudaStream_t stream, const DecodeInlineTables* inline_tab = nullptr,
+                          bool paged = false);
 // one-time per-device kernel attribute set-up (dynamic shared memory opt-in)
 cudaError_t decode_kernel_setup();
 
@@ -116,6 +132,16 @@ cudaError_t launch_decode_fp8(const DecodeFp8Params& p, const CUtensorMap& tmK, 
                               int num_groups, cudaStream_t stream, const DecodeInlineTables* inline_tab);
 cudaError_t decode_fp8_kernel_setup();
 
+// ---- decode over a paged 4-bit cache, head dimension 128 ---------------------------------------
+// k / v: uint8 maps over the [rows, 64] code bytes, box {64, box}, 64-byte swizzle; k_scale / v_scale: uint8
+// maps over the scales as [rows / 16, 128], box {128, box / 16}, no swizzle (box = min(P, the kernel's tile)).
+struct PagedQ4Maps {
+    CUtensorMap k, k_scale, v, v_scale;
+};
+cudaError_t launch_decode_q4(const DecodeParams& p, const PagedQ4Maps& maps, int num_groups, cudaStream_t stream,
+                             const DecodeInlineTables* inline_tab);
+cudaError_t decode_q4_kernel_setup();
+
 struct ChunkParams {
     __nv_bfloat16* O;           // [B*Hq*T, d]
     float* lse;                 // [B*Hq*T] or null
@@ -131,6 +157,7 @@ struct ChunkParams {
     int32_t d;
     int32_t window;             // sliding window C, 0 = none
     int32_t force_partial;      // write every segment to its partial slot, even of an unsplit stream
+    PageMap pages;              // paged cache only
 };
 // tmQ: [B*Hq*T, d] box {64, 128}; tmK / tmV: [rows, d] box {64, kChunkTileN}; 128-byte swizzle.
 // Grid = num_groups * m_tiles CTAs, the row tile varying fastest so that the CTAs that walk the
@@ -182,6 +209,40 @@ cudaError_t launch_kv_append(const KvAppendParams& p, const KvAppendTables& tab,
 cudaError_t launch_fold_gain(const __nv_bfloat16* g, const __nv_bfloat16* W, __nv_bfloat16* Wg, int64_t d_model,
                              int64_t n_out, cudaStream_t stream);
 cudaError_t read_and_clear_kv_append_status(int32_t* word, cudaStream_t stream);
+cudaError_t kv_append_status_address(int32_t** word);    // on the current device
 cudaError_t kv_append_kernel_setup();
+
+// ---- rows of a paged cache: append with rotation, read back, rotation of the queries --------------
+constexpr int kQ4Group = 32;            // channels of a 4-bit row that share a scale
+constexpr float kQ4ScaleMax = 448.f;    // largest scale a 4-bit row is given
+struct SeqTable {               // per sequence, as kernel parameters
+    int32_t pos0[kAppendMaxSequences];       // position of the sequence's first token of this call
+    int32_t tok0[kAppendMaxSequences + 1];   // its first token among all tokens of the call
+};
+struct Rotation {
+    const float* cos_sin;       // [max_pos, d]: d/2 cosines, d/2 sines of a position; null = no rotation
+    int32_t neighbours;         // 0: channels (c, c + d/2) turn together; 1: (2c, 2c + 1)
+};
+struct PagedRowsParams {
+    PageMap pages;
+    Rotation rot;
+    const __nv_bfloat16* k_src; // append: new rows, src_stride elements between tokens, heads consecutive
+    const __nv_bfloat16* v_src;
+    int64_t src_stride;
+    void* k_pool;               // bf16 rows, or 4-bit codes (d/2 bytes a row)
+    void* v_pool;
+    __half* k_scale;            // 4-bit rows: d/32 scales a row
+    __half* v_scale;
+    __nv_bfloat16* k_out;       // gather: packed head-major rows
+    __nv_bfloat16* v_out;
+    int32_t* status;
+    int32_t B, d, tokens;
+    int32_t tokens_per_seq;     // > 0: every sequence has so many; 0: see SeqTable::tok0
+};
+cudaError_t launch_paged_append(const PagedRowsParams& p, const SeqTable& tab, bool q4, cudaStream_t stream);
+cudaError_t launch_paged_gather(const PagedRowsParams& p, const SeqTable& tab, bool q4, cudaStream_t stream);
+// Qr[b, h, t] = Q[b, h, t] turned by the angles of position tab.pos0[b] + t (rows at negative positions are copied)
+cudaError_t launch_rope_q(const __nv_bfloat16* Q, __nv_bfloat16* Qr, int32_t B, int32_t Hq, int32_t T, int32_t d,
+                          const Rotation& rot, const SeqTable& tab, cudaStream_t stream);
 
 }  // namespace yoco

@@ -482,6 +482,10 @@ cudaError_t read_and_clear_kv_append_status(int32_t* word, cudaStream_t stream) 
     return e != cudaSuccess ? e : cudaStreamSynchronize(stream);
 }
 
+cudaError_t kv_append_status_address(int32_t** word) {
+    return cudaGetSymbolAddress(reinterpret_cast<void**>(word), g_kv_append_status);
+}
+
 cudaError_t kv_append_kernel_setup() {
     cudaError_t e = cudaFuncSetAttribute(kv_append_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
     if (e != cudaSuccess) return e;

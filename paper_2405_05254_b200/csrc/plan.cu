@@ -37,7 +37,7 @@ int32_t validate_layout(const yoco_xattn_shape& s, const int32_t* cu_kv_host, co
 
 int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const int32_t* kv_len_host,
                   int32_t sm_count, int32_t mode, Plan& plan, int32_t max_sub_items,
-                  const int32_t* key_offset_host, const int32_t* kv_total_host, bool eight_bit_cache) {
+                  const int32_t* key_offset_host, const int32_t* kv_total_host, const CacheForm& form) {
     int32_t rc = validate_shape(s, mode);
     if (rc != YOCO_OK) return rc;
     if (sm_count <= 0) return YOCO_ERR_INVALID_ARG;
@@ -47,7 +47,7 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
     const int rows_per_stream = G * s.T;
     const int tile_n = mode == YOCO_MODE_DECODE ? kDecodeTileN : kChunkTileN;
     const int tile_m = mode == YOCO_MODE_DECODE ? kDecodeTileM
-                       : (rows_per_stream > kChunkTileM || eight_bit_cache) ? kChunkPairTileM : kChunkTileM;
+                       : (rows_per_stream > kChunkTileM || form.pair_tiles) ? kChunkPairTileM : kChunkTileM;
     const int m_tiles = (rows_per_stream + tile_m - 1) / tile_m;
     const int num_streams = s.B * s.Hkv;
 
@@ -71,7 +71,7 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
         if (cu_kv_host) tok_off[i] = cu_kv_host[i];
         const int64_t head_rows = s.kv_head_stride ? s.kv_head_stride / s.d : len[i];
         if (!cu_kv_host) tok_off[i + 1] = tok_off[i] + head_rows;
-        if (len[i] > 0)
+        if (len[i] > 0 && !form.paged)
             extent = std::max(extent, tok_off[i] * s.Hkv + (int64_t)(s.Hkv - 1) * head_rows + len[i]);
     }
     if (extent >= (1ll << 31)) return YOCO_ERR_UNSUPPORTED;
@@ -121,7 +121,7 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
                 DevSegment d{};
                 d.k_begin = (int32_t)(t * tile_n);
                 d.k_end = (int32_t)std::min<int64_t>(t_end * tile_n, len_vis[b]);
-                d.kv_row0 = (int32_t)(tok_off[b] * s.Hkv + c * head_rows + d.k_begin);
+                d.kv_row0 = form.paged ? 0 : (int32_t)(tok_off[b] * s.Hkv + c * head_rows + d.k_begin);
                 d.q_row0 = (b * s.Hq + c * G) * s.T;
                 d.slot = (int32_t)dev.size();
                 d.n_kv = len[b];
@@ -139,7 +139,7 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
     // Pieces pay when a group is one long run of a stream.  When groups are chains of short streams
     // (more than two segments per group on average) most streams are not split at all and are written
     // without a merge; pieces would split every one of them.
-    int R = mode == YOCO_MODE_DECODE ? choose_sub_items(total_tiles / num_groups / (eight_bit_cache ? 2 : 1), max_sub_items) : 1;
+    int R = mode == YOCO_MODE_DECODE ? choose_sub_items(total_tiles / num_groups / form.piece_divisor, max_sub_items) : 1;
     if ((int64_t)dev.size() > 2 * num_groups) R = 1;
     int32_t max_splits = 0, needs_combine = R > 1 ? 1 : 0;
     for (int st = 0; st < num_streams; ++st) {

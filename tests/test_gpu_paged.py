@@ -1,0 +1,360 @@
+"""The paged cache on the GPU: append with rotation (bf16 and 4-bit rows), read-back, rotation of the queries, and
+decode attention, against plain numpy (bit for bit where every rounding is fixed by the definition, in 64 bits otherwise).
+
+Tolerances of the attention tests are those of the packed paths (helpers.py).  What the 4-bit path adds: P * s is rounded to
+fp16, half a step 2^-11 relative per term, below the bf16 half step 2^-9 that the bf16 path has there; the codes are exact,
+the scores are fp32 sums of exact products.  The output's bf16 half step (2^-9) stays the largest single term."""
+import numpy as np
+import pytest
+
+import paged_ref as pr
+import synth_inputs as si
+from helpers import assert_close, assert_lse_close
+
+pytestmark = pytest.mark.gpu
+
+
+def q_bits(seed, B, Hq, T, d, gain=1.0):
+    return pr.bf16(np.random.default_rng(seed + 1000).standard_normal((B, Hq, T, d)) * gain)[0]
+
+
+def f64(bits):
+    return si.bf16_bits_to_f32(bits).astype(np.float64)
+
+
+# ---- append, gather, rope ---------------------------------------------------------------------------
+
+APPEND = [
+    # lens (with the new tokens), new tokens, P, Hkv, d, pairs, src_extra, wide pages
+    ([1], [1], 16, 1, 128, 0, 0, False),
+    ([64, 65, 130], [1, 1, 1], 64, 8, 128, 0, 2048, False),
+    ([40, 7, 300], [40, 0, 33], 32, 2, 64, 1, 64, True),
+    ([257, 256, 16, 1], [257, 100, 16, 1], 16, 3, 128, 1, 0, False),
+    ([512], [301], 256, 4, 128, None, 8, True),
+    ([90, 0, 55], [90, 0, 55], 128, 5, 64, 0, 0, False),
+]
+
+
+def append_case(case, q4, seed=3):
+    import torch
+    from paper_2405_05254_b200 import binding as bd
+    lens, new, P, H, d, pairs, extra, wide = case
+    d = 128 if q4 else d
+    lens, new = np.asarray(lens, np.int32), np.asarray(new, np.int32)
+    cache = pr.PagedCache(seed, lens, P, H, d, q4, page_rows=2 * H * P if wide else 0, slack_nan=False)
+    cs = None if pairs is None else pr.cos_sin(int(lens.max()), d)
+    dev = pr.DevCache(cache, cs, pairs or 0)
+    tokens, stride = int(new.sum()), H * d + extra
+    r = np.random.default_rng(seed)
+    src = [pr.bf16(r.standard_normal((tokens, stride)) * np.exp(r.standard_normal((1, stride))))[0] for _ in range(2)]
+    if q4:        # rows that reach the corners of the format: zeros, one huge value, tiny values
+        for s in src:
+            s[0, :32] = 0
+            s[0, 32:64] = pr.bf16(np.full(32, 1e-9, np.float32))[0]
+            s[-1, 0] = pr.bf16(np.full(1, 3e38, np.float32))[0][0]
+            s[-1, 40] = 0x7F80                                             # +inf
+    kd, vd = pr.bits_to_dev(src[0]), pr.bits_to_dev(src[1])
+    shape = bd.PagedAppendShape(len(lens), H, d, 0, stride)
+    fn = bd.yoco_paged_append_q4 if q4 else bd.yoco_paged_append
+    fn(shape, dev.layout, kd, vd, *dev.pools, dev.table, new, lens)
+    assert bd.yoco_kv_append_status() == 0
+    # the same in numpy, in place
+    want = [tuple(a.copy() for a in p) if q4 else p.copy() for p in cache.pools]
+    at = 0
+    for b in range(len(lens)):
+        pos = np.arange(lens[b] - new[b], lens[b])
+        for h in range(H):
+            rows = cache.row_numbers(b, h, int(lens[b]))[pos]
+            for which in range(2):
+                x = si.bf16_bits_to_f32(src[which][at:at + new[b], h * d:(h + 1) * d])
+                if which == 0 and cs is not None:
+                    with np.errstate(invalid="ignore", over="ignore"):
+                        x = pr.rotate(x, cs[pos], pairs)
+                if q4:
+                    with np.errstate(invalid="ignore"):
+                        want[which][0][rows], want[which][1][rows] = pr.quantise(x)
+                else:
+                    want[which][rows] = pr.bf16(x)[0]
+        at += new[b]
+    return cache, dev, want, lens, new, src
+
+
+@pytest.mark.parametrize("case", APPEND)
+def test_append_bf16_bit_for_bit_and_nothing_else_touched(case):
+    cache, dev, want, *_ = append_case(case, False)
+    for t, w in zip(dev.pools, want):
+        assert np.array_equal(pr.dev_bits(t).reshape(w.shape), w)
+
+
+@pytest.mark.parametrize("case", APPEND)
+def test_append_q4_bit_for_bit_and_nothing_else_touched(case):
+    cache, dev, want, lens, new, src = append_case(case, True)
+    for which in range(2):
+        codes, s = dev.pools[2 * which].cpu().numpy(), dev.pools[2 * which + 1].cpu().numpy()
+        assert np.array_equal(s.view(np.uint16), want[which][1].view(np.uint16)), "scales"
+        assert np.array_equal(codes, want[which][0]), "codes"
+
+
+@pytest.mark.parametrize("q4", [False, True])
+@pytest.mark.parametrize("lens,lo,P,H,d", [([5], [0], 16, 1, 128), ([200, 33, 64], [50, 33, 0], 32, 4, 64), ([300, 1], [299, 0], 256, 3, 128)])
+def test_gather_reads_the_rows_back(q4, lens, lo, P, H, d):
+    import torch
+    from paper_2405_05254_b200 import binding as bd
+    d = 128 if q4 else d
+    cache = pr.PagedCache(5, lens, P, H, d, q4)
+    dev = pr.DevCache(cache)
+    lo, hi = np.asarray(lo, np.int32), np.asarray(lens, np.int32)
+    n = int((hi - lo).sum()) * H * d
+    out = [torch.full((n + 64,), 777.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    fn = bd.yoco_paged_gather_q4 if q4 else bd.yoco_paged_gather
+    fn(bd.PagedAppendShape(len(lens), H, d, 0, 0), dev.layout, *dev.pools, dev.table, lo, hi, out[0][:n], out[1][:n])
+    assert bd.yoco_kv_append_status() == 0
+    for which in range(2):
+        want = np.concatenate([np.stack([cache.rows(which, b, h)[lo[b]:] for h in range(H)]).reshape(-1) for b in range(len(lens))])
+        assert np.array_equal(pr.dev_bits(out[which][:n]), pr.bf16(want)[0])
+        assert (out[which][n:] == 777.0).all()
+
+
+@pytest.mark.parametrize("pairs", [0, 1])
+@pytest.mark.parametrize("B,Hq,T,d,lens", [(1, 1, 1, 64, [1]), (3, 6, 5, 128, [100, 5, 3])])
+def test_rope_q_bit_for_bit_also_in_place(pairs, B, Hq, T, d, lens):
+    import torch
+    from paper_2405_05254_b200 import binding as bd
+    bits = q_bits(9, B, Hq, T, d)
+    cs = pr.cos_sin(120, d)
+    table = torch.from_numpy(cs).cuda()
+    layout = bd.make_paged_layout(16, 1, 1, cos_sin=table, rope_pairs=pairs)
+    Q = pr.bits_to_dev(bits)
+    R = torch.empty_like(Q)
+    shape = bd.make_shape(B, Hq, 1, d, T)
+    bd.yoco_rope_q(shape, layout, Q, np.asarray(lens, np.int32), R)
+    want = bits.copy()
+    for b in range(B):
+        for t in range(T):
+            pos = lens[b] - T + t
+            if pos >= 0:
+                want[b, :, t] = pr.bf16(pr.rotate(si.bf16_bits_to_f32(bits[b, :, t]), cs[pos], pairs))[0]
+    assert np.array_equal(pr.dev_bits(R), want)
+    bd.yoco_rope_q(shape, layout, Q, np.asarray(lens, np.int32), Q)
+    assert np.array_equal(pr.dev_bits(Q), want)
+
+
+# ---- decode -----------------------------------------------------------------------------------------
+
+DECODE = [
+    # lens, Hq, Hkv, T, P, window, d
+    ([1], 1, 1, 1, 16, 0, 128),
+    ([63, 64, 65], 8, 2, 1, 16, 0, 64),
+    ([0, 17, 128], 12, 4, 2, 32, 0, 128),              # an empty sequence; G * T = 6
+    ([2, 700], 4, 1, 4, 64, 0, 128),                   # T > N: rows without a key; 16 rows
+    ([1000, 31, 513], 32, 8, 1, 128, 100, 128),        # sliding window
+    ([5000], 16, 2, 2, 256, 0, 128),                   # 16 rows per KV head
+    ([20000, 3000], 32, 8, 1, 64, 0, 128),             # split and merged
+    ([4097, 90], 24, 8, 3, 16, 1, 64),                 # window 1: every row sees itself only
+    ([9000], 3, 3, 1, 32, 777, 128),
+]
+
+
+@pytest.mark.parametrize("q4", [False, True])
+@pytest.mark.parametrize("lens,Hq,Hkv,T,P,window,d", DECODE)
+def test_decode_matches_the_definition(q4, lens, Hq, Hkv, T, P, window, d):
+    d = 128 if q4 else d
+    cache = pr.PagedCache(11, lens, P, Hkv, d, q4)
+    dev = pr.DevCache(cache)
+    Q = q_bits(11, len(lens), Hq, T, d)
+    o, lse, _ = dev.attend(Q, T, window=window)
+    assert dev.status[0] == 0
+    ref, lref = pr.attention(cache, f64(Q), T, window=window)
+    assert_close(o, ref, "O")
+    assert_lse_close(lse, lref, "LSE")
+
+
+def test_decode_bf16_gives_the_bits_of_the_packed_cache():
+    """Same tiles, same plan: a paged cache with the same rows gives the same output bits as the packed one."""
+    from helpers import GpuRunner
+    lens, H, Hq, d, T = [3000, 77, 1200], 4, 16, 128, 1
+    cache = pr.PagedCache(13, lens, 32, H, d, False)
+    dev = pr.DevCache(cache)
+    packed = [np.concatenate([np.concatenate([pr.bf16(cache.rows(w, b, h))[0].reshape(-1) for h in range(H)]) for b in range(len(lens))])
+              for w in range(2)]
+    Q = q_bits(13, len(lens), Hq, T, d)
+    o, lse, O = dev.attend(Q, T)
+    po, plse, PO = GpuRunner(len(lens), Hq, H, d, T, lens, packed[0], packed[1]).run(Q)
+    assert np.array_equal(pr.dev_bits(O), pr.dev_bits(PO)) and np.array_equal(lse, plse)
+
+
+@pytest.mark.parametrize("q4", [False, True])
+def test_peaked_scores_and_a_late_maximum(q4):
+    """Scores over hundreds: the running maximum moves late, most weights vanish."""
+    cache = pr.PagedCache(17, [6000], 64, 2, 128, q4, gain=12.0)
+    dev = pr.DevCache(cache)
+    Q = q_bits(17, 1, 8, 2, 128, gain=3.0)
+    o, lse, _ = dev.attend(Q, 2)
+    ref, lref = pr.attention(cache, f64(Q), 2)
+    assert_close(o, ref, "O")
+    # fp32 scores of some hundreds: their rounding 2^-24 times the sum of |products| (about 128 * 36) is below 3e-4
+    assert_lse_close(lse, lref, "LSE")
+
+
+def test_q4_many_keys_with_small_weights_are_not_lost():
+    """One key leads by 12 nats, tens of thousands share the rest: their weights times a small scale are far below the normal
+    range of fp16 unless P carries spare bits."""
+    n = 40000
+    cache = pr.PagedCache(19, [n], 64, 1, 128, True)
+    kc, ks = cache.pools[0]
+    rows = cache.row_numbers(0, 0, n)
+    kc[rows], ks[rows] = 0x88, np.float16(1)                       # every key is zero ...
+    x = np.zeros(128, np.float32)
+    x[0] = 7
+    kc[rows[123]], ks[rows[123]] = pr.quantise(x[None])
+    vc, vs = cache.pools[1]
+    vc[rows], vs[rows] = 0xCC, np.float16(0.02)                    # ... and every value 4 * 0.02
+    vc[rows[123]] = 0x88
+    q = np.zeros((1, 1, 1, 128), np.float32)
+    q[..., 0] = 12.0 / 7.0 * 128 ** 0.5
+    Q = pr.bf16(q)[0]
+    o, lse, _ = pr.DevCache(cache).attend(Q, 1)
+    ref, lref = pr.attention(cache, f64(Q), 1)
+    assert_close(o, ref)
+    assert_lse_close(lse, lref)
+
+
+@pytest.mark.parametrize("q4", [False, True])
+def test_pages_shared_by_sequences_and_pools_side_by_side(q4):
+    cache = pr.PagedCache(23, [400, 700, 333], 32, 2, 128, q4, shared=5, page_rows=4 * 32 + 32)
+    dev = pr.DevCache(cache)
+    Q = q_bits(23, 3, 8, 1, 128)
+    o, lse, _ = dev.attend(Q, 1)
+    ref, lref = pr.attention(cache, f64(Q), 1)
+    assert_close(o, ref)
+    assert_lse_close(lse, lref)
+
+
+@pytest.mark.parametrize("mode", ["decode"])
+@pytest.mark.parametrize("q4", [False, True])
+def test_a_bad_page_is_reported_and_harms_nobody_else(q4, mode):
+    """Entries outside the pool are read as zeros: the call returns, says BAD_PAGE, the other sequence is right."""
+    for bad in (-1, 10**9, -2**31):
+        cache = pr.PagedCache(29, [500, 600], 16, 2, 128, q4)
+        Q = q_bits(29, 2, 4, 1, 128)
+        ref, lref = pr.attention(cache, f64(Q), 1)
+        cache.table[0, 7] = bad
+        dev = pr.DevCache(cache)
+        o, lse, _ = dev.attend(Q, 1, mode=mode)
+        assert dev.status[:2] == (dev.bd.ERR_BAD_PAGE, dev.bd.STATUS_BAD_PAGE)
+        assert_close(o[1], ref[1])
+        assert np.isfinite(o[0]).all()
+        cache.table[0, 7] = 0
+        dev = pr.DevCache(cache)
+        dev.attend(Q, 1, mode=mode)
+        assert dev.status[0] == 0                       # the next call starts clean
+
+
+@pytest.mark.parametrize("q4", [False, True])
+def test_append_skips_a_bad_page_and_says_so(q4):
+    import torch
+    from paper_2405_05254_b200 import binding as bd
+    cache = pr.PagedCache(31, [40, 40], 16, 2, 128, q4, slack_nan=False)
+    cache.table[1, 2] = cache.num_pages
+    dev = pr.DevCache(cache)
+    before = [t.clone() for t in dev.pools]
+    x = pr.bits_to_dev(q_bits(31, 1, 1, 2, 256).reshape(2, 256))
+    fn = bd.yoco_paged_append_q4 if q4 else bd.yoco_paged_append
+    fn(bd.PagedAppendShape(2, 2, 128, 1, 0), dev.layout, x, x, *dev.pools, dev.table, None, cache.lens)
+    assert bd.yoco_kv_append_status_detail()[:2] == (bd.ERR_BAD_PAGE, bd.STATUS_BAD_PAGE)
+    assert bd.yoco_kv_append_status() == 0
+    changed = [(a.view(cache.num_pages * 2 * 16, -1) != b.view(cache.num_pages * 2 * 16, -1)).any(1).sum().item()
+               for a, b in zip(before, dev.pools)]
+    assert all(c == 2 for c in changed), changed         # the two heads of the one good row
+
+
+@pytest.mark.parametrize("q4", [False, True])
+def test_a_recorded_step_follows_the_page_table_and_two_streams_do_not_meet(q4):
+    import torch
+    from paper_2405_05254_b200 import binding as bd
+    caches = [pr.PagedCache(37 + i, [900, 150], 64, 2, 128, q4) for i in range(2)]
+    devs = [pr.DevCache(c) for c in caches]
+    Qb = [q_bits(37 + i, 2, 8, 1, 128) for i in range(2)]
+    calls, outs, streams, graphs = [], [], [torch.cuda.Stream() for _ in range(2)], []
+    for i in range(2):
+        c, dev = caches[i], devs[i]
+        shape = bd.make_shape(2, 8, 2, 128, 1)
+        ws = torch.empty(bd.yoco_xattn_workspace_size_paged(shape, dev.layout, c.lens, bd.MODE_DECODE, q4), dtype=torch.uint8, device="cuda")
+        O = torch.empty(2 * 8 * 128, dtype=torch.bfloat16, device="cuda")
+        name = "yoco_xattn_decode_paged" + ("_q4" if q4 else "")
+        call = bd.prepare_paged(name, shape, dev.layout, pr.bits_to_dev(Qb[i]), *dev.pools, dev.table, c.lens, O, None, ws, stream=streams[i])
+        torch.cuda.synchronize()
+        call.run()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=streams[i]):
+            call.run()
+        calls.append(call), outs.append(O), graphs.append(g)
+    # the second sequence moves to other pages: same rows, other places
+    refs = [pr.attention(caches[i], f64(Qb[i]), 1)[0] for i in range(2)]
+    dev, c = devs[0], caches[0]
+    old, new = int(c.table[1, 0]), int(np.setdiff1d(np.arange(c.num_pages), np.concatenate([c.table[0, :15], c.table[1, :3]]))[0])
+    R = 2 * 64
+    for t in dev.pools:
+        v = t.view(c.num_pages, R, -1)
+        v[new] = v[old]
+        v[old] = 255 if t.dtype == torch.uint8 else float("nan")
+    dev.table[1, 0] = new
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+    torch.cuda.synchronize()
+    from helpers import bf16_dev_to_f64
+    for i in range(2):
+        assert_close(bf16_dev_to_f64(outs[i]).reshape(refs[i].shape), refs[i])
+
+
+@pytest.mark.parametrize("q4", [False, True])
+def test_a_serving_run_append_rotate_attend_step_by_step(q4):
+    """Tokens arrive one by one and in a chunk, keys and queries are rotated by one table, every step is attended over the
+    cache so far; the plain form quantises (or rounds) the same rows and evaluates the definition."""
+    import torch
+    from paper_2405_05254_b200 import binding as bd
+    H, Hq, d, P, B = 2, 8, 128, 16, 3
+    steps = [([40, 3, 17], 40), ([1, 1, 1], 1), ([2, 2, 2], 2), ([1, 1, 1], 1)]
+    final = np.sum([s[0] for s in steps], 0)
+    cache = pr.PagedCache(41, final, P, H, d, q4)
+    cs = pr.cos_sin(64, d)
+    dev = pr.DevCache(cache, cs)
+    r = np.random.default_rng(41)
+    lens = np.zeros(B, np.int32)
+    for new, _ in steps:
+        new = np.asarray(new, np.int32)
+        lens = (lens + new).astype(np.int32)
+        src = [pr.bf16(r.standard_normal((int(new.sum()), H * d)))[0] for _ in range(2)]
+        fn = bd.yoco_paged_append_q4 if q4 else bd.yoco_paged_append
+        fn(bd.PagedAppendShape(B, H, d, 0, 0), dev.layout, pr.bits_to_dev(src[0]), pr.bits_to_dev(src[1]), *dev.pools, dev.table, new, lens)
+        at = 0
+        for b in range(B):
+            pos = np.arange(lens[b] - new[b], lens[b])
+            for h in range(H):
+                rows = cache.row_numbers(b, h, int(lens[b]))[pos]
+                for w in range(2):
+                    x = si.bf16_bits_to_f32(src[w][at:at + new[b], h * d:(h + 1) * d])
+                    x = pr.rotate(x, cs[pos], 0) if w == 0 else x
+                    if q4:
+                        cache.pools[w][0][rows], cache.pools[w][1][rows] = pr.quantise(x)
+                    else:
+                        cache.pools[w][rows] = pr.bf16(x)[0]
+            at += new[b]
+        T = int(new.min())
+        if T > 2:
+            continue                                        # the prompt is only stored
+        cache.lens = lens
+        Q = q_bits(41, B, Hq, T, d)
+        shape = bd.make_shape(B, Hq, H, d, T)
+        Qd = pr.bits_to_dev(Q)
+        bd.yoco_rope_q(shape, dev.layout, Qd, lens, Qd)
+        Qr = pr.dev_bits(Qd)
+        o, lse, _ = dev.attend(Qr, T)
+        ref, lref = pr.attention(cache, f64(Qr), T)
+        assert_close(o, ref)
+        assert_lse_close(lse, lref)
+    assert bd.yoco_kv_append_status() == 0
