@@ -416,11 +416,18 @@ int32_t run(const yoco_xattn_shape* shape, int32_t mode, const void* Q, const vo
                                             inline_tables ? &ready->decode_tab : nullptr, paged != nullptr));
             }
         } else {
-            if (paged) return YOCO_ERR_UNSUPPORTED;
             CUtensorMap tmQ, tmK, tmV;
+            PagedQ4Maps q4;
+            const bool four_bit = paged && paged->k_scale;
             const int64_t q_rows = (int64_t)shape->B * shape->Hq * shape->T;
             if ((rc = make_map_2d(&tmQ, Q, q_rows, shape->d, kChunkTileM)) != YOCO_OK) return rc;
-            if (fp8) {
+            if (four_bit) {
+                if ((rc = make_q4_maps(&q4, K, paged->k_scale, V, paged->v_scale, paged->pages, 32)) != YOCO_OK) return rc;
+            } else if (paged) {
+                const int32_t box = std::min(1 << paged->pages.page_shift, kChunkTileN);
+                if ((rc = make_map_2d(&tmK, K, paged->pages.rows, shape->d, box)) != YOCO_OK) return rc;
+                if ((rc = make_map_2d(&tmV, V, paged->pages.rows, shape->d, box)) != YOCO_OK) return rc;
+            } else if (fp8) {
                 if ((rc = make_map_2d_u8(&tmK, K, plan.kv_rows_extent, kChunkTileN)) != YOCO_OK) return rc;
                 if ((rc = make_map_2d_u8(&tmV, V, plan.kv_rows_extent, kChunkTileN)) != YOCO_OK) return rc;
             } else {
@@ -442,7 +449,10 @@ int32_t run(const yoco_xattn_shape* shape, int32_t mode, const void* Q, const vo
             p.d = shape->d;
             p.window = shape->window;
             p.force_partial = part_out ? 1 : 0;
-            if (fp8) {
+            if (paged) p.pages = paged->pages;
+            if (four_bit) {
+                YOCO_CUDA_TRY(launch_chunk_pair_q4(p, tmQ, q4, plan.info.num_groups, stream));
+            } else if (fp8) {
                 ChunkFp8Scales cs{};
                 cs.Hkv = shape->Hkv;
                 for (int c = 0; c < shape->Hkv; ++c) {
@@ -451,9 +461,9 @@ int32_t run(const yoco_xattn_shape* shape, int32_t mode, const void* Q, const vo
                 }
                 YOCO_CUDA_TRY(launch_chunk_pair(p, tmQ, tmK, tmV, plan.info.num_groups, stream, &cs));
             } else if (plan.info.tile_m == kChunkPairTileM)
-                YOCO_CUDA_TRY(launch_chunk_pair(p, tmQ, tmK, tmV, plan.info.num_groups, stream));
+                YOCO_CUDA_TRY(launch_chunk_pair(p, tmQ, tmK, tmV, plan.info.num_groups, stream, nullptr, paged != nullptr));
             else
-                YOCO_CUDA_TRY(launch_chunk(p, tmQ, tmK, tmV, plan.info.num_groups, stream));
+                YOCO_CUDA_TRY(launch_chunk(p, tmQ, tmK, tmV, plan.info.num_groups, stream, paged != nullptr));
         }
         if (prof) {
             ev = prof_event(true, &prof);

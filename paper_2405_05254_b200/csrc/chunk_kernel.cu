@@ -12,6 +12,7 @@
 // All shared-memory operand tiles use the 128-byte swizzle that TMA writes and the tensor-core
 // descriptors read.  Every wait is bounded and reports through the status word.
 #include "kernels.h"
+#include "page_map.cuh"
 #include "ptx.cuh"
 #include "tcgen05.cuh"
 
@@ -40,7 +41,8 @@ struct CCfg {
     static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16;
 };
 
-template <int D>
+// PAGED: the rows of a tile are found through a page table (page_map.cuh); each cursor keeps its own place in it.
+template <int D, bool PAGED>
 __global__ void __launch_bounds__(kThreads, 1)
 chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
              const __grid_constant__ CUtensorMap tmV, const ChunkParams p) {
@@ -112,6 +114,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             struct Cursor {
                 int si, k0, k_end, row0;       // segment, next key, end of the segment's keys, K/V row of key 0
                 bool fresh;                    // the segment's Q has not been requested yet (K cursor)
+                PageCursor<BN, 1> pc;             // paged cache
             };
             auto enter = [&](Cursor& c) {      // c.si < seg_hi: read the segment
                 const DevSegment sg = p.segments[c.si];
@@ -119,8 +122,18 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                 c.k_end = sg.k_end;
                 c.row0 = sg.kv_row0 - sg.k_begin;
                 c.fresh = true;
+                if (PAGED) c.pc.start(p.pages, sg.stream, sg.k_begin, sg.k_end);
             };
-            Cursor ck{seg_lo, 0, 0, 0, false}, cv{seg_lo, 0, 0, 0, false};
+            auto load_pages = [&](Cursor& c, uint8_t* tile, const CUtensorMap& tm, uint64_t* bar) {
+                mbar_expect_tx(bar, c.pc.rows() * (D * 2));
+                c.pc.for_each_box(ab.status, [&](int dst_row, int row) {
+                    for (int h = 0; h < HALVES; ++h)
+                        tma_load_2d(tile + h * HALF_BYTES + dst_row * 128, &tm, h * 64, row, bar);
+                });
+                c.pc.next();
+            };
+            Cursor ck{}, cv{};
+            ck.si = cv.si = seg_lo;
             if (seg_lo < seg_hi) {
                 enter(ck);
                 enter(cv);
@@ -148,9 +161,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                     } else if (mbar_try_wait(&k_empty[k_armed & 1u], ((k_armed >> 1) & 1u) ^ 1u)) {
                         const uint32_t b = k_armed & 1u;
                         ++k_armed;
-                        mbar_expect_tx(&k_full[b], C::TILE_BYTES);
-                        for (int h = 0; h < HALVES; ++h)
-                            tma_load_2d(smem + C::OFF_K + b * C::TILE_BYTES + h * HALF_BYTES, &tmK, h * 64, ck.row0 + ck.k0, &k_full[b]);
+                        if (PAGED) {
+                            load_pages(ck, smem + C::OFF_K + b * C::TILE_BYTES, tmK, &k_full[b]);
+                        } else {
+                            mbar_expect_tx(&k_full[b], C::TILE_BYTES);
+                            for (int h = 0; h < HALVES; ++h)
+                                tma_load_2d(smem + C::OFF_K + b * C::TILE_BYTES + h * HALF_BYTES, &tmK, h * 64, ck.row0 + ck.k0, &k_full[b]);
+                        }
                         ck.k0 += BN;
                         moved = true;
                     }
@@ -162,9 +179,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                     } else if (mbar_try_wait(&v_empty[v_armed & 1u], ((v_armed >> 1) & 1u) ^ 1u)) {
                         const uint32_t b = v_armed & 1u;
                         ++v_armed;
-                        mbar_expect_tx(&v_full[b], C::TILE_BYTES);
-                        for (int h = 0; h < HALVES; ++h)
-                            tma_load_2d(smem + C::OFF_V + b * C::TILE_BYTES + h * HALF_BYTES, &tmV, h * 64, cv.row0 + cv.k0, &v_full[b]);
+                        if (PAGED) {
+                            load_pages(cv, smem + C::OFF_V + b * C::TILE_BYTES, tmV, &v_full[b]);
+                        } else {
+                            mbar_expect_tx(&v_full[b], C::TILE_BYTES);
+                            for (int h = 0; h < HALVES; ++h)
+                                tma_load_2d(smem + C::OFF_V + b * C::TILE_BYTES + h * HALF_BYTES, &tmV, h * 64, cv.row0 + cv.k0, &v_full[b]);
+                        }
                         cv.k0 += BN;
                         moved = true;
                     }
@@ -444,28 +465,36 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
     }
 }
 
-template <int D>
+template <int D, bool PAGED>
 cudaError_t launch_one(const ChunkParams& p, const CUtensorMap& tmQ, const CUtensorMap& tmK,
                        const CUtensorMap& tmV, int num_groups, cudaStream_t stream) {
-    chunk_kernel<D><<<num_groups * p.m_tiles, kThreads, CCfg<D>::SMEM_BYTES, stream>>>(tmQ, tmK, tmV, p);
+    chunk_kernel<D, PAGED><<<num_groups * p.m_tiles, kThreads, CCfg<D>::SMEM_BYTES, stream>>>(tmQ, tmK, tmV, p);
     return cudaGetLastError();
+}
+
+template <int D, bool PAGED>
+cudaError_t setup_one() {
+    return cudaFuncSetAttribute(chunk_kernel<D, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, CCfg<D>::SMEM_BYTES);
 }
 
 }  // namespace
 
 cudaError_t chunk_kernel_setup() {
-    cudaError_t e = cudaFuncSetAttribute(chunk_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         CCfg<128>::SMEM_BYTES);
+    cudaError_t e = setup_one<128, false>();
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(chunk_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                CCfg<64>::SMEM_BYTES);
+    if ((e = setup_one<64, false>()) != cudaSuccess) return e;
+    if ((e = setup_one<128, true>()) != cudaSuccess) return e;
+    return setup_one<64, true>();
 }
 
 cudaError_t launch_chunk(const ChunkParams& p, const CUtensorMap& tmQ, const CUtensorMap& tmK,
-                         const CUtensorMap& tmV, int num_groups, cudaStream_t stream) {
+                         const CUtensorMap& tmV, int num_groups, cudaStream_t stream, bool paged) {
     if (num_groups <= 0) return cudaSuccess;
-    return p.d == 128 ? launch_one<128>(p, tmQ, tmK, tmV, num_groups, stream)
-                      : launch_one<64>(p, tmQ, tmK, tmV, num_groups, stream);
+    if (paged)
+        return p.d == 128 ? launch_one<128, true>(p, tmQ, tmK, tmV, num_groups, stream)
+                          : launch_one<64, true>(p, tmQ, tmK, tmV, num_groups, stream);
+    return p.d == 128 ? launch_one<128, false>(p, tmQ, tmK, tmV, num_groups, stream)
+                      : launch_one<64, false>(p, tmQ, tmK, tmV, num_groups, stream);
 }
 
 }  // namespace yoco

@@ -28,10 +28,18 @@
 // half goes, so a thread only ever overwrites its own source row), Q is converted bf16 -> fp16 in
 // place once per segment, P is rounded to fp16, and all products run fp16 x fp16.  k_scale folds
 // into the softmax scale, v_scale multiplies the normalised output.
+//
+// A paged cache (kPaged16: bf16 rows, kPaged4: 4-bit rows) differs in where the producer finds the rows of a tile
+// (page_map.cuh).  4-bit rows take the way of the 8-bit cache: the 32 rows of a widening warp land, codes and scales,
+// inside the part of the upper half tile that the same warp's fp16 rows will fill, so a warp has read all of its
+// source (one __syncwarp) before it overwrites any of it, and no two warps meet.  A value (code - 8) * scale is
+// rounded to fp16 once (half a step, 2^-11).
 #include <cuda_fp16.h>
 
 #include "kernels.h"
+#include "page_map.cuh"
 #include "ptx.cuh"
+#include "q4.cuh"
 #include "tcgen05.cuh"
 
 namespace yoco {
@@ -41,9 +49,16 @@ namespace {
 constexpr int BM = 128;                        // rows of one tensor-core tile
 constexpr int BN = kChunkTileN;                // 128 keys per shared-memory tile
 constexpr int BH = BN / 2;                     // keys per half step
-// three warpgroups for a bf16 cache; a fourth one widens the tiles of an 8-bit cache
+enum CacheKind { kPacked16, kPacked8, kPaged16, kPaged4 };
+// caches whose tiles are widened to fp16 on the way
+__host__ __device__ constexpr bool widened(CacheKind kind) { return kind == kPacked8 || kind == kPaged4; }
+// three warpgroups for a bf16 cache; a fourth one widens the tiles of a narrow cache
 template <bool FP8>
 constexpr int kThreadsOf = FP8 ? 512 : 384;
+// a widening warp's share of a 4-bit tile as it arrives: 32 rows of codes, then their scales
+constexpr int Q4_WARP_STRIDE = 32 * 128;       // from one warp's share to the next: its rows of the half tile
+constexpr int Q4_OFF_SCALE = 32 * 64;
+constexpr int Q4_ROW_BYTES = 64 + 8;
 constexpr int HALF_BYTES = 128 * 128;          // 128 rows x 64 bf16: one swizzled half tile
 constexpr uint32_t TMEM_COLS = 512;
 constexpr float kRescaleThreshold = 8.f;       // in log2 units: P stays below 2^8
@@ -96,12 +111,15 @@ __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {
     return pack_f16x2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
 }
 
-template <int D, bool FP8>
-__global__ void __launch_bounds__(kThreadsOf<FP8>, 1)
+// tmKs, tmVs: maps of the scales of 4-bit rows (otherwise not read)
+template <int D, CacheKind KIND>
+__global__ void __launch_bounds__(kThreadsOf<widened(KIND)>, 1)
 chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                  const __grid_constant__ CUtensorMap tmV, const ChunkParams p,
+                  const __grid_constant__ CUtensorMap tmKs, const __grid_constant__ CUtensorMap tmV,
+                  const __grid_constant__ CUtensorMap tmVs, const ChunkParams p,
                   const __grid_constant__ ChunkFp8Scales sc) {
-    static_assert(!FP8 || D == 128, "the 8-bit cache path is built for head dimension 128");
+    constexpr bool FP8 = widened(KIND);            // fp16 products, widening warpgroup
+    static_assert(!FP8 || D == 128, "the narrow cache paths are built for head dimension 128");
     using C = PCfg<D>;
     constexpr int HALVES = C::HALVES;
     constexpr int KS = C::K_STAGES, VS = C::V_STAGES;
@@ -189,12 +207,38 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     for (int h = 0; h < HALVES; ++h)
                         tma_load_2d(smem + C::OFF_Q + r * C::TILE_BYTES + h * HALF_BYTES, &tmQ, h * 64,
                                     seg.q_row0 + (m_tile * 2 + r) * BM, q_full);
+                PageCursor<BN, 1> pc;
+                if (KIND == kPaged16 || KIND == kPaged4) pc.start(p.pages, seg.stream, seg.k_begin, seg.k_end);
+                // the boxes of one tile of a paged cache
+                auto load_pages = [&](uint8_t* tile, const CUtensorMap& tm, const CUtensorMap& tmS, uint64_t* bar) {
+                    const int P = 1 << p.pages.page_shift;
+                    if (KIND == kPaged4) {
+                        mbar_expect_tx(bar, pc.rows() * Q4_ROW_BYTES);
+                        const int box = min(P, 32), n = min(P, BN);      // no box spans two widening warps' rows
+                        pc.for_each_box(ab.status, [&](int dst_row, int row) {
+                            for (int i = 0; i < n; i += box) {
+                                const int at = dst_row + i;
+                                uint8_t* dst = tile + HALF_BYTES + (at >> 5) * Q4_WARP_STRIDE;
+                                tma_load_2d(dst + (at & 31) * 64, &tm, 0, row + i, bar);
+                                tma_load_2d(dst + Q4_OFF_SCALE + (at & 31) * 8, &tmS, 0, (row + i) >> 4, bar);
+                            }
+                        });
+                    } else {
+                        mbar_expect_tx(bar, pc.rows() * (D * 2));
+                        pc.for_each_box(ab.status, [&](int dst_row, int row) {
+                            for (int h = 0; h < HALVES; ++h)
+                                tma_load_2d(tile + h * HALF_BYTES + dst_row * 128, &tm, h * 64, row, bar);
+                        });
+                    }
+                };
                 for (int k0 = seg.k_begin; k0 < seg.k_end; k0 += BN, ++it) {
                     const int row = seg.kv_row0 + (k0 - seg.k_begin);
                     const uint32_t kb = it % KS, kn = it / KS;
                     if (!(ok = wait_or_abort(&k_empty[kb], (kn & 1u) ^ 1u, ab, kWaitRingEmpty))) break;
                     ++k_armed;
-                    if (FP8) {      // 128 keys x 128 bytes into the upper half of the stage
+                    if (KIND == kPaged16 || KIND == kPaged4) {
+                        load_pages(smem + C::OFF_K + kb * C::TILE_BYTES, tmK, tmKs, &k_full[kb]);
+                    } else if (FP8) {      // 128 keys x 128 bytes into the upper half of the stage
                         mbar_expect_tx(&k_full[kb], HALF_BYTES);
                         tma_load_2d(smem + C::OFF_K + kb * C::TILE_BYTES + HALF_BYTES, &tmK, 0, row, &k_full[kb]);
                     } else {
@@ -206,7 +250,10 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     const uint32_t vb = it % VS, vn = it / VS;
                     if (!(ok = wait_or_abort(&v_empty[vb], (vn & 1u) ^ 1u, ab, kWaitRingEmpty))) break;
                     ++v_armed;
-                    if (FP8) {
+                    if (KIND == kPaged16 || KIND == kPaged4) {
+                        load_pages(smem + C::OFF_V + vb * C::TILE_BYTES, tmV, tmVs, &v_full[vb]);
+                        pc.next();
+                    } else if (FP8) {
                         mbar_expect_tx(&v_full[vb], HALF_BYTES);
                         tma_load_2d(smem + C::OFF_V + vb * C::TILE_BYTES + HALF_BYTES, &tmV, 0, row, &v_full[vb]);
                     } else {
@@ -320,7 +367,31 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             // c ^ (r & 7)); the fp16 row goes out in the same swizzle, channels 0-63 to row r of the lower
             // half tile and 64-127 to row r of the upper one, i.e. over the bytes just read.
             auto widen_tile = [&](uint8_t* tile) {
-                {
+                if (KIND == kPaged4) {
+                    const int rr = wq * 32 + lane;
+                    const uint8_t* src = tile + HALF_BYTES + wq * Q4_WARP_STRIDE;
+                    uint4 raw[4];          // 32 channels each; 64-byte swizzle: chunk c at position c ^ ((row / 2) & 3)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        raw[c] = *reinterpret_cast<const uint4*>(src + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4));
+                    const uint2 sw = *reinterpret_cast<const uint2*>(src + Q4_OFF_SCALE + lane * 8);
+                    const uint32_t s2[4] = {__byte_perm(sw.x, 0u, 0x1010), __byte_perm(sw.x, 0u, 0x3232),
+                                            __byte_perm(sw.y, 0u, 0x1010), __byte_perm(sw.y, 0u, 0x3232)};
+                    __syncwarp();          // every lane has its source before any row is written
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {                // channels 32 c + 8 q .. + 7: one 16-byte chunk
+                            const uint32_t l0 = q4_signed_lo(w[q]), h0 = q4_signed_hi(w[q]);             // (0, 4), (1, 5)
+                            const uint32_t l1 = q4_signed_lo(w[q] >> 8), h1 = q4_signed_hi(w[q] >> 8);   // (2, 6), (3, 7)
+                            const uint4 f = make_uint4(h2_mul(__byte_perm(l0, h0, 0x5410), s2[c]), h2_mul(__byte_perm(l1, h1, 0x5410), s2[c]),
+                                                       h2_mul(__byte_perm(l0, h0, 0x7632), s2[c]), h2_mul(__byte_perm(l1, h1, 0x7632), s2[c]));
+                            const int c0 = (c & 1) * 4 + q;
+                            *reinterpret_cast<uint4*>(tile + (c >> 1) * HALF_BYTES + rr * 128 + ((c0 ^ (rr & 7)) << 4)) = f;
+                        }
+                    }
+                } else {
                     const int rr = wq * 32 + lane;
                     uint8_t* src = tile + HALF_BYTES + rr * 128;
                     uint4 raw[8];
@@ -424,9 +495,9 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             const uint32_t seg_first_it = it, seg_first_u = 2 * it;
             // 8-bit cache: the key scale of this KV head folds into the softmax scale, the value scale
             // multiplies the normalised output
-            const int head = FP8 ? seg.stream % sc.Hkv : 0;
-            const float scale_log2 = FP8 ? sc.score_scale_log2[head] : p.scale_log2;
-            const float out_scale = FP8 ? sc.v_scale[head] : 1.f;
+            const int head = KIND == kPacked8 ? seg.stream % sc.Hkv : 0;
+            const float scale_log2 = KIND == kPacked8 ? sc.score_scale_log2[head] : p.scale_log2;
+            const float out_scale = KIND == kPacked8 ? sc.v_scale[head] : 1.f;
             for (int k0 = seg.k_begin; k0 < seg.k_end; k0 += BN, ++it) {
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
@@ -607,44 +678,60 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     }
 }
 
-template <int D, bool FP8>
-cudaError_t launch_one(const ChunkParams& p, const CUtensorMap& tmQ, const CUtensorMap& tmK,
-                       const CUtensorMap& tmV, int num_groups, cudaStream_t stream, const ChunkFp8Scales& sc) {
-    chunk_pair_kernel<D, FP8><<<num_groups * p.m_tiles, kThreadsOf<FP8>, PCfg<D>::SMEM_BYTES, stream>>>(tmQ, tmK, tmV, p, sc);
+template <int D, CacheKind KIND>
+cudaError_t launch_one(const ChunkParams& p, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmKs,
+                       const CUtensorMap& tmV, const CUtensorMap& tmVs, int num_groups, cudaStream_t stream,
+                       const ChunkFp8Scales& sc) {
+    chunk_pair_kernel<D, KIND><<<num_groups * p.m_tiles, kThreadsOf<widened(KIND)>, PCfg<D>::SMEM_BYTES, stream>>>(
+        tmQ, tmK, tmKs, tmV, tmVs, p, sc);
     return cudaGetLastError();
 }
 
-template <int D, bool FP8>
+template <int D, CacheKind KIND>
 cudaError_t setup_one() {
-    cudaError_t e = cudaFuncSetAttribute(chunk_pair_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    cudaError_t e = cudaFuncSetAttribute(chunk_pair_kernel<D, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          PCfg<D>::SMEM_BYTES);
     if (e != cudaSuccess) return e;
     // the register split inside the kernel assumes the launch allocation it was written for
     cudaFuncAttributes attr;
-    if ((e = cudaFuncGetAttributes(&attr, chunk_pair_kernel<D, FP8>)) != cudaSuccess) return e;
-    return attr.numRegs >= Regs<FP8>::kLaunch ? cudaSuccess : cudaErrorLaunchOutOfResources;
+    if ((e = cudaFuncGetAttributes(&attr, chunk_pair_kernel<D, KIND>)) != cudaSuccess) return e;
+    return attr.numRegs >= Regs<widened(KIND)>::kLaunch ? cudaSuccess : cudaErrorLaunchOutOfResources;
 }
 
 }  // namespace
 
 cudaError_t chunk_pair_kernel_setup() {
-    cudaError_t e = setup_one<128, false>();
+    cudaError_t e = setup_one<128, kPacked16>();
     if (e != cudaSuccess) return e;
-    if ((e = setup_one<64, false>()) != cudaSuccess) return e;
-    return setup_one<128, true>();
+    if ((e = setup_one<64, kPacked16>()) != cudaSuccess) return e;
+    if ((e = setup_one<128, kPacked8>()) != cudaSuccess) return e;
+    if ((e = setup_one<128, kPaged16>()) != cudaSuccess) return e;
+    if ((e = setup_one<64, kPaged16>()) != cudaSuccess) return e;
+    return setup_one<128, kPaged4>();
 }
 
 cudaError_t launch_chunk_pair(const ChunkParams& p, const CUtensorMap& tmQ, const CUtensorMap& tmK,
                               const CUtensorMap& tmV, int num_groups, cudaStream_t stream,
-                              const ChunkFp8Scales* fp8_scales) {
+                              const ChunkFp8Scales* fp8_scales, bool paged) {
     if (num_groups <= 0) return cudaSuccess;
     if (fp8_scales) {
         if (p.d != 128) return cudaErrorInvalidValue;
-        return launch_one<128, true>(p, tmQ, tmK, tmV, num_groups, stream, *fp8_scales);
+        return launch_one<128, kPacked8>(p, tmQ, tmK, tmK, tmV, tmV, num_groups, stream, *fp8_scales);
     }
     const ChunkFp8Scales none{};
-    return p.d == 128 ? launch_one<128, false>(p, tmQ, tmK, tmV, num_groups, stream, none)
-                      : launch_one<64, false>(p, tmQ, tmK, tmV, num_groups, stream, none);
+    if (paged)
+        return p.d == 128 ? launch_one<128, kPaged16>(p, tmQ, tmK, tmK, tmV, tmV, num_groups, stream, none)
+                          : launch_one<64, kPaged16>(p, tmQ, tmK, tmK, tmV, tmV, num_groups, stream, none);
+    return p.d == 128 ? launch_one<128, kPacked16>(p, tmQ, tmK, tmK, tmV, tmV, num_groups, stream, none)
+                      : launch_one<64, kPacked16>(p, tmQ, tmK, tmK, tmV, tmV, num_groups, stream, none);
+}
+
+cudaError_t launch_chunk_pair_q4(const ChunkParams& p, const CUtensorMap& tmQ, const PagedQ4Maps& m, int num_groups,
+                                 cudaStream_t stream) {
+    if (num_groups <= 0) return cudaSuccess;
+    if (p.d != 128) return cudaErrorInvalidValue;
+    const ChunkFp8Scales none{};
+    return launch_one<128, kPaged4>(p, tmQ, m.k, m.k_scale, m.v, m.v_scale, num_groups, stream, none);
 }
 
 }  // namespace yoco

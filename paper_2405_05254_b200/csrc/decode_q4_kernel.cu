@@ -24,6 +24,7 @@
 #include "kernels.h"
 #include "page_map.cuh"
 #include "ptx.cuh"
+#include "q4.cuh"
 
 namespace yoco {
 
@@ -62,27 +63,6 @@ __device__ __forceinline__ void mma_f16_from(float (&d)[4], const float (&c)[2],
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]));
 }
-__device__ __forceinline__ float2 h2_to_f2(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
-__device__ __forceinline__ uint32_t h2_mul(uint32_t a, uint32_t b) {
-    __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-    return *reinterpret_cast<uint32_t*>(&r);
-}
-// two codes at bits 0-3 and 16-19 -> (n - 8) as fp16, exact
-__device__ __forceinline__ uint32_t signed_lo(uint32_t w) {
-    const uint32_t x = (w & 0x000F000Fu) | 0x64006400u;               // 1024 + n
-    const uint32_t off = 0xE408E408u;                                 // -1032
-    __half2 r = __hadd2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&off));
-    return *reinterpret_cast<uint32_t*>(&r);
-}
-// two codes at bits 4-7 and 20-23 -> (n - 8)
-__device__ __forceinline__ uint32_t signed_hi(uint32_t w) {
-    const uint32_t x = (w & 0x00F000F0u) | 0x64006400u;               // 1024 + 16 n
-    const uint32_t sixteenth = 0x2C002C00u, off = 0xD480D480u;        // 1/16, -72
-    __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&sixteenth),
-                        *reinterpret_cast<const __half2*>(&off));
-    return *reinterpret_cast<uint32_t*>(&r);
-}
-
 template <int ROWS>
 __device__ __forceinline__ void decode_q4_body(const CUtensorMap& tmK, const CUtensorMap& tmKs, const CUtensorMap& tmV,
                                                const CUtensorMap& tmVs, const DecodeParams& p,
@@ -444,8 +424,8 @@ __device__ __forceinline__ void decode_q4_body(const CUtensorMap& tmK, const CUt
                     for (int h = 0; h < 2; ++h) {
                         const int j = 2 * jj + h;
                         const uint32_t a = r[2 * h], b = r[2 * h + 1], a8 = a >> 8, b8 = b >> 8;
-                        const uint32_t a0 = signed_lo(a), a1 = signed_hi(a), a2 = signed_lo(b), a3 = signed_hi(b);
-                        const uint32_t c0 = signed_lo(a8), c1 = signed_hi(a8), c2 = signed_lo(b8), c3 = signed_hi(b8);
+                        const uint32_t a0 = q4_signed_lo(a), a1 = q4_signed_hi(a), a2 = q4_signed_lo(b), a3 = q4_signed_hi(b);
+                        const uint32_t c0 = q4_signed_lo(a8), c1 = q4_signed_hi(a8), c2 = q4_signed_lo(b8), c3 = q4_signed_hi(b8);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             const uint32_t p0 = h2_mul(pb[nt][kg][0], sv[0][j]), p1 = h2_mul(pb[nt][kg][1], sv[1][j]);

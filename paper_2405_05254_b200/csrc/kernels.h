@@ -163,10 +163,11 @@ struct ChunkParams {
 // Grid = num_groups * m_tiles CTAs, the row tile varying fastest so that the CTAs that walk the
 // same K/V range run side by side and share it through L2.
 cudaError_t launch_chunk(const ChunkParams& p, const CUtensorMap& tmQ, const CUtensorMap& tmK,
-                         const CUtensorMap& tmV, int num_groups, cudaStream_t stream);
+                         const CUtensorMap& tmV, int num_groups, cudaStream_t stream, bool paged = false);
 cudaError_t chunk_kernel_setup();
 // Same interface for streams with more than 128 rows: one CTA owns two 128-row tiles (m_tiles =
 // ceil(rows_per_stream / 256)), tmQ box is still {64, 128}.
+// paged: rows are found through p.pages, tmK / tmV boxes are {64, min(P, kChunkTileN)}.
 // fp8_scales (host, may be null): K and V are an 8-bit cache (tmK / tmV then are uint8 maps over the
 // [rows, 128] byte view, box {128, kChunkTileN}); head dimension 128 only.
 struct ChunkFp8Scales {
@@ -176,7 +177,10 @@ struct ChunkFp8Scales {
 };
 cudaError_t launch_chunk_pair(const ChunkParams& p, const CUtensorMap& tmQ, const CUtensorMap& tmK,
                               const CUtensorMap& tmV, int num_groups, cudaStream_t stream,
-                              const ChunkFp8Scales* fp8_scales = nullptr);
+                              const ChunkFp8Scales* fp8_scales = nullptr, bool paged = false);
+// The same over 4-bit pages, maps with boxes of min(P, 32) rows.
+cudaError_t launch_chunk_pair_q4(const ChunkParams& p, const CUtensorMap& tmQ, const PagedQ4Maps& maps, int num_groups,
+                                 cudaStream_t stream);
 cudaError_t chunk_pair_kernel_setup();
 
 // ---- writing the cache: K^ = RMSNorm(X) W_K, V^ = RMSNorm(X) W_V appended head-major ------------

@@ -18,12 +18,11 @@ __device__ __forceinline__ int page_row(const PageMap& pm, int page, int head, i
 }
 
 // The producer's position in a run of TILE-key tiles of one (sequence, KV head) stream.  The page numbers of
-// the next two tiles are already requested when a tile's copies are issued, so that a table read is
+// the next AHEAD tiles are already requested when a tile's copies are issued, so that a table read is
 // not waited for between two copies.
-template <int TILE>
+template <int TILE, int AHEAD = 2>
 struct PageCursor {
     static constexpr int MAX_IDS = TILE / 16;      // pages hold at least 16 keys
-    static constexpr int AHEAD = 2;
     const PageMap* pm;
     const int32_t* entries;                        // this sequence's row of the table
     int head, k0, k_hi;

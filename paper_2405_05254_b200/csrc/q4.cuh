@@ -1,0 +1,31 @@
+// 4-bit codes to fp16 without conversion instructions, and fp16 pairs.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include <cstdint>
+
+namespace yoco {
+
+__device__ __forceinline__ float2 h2_to_f2(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+__device__ __forceinline__ uint32_t h2_mul(uint32_t a, uint32_t b) {
+    __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<uint32_t*>(&r);
+}
+// two codes at bits 0-3 and 16-19 -> (n - 8) as fp16, exact
+__device__ __forceinline__ uint32_t q4_signed_lo(uint32_t w) {
+    const uint32_t x = (w & 0x000F000Fu) | 0x64006400u;               // 1024 + n
+    const uint32_t off = 0xE408E408u;                                 // -1032
+    __half2 r = __hadd2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&off));
+    return *reinterpret_cast<uint32_t*>(&r);
+}
+// two codes at bits 4-7 and 20-23 -> (n - 8)
+__device__ __forceinline__ uint32_t q4_signed_hi(uint32_t w) {
+    const uint32_t x = (w & 0x00F000F0u) | 0x64006400u;               // 1024 + 16 n
+    const uint32_t sixteenth = 0x2C002C00u, off = 0xD480D480u;        // 1/16, -72
+    __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&sixteenth),
+                        *reinterpret_cast<const __half2*>(&off));
+    return *reinterpret_cast<uint32_t*>(&r);
+}
+
+}  // namespace yoco

@@ -1,9 +1,9 @@
 """The paged cache on the GPU: append with rotation (bf16 and 4-bit rows), read-back, rotation of the queries, and
-decode attention, against plain numpy (bit for bit where every rounding is fixed by the definition, in 64 bits otherwise).
+decode and chunk attention, against plain numpy (bit for bit where every rounding is fixed by the definition, in 64 bits otherwise).
 
 Tolerances of the attention tests are those of the packed paths (helpers.py).  What the 4-bit path adds: P * s is rounded to
 fp16, half a step 2^-11 relative per term, below the bf16 half step 2^-9 that the bf16 path has there; the codes are exact,
-the scores are fp32 sums of exact products.  The output's bf16 half step (2^-9) stays the largest single term."""
+the decode scores are fp32 sums of exact products, the chunk path's K and V values are rounded to fp16 once (2^-11).  The output's bf16 half step (2^-9) stays the largest single term."""
 import numpy as np
 import pytest
 
@@ -169,6 +169,47 @@ def test_decode_matches_the_definition(q4, lens, Hq, Hkv, T, P, window, d):
     assert_lse_close(lse, lref, "LSE")
 
 
+CHUNK = [
+    # lens, Hq, Hkv, T, P, window, d
+    ([1], 1, 1, 1, 16, 0, 128),
+    ([5, 0, 127], 4, 2, 3, 16, 0, 64),                 # an empty sequence, T > N in none
+    ([100, 128, 129], 8, 2, 30, 32, 0, 128),           # 120 rows: the one-tile kernel
+    ([300], 12, 4, 50, 64, 0, 128),                    # 150 rows: two tiles
+    ([700, 90], 8, 2, 100, 128, 33, 128),              # 400 rows, window; more rows than keys
+    ([5000, 1300], 16, 4, 65, 256, 0, 128),            # split and merged
+    ([2600], 8, 8, 300, 16, 0, 64),
+    ([3001, 40], 32, 8, 40, 16, 0, 128),               # 160 rows per KV head, small pages
+    ([9000, 2000], 4, 1, 9, 64, 500, 128),             # few rows, window, split
+]
+
+
+@pytest.mark.parametrize("q4", [False, True])
+@pytest.mark.parametrize("lens,Hq,Hkv,T,P,window,d", CHUNK)
+def test_chunk_matches_the_definition(q4, lens, Hq, Hkv, T, P, window, d):
+    d = 128 if q4 else d
+    cache = pr.PagedCache(12, lens, P, Hkv, d, q4)
+    dev = pr.DevCache(cache)
+    Q = q_bits(12, len(lens), Hq, T, d)
+    o, lse, _ = dev.attend(Q, T, mode="chunk", window=window)
+    assert dev.status[0] == 0
+    ref, lref = pr.attention(cache, f64(Q), T, window=window)
+    assert_close(o, ref, "O")
+    assert_lse_close(lse, lref, "LSE")
+
+
+@pytest.mark.parametrize("T,d", [(5, 64), (60, 128), (90, 64), (110, 128)])
+def test_chunk_bf16_gives_the_bits_of_the_packed_cache(T, d):
+    from helpers import GpuRunner
+    lens, H, Hq = [1500, 177], 2, 8
+    cache = pr.PagedCache(14, lens, 32, H, d, False)
+    packed = [np.concatenate([np.concatenate([pr.bf16(cache.rows(w, b, h))[0].reshape(-1) for h in range(H)]) for b in range(len(lens))])
+              for w in range(2)]
+    Q = q_bits(14, len(lens), Hq, T, d)
+    o, lse, O = pr.DevCache(cache).attend(Q, T, mode="chunk")
+    po, plse, PO = GpuRunner(len(lens), Hq, H, d, T, lens, packed[0], packed[1]).run(Q, mode="chunk")
+    assert np.array_equal(pr.dev_bits(O), pr.dev_bits(PO)) and np.array_equal(lse, plse)
+
+
 def test_decode_bf16_gives_the_bits_of_the_packed_cache():
     """Same tiles, same plan: a paged cache with the same rows gives the same output bits as the packed one."""
     from helpers import GpuRunner
@@ -230,7 +271,7 @@ def test_pages_shared_by_sequences_and_pools_side_by_side(q4):
     assert_lse_close(lse, lref)
 
 
-@pytest.mark.parametrize("mode", ["decode"])
+@pytest.mark.parametrize("mode", ["decode", "chunk"])
 @pytest.mark.parametrize("q4", [False, True])
 def test_a_bad_page_is_reported_and_harms_nobody_else(q4, mode):
     """Entries outside the pool are read as zeros: the call returns, says BAD_PAGE, the other sequence is right."""
