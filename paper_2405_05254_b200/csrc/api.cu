@@ -244,8 +244,8 @@ int32_t make_q4_maps(PagedQ4Maps* m, const void* K, const void* k_scale, const v
                      const PageMap& pages, int32_t tile) {
     const int32_t box = std::min(1 << pages.page_shift, tile);
     int32_t rc;
-    if ((rc = make_map(&m->k, K, pages.rows, 64, 64, box, false, CU_TENSOR_MAP_SWIZZLE_64B)) != YOCO_OK) return rc;
-    if ((rc = make_map(&m->v, V, pages.rows, 64, 64, box, false, CU_TENSOR_MAP_SWIZZLE_64B)) != YOCO_OK) return rc;
+    if ((rc = make_map(&m->k, K, pages.rows / 2, 128, 128, box / 2, false, CU_TENSOR_MAP_SWIZZLE_128B)) != YOCO_OK) return rc;
+    if ((rc = make_map(&m->v, V, pages.rows / 2, 128, 128, box / 2, false, CU_TENSOR_MAP_SWIZZLE_128B)) != YOCO_OK) return rc;
     if ((rc = make_map(&m->k_scale, k_scale, pages.rows / 16, 128, 128, box / 16, false, CU_TENSOR_MAP_SWIZZLE_NONE)) != YOCO_OK)
         return rc;
     return make_map(&m->v_scale, v_scale, pages.rows / 16, 128, 128, box / 16, false, CU_TENSOR_MAP_SWIZZLE_NONE);

@@ -102,10 +102,17 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
 
     if (warp == 0) {
         // ======================================= TMA producer ================================
-        if (lane == 0 && aligned_ok) {
-            tma_prefetch_desc(&tmQ);
-            tma_prefetch_desc(&tmK);
-            tma_prefetch_desc(&tmV);
+        if ((PAGED || lane == 0) && aligned_ok) {
+            if (lane == 0) {
+                tma_prefetch_desc(&tmQ);
+                tma_prefetch_desc(&tmK);
+                tma_prefetch_desc(&tmV);
+            }
+            // one answer for the whole warp where the whole warp walks (paged cache)
+            auto is_free = [&](uint64_t* bar, uint32_t parity) {
+                const bool r = mbar_try_wait(bar, parity);
+                return PAGED ? __all_sync(0xffffffffu, r) != 0 : r;
+            };
             // Two cursors walk the tiles of the group, one for K (which also brings a segment's Q, ahead of
             // its first K tile) and one for V, each as far ahead as its ring has room: the score
             // product frees a K stage long before the second product frees the V stage of the same
@@ -114,7 +121,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             struct Cursor {
                 int si, k0, k_end, row0;       // segment, next key, end of the segment's keys, K/V row of key 0
                 bool fresh;                    // the segment's Q has not been requested yet (K cursor)
-                PageCursor<BN, 1> pc;             // paged cache
+                PageCursor<BN> pc;                // paged cache
             };
             auto enter = [&](Cursor& c) {      // c.si < seg_hi: read the segment
                 const DevSegment sg = p.segments[c.si];
@@ -122,15 +129,19 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                 c.k_end = sg.k_end;
                 c.row0 = sg.kv_row0 - sg.k_begin;
                 c.fresh = true;
-                if (PAGED) c.pc.start(p.pages, sg.stream, sg.k_begin, sg.k_end);
+                if (PAGED) c.pc.start(p.pages, sg.stream, sg.k_begin, sg.k_end, ab.status);
             };
             auto load_pages = [&](Cursor& c, uint8_t* tile, const CUtensorMap& tm, uint64_t* bar) {
-                mbar_expect_tx(bar, c.pc.rows() * (D * 2));
-                c.pc.for_each_box(ab.status, [&](int dst_row, int row) {
-                    for (int h = 0; h < HALVES; ++h)
-                        tma_load_2d(tile + h * HALF_BYTES + dst_row * 128, &tm, h * 64, row, bar);
-                });
-                c.pc.next();
+                const int n_box = c.pc.enter(c.k0), rows = c.pc.box_rows();
+                for (int j = 0; j < n_box; ++j) {
+                    const int row = c.pc.row(c.k0, j);
+                    if (elect_one()) {
+                        if (j == 0) mbar_expect_tx(bar, n_box * rows * (D * 2));
+                        for (int h = 0; h < HALVES; ++h)
+                            tma_load_2d(tile + h * HALF_BYTES + j * rows * 128, &tm, h * 64, row, bar);
+                    }
+                    __syncwarp();
+                }
             };
             Cursor ck{}, cv{};
             ck.si = cv.si = seg_lo;
@@ -146,19 +157,21 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                 bool moved = false;
                 if (ck.si < seg_hi) {
                     if (ck.fresh) {            // every segment, also one without keys, gets its Q (the others wait for it)
-                        if (mbar_try_wait(q_empty, (q_armed & 1u) ^ 1u)) {
+                        if (is_free(q_empty, (q_armed & 1u) ^ 1u)) {
                             ++q_armed;
-                            mbar_expect_tx(q_full, C::TILE_BYTES);
-                            for (int h = 0; h < HALVES; ++h)
-                                tma_load_2d(smem + C::OFF_Q + h * HALF_BYTES, &tmQ, h * 64,
-                                            p.segments[ck.si].q_row0 + m_tile * BM, q_full);
+                            if (lane == 0) {
+                                mbar_expect_tx(q_full, C::TILE_BYTES);
+                                for (int h = 0; h < HALVES; ++h)
+                                    tma_load_2d(smem + C::OFF_Q + h * HALF_BYTES, &tmQ, h * 64,
+                                                p.segments[ck.si].q_row0 + m_tile * BM, q_full);
+                            }
                             ck.fresh = false;
                             moved = true;
                         }
                     } else if (ck.k0 >= ck.k_end) {
                         if (++ck.si < seg_hi) enter(ck);
                         moved = true;
-                    } else if (mbar_try_wait(&k_empty[k_armed & 1u], ((k_armed >> 1) & 1u) ^ 1u)) {
+                    } else if (is_free(&k_empty[k_armed & 1u], ((k_armed >> 1) & 1u) ^ 1u)) {
                         const uint32_t b = k_armed & 1u;
                         ++k_armed;
                         if (PAGED) {
@@ -176,7 +189,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                     if (cv.k0 >= cv.k_end) {
                         if (++cv.si < seg_hi) enter(cv);
                         moved = true;
-                    } else if (mbar_try_wait(&v_empty[v_armed & 1u], ((v_armed >> 1) & 1u) ^ 1u)) {
+                    } else if (is_free(&v_empty[v_armed & 1u], ((v_armed >> 1) & 1u) ^ 1u)) {
                         const uint32_t b = v_armed & 1u;
                         ++v_armed;
                         if (PAGED) {
@@ -200,14 +213,15 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                         report_give_up(ab, kWaitRingEmpty);
                         ok = false;
                     }
+                    if (PAGED) ok = __all_sync(0xffffffffu, ok) != 0;
                 }
             }
             // Every copy this thread started must have landed before the CTA may end (at once when all
             // went well: the tiles were consumed long ago).
-            bool drained = q_armed == 0 || drain_wait(q_full, (q_armed - 1) & 1u, ab);
-            for (uint32_t k = k_armed > 2 ? k_armed - 2 : 0; drained && k < k_armed; ++k)
+            bool drained = lane != 0 || q_armed == 0 || drain_wait(q_full, (q_armed - 1) & 1u, ab);
+            for (uint32_t k = k_armed > 2 ? k_armed - 2 : 0; lane == 0 && drained && k < k_armed; ++k)
                 drained = drain_wait(&k_full[k & 1u], (k >> 1) & 1u, ab);
-            for (uint32_t k = v_armed > 2 ? v_armed - 2 : 0; drained && k < v_armed; ++k)
+            for (uint32_t k = v_armed > 2 ? v_armed - 2 : 0; lane == 0 && drained && k < v_armed; ++k)
                 drained = drain_wait(&v_full[k & 1u], (k >> 1) & 1u, ab);
         }
     } else if (warp == 1) {

@@ -189,55 +189,65 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 
     if (warp < 4) {
         setmaxnreg_dec<Regs<FP8>::kOther>();
-        if (warp == 0 && lane == 0 && aligned_ok) {
+        constexpr bool PAGED = KIND == kPaged16 || KIND == kPaged4;
+        if (warp == 0 && (PAGED || lane == 0) && aligned_ok) {
             // =================================== TMA producer ================================
-            tma_prefetch_desc(&tmQ);
-            tma_prefetch_desc(&tmK);
-            tma_prefetch_desc(&tmV);
+            // (a whole warp when the cache is paged: the lanes keep the page numbers)
+            if (lane == 0) {
+                tma_prefetch_desc(&tmQ);
+                tma_prefetch_desc(&tmK);
+                tma_prefetch_desc(&tmV);
+            }
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                return PAGED ? warp_wait(bar, parity, ab, kWaitRingEmpty) : wait_or_abort(bar, parity, ab, kWaitRingEmpty);
+            };
             uint32_t it = 0;
             uint32_t q_armed = 0, k_armed = 0, v_armed = 0;   // copies started, for the drain on the way out
             bool ok = true;
             for (int si = seg_lo; si < seg_hi && ok; ++si) {
                 const DevSegment seg = p.segments[si];
                 if (seg.k_end <= seg.k_begin) continue;
-                if (!(ok = wait_or_abort(q_empty, (q_armed & 1u) ^ 1u, ab, kWaitRingEmpty))) break;
+                if (!(ok = wait(q_empty, (q_armed & 1u) ^ 1u))) break;
                 ++q_armed;
-                mbar_expect_tx(q_full, 2 * C::TILE_BYTES);
-                for (int r = 0; r < 2; ++r)
-                    for (int h = 0; h < HALVES; ++h)
-                        tma_load_2d(smem + C::OFF_Q + r * C::TILE_BYTES + h * HALF_BYTES, &tmQ, h * 64,
-                                    seg.q_row0 + (m_tile * 2 + r) * BM, q_full);
-                PageCursor<BN, 1> pc;
-                if (KIND == kPaged16 || KIND == kPaged4) pc.start(p.pages, seg.stream, seg.k_begin, seg.k_end);
+                if (lane == 0) {
+                    mbar_expect_tx(q_full, 2 * C::TILE_BYTES);
+                    for (int r = 0; r < 2; ++r)
+                        for (int h = 0; h < HALVES; ++h)
+                            tma_load_2d(smem + C::OFF_Q + r * C::TILE_BYTES + h * HALF_BYTES, &tmQ, h * 64,
+                                        seg.q_row0 + (m_tile * 2 + r) * BM, q_full);
+                }
+                PageCursor<BN> pc;
+                if (PAGED) pc.start(p.pages, seg.stream, seg.k_begin, seg.k_end, ab.status);
                 // the boxes of one tile of a paged cache
-                auto load_pages = [&](uint8_t* tile, const CUtensorMap& tm, const CUtensorMap& tmS, uint64_t* bar) {
-                    const int P = 1 << p.pages.page_shift;
-                    if (KIND == kPaged4) {
-                        mbar_expect_tx(bar, pc.rows() * Q4_ROW_BYTES);
-                        const int box = min(P, 32), n = min(P, BN);      // no box spans two widening warps' rows
-                        pc.for_each_box(ab.status, [&](int dst_row, int row) {
-                            for (int i = 0; i < n; i += box) {
-                                const int at = dst_row + i;
-                                uint8_t* dst = tile + HALF_BYTES + (at >> 5) * Q4_WARP_STRIDE;
-                                tma_load_2d(dst + (at & 31) * 64, &tm, 0, row + i, bar);
-                                tma_load_2d(dst + Q4_OFF_SCALE + (at & 31) * 8, &tmS, 0, (row + i) >> 4, bar);
+                auto load_pages = [&](uint8_t* tile, const CUtensorMap& tm, const CUtensorMap& tmS, uint64_t* bar, int k0) {
+                    const int n_box = pc.enter(k0), rows = pc.box_rows();
+                    for (int j = 0; j < n_box; ++j) {
+                        const int row = pc.row(k0, j);
+                        if (elect_one()) {
+                            if (j == 0) mbar_expect_tx(bar, n_box * rows * (KIND == kPaged4 ? Q4_ROW_BYTES : D * 2));
+                            if (KIND == kPaged4) {
+                                const int box = min(rows, 32);           // no box spans two widening warps' rows
+                                for (int i = 0; i < rows; i += box) {
+                                    const int at = j * rows + i;
+                                    uint8_t* dst = tile + HALF_BYTES + (at >> 5) * Q4_WARP_STRIDE;
+                                    tma_load_2d(dst + (at & 31) * 64, &tm, 0, (row + i) >> 1, bar);
+                                    tma_load_2d(dst + Q4_OFF_SCALE + (at & 31) * 8, &tmS, 0, (row + i) >> 4, bar);
+                                }
+                            } else {
+                                for (int h = 0; h < HALVES; ++h)
+                                    tma_load_2d(tile + h * HALF_BYTES + j * rows * 128, &tm, h * 64, row, bar);
                             }
-                        });
-                    } else {
-                        mbar_expect_tx(bar, pc.rows() * (D * 2));
-                        pc.for_each_box(ab.status, [&](int dst_row, int row) {
-                            for (int h = 0; h < HALVES; ++h)
-                                tma_load_2d(tile + h * HALF_BYTES + dst_row * 128, &tm, h * 64, row, bar);
-                        });
+                        }
+                        __syncwarp();
                     }
                 };
                 for (int k0 = seg.k_begin; k0 < seg.k_end; k0 += BN, ++it) {
                     const int row = seg.kv_row0 + (k0 - seg.k_begin);
                     const uint32_t kb = it % KS, kn = it / KS;
-                    if (!(ok = wait_or_abort(&k_empty[kb], (kn & 1u) ^ 1u, ab, kWaitRingEmpty))) break;
+                    if (!(ok = wait(&k_empty[kb], (kn & 1u) ^ 1u))) break;
                     ++k_armed;
-                    if (KIND == kPaged16 || KIND == kPaged4) {
-                        load_pages(smem + C::OFF_K + kb * C::TILE_BYTES, tmK, tmKs, &k_full[kb]);
+                    if (PAGED) {
+                        load_pages(smem + C::OFF_K + kb * C::TILE_BYTES, tmK, tmKs, &k_full[kb], k0);
                     } else if (FP8) {      // 128 keys x 128 bytes into the upper half of the stage
                         mbar_expect_tx(&k_full[kb], HALF_BYTES);
                         tma_load_2d(smem + C::OFF_K + kb * C::TILE_BYTES + HALF_BYTES, &tmK, 0, row, &k_full[kb]);
@@ -248,11 +258,10 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                                         &k_full[kb]);
                     }
                     const uint32_t vb = it % VS, vn = it / VS;
-                    if (!(ok = wait_or_abort(&v_empty[vb], (vn & 1u) ^ 1u, ab, kWaitRingEmpty))) break;
+                    if (!(ok = wait(&v_empty[vb], (vn & 1u) ^ 1u))) break;
                     ++v_armed;
-                    if (KIND == kPaged16 || KIND == kPaged4) {
-                        load_pages(smem + C::OFF_V + vb * C::TILE_BYTES, tmV, tmVs, &v_full[vb]);
-                        pc.next();
+                    if (PAGED) {
+                        load_pages(smem + C::OFF_V + vb * C::TILE_BYTES, tmV, tmVs, &v_full[vb], k0);
                     } else if (FP8) {
                         mbar_expect_tx(&v_full[vb], HALF_BYTES);
                         tma_load_2d(smem + C::OFF_V + vb * C::TILE_BYTES + HALF_BYTES, &tmV, 0, row, &v_full[vb]);
@@ -266,10 +275,10 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             }
             // Every copy this thread started must have landed before the CTA may end (at once when all
             // went well: the tiles were consumed long ago).
-            bool drained = q_armed == 0 || drain_wait(q_full, (q_armed - 1) & 1u, ab);
-            for (uint32_t k = k_armed > (uint32_t)KS ? k_armed - KS : 0; drained && k < k_armed; ++k)
+            bool drained = lane != 0 || q_armed == 0 || drain_wait(q_full, (q_armed - 1) & 1u, ab);
+            for (uint32_t k = k_armed > (uint32_t)KS ? k_armed - KS : 0; lane == 0 && drained && k < k_armed; ++k)
                 drained = drain_wait(&k_full[k % KS], (k / KS) & 1u, ab);
-            for (uint32_t k = v_armed > (uint32_t)VS ? v_armed - VS : 0; drained && k < v_armed; ++k)
+            for (uint32_t k = v_armed > (uint32_t)VS ? v_armed - VS : 0; lane == 0 && drained && k < v_armed; ++k)
                 drained = drain_wait(&v_full[k % VS], (k / VS) & 1u, ab);
         } else if ((warp == 1 || warp == 2) && aligned_ok) {
             // =================================== MMA issuers =================================
@@ -370,21 +379,23 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 if (KIND == kPaged4) {
                     const int rr = wq * 32 + lane;
                     const uint8_t* src = tile + HALF_BYTES + wq * Q4_WARP_STRIDE;
-                    uint4 raw[4];          // 32 channels each; 64-byte swizzle: chunk c at position c ^ ((row / 2) & 3)
+                    uint4 raw[4];          // 32 channels each; two rows to a 128-byte line, 128-byte swizzle
+                    const int line = lane >> 1, first = (lane & 1) << 2;
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
-                        raw[c] = *reinterpret_cast<const uint4*>(src + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4));
+                        raw[c] = *reinterpret_cast<const uint4*>(src + line * 128 + (((first | c) ^ (line & 7)) << 4));
                     const uint2 sw = *reinterpret_cast<const uint2*>(src + Q4_OFF_SCALE + lane * 8);
                     const uint32_t s2[4] = {__byte_perm(sw.x, 0u, 0x1010), __byte_perm(sw.x, 0u, 0x3232),
                                             __byte_perm(sw.y, 0u, 0x1010), __byte_perm(sw.y, 0u, 0x3232)};
+                    const uint32_t magic = q4_magic();
                     __syncwarp();          // every lane has its source before any row is written
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {                // channels 32 c + 8 q .. + 7: one 16-byte chunk
-                            const uint32_t l0 = q4_signed_lo(w[q]), h0 = q4_signed_hi(w[q]);             // (0, 4), (1, 5)
-                            const uint32_t l1 = q4_signed_lo(w[q] >> 8), h1 = q4_signed_hi(w[q] >> 8);   // (2, 6), (3, 7)
+                            const uint32_t l0 = q4_signed_lo(w[q], magic), h0 = q4_signed_hi(w[q], magic);             // (0, 4), (1, 5)
+                            const uint32_t l1 = q4_signed_lo(w[q] >> 8, magic), h1 = q4_signed_hi(w[q] >> 8, magic);   // (2, 6), (3, 7)
                             const uint4 f = make_uint4(h2_mul(__byte_perm(l0, h0, 0x5410), s2[c]), h2_mul(__byte_perm(l1, h1, 0x5410), s2[c]),
                                                        h2_mul(__byte_perm(l0, h0, 0x7632), s2[c]), h2_mul(__byte_perm(l1, h1, 0x7632), s2[c]));
                             const int c0 = (c & 1) * 4 + q;

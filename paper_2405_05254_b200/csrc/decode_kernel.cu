@@ -20,10 +20,11 @@
 //
 // PAGED = true finds the rows of a tile through a page table: a page holds P consecutive keys of
 // every KV head, so a 64-key tile is one box of a page (P >= 64) or 64 / P boxes of as many pages.
-// Only the producer knows; its page numbers are read two tiles ahead of the copies that use them.
+// Only the producer knows; its whole warp then walks the tiles, since the lanes keep the page numbers.
 #include "kernels.h"
 #include "page_map.cuh"
 #include "ptx.cuh"
+#include "tcgen05.cuh"
 
 namespace yoco {
 
@@ -104,17 +105,24 @@ __device__ __forceinline__ void decode_body(const CUtensorMap& tmK, const CUtens
 
     if (warp == kConsumerWarps) {
         // ------------------------------- producer ---------------------------------------
-        if (lane == 0) {
-            tma_prefetch_desc(&tmK);
-            tma_prefetch_desc(&tmV);
+        if (PAGED || lane == 0) {
+            if (lane == 0) {
+                tma_prefetch_desc(&tmK);
+                tma_prefetch_desc(&tmV);
+            }
+            auto wait = [&](uint64_t* bar, uint32_t parity, int32_t wait_class) {
+                return PAGED ? warp_wait(bar, parity, ab, wait_class) : wait_or_abort(bar, parity, ab, wait_class);
+            };
             uint32_t it = 0;
             bool ok = true;
             int item = blockIdx.x;
             for (uint32_t n = 0; ok; ++n) {
                 // hand the item (or the end mark) to the consumers
-                if (!wait_or_abort(&item_empty[n & 1u], ((n >> 1) & 1u) ^ 1u, ab, kWaitItemQueue)) break;
-                item_q[n & 1u] = item;
-                mbar_arrive(&item_full[n & 1u]);
+                if (!wait(&item_empty[n & 1u], ((n >> 1) & 1u) ^ 1u, kWaitItemQueue)) break;
+                if (lane == 0) {
+                    item_q[n & 1u] = item;
+                    mbar_arrive(&item_full[n & 1u]);
+                }
                 if (item >= n_items) break;
                 const int grp = item % n_groups, piece = item / n_groups;
                 const int seg_lo = p.group_begin[grp], seg_hi = p.group_begin[grp + 1];
@@ -135,28 +143,32 @@ __device__ __forceinline__ void decode_body(const CUtensorMap& tmK, const CUtens
                     const int k_lo = seg.k_begin + s_lo * TILE_N;
                     const int k_hi = min(seg.k_begin + s_hi * TILE_N, seg.k_end);
                     PageCursor<TILE_N> pc;
-                    if (PAGED) pc.start(p.pages, seg.stream, k_lo, k_hi);
+                    if (PAGED) pc.start(p.pages, seg.stream, k_lo, k_hi, ab.status);
                     for (int k0 = k_lo; k0 < k_hi; k0 += TILE_N, ++it) {
                         const uint32_t stage = it % STAGES, round = it / STAGES;
                         // self-test of the give-up path: nothing is armed, so no stage is needed either
                         // and the wait that runs out is the consumers' first wait for a tile
                         if (p.selftest_skip_loads) continue;
-                        if (!wait_or_abort(&empty_bar[stage], (round & 1u) ^ 1u, ab, kWaitRingEmpty)) {
+                        if (!wait(&empty_bar[stage], (round & 1u) ^ 1u, kWaitRingEmpty)) {
                             ok = false;
                             break;
                         }
                         uint8_t* kdst = stage_mem + stage * C::STAGE_BYTES;
                         uint8_t* vdst = kdst + C::TENSOR_BYTES;
                         if (PAGED) {
-                            mbar_expect_tx(&full_bar[stage], pc.rows() * (D * 2 * 2));
-                            pc.for_each_box(ab.status, [&](int dst_row, int row) {
+                            const int n_box = pc.enter(k0), rows = pc.box_rows();
+                            for (int j = 0; j < n_box; ++j) {
+                                const int row = pc.row(k0, j), at = j * rows * 128;
+                                if (elect_one()) {
+                                    if (j == 0) mbar_expect_tx(&full_bar[stage], n_box * rows * (D * 2 * 2));
 #pragma unroll
-                                for (int h = 0; h < C::HALVES; ++h) {
-                                    tma_load_2d(kdst + h * HALF_BYTES + dst_row * 128, &tmK, h * 64, row, &full_bar[stage]);
-                                    tma_load_2d(vdst + h * HALF_BYTES + dst_row * 128, &tmV, h * 64, row, &full_bar[stage]);
+                                    for (int h = 0; h < C::HALVES; ++h) {
+                                        tma_load_2d(kdst + h * HALF_BYTES + at, &tmK, h * 64, row, &full_bar[stage]);
+                                        tma_load_2d(vdst + h * HALF_BYTES + at, &tmV, h * 64, row, &full_bar[stage]);
+                                    }
                                 }
-                            });
-                            pc.next();
+                                __syncwarp();
+                            }
                             continue;
                         }
                         mbar_expect_tx(&full_bar[stage], C::STAGE_BYTES);
@@ -169,13 +181,17 @@ __device__ __forceinline__ void decode_body(const CUtensorMap& tmK, const CUtens
                     }
                 }
                 // all loads of this item are on their way: claim the next one
-                item = R > 1 ? n_groups + atomicAdd(p.work_counter, 1) : n_items;
+                item = n_items;
+                if (R > 1) {
+                    if (lane == 0) item = n_groups + atomicAdd(p.work_counter, 1);
+                    if (PAGED) item = __shfl_sync(0xffffffffu, item, 0);
+                }
             }
             // Before this thread leaves, every copy it armed must have landed: the CTA ends when its
             // last thread does, and a copy that lands later would write into (and arrive on barriers
             // in) shared memory that already belongs to another CTA.  When all went well the
             // consumers are still reading these tiles and the waits return at once.
-            if (!p.selftest_skip_loads) {
+            if (!p.selftest_skip_loads && lane == 0) {
                 const uint32_t in_flight = it < (uint32_t)STAGES ? it : (uint32_t)STAGES;
                 for (uint32_t k = it - in_flight; k < it; ++k)
                     if (!drain_wait(&full_bar[k % STAGES], (k / STAGES) & 1u, ab)) break;

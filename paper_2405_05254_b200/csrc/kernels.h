@@ -133,7 +133,8 @@ cudaError_t launch_decode_fp8(const DecodeFp8Params& p, const CUtensorMap& tmK, 
 cudaError_t decode_fp8_kernel_setup();
 
 // ---- decode over a paged 4-bit cache, head dimension 128 ---------------------------------------
-// k / v: uint8 maps over the [rows, 64] code bytes, box {64, box}, 64-byte swizzle; k_scale / v_scale: uint8
+// k / v: uint8 maps over the codes as [rows / 2, 128] bytes (two keys to a line), box {128, box / 2}, 128-byte swizzle
+// (a copy moves a line of up to 128 bytes as fast as one of 64); k_scale / v_scale: uint8
 // maps over the scales as [rows / 16, 128], box {128, box / 16}, no swizzle (box = min(P, the kernel's tile)).
 struct PagedQ4Maps {
     CUtensorMap k, k_scale, v, v_scale;

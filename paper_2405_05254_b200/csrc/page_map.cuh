@@ -9,70 +9,61 @@ __device__ __forceinline__ void report_bad_page(int32_t* status) {
     atomicCAS(status, 0, status_word(kBadPage, (int32_t)(blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z))));
 }
 
-// Row of (page, head, slot 0), or a row behind the pool (which a tensor copy fills with zeros) when the
-// page table entry is not a page of the pool.
-__device__ __forceinline__ int page_row(const PageMap& pm, int page, int head, int32_t* status) {
-    if ((uint32_t)page < (uint32_t)pm.num_pages) return page * pm.page_rows + (head << pm.page_shift);
-    report_bad_page(status);
-    return pm.rows;
-}
-
-// The producer's position in a run of TILE-key tiles of one (sequence, KV head) stream.  The page numbers of
-// the next AHEAD tiles are already requested when a tile's copies are issued, so that a table read is
-// not waited for between two copies.
-template <int TILE, int AHEAD = 2>
+// A producer warp's view of the pages of one (sequence, KV head) stream.  Every lane holds one page, 32 at a time:
+// the pool row of its first slot, so that a tile costs one shuffle per box; the next 32 are already requested, so a
+// table read is waited for once per run.  (A producer is one warp working through a chain of dependent
+// instructions: what it does per tile has to fit in the time of a tile.  Page numbers looked up, checked and
+// multiplied tile by tile, or kept in registers of one thread and shifted along, where a move waits for its load, did
+// not.)  All lanes call it together; keys only grow; k_lo is a multiple of TILE.
+template <int TILE>
 struct PageCursor {
-    static constexpr int MAX_IDS = TILE / 16;      // pages hold at least 16 keys
-    const PageMap* pm;
+    static constexpr int MAX_BOXES = TILE / 16;    // pages hold at least 16 keys
+    // copies, not a reference to the kernel's parameters: those would be read again after every barrier wait
+    int shift, num_pages, page_rows, pool_rows, head_row;
     const int32_t* entries;                        // this sequence's row of the table
-    int head, k0, k_hi;
-    int32_t id[AHEAD + 1][MAX_IDS];
+    int32_t* status;
+    int first, last, lane;
+    int32_t now;                                   // row of page first + lane
+    int32_t later;                                 // number of page first + 32 + lane
 
-    __device__ __forceinline__ void fetch(int32_t (&out)[MAX_IDS], int k) const {
-        const int P = 1 << pm->page_shift;
-#pragma unroll
-        for (int j = 0; j < MAX_IDS; ++j) {
-            const int key = k + j * P;             // one page when P >= TILE
-            out[j] = (j == 0 || j * P < TILE) && key < k_hi ? __ldg(entries + (key >> pm->page_shift)) : 0;
-        }
+    __device__ __forceinline__ int32_t fetch(int page) const { return page <= last ? __ldg(entries + page) : 0; }
+    __device__ __forceinline__ int32_t row_of(int32_t page) const {
+        if ((uint32_t)page < (uint32_t)num_pages) return page * page_rows + head_row;
+        report_bad_page(status);                   // (entries behind the run were replaced by page 0)
+        return pool_rows;
     }
-    __device__ __forceinline__ void start(const PageMap& map, int stream, int k_lo, int k_end) {
-        pm = &map;
+    __device__ __forceinline__ void start(const PageMap& map, int stream, int k_lo, int k_end, int32_t* status_word) {
+        shift = map.page_shift;
+        num_pages = map.num_pages;
+        page_rows = map.page_rows;
+        pool_rows = map.rows;
+        status = status_word;
         const int b = stream / map.Hkv;
-        head = stream - b * map.Hkv;
+        head_row = (stream - b * map.Hkv) << shift;
         entries = map.table + (int64_t)b * map.table_stride;
-        k0 = k_lo;
-        k_hi = k_end;
-#pragma unroll
-        for (int a = 0; a <= AHEAD; ++a) fetch(id[a], k_lo + a * TILE);
+        lane = (int)(threadIdx.x & 31u);
+        first = k_lo >> shift;
+        last = (k_end - 1) >> shift;
+        const int32_t page = fetch(first + lane);
+        later = fetch(first + 32 + lane);
+        now = row_of(page);
     }
-    // rows that the boxes of this tile bring: whole boxes, those with at least one key of the run
-    __device__ __forceinline__ int rows() const {
-        const int P = 1 << pm->page_shift;
-        return P >= TILE ? TILE : min(TILE, ((k_hi - k0 + P - 1) >> pm->page_shift) << pm->page_shift);
-    }
-    // f(first row inside the tile, first row in the pool) for every box
-    template <class F>
-    __device__ __forceinline__ void for_each_box(int32_t* status, F f) const {
-        const int P = 1 << pm->page_shift;
-        if (P >= TILE) {
-            const int r = page_row(*pm, id[0][0], head, status);
-            f(0, r == pm->rows ? r : r + (k0 & (P - 1)));
-            return;
+    // To be called for every tile before row(): the 32 pages at hand cover it (a tile never straddles two batches,
+    // both are multiples of the tile's pages).  Returns how many boxes the tile has: those with at least one key.
+    __device__ __forceinline__ int enter(int k0) {
+        const int page = k0 >> shift;
+        if (page - first >= 32) {
+            first += 32;
+            now = row_of(later);
+            later = fetch(first + 32 + lane);
         }
-#pragma unroll
-        for (int j = 0; j < MAX_IDS; ++j) {
-            if (j * P < TILE && k0 + j * P < k_hi) f(j * P, page_row(*pm, id[0][j], head, status));
-        }
+        return min(max(1, TILE >> shift), last + 1 - page);
     }
-    __device__ __forceinline__ void next() {
-        k0 += TILE;
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a)
-#pragma unroll
-            for (int j = 0; j < MAX_IDS; ++j) id[a][j] = id[a + 1][j];
-        fetch(id[AHEAD], k0 + AHEAD * TILE);
+    // pool row that box j of the tile at key k0 starts at; it brings box_rows() rows
+    __device__ __forceinline__ int row(int k0, int j) const {
+        return __shfl_sync(0xffffffffu, now, (k0 >> shift) + j - first) + ((1 << shift) > TILE ? k0 & ((1 << shift) - 1) : 0);
     }
+    __device__ __forceinline__ int box_rows() const { return min(TILE, 1 << shift); }
 };
 
 }  // namespace yoco

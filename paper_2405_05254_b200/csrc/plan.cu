@@ -91,7 +91,7 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
     // number of CTA groups
     int64_t target;
     if (mode == YOCO_MODE_DECODE)
-        target = (int64_t)sm_count * kDecodeGroupsPerSm;
+        target = (int64_t)sm_count * form.groups_per_sm;
     else
         target = std::max<int64_t>(1, sm_count / m_tiles);
     const int64_t num_groups = std::max<int64_t>(1, std::min<int64_t>(target, total_tiles));
@@ -139,7 +139,8 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
     // Pieces pay when a group is one long run of a stream.  When groups are chains of short streams
     // (more than two segments per group on average) most streams are not split at all and are written
     // without a merge; pieces would split every one of them.
-    int R = mode == YOCO_MODE_DECODE ? choose_sub_items(total_tiles / num_groups / form.piece_divisor, max_sub_items) : 1;
+    int R = mode == YOCO_MODE_DECODE ? choose_sub_items(total_tiles / num_groups / form.piece_divisor,
+                                                           std::min(max_sub_items, form.max_pieces)) : 1;
     if ((int64_t)dev.size() > 2 * num_groups) R = 1;
     int32_t max_splits = 0, needs_combine = R > 1 ? 1 : 0;
     for (int st = 0; st < num_streams; ++st) {

@@ -100,14 +100,17 @@ struct CacheForm {
     bool pair_tiles = false;
     int piece_divisor = 1;
     bool paged = false;
+    int groups_per_sm = kDecodeGroupsPerSm;   // resident decode CTAs per SM
+    int max_pieces = 4;                       // most pieces per decode group
     bool operator==(const CacheForm& o) const {
-        return pair_tiles == o.pair_tiles && piece_divisor == o.piece_divisor && paged == o.paged;
+        return pair_tiles == o.pair_tiles && piece_divisor == o.piece_divisor && paged == o.paged && groups_per_sm == o.groups_per_sm &&
+               max_pieces == o.max_pieces;
     }
 };
-constexpr CacheForm kBf16Cache{false, 1, false};
+constexpr CacheForm kBf16Cache{};
 constexpr CacheForm kFp8Cache{true, 2, false};
 constexpr CacheForm kPagedCache{false, 1, true};
-constexpr CacheForm kPagedQ4Cache{true, 4, true};
+constexpr CacheForm kPagedQ4Cache{true, 1, true, 1, 1};
 
 // Returns YOCO_OK or an error code; fills `plan`.  cu_kv_host may be null (tight packing).
 // max_sub_items: upper limit of pieces per decode group (1 = every group is one piece).
