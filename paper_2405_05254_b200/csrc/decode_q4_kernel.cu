@@ -44,16 +44,11 @@ constexpr uint32_t kMinus8 = 0x80088008u, kMinus128 = 0x80808080u;
 constexpr float kPShift = 7.f;                // P = 2^(s - max + kPShift)
 
 // W warps per CTA, one CTA per SM; every warp has KH places for tiles of K and VH for tiles of V of its own.
-#ifndef QW
-#define QW 12
-#define QKH 2
-#define QVH 1
-#endif
 template <int ROWS>
 struct CfgQ4 {
-    static constexpr int W = ROWS == 8 ? QW : 8;
-    static constexpr int KH = ROWS == 8 ? QKH : 2;
-    static constexpr int VH = ROWS == 8 ? QVH : 2;
+    static constexpr int W = ROWS == 8 ? kQ4Warps8 : kQ4Warps16;
+    static constexpr int KH = 2;
+    static constexpr int VH = ROWS == 8 ? 1 : 2;
     static constexpr int H = KH + VH;
     static constexpr int THREADS = W * 32;
     static constexpr int OFF_SCALES = W * H * CODE_BYTES;

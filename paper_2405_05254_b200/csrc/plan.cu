@@ -94,7 +94,24 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
         target = (int64_t)sm_count * form.groups_per_sm;
     else
         target = std::max<int64_t>(1, sm_count / m_tiles);
-    const int64_t num_groups = std::max<int64_t>(1, std::min<int64_t>(target, total_tiles));
+    int64_t num_groups = std::max<int64_t>(1, std::min<int64_t>(target, total_tiles));
+    // first flat tile of every group: equal shares, or handfuls that end with their stream (CacheForm)
+    std::vector<int64_t> bounds;
+    const int handful = mode != YOCO_MODE_DECODE ? 0 : rows_per_stream <= 8 ? form.side_by_side8 : form.side_by_side16;
+    if (handful > 0 && total_tiles > 0) {
+        int64_t groups = 0, flat_lo = 0;
+        for (int i = 0; i < s.B; ++i)
+            groups += s.Hkv * (((len_vis[i] + tile_n - 1) / tile_n - tile_lo[i] + handful - 1) / handful);
+        if (groups <= target) {
+            for (int i = 0; i < s.B; ++i) {
+                const int64_t nt = (len_vis[i] + tile_n - 1) / tile_n - tile_lo[i], k = (nt + handful - 1) / handful;
+                for (int c = 0; c < s.Hkv; ++c, flat_lo += nt)
+                    for (int64_t j = 0; j < k; ++j) bounds.push_back(flat_lo + j * nt / k);
+            }
+            bounds.push_back(total_tiles);
+            num_groups = groups;
+        }
+    }
 
     plan = Plan{};
     plan.rows_per_stream = rows_per_stream;
@@ -106,7 +123,7 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
     // walk the flat tile space: streams in (b, c) order
     int64_t flat = 0;       // flat index of the current stream's first tile
     int64_t g = 0;          // current group
-    auto group_lo = [&](int64_t p) { return p * total_tiles / num_groups; };
+    auto group_lo = [&](int64_t p) { return bounds.empty() ? p * total_tiles / num_groups : bounds[(size_t)p]; };
     for (int b = 0; b < s.B; ++b) {
         const int64_t nt = (len_vis[b] + tile_n - 1) / tile_n;
         const int64_t head_rows = s.kv_head_stride ? s.kv_head_stride / s.d : len[b];

@@ -89,6 +89,9 @@ struct Plan {
                                                  // = coarse_segments * sub_items
 };
 
+// Warps of the 4-bit decode kernel for up to 8 query rows per stream, and above.
+constexpr int kQ4Warps8 = 12, kQ4Warps16 = 8;
+
 // What the cache of a plan is made of.
 // pair_tiles: chunk plans use the two-row-tile CTA (kChunkPairTileM) whatever G*T is (an 8-bit or 4-bit cache is
 // read by that kernel only).
@@ -102,15 +105,21 @@ struct CacheForm {
     bool paged = false;
     int groups_per_sm = kDecodeGroupsPerSm;   // resident decode CTAs per SM
     int max_pieces = 4;                       // most pieces per decode group
+    // Tiles that a CTA's warps work off side by side (whole tiles per warp), up to 8 and above 8 query rows; 0: tiles
+    // are shared by the warps.  A problem so small that no CTA would need a second turn is then cut at the
+    // streams' ends: as many groups per stream as it has such handfuls, each a run of its own.  (Measured, 8
+    // sequences of 700 to 1,100 keys, 8 KV heads: groups of equal size, most of them in two streams, 16.1 us;
+    // groups that end with their stream 12.8 us, and streams of at most 12 tiles need no merge.)
+    int side_by_side8 = 0, side_by_side16 = 0;
     bool operator==(const CacheForm& o) const {
         return pair_tiles == o.pair_tiles && piece_divisor == o.piece_divisor && paged == o.paged && groups_per_sm == o.groups_per_sm &&
-               max_pieces == o.max_pieces;
+               max_pieces == o.max_pieces && side_by_side8 == o.side_by_side8 && side_by_side16 == o.side_by_side16;
     }
 };
 constexpr CacheForm kBf16Cache{};
 constexpr CacheForm kFp8Cache{true, 2, false};
 constexpr CacheForm kPagedCache{false, 1, true};
-constexpr CacheForm kPagedQ4Cache{true, 1, true, 1, 1};
+constexpr CacheForm kPagedQ4Cache{true, 1, true, 1, 1, kQ4Warps8, kQ4Warps16};
 
 // Returns YOCO_OK or an error code; fills `plan`.  cu_kv_host may be null (tight packing).
 // max_sub_items: upper limit of pieces per decode group (1 = every group is one piece).
