@@ -155,10 +155,11 @@ __device__ __forceinline__ void decode_q4_body(const CUtensorMap& tmK, const CUt
     uint32_t done_tiles = 0;             // tiles worked off before this run
     uint32_t issued_k = 0, issued_v = 0; // halves asked for in this run
     int m_count = 0, batch = 0;          // tiles of this warp in the run; first tile of the batch whose rows are held
-    int32_t box_row = 0;
+    int32_t box_row = 0, earlier_row = 0;   // of this batch, and of the one before: V is asked for later than K
     bool ok = true;
     auto load_batch = [&](int first) {
         batch = first;
+        earlier_row = box_row;
         const int j = lane & ((1 << nb_shift) - 1);
         const int key = run.k_begin + (warp + W * (first + (lane >> nb_shift))) * TILE_N + (j << shift);
         box_row = 0;
@@ -177,8 +178,9 @@ __device__ __forceinline__ void decode_q4_body(const CUtensorMap& tmK, const CUt
     auto issue = [&](const CUtensorMap& tm, const CUtensorMap& tms, int m, uint32_t place) {
         if (((m - batch) << nb_shift) >= 32) load_batch(m);
         const uint32_t bar = bar0 + 8 * place, codes = codes0 + place * CODE_BYTES, scales = scales0 + place * SCALE_BYTES;
-        const int from = (m - batch) << nb_shift;
-        const int row = __shfl_sync(0xffffffffu, box_row, from);
+        const int from = (m - batch) << nb_shift;           // below 0: in the batch before
+        const int32_t held = from < 0 ? earlier_row : box_row;
+        const int row = __shfl_sync(0xffffffffu, held, from & 31);
         if (nb_shift == 0) {
             if (elect_one()) {
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(TILE_N * ROW_BYTES) : "memory");
@@ -189,7 +191,7 @@ __device__ __forceinline__ void decode_q4_body(const CUtensorMap& tmK, const CUt
             const int k0 = run.k_begin + (warp + W * m) * TILE_N, rows = 1 << row_shift;
             const int n_box = min(1 << nb_shift, (run.k_end - k0 + rows - 1) >> row_shift);
             for (int j = 0; j < n_box; ++j) {
-                const int r = __shfl_sync(0xffffffffu, box_row, from + j);
+                const int r = __shfl_sync(0xffffffffu, held, (from & 31) + j);
                 if (elect_one()) {
                     if (j == 0)
                         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((n_box * ROW_BYTES) << row_shift) : "memory");

@@ -169,6 +169,51 @@ def test_decode_matches_the_definition(q4, lens, Hq, Hkv, T, P, window, d):
     assert_lse_close(lse, lref, "LSE")
 
 
+def attention_on_gpu(cache, dev, Q_bits, T):
+    """The definition in 64 bits with torch on the GPU, for caches that numpy would take minutes over."""
+    import torch
+    c = cache
+    B, Hq = Q_bits.shape[:2]
+    G = Hq // c.Hkv
+    Q = pr.bits_to_dev(Q_bits).double()
+    O, L = torch.zeros(Q.shape, dtype=torch.float64, device="cuda"), torch.full(Q.shape[:3], -torch.inf, dtype=torch.float64, device="cuda")
+    for b in range(B):
+        n = int(c.lens[b])
+        seen = torch.arange(n, device="cuda")[None] <= torch.arange(n - T, n, device="cuda")[:, None]
+        for h in range(c.Hkv):
+            at = torch.from_numpy(c.row_numbers(b, h, n)).cuda()
+            rows = []
+            for w in range(2):
+                if c.q4:
+                    codes, s = dev.pools[2 * w][at].int(), dev.pools[2 * w + 1][at].double()
+                    x = torch.stack([codes & 15, codes >> 4], -1).reshape(n, -1).double() - 8
+                    rows.append(x * s.repeat_interleave(32, 1))
+                else:
+                    rows.append(dev.pools[w][at].double())
+            for g in range(G):
+                s = (Q[b, h * G + g] @ rows[0].T) * c.d ** -0.5
+                s = s.masked_fill(~seen, -torch.inf)
+                L[b, h * G + g] = torch.logsumexp(s, 1)
+                O[b, h * G + g] = torch.softmax(s, 1) @ rows[1]
+    return O.cpu().numpy(), L.cpu().numpy()
+
+
+@pytest.mark.parametrize("q4", [False, True])
+@pytest.mark.parametrize("lens,Hq,Hkv,T,P", [
+    ([150000, 70001], 8, 8, 1, 16),          # small pages: many batches of page numbers per warp
+    ([600000], 16, 8, 2, 64),                # more than 32 tiles per warp of the 4-bit kernel
+    ([260000], 32, 4, 2, 32),                # 16 query rows per KV head
+])
+def test_decode_of_long_caches(q4, lens, Hq, Hkv, T, P):
+    cache = pr.PagedCache(47, lens, P, Hkv, 128, q4)
+    dev = pr.DevCache(cache)
+    Q = q_bits(47, len(lens), Hq, T, 128)
+    o, lse, _ = dev.attend(Q, T)
+    ref, lref = attention_on_gpu(cache, dev, Q, T)
+    assert_close(o, ref, "O")
+    assert_lse_close(lse, lref, "LSE")
+
+
 CHUNK = [
     # lens, Hq, Hkv, T, P, window, d
     ([1], 1, 1, 1, 16, 0, 128),
