@@ -649,8 +649,7 @@ int32_t paged_rows(const yoco_paged_append_shape* shape, const yoco_paged_layout
             },
             [&](int32_t i) -> int64_t { return end_host[i]; }, &tab, &tokens, &p.tokens_per_seq);
         if (rc != YOCO_OK) return rc;
-        // grids are counted in 32 bits
-        if (tokens * s.Hkv * (s.d / 8) >= (1ll << 37)) return YOCO_ERR_UNSUPPORTED;
+        if (s.Hkv > 65535) return YOCO_ERR_UNSUPPORTED;      // a grid dimension
         if (append) {
             int64_t max_len = 0;
             for (int32_t i = 0; i < s.B; ++i) max_len = std::max<int64_t>(max_len, end_host[i]);
