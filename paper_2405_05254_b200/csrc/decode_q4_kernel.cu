@@ -85,7 +85,8 @@ __device__ __forceinline__ void mma_tf32_twice(float (&d)[4], const float (&c)[4
           "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 
-template <int ROWS>
+// NB: boxes of a 64-key tile, 1 with pages of 64 keys and more, else 64 / P
+template <int ROWS, int NB>
 __device__ __forceinline__ void decode_q4_body(const CUtensorMap& tmK, const CUtensorMap& tmKs, const CUtensorMap& tmV,
                                                const CUtensorMap& tmVs, const DecodeParams& p,
                                                const DevSegment* segments, const int32_t* group_begin) {
@@ -149,7 +150,8 @@ __device__ __forceinline__ void decode_q4_body(const CUtensorMap& tmK, const CUt
     //      places that nobody else touches: a place has one barrier, is never waited for to become free, and the
     //      warp sees every phase of its barriers.  Lane l holds the pool row of box l % nb of the tile number l / nb of a
     //      batch (nb boxes to a tile: 1, or 64 / P for small pages) ----
-    const int shift = p.pages.page_shift, nb_shift = max(0, 6 - shift), row_shift = min(6, shift);
+    constexpr int nb_shift = NB == 1 ? 0 : NB == 2 ? 1 : 2, row_shift = 6 - nb_shift;
+    const int shift = NB == 1 ? p.pages.page_shift : row_shift;
     const uint32_t codes0 = smem_u32(smem) + warp * (H * CODE_BYTES), scales0 = smem_u32(smem) + C::OFF_SCALES + warp * (H * SCALE_BYTES);
     const uint32_t bar0 = smem_u32(full_bar + warp * H);
     uint32_t done_tiles = 0;             // tiles worked off before this run
@@ -174,31 +176,37 @@ __device__ __forceinline__ void decode_q4_body(const CUtensorMap& tmK, const CUt
             }
         }
     };
-    // asks for K (or V) of tile m into place `place` of the warp
+    // Asks for K (or V) of tile m into place `place` of the warp.
+    // (The count of boxes is a constant of the kernel, so that one elected stretch issues them all: a turn of its own per
+    // box, or a count known at run time only, cost 15 to 25 % of the bandwidth at P = 16 and 32.)
     auto issue = [&](const CUtensorMap& tm, const CUtensorMap& tms, int m, uint32_t place) {
         if (((m - batch) << nb_shift) >= 32) load_batch(m);
-        const uint32_t bar = bar0 + 8 * place, codes = codes0 + place * CODE_BYTES, scales = scales0 + place * SCALE_BYTES;
         const int from = (m - batch) << nb_shift;           // below 0: in the batch before
         const int32_t held = from < 0 ? earlier_row : box_row;
-        const int row = __shfl_sync(0xffffffffu, held, from & 31);
-        if (nb_shift == 0) {
+        const uint32_t bar = bar0 + 8 * place, codes = codes0 + place * CODE_BYTES, scales = scales0 + place * SCALE_BYTES;
+        int row[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) row[j] = __shfl_sync(0xffffffffu, held, (from & 31) + j);
+        const int left = NB == 1 ? TILE_N : run.k_end - (run.k_begin + (warp + W * m) * TILE_N);
+        if (left >= TILE_N) {
             if (elect_one()) {
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(TILE_N * ROW_BYTES) : "memory");
-                tma_load_2d(codes, &tm, 0, row >> 1, bar);
-                tma_load_2d(scales, &tms, 0, row >> 4, bar);
-            }
-        } else {                          // small pages: one box per page that holds a key of the run
-            const int k0 = run.k_begin + (warp + W * m) * TILE_N, rows = 1 << row_shift;
-            const int n_box = min(1 << nb_shift, (run.k_end - k0 + rows - 1) >> row_shift);
-            for (int j = 0; j < n_box; ++j) {
-                const int r = __shfl_sync(0xffffffffu, held, (from & 31) + j);
-                if (elect_one()) {
-                    if (j == 0)
-                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((n_box * ROW_BYTES) << row_shift) : "memory");
-                    tma_load_2d(codes + ((j * (D / 2)) << row_shift), &tm, 0, r >> 1, bar);
-                    tma_load_2d(scales + ((j * 2 * GROUPS) << row_shift), &tms, 0, r >> 4, bar);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    tma_load_2d(codes + j * (CODE_BYTES / NB), &tm, 0, row[j] >> 1, bar);
+                    tma_load_2d(scales + j * (SCALE_BYTES / NB), &tms, 0, row[j] >> 4, bar);
                 }
-                __syncwarp();
+            }
+        } else {                          // the last tile of a sequence: only the pages that hold a key of it
+            const int n_box = (left + (1 << row_shift) - 1) >> row_shift;
+            if (elect_one()) {
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((n_box * ROW_BYTES) << row_shift) : "memory");
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+                    if (j < n_box) {
+                        tma_load_2d(codes + j * (CODE_BYTES / NB), &tm, 0, row[j] >> 1, bar);
+                        tma_load_2d(scales + j * (SCALE_BYTES / NB), &tms, 0, row[j] >> 4, bar);
+                    }
             }
         }
         __syncwarp();
@@ -571,54 +579,69 @@ __device__ __forceinline__ void decode_q4_body(const CUtensorMap& tmK, const CUt
     }
 }
 
-template <int ROWS>
+template <int ROWS, int NB>
 __global__ void __launch_bounds__(CfgQ4<ROWS>::THREADS, 1)
 decode_q4_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmKs,
                  const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmVs,
                  const __grid_constant__ DecodeParams p) {
-    decode_q4_body<ROWS>(tmK, tmKs, tmV, tmVs, p, p.segments, p.group_begin);
+    decode_q4_body<ROWS, NB>(tmK, tmKs, tmV, tmVs, p, p.segments, p.group_begin);
 }
 
 // work tables as kernel parameters
-template <int ROWS>
+template <int ROWS, int NB>
 __global__ void __launch_bounds__(CfgQ4<ROWS>::THREADS, 1)
 decode_q4_kernel_inline(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmKs,
                         const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmVs,
                         const __grid_constant__ DecodeParams p, const __grid_constant__ DecodeInlineTables tab) {
-    decode_q4_body<ROWS>(tmK, tmKs, tmV, tmVs, p, tab.seg, tab.group_begin);
+    decode_q4_body<ROWS, NB>(tmK, tmKs, tmV, tmVs, p, tab.seg, tab.group_begin);
 }
 
-template <int ROWS>
+template <int ROWS, int NB>
 cudaError_t launch_one(const DecodeParams& p, const PagedQ4Maps& m, int num_groups, cudaStream_t stream,
                        const DecodeInlineTables* tab) {
     if (tab)
-        decode_q4_kernel_inline<ROWS><<<num_groups, CfgQ4<ROWS>::THREADS, CfgQ4<ROWS>::SMEM_BYTES, stream>>>(m.k, m.k_scale, m.v, m.v_scale, p, *tab);
+        decode_q4_kernel_inline<ROWS, NB><<<num_groups, CfgQ4<ROWS>::THREADS, CfgQ4<ROWS>::SMEM_BYTES, stream>>>(m.k, m.k_scale, m.v, m.v_scale, p, *tab);
     else
-        decode_q4_kernel<ROWS><<<num_groups, CfgQ4<ROWS>::THREADS, CfgQ4<ROWS>::SMEM_BYTES, stream>>>(m.k, m.k_scale, m.v, m.v_scale, p);
+        decode_q4_kernel<ROWS, NB><<<num_groups, CfgQ4<ROWS>::THREADS, CfgQ4<ROWS>::SMEM_BYTES, stream>>>(m.k, m.k_scale, m.v, m.v_scale, p);
     return cudaGetLastError();
 }
 
-template <int ROWS>
+template <int ROWS, int NB>
 cudaError_t setup_one() {
-    cudaError_t e = cudaFuncSetAttribute(decode_q4_kernel<ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    cudaError_t e = cudaFuncSetAttribute(decode_q4_kernel<ROWS, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          CfgQ4<ROWS>::SMEM_BYTES);
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(decode_q4_kernel_inline<ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    return cudaFuncSetAttribute(decode_q4_kernel_inline<ROWS, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 CfgQ4<ROWS>::SMEM_BYTES);
 }
 
 }  // namespace
 
 cudaError_t decode_q4_kernel_setup() {
-    cudaError_t e = setup_one<8>();
-    return e != cudaSuccess ? e : setup_one<16>();
+    cudaError_t e;
+    if ((e = setup_one<8, 1>()) != cudaSuccess) return e;
+    if ((e = setup_one<8, 2>()) != cudaSuccess) return e;
+    if ((e = setup_one<8, 4>()) != cudaSuccess) return e;
+    if ((e = setup_one<16, 1>()) != cudaSuccess) return e;
+    if ((e = setup_one<16, 2>()) != cudaSuccess) return e;
+    return setup_one<16, 4>();
 }
+
+namespace {
+template <int ROWS>
+cudaError_t launch_any(const DecodeParams& p, const PagedQ4Maps& maps, int num_groups, cudaStream_t stream,
+                       const DecodeInlineTables* tab) {
+    if (p.pages.page_shift == 4) return launch_one<ROWS, 4>(p, maps, num_groups, stream, tab);
+    if (p.pages.page_shift == 5) return launch_one<ROWS, 2>(p, maps, num_groups, stream, tab);
+    return launch_one<ROWS, 1>(p, maps, num_groups, stream, tab);
+}
+}  // namespace
 
 cudaError_t launch_decode_q4(const DecodeParams& p, const PagedQ4Maps& maps, int num_groups, cudaStream_t stream,
                              const DecodeInlineTables* tab) {
     if (num_groups <= 0) return cudaSuccess;
-    return p.rows_per_stream > 8 ? launch_one<16>(p, maps, num_groups, stream, tab)
-                                 : launch_one<8>(p, maps, num_groups, stream, tab);
+    return p.rows_per_stream > 8 ? launch_any<16>(p, maps, num_groups, stream, tab)
+                                 : launch_any<8>(p, maps, num_groups, stream, tab);
 }
 
 }  // namespace yoco
