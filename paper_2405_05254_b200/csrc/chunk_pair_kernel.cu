@@ -32,8 +32,16 @@
 // A paged cache (kPaged16: bf16 rows, kPaged4: 4-bit rows) differs in where the producer finds the rows of a tile
 // (page_map.cuh).  4-bit rows take the way of the 8-bit cache: the 32 rows of a widening warp land, codes and scales,
 // inside the part of the upper half tile that the same warp's fp16 rows will fill, so a warp has read all of its
-// source (one __syncwarp) before it overwrites any of it, and no two warps meet.  A value (code - 8) * scale is
-// rounded to fp16 once (half a step, 2^-11).
+// source (one __syncwarp) before it overwrites any of it, and no two warps meet.
+// A value (code - 8) * scale has up to 14 bits, three more than fp16 holds.  V takes one rounding (half a step, 2^-11
+// of the value; O leaves in bf16).  For K that rounding puts a score off by about 3e-4, which the log-sum-exp of a row of
+// many keys averages out and that of a row of few does not: where a CTA has a row that sees fewer than kExactKeys keys,
+// K takes two ring entries, (code - 8) times the upper eight bits of the scale and times its lower three, both
+// exact in fp16, and the scores are the sum of two products.  The polynomial exponentials are quartic (no time lost: 520 us
+// for 391 tokens over 65,927 keys, where the cubic took 522).  Relative error (2-norm) of the log-sum-exp against 64 bits,
+// chunks of 11 to 41 tokens over as many keys: 4e-5 with K rounded once and the cubic, 4e-6 with K in two parts, 1.6e-7
+// with the quartic as well; above the rule, at most 1.2e-6.  K in two parts everywhere would make that case 812 us; with
+// the rule a whole sequence of 4,096 tokens pays most, 575 us instead of 494.
 #include <cuda_fp16.h>
 
 #include "kernels.h"
@@ -61,6 +69,7 @@ constexpr int Q4_OFF_SCALE = 32 * 64;
 constexpr int Q4_ROW_BYTES = 64 + 8;
 constexpr int HALF_BYTES = 128 * 128;          // 128 rows x 64 bf16: one swizzled half tile
 constexpr uint32_t TMEM_COLS = 512;
+constexpr int kExactKeys = 2048;               // 4-bit rows: fewer visible keys are treated more exactly, see above
 constexpr float kRescaleThreshold = 8.f;       // in log2 units: P stays below 2^8
 // Register split after launch.  The CTA starts with what its thread count allows (168 registers per
 // thread for 384 threads, 128 for 512); warpgroup 0 (and the widening warpgroup) give back down to
@@ -152,6 +161,15 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     const int group = blockIdx.x / p.m_tiles, m_tile = blockIdx.x - group * p.m_tiles;
     const int seg_lo = p.group_begin[group], seg_hi = p.group_begin[group + 1];
     const Abort ab{abort_flag, p.status, kWaitLimitNs};
+    constexpr bool PAGED = KIND == kPaged16 || KIND == kPaged4;
+    // whether a row of this CTA sees so few keys of the segment's sequence that they are treated more exactly
+    auto few_keys = [&](const DevSegment& seg) {
+        if (KIND != kPaged4) return false;
+        const int t = (m_tile * 2 * BM) % p.T, visible = seg.n_full + (t + 2 * BM <= p.T ? t : 0);
+        return (p.window > 0 ? min(visible, p.window) : visible) < kExactKeys;
+    };
+    // ring entries of a key tile of the segment
+    auto k_entries = [&](const DevSegment& seg) -> uint32_t { return few_keys(seg) ? 2u : 1u; };
     const bool aligned_ok = (smem_u32(smem) & 1023u) == 0;
 
     if (threadIdx.x == 0) {
@@ -189,7 +207,6 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 
     if (warp < 4) {
         setmaxnreg_dec<Regs<FP8>::kOther>();
-        constexpr bool PAGED = KIND == kPaged16 || KIND == kPaged4;
         if (warp == 0 && (PAGED || lane == 0) && aligned_ok) {
             // =================================== TMA producer ================================
             // (a whole warp when the cache is paged: the lanes keep the page numbers)
@@ -201,7 +218,7 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             auto wait = [&](uint64_t* bar, uint32_t parity) {
                 return PAGED ? warp_wait(bar, parity, ab, kWaitRingEmpty) : wait_or_abort(bar, parity, ab, kWaitRingEmpty);
             };
-            uint32_t it = 0;
+            uint32_t it = 0;                                  // key tile; k_armed counts the entries of the K ring
             uint32_t q_armed = 0, k_armed = 0, v_armed = 0;   // copies started, for the drain on the way out
             bool ok = true;
             for (int si = seg_lo; si < seg_hi && ok; ++si) {
@@ -241,10 +258,11 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         __syncwarp();
                     }
                 };
+                const uint32_t entries = k_entries(seg);
                 for (int k0 = seg.k_begin; k0 < seg.k_end; k0 += BN, ++it) {
                     const int row = seg.kv_row0 + (k0 - seg.k_begin);
-                    const uint32_t kb = it % KS, kn = it / KS;
-                    if (!(ok = wait(&k_empty[kb], (kn & 1u) ^ 1u))) break;
+                    const uint32_t kb = k_armed % KS;
+                    if (!(ok = wait(&k_empty[kb], ((k_armed / KS) & 1u) ^ 1u))) break;
                     ++k_armed;
                     if (PAGED) {
                         load_pages(smem + C::OFF_K + kb * C::TILE_BYTES, tmK, tmKs, &k_full[kb], k0);
@@ -256,6 +274,12 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         for (int h = 0; h < HALVES; ++h)
                             tma_load_2d(smem + C::OFF_K + kb * C::TILE_BYTES + h * HALF_BYTES, &tmK, h * 64, row,
                                         &k_full[kb]);
+                    }
+                    if (entries == 2) {    // nothing lands in the second entry; the widening warps may write it
+                        const uint32_t lb = k_armed % KS;
+                        if (!(ok = wait(&k_empty[lb], ((k_armed / KS) & 1u) ^ 1u))) break;
+                        ++k_armed;
+                        if (lane == 0) mbar_arrive(&k_full[lb]);
                     }
                     const uint32_t vb = it % VS, vn = it / VS;
                     if (!(ok = wait(&v_empty[vb], (vn & 1u) ^ 1u))) break;
@@ -298,10 +322,11 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             const uint32_t tmem_o = tmem_base + 2 * BN + r * BN;
             bool ok = true;
             uint32_t it = 0, n_seg = 0;
+            uint32_t ke = 0;              // the K ring entry of the next key tile to be scored
 
-            // scores of half h of key tile `tile` (its K stage must have landed)
-            auto issue_scores = [&](uint32_t tile, int h, bool last_of_segment) {
-                const uint32_t kb = tile % KS;
+            // scores of half h of the key tile at `entry` of the K ring (it must have landed)
+            auto issue_scores = [&](uint32_t entry, uint32_t entries, int h, bool last_of_segment) {
+                const uint32_t kb = entry % KS;
                 tc_fence_after();
                 const uint32_t k_lo = desc_lo(sbase + C::OFF_K + kb * C::TILE_BYTES + h * BH * 128, 16);
                 if (elect_one()) {
@@ -311,9 +336,20 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         umma_ss(tmem_base + r * BN + h * BH, desc_from_lo(q_lo + off, 1024),
                                 desc_from_lo(k_lo + off, 1024), idesc_qk, ks > 0 ? 1u : 0u);
                     }
+                    if (KIND == kPaged4 && entries == 2) {     // ... plus the lower bits of the scales
+                        const uint32_t lb = (entry + 1) % KS;
+                        const uint32_t l_lo = desc_lo(sbase + C::OFF_K + lb * C::TILE_BYTES + h * BH * 128, 16);
+#pragma unroll
+                        for (int ks = 0; ks < KSTEPS_QK; ++ks) {
+                            const uint32_t off = ((ks >> 2) * HALF_BYTES + (ks & 3) * 32) >> 4;
+                            umma_ss(tmem_base + r * BN + h * BH, desc_from_lo(q_lo + off, 1024),
+                                    desc_from_lo(l_lo + off, 1024), idesc_qk, 1u);
+                        }
+                    }
                     umma_commit(&s_full[r * 2 + h]);
                     if (h == 1) {
                         umma_commit(&k_empty[kb]);
+                        if (KIND == kPaged4 && entries == 2) umma_commit(&k_empty[(entry + 1) % KS]);
                         if (last_of_segment) umma_commit(q_empty);   // this row tile's Q may be replaced
                     }
                 }
@@ -326,14 +362,16 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 // both halves of the first key tile of the segment (its Q and K have to be there)
                 if (!(ok = warp_wait(q_use, n_seg & 1u, ab, kWaitRingFull))) break;
                 ++n_seg;
-                if (!(ok = warp_wait(&k_use[it % KS], (it / KS) & 1u, ab, kWaitRingFull))) break;
-                issue_scores(it, 0, n_tiles == 1);
-                issue_scores(it, 1, n_tiles == 1);
+                const uint32_t entries = k_entries(p.segments[si]);
+                if (!(ok = warp_wait(&k_use[ke % KS], (ke / KS) & 1u, ab, kWaitRingFull))) break;
+                issue_scores(ke, entries, 0, n_tiles == 1);
+                issue_scores(ke, entries, 1, n_tiles == 1);
                 for (int t = 0; t < n_tiles && ok; ++t, ++it) {
+                    ke += entries;
                     const uint32_t vb = it % VS;
                     if (!(ok = warp_wait(&v_use[vb], (it / VS) & 1u, ab, kWaitRingFull))) break;
                     const bool more = t + 1 < n_tiles;
-                    if (more && !(ok = warp_wait(&k_use[(it + 1) % KS], ((it + 1) / KS) & 1u, ab, kWaitRingFull))) break;
+                    if (more && !(ok = warp_wait(&k_use[ke % KS], (ke / KS) & 1u, ab, kWaitRingFull))) break;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         if (!(ok = warp_wait(&p_full[r * 2 + h], it & 1u, ab, kWaitTensor))) break;
@@ -350,7 +388,7 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                             if (h == 1) umma_commit(&v_empty[vb]);
                         }
                         __syncwarp();
-                        if (more) issue_scores(it + 1, h, t + 2 == n_tiles);
+                        if (more) issue_scores(ke, entries, h, t + 2 == n_tiles);
                     }
                 }
             }
@@ -375,7 +413,8 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             // The bytes of row r were written by TMA with the 128-byte swizzle (16-byte chunk c at position
             // c ^ (r & 7)); the fp16 row goes out in the same swizzle, channels 0-63 to row r of the lower
             // half tile and 64-127 to row r of the upper one, i.e. over the bytes just read.
-            auto widen_tile = [&](uint8_t* tile) {
+            // lower (4-bit rows): nullptr, or the tile that takes the products with the scales' lower bits
+            auto widen_tile = [&](uint8_t* tile, uint8_t* lower) {
                 if (KIND == kPaged4) {
                     const int rr = wq * 32 + lane;
                     const uint8_t* src = tile + HALF_BYTES + wq * Q4_WARP_STRIDE;
@@ -385,23 +424,37 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     for (int c = 0; c < 4; ++c)
                         raw[c] = *reinterpret_cast<const uint4*>(src + line * 128 + (((first | c) ^ (line & 7)) << 4));
                     const uint2 sw = *reinterpret_cast<const uint2*>(src + Q4_OFF_SCALE + lane * 8);
-                    const uint32_t s2[4] = {__byte_perm(sw.x, 0u, 0x1010), __byte_perm(sw.x, 0u, 0x3232),
-                                            __byte_perm(sw.y, 0u, 0x1010), __byte_perm(sw.y, 0u, 0x3232)};
+                    uint32_t s2[4] = {__byte_perm(sw.x, 0u, 0x1010), __byte_perm(sw.x, 0u, 0x3232),
+                                      __byte_perm(sw.y, 0u, 0x1010), __byte_perm(sw.y, 0u, 0x3232)};
                     const uint32_t magic = q4_magic();
                     __syncwarp();          // every lane has its source before any row is written
+                    auto widen_into = [&](uint8_t* out) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
+                        for (int c = 0; c < 4; ++c) {
+                            const uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {                // channels 32 c + 8 q .. + 7: one 16-byte chunk
-                            const uint32_t l0 = q4_signed_lo(w[q], magic), h0 = q4_signed_hi(w[q], magic);             // (0, 4), (1, 5)
-                            const uint32_t l1 = q4_signed_lo(w[q] >> 8, magic), h1 = q4_signed_hi(w[q] >> 8, magic);   // (2, 6), (3, 7)
-                            const uint4 f = make_uint4(h2_mul(__byte_perm(l0, h0, 0x5410), s2[c]), h2_mul(__byte_perm(l1, h1, 0x5410), s2[c]),
-                                                       h2_mul(__byte_perm(l0, h0, 0x7632), s2[c]), h2_mul(__byte_perm(l1, h1, 0x7632), s2[c]));
-                            const int c0 = (c & 1) * 4 + q;
-                            *reinterpret_cast<uint4*>(tile + (c >> 1) * HALF_BYTES + rr * 128 + ((c0 ^ (rr & 7)) << 4)) = f;
+                            for (int q = 0; q < 4; ++q) {                // channels 32 c + 8 q .. + 7: one 16-byte chunk
+                                const uint32_t l0 = q4_signed_lo(w[q], magic), h0 = q4_signed_hi(w[q], magic);             // (0, 4), (1, 5)
+                                const uint32_t l1 = q4_signed_lo(w[q] >> 8, magic), h1 = q4_signed_hi(w[q] >> 8, magic);   // (2, 6), (3, 7)
+                                const uint4 f = make_uint4(h2_mul(__byte_perm(l0, h0, 0x5410), s2[c]), h2_mul(__byte_perm(l1, h1, 0x5410), s2[c]),
+                                                           h2_mul(__byte_perm(l0, h0, 0x7632), s2[c]), h2_mul(__byte_perm(l1, h1, 0x7632), s2[c]));
+                                const int c0 = (c & 1) * 4 + q;
+                                *reinterpret_cast<uint4*>(out + (c >> 1) * HALF_BYTES + rr * 128 + ((c0 ^ (rr & 7)) << 4)) = f;
+                            }
                         }
+                    };
+                    if (lower) {           // the scales' lower three bits, then (below) the eight above them
+                        uint32_t upper[4];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            upper[c] = s2[c] & 0xFFF8FFF8u;
+                            s2[c] = h2_sub(s2[c], upper[c]);
+                        }
+                        widen_into(lower);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) s2[c] = upper[c];
                     }
+                    widen_into(tile);
                 } else {
                     const int rr = wq * 32 + lane;
                     uint8_t* src = tile + HALF_BYTES + rr * 128;
@@ -426,11 +479,12 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 fence_proxy_async_smem();                          // generic writes -> tensor core reads
                 __syncwarp();
             };
-            uint32_t it = 0, n_seg = 0;
+            uint32_t it = 0, ke = 0, n_seg = 0;                     // key tile, entry of the K ring, segment
             bool ok = true;
             for (int si = seg_lo; si < seg_hi && ok; ++si) {
                 const int n_tiles = (p.segments[si].k_end - p.segments[si].k_begin + BN - 1) / BN;
                 if (n_tiles <= 0) continue;
+                const uint32_t entries = k_entries(p.segments[si]);
                 // Q: bf16 -> fp16 in place (element by element, so the swizzle does not matter)
                 if (!(ok = warp_wait(q_full, n_seg & 1u, ab, kWaitRingFull))) break;
                 ++n_seg;
@@ -444,13 +498,16 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_ready);
-                for (int t = 0; t < n_tiles && ok; ++t, ++it) {
-                    const uint32_t kb = it % KS, vb = it % VS;
-                    if (!(ok = warp_wait(&k_full[kb], (it / KS) & 1u, ab, kWaitRingFull))) break;
-                    widen_tile(smem + C::OFF_K + kb * C::TILE_BYTES);
+                for (int t = 0; t < n_tiles && ok; ++t, ++it, ke += entries) {
+                    const uint32_t kb = ke % KS, lb = (ke + 1) % KS, vb = it % VS;
+                    const bool split = KIND == kPaged4 && entries == 2;
+                    if (split && !(ok = warp_wait(&k_full[lb], ((ke + 1) / KS) & 1u, ab, kWaitRingFull))) break;
+                    if (!(ok = warp_wait(&k_full[kb], (ke / KS) & 1u, ab, kWaitRingFull))) break;
+                    widen_tile(smem + C::OFF_K + kb * C::TILE_BYTES, split ? smem + C::OFF_K + lb * C::TILE_BYTES : nullptr);
+                    if (lane == 0 && split) mbar_arrive(&k_ready[lb]);      // the issuers wait for the other one alone
                     if (lane == 0) mbar_arrive(&k_ready[kb]);
                     if (!(ok = warp_wait(&v_full[vb], (it / VS) & 1u, ab, kWaitRingFull))) break;
-                    widen_tile(smem + C::OFF_V + vb * C::TILE_BYTES);
+                    widen_tile(smem + C::OFF_V + vb * C::TILE_BYTES, nullptr);
                     if (lane == 0) mbar_arrive(&v_ready[vb]);
                 }
             }
@@ -601,7 +658,7 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                             const uint64_t x2 = f2_fma(f2_pack(s[c * 32 + 2 * j], s[c * 32 + 2 * j + 1]), scale2, negm2);
                             uint64_t e2;
                             if (poly_pair(j)) {
-                                e2 = f2_exp2_poly(x2);
+                                e2 = f2_exp2_poly<KIND == kPaged4>(x2);
                             } else {
                                 float x0, x1;
                                 f2_unpack(x2, x0, x1);

@@ -12,6 +12,10 @@ __device__ __forceinline__ uint32_t h2_mul(uint32_t a, uint32_t b) {
     __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
     return *reinterpret_cast<uint32_t*>(&r);
 }
+__device__ __forceinline__ uint32_t h2_sub(uint32_t a, uint32_t b) {
+    __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<uint32_t*>(&r);
+}
 // 1024 in both halves, in a register: AND with one constant and OR with another is one instruction only when the
 // second one is not an immediate.
 __device__ __forceinline__ uint32_t q4_magic() {

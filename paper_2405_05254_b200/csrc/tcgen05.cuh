@@ -124,9 +124,11 @@ __device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
 }
 // 2^x for a pair on the FMA pipe instead of the special-function unit: x = n + f with n the nearest
 // integer (magic-number rounding) and f in [-0.5, 0.5]; 2^f by a cubic fitted to 7.5e-5 relative
-// error (far below the bf16 rounding that follows); n is added to the exponent field.  x is
+// error (far below the bf16 rounding that follows), or by a quartic (2.7e-6) where P is rounded to fp16 and the
+// sum of a few of them has to be exact; n is added to the exponent field.  x is
 // clamped to >= -125 so that the exponent stays in range, and anything at or below the clamp (a
 // masked score is -inf) comes out as exactly 0, like the special-function unit's result.
+template <bool QUARTIC = false>
 __device__ __forceinline__ uint64_t f2_exp2_poly(uint64_t x2) {
     float x0, x1;
     f2_unpack(x2, x0, x1);
@@ -136,10 +138,17 @@ __device__ __forceinline__ uint64_t f2_exp2_poly(uint64_t x2) {
     const uint64_t t2 = f2_add(x2, magic);                         // low mantissa bits = round(x)
     const uint64_t n2 = f2_add(t2, neg_magic);                     // round(x) as a float
     const uint64_t f2 = f2_fma(n2, f2_pack(-1.f, -1.f), x2);       // x - round(x)
-    uint64_t p2 = f2_fma(f2, f2_pack(0.0551716648042202f, 0.0551716648042202f),
-                         f2_pack(0.2426111400127411f, 0.2426111400127411f));
-    p2 = f2_fma(p2, f2, f2_pack(0.6932609677314758f, 0.6932609677314758f));
-    p2 = f2_fma(p2, f2, f2_pack(0.9999280571937561f, 0.9999280571937561f));
+    uint64_t p2;
+    if (QUARTIC) {
+        p2 = f2_fma(f2, f2_pack(0.009570102207362652f, 0.009570102207362652f), f2_pack(0.05591785907745361f, 0.05591785907745361f));
+        p2 = f2_fma(p2, f2, f2_pack(0.240247443318367f, 0.240247443318367f));
+        p2 = f2_fma(p2, f2, f2_pack(0.6931217908859253f, 0.6931217908859253f));
+        p2 = f2_fma(p2, f2, f2_pack(0.9999992847442627f, 0.9999992847442627f));
+    } else {
+        p2 = f2_fma(f2, f2_pack(0.0551716648042202f, 0.0551716648042202f), f2_pack(0.2426111400127411f, 0.2426111400127411f));
+        p2 = f2_fma(p2, f2, f2_pack(0.6932609677314758f, 0.6932609677314758f));
+        p2 = f2_fma(p2, f2, f2_pack(0.9999280571937561f, 0.9999280571937561f));
+    }
     float p0, p1, t0, t1;
     f2_unpack(p2, p0, p1);
     f2_unpack(t2, t0, t1);

@@ -2,8 +2,9 @@
 decode and chunk attention, against plain numpy (bit for bit where every rounding is fixed by the definition, in 64 bits otherwise).
 
 Tolerances of the attention tests are those of the packed paths (helpers.py).  What the 4-bit path adds: P * s is rounded to
-fp16, half a step 2^-11 relative per term, below the bf16 half step 2^-9 that the bf16 path has there; the codes are exact,
-the decode scores are fp32 sums of exact products, the chunk path's K and V values are rounded to fp16 once (2^-11).  The output's bf16 half step (2^-9) stays the largest single term."""
+fp16, half a step 2^-11 relative per term, below the bf16 half step 2^-8 that the bf16 path has there; the codes are exact,
+the decode scores are fp32 sums of exact products, the chunk path's V values (and K values, with many keys) are rounded to fp16
+once (2^-11).  The output's bf16 half step (2^-8) stays the largest single term."""
 import numpy as np
 import pytest
 
@@ -240,6 +241,50 @@ def test_chunk_matches_the_definition(q4, lens, Hq, Hkv, T, P, window, d):
     ref, lref = pr.attention(cache, f64(Q), T, window=window)
     assert_close(o, ref, "O")
     assert_lse_close(lse, lref, "LSE")
+
+
+# lens, Hq, Hkv, T, P, window, mode: rows of few keys (the chunk kernel takes K in two parts there), and both kinds in one call
+EXACT_LSE = [
+    ([7, 24], 2, 1, 6, 16, 0, "chunk"),
+    ([24, 40, 0], 8, 2, 22, 64, 0, "chunk"),
+    ([200, 6000], 4, 2, 150, 32, 0, "chunk"),          # one sequence on either side of the rule; a row tile over two heads
+    ([700], 4, 4, 600, 256, 0, "chunk"),               # three row tiles of a head, the first with the shortest rows
+    ([3000], 4, 1, 40, 128, 70, "chunk"),
+    ([3, 40], 6, 2, 3, 16, 0, "decode"),
+    ([64, 900], 8, 1, 2, 32, 100, "decode"),
+]
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,T,P,window,mode", EXACT_LSE)
+def test_q4_log_sum_exp_of_few_keys_is_that_of_32_bits(lens, Hq, Hkv, T, P, window, mode):
+    """No operand of the scores is rounded, so what is left is: an exponential's relative error (2.7e-6 at most); 16 partial
+    products of the tensor core a score (256 channels in two parts), each cut at 2^-23 of the largest sum met, which
+    is at most scale * |codes * scale part| . |q| <= 2 scale * 8 s . |q| over a group (the offset of the codes counts: the decode
+    kernel adds it as a term of its own); fp32 sums of n weights (n 2^-24); and the fp32 log-sum-exp itself (2^-23).  The sequence of
+    6,000 keys takes K rounded to fp16: 2^-11 of a value, at most 2^-11 scale |k| . |q| of its score."""
+    cache = pr.PagedCache(15, lens, P, Hkv, 128, True)
+    dev = pr.DevCache(cache)
+    Q = q_bits(15, len(lens), Hq, T, 128)
+    o, lse, _ = dev.attend(Q, T, mode=mode, window=window)
+    assert dev.status[0] == 0
+    ref, lref = pr.attention(cache, f64(Q), T, window=window)
+    assert_close(o, ref, "O")
+    assert_lse_close(lse, lref, "LSE")
+    for b, n in enumerate(lens):
+        if not n:
+            continue
+        for h in range(Hkv):
+            s = cache.pools[0][1][cache.row_numbers(b, h, n)].astype(np.float64).max(0)          # largest scale per group
+            k = np.abs(cache.rows(0, b, h)).max(0)
+            for g in range(Hq // Hkv):
+                q = np.abs(f64(Q)[b, h * (Hq // Hkv) + g])                                        # [T, 128]
+                bound = 2 * 8 * (q.reshape(T, 4, 32).sum(2) @ s) * 128 ** -0.5 * 16 * 2.0 ** -23
+                if mode == "chunk" and n >= 2048 and not window:
+                    bound += 2.0 ** -11 * (q @ k) * 128 ** -0.5
+                bound += 2.7e-6 + n * 2.0 ** -24 + 2.0 ** -23 * np.maximum(1, np.abs(lref[b, h * (Hq // Hkv) + g]))
+                got, want = lse[b, h * (Hq // Hkv) + g].astype(np.float64), lref[b, h * (Hq // Hkv) + g]
+                seen = ~np.isneginf(want)
+                assert (np.abs(got[seen] - want[seen]) <= bound[seen]).all(), (b, h, g, np.abs(got[seen] - want[seen]).max(), bound.min())
 
 
 @pytest.mark.parametrize("T,d", [(5, 64), (60, 128), (90, 64), (110, 128)])
