@@ -112,6 +112,19 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
             num_groups = groups;
         }
     }
+    if (mode == YOCO_MODE_DECODE && bounds.empty() && form.stream_tiles > 0 && total_tiles > 0) {
+        // shares equal in time: a stream counts form.stream_tiles more than it has (fewer where shares are small)
+        const int64_t extra = std::min<int64_t>(form.stream_tiles, total_tiles / num_groups / 4);
+        const int64_t total = total_tiles + extra * num_streams;
+        int64_t weight = 0, flat_lo = 0;     // at the start of the stream
+        for (int i = 0; i < s.B; ++i) {
+            const int64_t nt = (len_vis[i] + tile_n - 1) / tile_n - tile_lo[i];
+            for (int c = 0; c < s.Hkv; ++c, weight += nt + extra, flat_lo += nt)
+                for (int64_t p = (int64_t)bounds.size(); p < num_groups && p * total / num_groups < weight + extra + nt; ++p)
+                    bounds.push_back(flat_lo + std::max<int64_t>(p * total / num_groups - weight - extra, 0));
+        }
+        bounds.push_back(total_tiles);
+    }
 
     plan = Plan{};
     plan.rows_per_stream = rows_per_stream;

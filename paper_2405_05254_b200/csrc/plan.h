@@ -111,15 +111,20 @@ struct CacheForm {
     // sequences of 700 to 1,100 keys, 8 KV heads: groups of equal size, most of them in two streams, 16.1 us;
     // groups that end with their stream 12.8 us, and streams of at most 12 tiles need no merge.)
     int side_by_side8 = 0, side_by_side16 = 0;
+    // What going over to another stream costs a group (the warps' unequal last turns, the merge, the first loads), in
+    // tiles: shares are equal with it counted in.  (Measured with 0 / 12 / 24 / 40: 16 sequences of 4,001 to 62,000
+    // keys 141 / 121 / 118 / 121 us, 64 of 1,000 to 8,000 keys 104 / 88 / 86 / 90 us, one of 1M keys 221 / 219 / 219 / 219 us.)
+    int stream_tiles = 0;
     bool operator==(const CacheForm& o) const {
         return pair_tiles == o.pair_tiles && piece_divisor == o.piece_divisor && paged == o.paged && groups_per_sm == o.groups_per_sm &&
-               max_pieces == o.max_pieces && side_by_side8 == o.side_by_side8 && side_by_side16 == o.side_by_side16;
+               max_pieces == o.max_pieces && side_by_side8 == o.side_by_side8 && side_by_side16 == o.side_by_side16 &&
+               stream_tiles == o.stream_tiles;
     }
 };
 constexpr CacheForm kBf16Cache{};
 constexpr CacheForm kFp8Cache{true, 2, false};
 constexpr CacheForm kPagedCache{false, 1, true};
-constexpr CacheForm kPagedQ4Cache{true, 1, true, 1, 1, kQ4Warps8, kQ4Warps16};
+constexpr CacheForm kPagedQ4Cache{true, 1, true, 1, 1, kQ4Warps8, kQ4Warps16, 24};
 
 // Returns YOCO_OK or an error code; fills `plan`.  cu_kv_host may be null (tight packing).
 // max_sub_items: upper limit of pieces per decode group (1 = every group is one piece).

@@ -187,7 +187,7 @@ def attention_on_gpu(cache, dev, Q_bits, T):
             for w in range(2):
                 if c.q4:
                     codes, s = dev.pools[2 * w][at].int(), dev.pools[2 * w + 1][at].double()
-                    x = torch.stack([codes & 15, codes >> 4], -1).reshape(n, -1).double() - 8
+                    x = torch.stack([codes & 15, codes >> 4], -1).reshape(n, c.d).double() - 8
                     rows.append(x * s.repeat_interleave(32, 1))
                 else:
                     rows.append(dev.pools[w][at].double())
@@ -204,6 +204,8 @@ def attention_on_gpu(cache, dev, Q_bits, T):
     ([150000, 70001], 8, 8, 1, 16),          # small pages: many batches of page numbers per warp
     ([600000], 16, 8, 2, 64),                # more than 32 tiles per warp of the 4-bit kernel
     ([260000], 32, 4, 2, 32),                # 16 query rows per KV head
+    ([40000, 17, 30000, 0, 5000, 1], 16, 8, 1, 64),     # CTAs that go from stream to stream, some of them empty
+    ([9000, 2, 130, 7000, 64, 65, 2500, 12000, 300, 5000, 1111, 640], 12, 4, 2, 16),
 ])
 def test_decode_of_long_caches(q4, lens, Hq, Hkv, T, P):
     cache = pr.PagedCache(47, lens, P, Hkv, 128, q4)
