@@ -357,7 +357,8 @@ int32_t yoco_kv_append_fp8(const yoco_kv_append_shape* shape, const void* X, con
  *          writes no larger one).
  * Pools start on 16-byte boundaries (scales too).  Pool, table, Q and O are device memory of the current device.
  *
- * Table entries are read on the device, only those that hold a key of the call.  One outside [0, num_pages) is
+ * Table entries are read on the device, only those that hold a key that some row of the call sees (with a window, pages
+ * wholly below every row's window may have been given away); slots of unseen keys may hold anything.  One outside [0, num_pages) is
  * never followed: attention and gather read zeros in its place, append stores nothing for it, and the call's status
  * (yoco_xattn_status of its workspace; yoco_kv_append_status for append and gather) becomes
  * YOCO_ERR_BAD_PAGE, wait class YOCO_STATUS_BAD_PAGE.  Results of other sequences are not affected. */
@@ -444,8 +445,8 @@ int32_t yoco_xattn_chunk_paged_q4(const yoco_xattn_shape* shape, const yoco_page
                                   void* workspace, size_t workspace_bytes, void* stream);
 
 /* (No counterpart in the paper.)  Synchronises `stream`; returns YOCO_OK, or YOCO_ERR_TIMEOUT if an
- * append kernel on the current device gave up a wait (YOCO_ERR_BAD_PAGE: a paged append or gather met a bad page) since the last call of this function (which
- * clears the record).  The _detail form also reports which wait and which CTA (see below). */
+ * append kernel on the current device gave up a wait (YOCO_ERR_BAD_PAGE: a paged append or gather met a bad page)
+ * since the last call of this function (which clears the record).  The _detail form also reports which wait and which CTA (see below). */
 int32_t yoco_kv_append_status(void* stream);
 int32_t yoco_kv_append_status_detail(void* stream, int32_t* wait_class, int32_t* cta);
 

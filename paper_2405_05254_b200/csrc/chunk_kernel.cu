@@ -129,7 +129,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                 c.k_end = sg.k_end;
                 c.row0 = sg.kv_row0 - sg.k_begin;
                 c.fresh = true;
-                if (PAGED) c.pc.start(p.pages, sg.stream, sg.k_begin, sg.k_end, ab.status);
+                if (PAGED) c.pc.start(p.pages, sg.stream, sg.k_begin, sg.k_end, first_seen(sg.n_full, p.window), ab.status);
             };
             auto load_pages = [&](Cursor& c, uint8_t* tile, const CUtensorMap& tm, uint64_t* bar) {
                 const int n_box = c.pc.enter(c.k0), rows = c.pc.box_rows();
@@ -322,6 +322,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             // sliding window: the row at position i keeps i - C < j; lo_max is the highest such bound
             const int lo = p.window > 0 ? max(0, n_full + (r_local % p.T) - p.window) : 0;
             const int lo_max = p.window > 0 ? n_full + p.T - 1 - p.window : 0;
+            const int seen = PAGED ? first_seen(n_full, p.window) : 0;    // V rows below it may hold anything
             float m_ref = -INFINITY, l = 0.f;
             const uint32_t seg_first_it = it;
 
@@ -403,11 +404,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                     l += (a0 + a1) + (b0 + b1);
                 }
 
-                // keys past the end of the sequence: their V rows may hold anything; zero them so
-                // that 0 * garbage cannot make NaN
-                if (k0 + BN > seg.n_kv) {
+                // keys past the end of the sequence (or before all windows): their V rows may hold anything; zero them
+                // so that 0 * garbage cannot make NaN
+                if (k0 + BN > seg.n_kv || k0 < seen) {
                     if (!(ok = warp_wait(&v_full[b], n & 1u, ab, kWaitRingFull))) continue;
-                    if (k0 + row >= seg.n_kv) {
+                    if (k0 + row >= seg.n_kv || k0 + row < seen) {
                         uint8_t* vrow = smem + C::OFF_V + b * C::TILE_BYTES + row * 128;
 #pragma unroll
                         for (int h = 0; h < HALVES; ++h)

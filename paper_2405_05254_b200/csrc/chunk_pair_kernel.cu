@@ -37,11 +37,13 @@
 // of the value; O leaves in bf16).  For K that rounding puts a score off by about 3e-4, which the log-sum-exp of a row of
 // many keys averages out and that of a row of few does not: where a CTA has a row that sees fewer than kExactKeys keys,
 // K takes two ring entries, (code - 8) times the upper eight bits of the scale and times its lower three, both
-// exact in fp16, and the scores are the sum of two products.  The polynomial exponentials are quartic (no time lost: 520 us
-// for 391 tokens over 65,927 keys, where the cubic took 522).  Relative error (2-norm) of the log-sum-exp against 64 bits,
-// chunks of 11 to 41 tokens over as many keys: 4e-5 with K rounded once and the cubic, 4e-6 with K in two parts, 1.6e-7
-// with the quartic as well; above the rule, at most 1.2e-6.  K in two parts everywhere would make that case 812 us; with
-// the rule a whole sequence of 4,096 tokens pays most, 575 us instead of 494.
+// exact in fp16, and the scores are the sum of two products.  The polynomial exponentials are quartic (no time lost:
+// 522 us with the cubic, 520 us with the quartic for 391 tokens over 65,927 keys).  Relative error (2-norm) of the log-sum-exp
+// against 64 bits, chunks of 11 to 41 tokens over as many keys: 4e-5 with K rounded once and the cubic, 4e-6 with K in two
+// parts, 1.6e-7 with the quartic as well; above the rule, at most 1.2e-6.  K in two parts everywhere would make that case
+// 812 us; with the rule a whole sequence of 4,096 tokens pays most, 575 us instead of 494.
+// V rows that a window has left behind are zeroed where they are widened; the softmax warps, which zero the rows
+// past the end, have no register left for it (595 us with the test there; 472 us as it is, 890 TFLOP/s).
 #include <cuda_fp16.h>
 
 #include "kernels.h"
@@ -234,7 +236,7 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                                         seg.q_row0 + (m_tile * 2 + r) * BM, q_full);
                 }
                 PageCursor<BN> pc;
-                if (PAGED) pc.start(p.pages, seg.stream, seg.k_begin, seg.k_end, ab.status);
+                if (PAGED) pc.start(p.pages, seg.stream, seg.k_begin, seg.k_end, first_seen(seg.n_full, p.window), ab.status);
                 // the boxes of one tile of a paged cache
                 auto load_pages = [&](uint8_t* tile, const CUtensorMap& tm, const CUtensorMap& tmS, uint64_t* bar, int k0) {
                     const int n_box = pc.enter(k0), rows = pc.box_rows();
@@ -414,7 +416,8 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             // c ^ (r & 7)); the fp16 row goes out in the same swizzle, channels 0-63 to row r of the lower
             // half tile and 64-127 to row r of the upper one, i.e. over the bytes just read.
             // lower (4-bit rows): nullptr, or the tile that takes the products with the scales' lower bits
-            auto widen_tile = [&](uint8_t* tile, uint8_t* lower) {
+            // dead (4-bit rows): this lane's row holds anything and must come out as zeros
+            auto widen_tile = [&](uint8_t* tile, uint8_t* lower, bool dead) {
                 if (KIND == kPaged4) {
                     const int rr = wq * 32 + lane;
                     const uint8_t* src = tile + HALF_BYTES + wq * Q4_WARP_STRIDE;
@@ -423,7 +426,7 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
                         raw[c] = *reinterpret_cast<const uint4*>(src + line * 128 + (((first | c) ^ (line & 7)) << 4));
-                    const uint2 sw = *reinterpret_cast<const uint2*>(src + Q4_OFF_SCALE + lane * 8);
+                    const uint2 sw = dead ? make_uint2(0u, 0u) : *reinterpret_cast<const uint2*>(src + Q4_OFF_SCALE + lane * 8);
                     uint32_t s2[4] = {__byte_perm(sw.x, 0u, 0x1010), __byte_perm(sw.x, 0u, 0x3232),
                                       __byte_perm(sw.y, 0u, 0x1010), __byte_perm(sw.y, 0u, 0x3232)};
                     const uint32_t magic = q4_magic();
@@ -485,6 +488,8 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 const int n_tiles = (p.segments[si].k_end - p.segments[si].k_begin + BN - 1) / BN;
                 if (n_tiles <= 0) continue;
                 const uint32_t entries = k_entries(p.segments[si]);
+                const int k_begin = p.segments[si].k_begin;
+                const int seen = first_seen(p.segments[si].n_full, p.window);
                 // Q: bf16 -> fp16 in place (element by element, so the swizzle does not matter)
                 if (!(ok = warp_wait(q_full, n_seg & 1u, ab, kWaitRingFull))) break;
                 ++n_seg;
@@ -503,11 +508,12 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     const bool split = KIND == kPaged4 && entries == 2;
                     if (split && !(ok = warp_wait(&k_full[lb], ((ke + 1) / KS) & 1u, ab, kWaitRingFull))) break;
                     if (!(ok = warp_wait(&k_full[kb], (ke / KS) & 1u, ab, kWaitRingFull))) break;
-                    widen_tile(smem + C::OFF_K + kb * C::TILE_BYTES, split ? smem + C::OFF_K + lb * C::TILE_BYTES : nullptr);
+                    widen_tile(smem + C::OFF_K + kb * C::TILE_BYTES, split ? smem + C::OFF_K + lb * C::TILE_BYTES : nullptr, false);
                     if (lane == 0 && split) mbar_arrive(&k_ready[lb]);      // the issuers wait for the other one alone
                     if (lane == 0) mbar_arrive(&k_ready[kb]);
                     if (!(ok = warp_wait(&v_full[vb], (it / VS) & 1u, ab, kWaitRingFull))) break;
-                    widen_tile(smem + C::OFF_V + vb * C::TILE_BYTES, nullptr);
+                    const int key = k_begin + t * BN + wq * 32 + lane;
+                    widen_tile(smem + C::OFF_V + vb * C::TILE_BYTES, nullptr, KIND == kPaged4 && key < seen);
                     if (lane == 0) mbar_arrive(&v_ready[vb]);
                 }
             }
@@ -559,6 +565,7 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             // sliding window: the row at position i keeps i - C < j; lo_max is the highest such bound
             const int lo = p.window > 0 ? max(0, n_full + (r_local % p.T) - p.window) : 0;
             const int lo_max = p.window > 0 ? n_full + p.T - 1 - p.window : 0;
+            const int seen = first_seen(n_full, p.window);     // V rows below it may hold anything
             float m_ref = -INFINITY, l = 0.f;
             const uint32_t seg_first_it = it, seg_first_u = 2 * it;
             // 8-bit cache: the key scale of this KV head folds into the softmax scale, the value scale
@@ -627,16 +634,16 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     }
                     const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;
 
-                    // keys past the end of the sequence: their V rows may hold anything; zero them so
+                    // keys past the end of the sequence (or before all windows): their V rows may hold anything; zero them so
                     // that 0 * garbage cannot make NaN.  Both warpgroups write the same zeros in
                     // the first half step, each before it releases its own first product on this tile.
-                    if (h == 0 && k0 + BN > seg.n_kv) {
+                    if (h == 0 && (k0 + BN > seg.n_kv || (KIND == kPaged16 && k0 < seen))) {
                         const uint32_t vb = it % VS, vn = it / VS;
                         if (!(ok = warp_wait(&v_use[vb], vn & 1u, ab, kWaitRingFull))) {
                             skip_turn(u);
                             continue;
                         }
-                        if (k0 + row >= seg.n_kv) {
+                        if (k0 + row >= seg.n_kv || (KIND == kPaged16 && k0 + row < seen)) {
                             uint8_t* vrow = smem + C::OFF_V + vb * C::TILE_BYTES + row * 128;
 #pragma unroll 1
                             for (int q = 0; q < 8 * HALVES; ++q)

@@ -143,7 +143,7 @@ __device__ __forceinline__ void decode_body(const CUtensorMap& tmK, const CUtens
                     const int k_lo = seg.k_begin + s_lo * TILE_N;
                     const int k_hi = min(seg.k_begin + s_hi * TILE_N, seg.k_end);
                     PageCursor<TILE_N> pc;
-                    if (PAGED) pc.start(p.pages, seg.stream, k_lo, k_hi, ab.status);
+                    if (PAGED) pc.start(p.pages, seg.stream, k_lo, k_hi, first_seen(seg.n_full, p.window), ab.status);
                     for (int k0 = k_lo; k0 < k_hi; k0 += TILE_N, ++it) {
                         const uint32_t stage = it % STAGES, round = it / STAGES;
                         // self-test of the give-up path: nothing is armed, so no stage is needed either
@@ -260,6 +260,7 @@ __device__ __forceinline__ void decode_body(const CUtensorMap& tmK, const CUtens
             const int n_edge = min(n_full, seg.n_kv);      // tiles that end at or below it need no mask
             const int vis0 = min(seg.n_kv, max(0, n_full + (g % p.T)));
             const int vis1 = min(seg.n_kv, max(0, n_full + ((g + 8) % p.T)));
+            const int seen = PAGED ? first_seen(n_full, p.window) : 0;    // rows below it may hold anything
 
             float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
             float o[NT_O][4];
@@ -359,12 +360,13 @@ __device__ __forceinline__ void decode_body(const CUtensorMap& tmK, const CUtens
                             o[nt][2] *= alpha1; o[nt][3] *= alpha1;
                         }
                     }
-                    // ---- rows past the end of the sequence may hold anything: zero them so that
-                    //      0 * garbage cannot produce NaN in O += P V ----
-                    if (kw + 16 > seg.n_kv) {
-                        const int first_bad = max(seg.n_kv - kw, 0);          // 0..15
+                    // ---- rows past the end of the sequence (or before all windows) may hold anything: zero them so
+                    //      that 0 * garbage cannot produce NaN in O += P V ----
+                    if (kw + 16 > seg.n_kv || kw < seen) {
+                        const int first_bad = min(max(seg.n_kv - kw, 0), 16);
                         uint8_t* vrow = stage_mem + stage * C::STAGE_BYTES + C::TENSOR_BYTES;
-                        for (int r = first_bad; r < 16; ++r) {
+                        for (int r = kw < seen ? 0 : first_bad; r < 16; ++r) {
+                            if (r < first_bad && kw + r >= seen) continue;
                             const int key_l = warp * 16 + r;
                             for (int b = lane * 16; b < C::HALVES * 128; b += 512) {
                                 const int h = b >> 7, off = b & 127;
@@ -390,7 +392,7 @@ __device__ __forceinline__ void decode_body(const CUtensorMap& tmK, const CUtens
                             mma_bf16_16816(o[nt + 1], pa, b2, b3);
                         }
                     }
-                    if (kw + 16 > seg.n_kv) fence_proxy_async_smem();   // generic writes before TMA reuse
+                    if (kw + 16 > seg.n_kv || kw < seen) fence_proxy_async_smem();   // generic writes before TMA reuse
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&empty_bar[stage]);

@@ -9,6 +9,10 @@ __device__ __forceinline__ void report_bad_page(int32_t* status) {
     atomicCAS(status, 0, status_word(kBadPage, (int32_t)(blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z))));
 }
 
+// Lowest key that any row of a segment sees: with a window, row 0's first one.  Keys below it in the same tile are read by
+// nobody: their pages may be gone and their rows may hold anything.
+__device__ __forceinline__ int first_seen(int n_full, int window) { return window > 0 ? max(0, n_full - window) : 0; }
+
 // A producer warp's view of the pages of one (sequence, KV head) stream.  Every lane holds one page, 32 at a time:
 // the pool row of its first slot, so that a tile costs one shuffle per box; the next 32 are already requested, so a
 // table read is waited for once per run.  (A producer is one warp working through a chain of dependent
@@ -17,22 +21,22 @@ __device__ __forceinline__ void report_bad_page(int32_t* status) {
 // not.)  All lanes call it together; keys only grow; k_lo is a multiple of TILE.
 template <int TILE>
 struct PageCursor {
-    static constexpr int MAX_BOXES = TILE / 16;    // pages hold at least 16 keys
     // copies, not a reference to the kernel's parameters: those would be read again after every barrier wait
     int shift, num_pages, page_rows, pool_rows, head_row;
     const int32_t* entries;                        // this sequence's row of the table
     int32_t* status;
     int first, last, lane;
+    int seen;                                      // first page with a key that somebody sees
     int32_t now;                                   // row of page first + lane
     int32_t later;                                 // number of page first + 32 + lane
 
     __device__ __forceinline__ int32_t fetch(int page) const { return page <= last ? __ldg(entries + page) : 0; }
-    __device__ __forceinline__ int32_t row_of(int32_t page) const {
-        if ((uint32_t)page < (uint32_t)num_pages) return page * page_rows + head_row;
-        report_bad_page(status);                   // (entries behind the run were replaced by page 0)
+    __device__ __forceinline__ int32_t row_of(int32_t page) const {      // `page` is the entry first + lane
+        if ((uint32_t)page < (uint32_t)num_pages && first + lane >= seen) return page * page_rows + head_row;
+        if (first + lane >= seen) report_bad_page(status);               // (entries behind the run were replaced by page 0)
         return pool_rows;
     }
-    __device__ __forceinline__ void start(const PageMap& map, int stream, int k_lo, int k_end, int32_t* status_word) {
+    __device__ __forceinline__ void start(const PageMap& map, int stream, int k_lo, int k_end, int key_seen, int32_t* status_word) {
         shift = map.page_shift;
         num_pages = map.num_pages;
         page_rows = map.page_rows;
@@ -44,6 +48,7 @@ struct PageCursor {
         lane = (int)(threadIdx.x & 31u);
         first = k_lo >> shift;
         last = (k_end - 1) >> shift;
+        seen = key_seen >> shift;
         const int32_t page = fetch(first + lane);
         later = fetch(first + 32 + lane);
         now = row_of(page);

@@ -384,6 +384,34 @@ def test_a_bad_page_is_reported_and_harms_nobody_else(q4, mode):
 
 
 @pytest.mark.parametrize("q4", [False, True])
+@pytest.mark.parametrize("lens,Hq,T,P,window,mode", [
+    ([900, 333], 8, 1, 16, 100, "decode"), ([900, 333, 20], 8, 2, 32, 70, "decode"), ([5000], 4, 3, 128, 1, "decode"),
+    ([900, 333], 8, 20, 16, 100, "chunk"),                     # 80 rows: the one-tile kernel of the bf16 cache
+    ([900, 5000], 8, 90, 32, 130, "chunk"), ([700], 4, 300, 64, 257, "chunk"), ([5000], 4, 9, 256, 1, "chunk"),
+])
+def test_pages_below_every_window_may_be_gone(q4, lens, Hq, T, P, window, mode):
+    """Entries of pages that no row sees any more are nonsense, and unseen rows of the first seen page are NaN."""
+    cache = pr.PagedCache(43, lens, P, 2, 128, q4)
+    Q = q_bits(43, len(lens), Hq, T, 128)
+    ref, lref = pr.attention(cache, f64(Q), T, window=window)
+    for b, n in enumerate(lens):
+        lo = max(0, n - T + 1 - window)
+        for h in range(2):
+            at = cache.row_numbers(b, h, lo)
+            for pool in cache.pools:
+                if q4:
+                    pool[0][at], pool[1][at] = 0, np.nan
+                else:
+                    pool[at] = 0x7FC0 if h else 0x7F80               # NaN, +inf
+        cache.table[b, :lo // P] = [-1, 10**9, cache.num_pages][b % 3]
+    dev = pr.DevCache(cache)
+    o, lse, _ = dev.attend(Q, T, mode=mode, window=window)
+    assert dev.status[0] == 0
+    assert_close(o, ref, "O")
+    assert_lse_close(lse, lref, "LSE")
+
+
+@pytest.mark.parametrize("q4", [False, True])
 def test_append_skips_a_bad_page_and_says_so(q4):
     import torch
     from paper_2405_05254_b200 import binding as bd
