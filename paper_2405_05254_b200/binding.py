@@ -477,24 +477,29 @@ _PAGED_TYPES = {"q": "torch.bfloat16", "g": "torch.bfloat16", "x": "torch.bfloat
 
 class PreparedPagedCall:
     """A call of one of the paged-cache functions whose arguments are checked and marshalled once; run() only
-    enqueues.  The tensors and host arrays are kept alive; host int32 arrays are read at every run(), so a serving
-    loop may advance its lengths in place."""
+    enqueues, on ``stream`` or, without one, on the stream that is current then.  The tensors are kept alive; shape, layout
+    and the numbers of rows (``new_len``, ``begin``, ``end``) are copied.  ``kv_len``, if a contiguous int32 array, is read
+    at every run(), so a serving loop may advance its lengths in place."""
 
     def __init__(self, fn_name, shape, layout, *args, stream=None):
         import torch
         kinds = _PAGED_ARGS[fn_name]
         if len(args) != len(kinds):
             raise TypeError(f"{fn_name} takes {len(kinds)} arguments after the layout, got {len(args)}")
-        self._keep = [shape, layout, stream]
-        out, device, host = [ctypes.byref(shape), ctypes.byref(layout)], torch.cuda.current_device(), []
+        self._keep = [layout, stream]
+        shape, cos_sin = type(shape).from_buffer_copy(shape), getattr(layout, "tensor", None)
+        layout = PagedLayout.from_buffer_copy(layout)
+        self._keep += [shape, layout]
+        out, device, host = [ctypes.addressof(shape), ctypes.addressof(layout)], torch.cuda.current_device(), []
         for n, (kind, a) in enumerate(zip(kinds, args)):
             if kind == "n":
-                keep, p = _host_i32(a)
+                lengths = kinds == "qnq" or "w" in kinds or ("x" in kinds and n == len(kinds) - 1)      # kv_len
+                keep = _host_i32(a if lengths or a is None else np.array(a, dtype=np.int32))[0]
                 if keep is not None and keep.size < shape.B:
                     raise ValueError(f"{fn_name}: host array {n} has {keep.size} entries for {shape.B} sequences")
                 self._keep.append(keep)
                 host.append(keep)
-                out.append(p)
+                out.append(None if keep is None else keep.ctypes.data)
                 continue
             if a is None and kind == "l":
                 out.append(None)
@@ -503,15 +508,51 @@ class PreparedPagedCall:
                 raise ValueError(f"{fn_name}: tensor {n} is on {a.device}, the current device is cuda:{device}")
             if str(a.dtype) != _PAGED_TYPES.get(kind, str(a.dtype)):
                 raise ValueError(f"{fn_name}: tensor {n} has type {a.dtype}, not {_PAGED_TYPES[kind]}")
-            if kind not in "xkcs" and not a.is_contiguous():
-                raise ValueError(f"{fn_name}: tensor {n} must be contiguous")
+            if not self._in_order(kind, a, shape, layout):
+                raise ValueError(f"{fn_name}: tensor {n} has strides {a.stride()}, which are not those of the call")
             self._keep.append(a)
-            out.append(_ptr(a))
+            out.append(a.data_ptr())
             if kind == "w":
-                out.append(ctypes.c_size_t(a.numel() * a.element_size()))
+                out.append(a.numel() * a.element_size())
+        if cos_sin is not None and (cos_sin.shape[1] != shape.d or cos_sin.device != torch.device("cuda", device)):
+            raise ValueError(f"{fn_name}: cos_sin is {tuple(cos_sin.shape)} on {cos_sin.device} for head dimension {shape.d}")
         self._check_sizes(fn_name, kinds, shape, layout, args, host)
-        out.append(_stream_ptr(stream))
-        self._name, self._fn, self._args = fn_name, getattr(lib(), fn_name), tuple(out)
+        self._stream = None if stream is None else stream.cuda_stream
+        self._current_stream, self._device = torch._C._cuda_getCurrentRawStream, device
+        self._others = torch.cuda.device_count() > 1
+        # every argument is a pointer or a size: a prototype of integers costs 0.2 us less a call than pointer objects
+        proto = ctypes.CFUNCTYPE(ctypes.c_int32, *[ctypes.c_void_p] * (len(out) + 1))
+        self._name, self._fn, self._args = fn_name, proto((fn_name, lib())), tuple(out)
+
+    @staticmethod
+    def _in_order(kind, a, shape, layout):
+        """Whether the tensor's strides are those that the call goes by: contiguous, or rows (of all heads of a token, of a
+        page, of a sequence's table) that lie src_stride, page_rows or table_stride apart."""
+        if kind == "i" and a.dim() == 2 and a.shape[0] > 1 and a.stride(0) != layout.table_stride:
+            return False
+        if a.is_contiguous():
+            return True
+        elems = {"k": shape.d, "c": shape.d // 2, "s": shape.d // 32}.get(kind)
+        if kind == "x":
+            width, apart = shape.Hkv * shape.d, shape.src_stride or shape.Hkv * shape.d
+        elif kind == "i":
+            width, apart = a.shape[-1], layout.table_stride
+        elif elems:
+            width = shape.Hkv * layout.page_size * elems
+            apart = layout.page_rows * elems or width
+        else:
+            return False
+        n, i = 1, a.dim()
+        while i > 0 and n < width:                 # the dimensions of one row, densely
+            i -= 1
+            if a.shape[i] != 1 and a.stride(i) != n:
+                return False
+            n *= a.shape[i]
+        for j in reversed(range(i)):               # the rows, `apart` from one another
+            if a.shape[j] != 1 and a.stride(j) != apart:
+                return False
+            apart *= a.shape[j]
+        return True
 
     @staticmethod
     def _check_sizes(fn_name, kinds, shape, layout, args, host):
@@ -527,9 +568,6 @@ class PreparedPagedCall:
             need["x"] = max(0, tokens - 1) * (shape.src_stride or shape.Hkv * shape.d) + shape.Hkv * shape.d if tokens else 0
         elif host[0] is not None and host[1] is not None:
             need["g"] = int((host[1][:B].astype(np.int64) - host[0][:B]).sum()) * shape.Hkv * shape.d
-        cos_sin = getattr(layout, "tensor", None)
-        if cos_sin is not None and (cos_sin.shape[1] != shape.d or not cos_sin.is_cuda):
-            raise ValueError(f"{fn_name}: cos_sin is {tuple(cos_sin.shape)} on {cos_sin.device} for head dimension {shape.d}")
         for n, (kind, a) in enumerate(zip(kinds, args)):
             if a is not None and kind in need:
                 have = a.untyped_storage().nbytes() // a.element_size() - a.storage_offset()
@@ -537,7 +575,12 @@ class PreparedPagedCall:
                     raise ValueError(f"{fn_name}: tensor {n} holds {have} elements, the call needs {need[kind]}")
 
     def run(self) -> None:
-        rc = self._fn(*self._args)
+        if self._others:
+            import torch
+            if torch.cuda.current_device() != self._device:
+                raise ValueError(f"{self._name}: prepared for cuda:{self._device}, the current device is cuda:{torch.cuda.current_device()}")
+        stream = self._stream
+        rc = self._fn(*self._args, self._current_stream(self._device) if stream is None else stream)
         if rc != OK:
             raise YocoError(rc, self._name)
 

@@ -473,6 +473,118 @@ def test_a_recorded_step_follows_the_page_table_and_two_streams_do_not_meet(q4):
 
 
 @pytest.mark.parametrize("q4", [False, True])
+def test_a_prepared_call_follows_its_lengths_and_the_current_stream(q4):
+    """kv_len is read at every run(), numbers of new tokens are those of the preparation, and run() goes to the stream that
+    is current then (a call given a stream stays on it)."""
+    import torch
+    from helpers import bf16_dev_to_f64
+    from paper_2405_05254_b200 import binding as bd
+    H, Hq, P, steps = 2, 8, 16, 5
+    tail = "_q4" if q4 else ""
+    lens = np.array([30, 63], np.int32)
+    cache = pr.PagedCache(53, lens + steps, P, H, 128, q4, slack_nan=False)
+    dev = pr.DevCache(cache)
+    dev.layout.page_rows = cache.page_rows
+    new, B = np.array([1, 1], np.int32), 2
+    shape = bd.make_shape(B, Hq, H, 128, 1)
+    r = np.random.default_rng(53)
+    x = torch.empty(B, 2 * H * 128, dtype=torch.bfloat16, device="cuda")
+    Q, O = torch.empty(B, Hq, 1, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(B, Hq, 1, 128, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(bd.yoco_xattn_workspace_size_paged(shape, dev.layout, lens + steps, bd.MODE_DECODE, q4) + 4096, dtype=torch.uint8, device="cuda")
+    store = bd.prepare_paged("yoco_paged_append" + tail, bd.PagedAppendShape(B, H, 128, 0, 2 * H * 128), dev.layout, x[:, :H * 128],
+                             x[:, H * 128:], *dev.pools, dev.table, new, lens)
+    attend = bd.prepare_paged("yoco_xattn_decode_paged" + tail, shape, dev.layout, Q, *dev.pools, dev.table, lens, O, None, ws)
+    new[:] = 10**6                                        # not read again
+    shape.T, dev.layout.num_pages = 50, 1                 # neither are these
+    side = torch.cuda.Stream()
+    for step in range(steps):
+        lens += 1
+        src = pr.bf16(r.standard_normal((B, 2 * H * 128)))[0]
+        Qb = q_bits(60 + step, B, Hq, 1, 128)
+        for b in range(B):
+            for h in range(H):
+                at = cache.row_numbers(b, h, int(lens[b]))[-1]
+                for w in range(2):
+                    y = si.bf16_bits_to_f32(src[b, (w * H + h) * 128:(w * H + h + 1) * 128])[None]
+                    if q4:
+                        cache.pools[w][0][at], cache.pools[w][1][at] = (a[0] for a in pr.quantise(y))
+                    else:
+                        cache.pools[w][at] = pr.bf16(y)[0][0]
+        xd, qd = pr.bits_to_dev(src), pr.bits_to_dev(Qb)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side if step % 2 else torch.cuda.current_stream()):
+            torch.cuda._sleep(2_000_000)                  # about a millisecond: a call on another stream would be too early
+            x.copy_(xd.view_as(x))
+            Q.copy_(qd.view_as(Q))
+            store.run()
+            attend.run()
+        torch.cuda.synchronize()
+        cache.lens = lens.copy()
+        assert_close(bf16_dev_to_f64(O), pr.attention(cache, f64(Qb), 1)[0])
+
+
+@pytest.mark.parametrize("q4", [False, True])
+def test_a_recorded_prompt_step_and_the_same_bits_every_time(q4):
+    """Append, rotation and chunk attention in one graph, replayed with other rows, other queries and other pages, give the
+    bits of the calls made one by one; repeated calls give the same bits."""
+    import torch
+    from paper_2405_05254_b200 import binding as bd
+    H, Hq, P, T, B = 2, 8, 32, 70, 2
+    tail = "_q4" if q4 else ""
+    lens = np.array([1900, 70], np.int32)
+    cache = pr.PagedCache(59, lens, P, H, 128, q4, spare_pages=70, slack_nan=False)
+    dev = pr.DevCache(cache, pr.cos_sin(2000, 128), 1)
+    shape, rows = bd.make_shape(B, Hq, H, 128, T), bd.PagedAppendShape(B, H, 128, T, 0)
+    k, v = (torch.randn(B * T, H * 128, device="cuda").to(torch.bfloat16) for _ in range(2))
+    Q = torch.randn(B, Hq, T, 128, device="cuda").to(torch.bfloat16)
+    R, O, L = torch.empty_like(Q), torch.empty_like(Q), torch.empty(B, Hq, T, device="cuda")
+    ws = torch.empty(bd.yoco_xattn_workspace_size_paged(shape, dev.layout, lens, bd.MODE_CHUNK, q4), dtype=torch.uint8, device="cuda")
+    calls = [bd.prepare_paged("yoco_paged_append" + tail, rows, dev.layout, k, v, *dev.pools, dev.table, None, lens),
+             bd.prepare_paged("yoco_rope_q", shape, dev.layout, Q, lens, R),
+             bd.prepare_paged("yoco_xattn_chunk_paged" + tail, shape, dev.layout, R, *dev.pools, dev.table, lens, O, L, ws)]
+
+    def step():
+        for c in calls:
+            c.run()
+
+    def result():
+        torch.cuda.synchronize()
+        assert bd.yoco_xattn_status(ws) == 0 and bd.yoco_kv_append_status() == 0
+        return [t.clone().view(torch.uint8) for t in (O, L, *dev.pools)]
+
+    step()
+    first = result()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for t in (O, L):
+        t.fill_(7.0)
+    for _ in range(3):
+        g.replay()
+        assert all(torch.equal(a, b) for a, b in zip(result(), first))
+    k.normal_(), v.normal_(), Q.normal_()
+    spare = np.setdiff1d(np.arange(cache.num_pages), np.concatenate([cache.table[0], cache.table[1, :3]]))
+    dev.table[0, :60] = torch.from_numpy(spare[:60].astype(np.int32)).cuda()          # pages with other rows
+    g.replay()
+    replayed = result()
+    assert not torch.equal(replayed[0], first[0])
+    O.fill_(7.0)
+    step()
+    assert all(torch.equal(a, b) for a, b in zip(result(), replayed))
+
+
+@pytest.mark.parametrize("lens,Hq,T,P,mode", [([70000, 9], 16, 1, 16, "decode"), ([30000] * 3, 32, 2, 64, "decode"), ([9000, 130], 8, 70, 128, "chunk")])
+@pytest.mark.parametrize("q4", [False, True])
+def test_the_same_call_gives_the_same_bits(q4, lens, Hq, T, P, mode):
+    cache = pr.PagedCache(61, lens, P, 4, 128, q4)
+    dev = pr.DevCache(cache)
+    Q = q_bits(61, len(lens), Hq, T, 128)
+    runs = [dev.attend(Q, T, mode=mode) for _ in range(6)]
+    for o, lse, _ in runs[1:]:
+        assert np.array_equal(o, runs[0][0]) and np.array_equal(lse, runs[0][1])
+
+
+@pytest.mark.parametrize("q4", [False, True])
 def test_a_serving_run_append_rotate_attend_step_by_step(q4):
     """Tokens arrive one by one and in a chunk, keys and queries are rotated by one table, every step is attended over the
     cache so far; the plain form quantises (or rounds) the same rows and evaluates the definition."""

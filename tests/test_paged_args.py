@@ -176,3 +176,30 @@ def test_the_binding_checks_tensors_before_the_call():
         bd.prepare_paged("yoco_rope_q", bd.make_shape(1, 1, 1, 64, 1), layout())
     with pytest.raises(ValueError):
         bd.make_paged_layout(16, 1, 1, cos_sin=torch.zeros(4, 128, dtype=torch.float64))
+
+
+def test_the_binding_checks_strides():
+    """What a call goes by is the base address and its row distances; a tensor that lies otherwise is refused."""
+    import torch
+    order = bd.PreparedPagedCall._in_order
+    lay, wide = layout(P=16, pages=5, stride=7), layout(P=16, pages=5, stride=7, page_rows=2 * 3 * 16)
+    new = bd.PagedAppendShape(2, 3, 64, 1, 0)
+    fused = torch.zeros(9, 3 * 3 * 64)                                     # K, V and something else of every token
+    slices = bd.PagedAppendShape(2, 3, 64, 1, 9 * 64)
+    assert order("x", fused[:, :192], slices, lay) and order("x", fused[:, 192:384], slices, lay)
+    assert order("x", fused.view(9, 9, 64)[:, 3:6], slices, lay) and order("x", fused.view(3, 3, 9, 64)[:, :, 3:6], slices, lay)
+    assert not order("x", fused[:, :192], new, lay)                        # its tokens are not 192 elements apart
+    assert not order("x", fused.t(), slices, lay) and not order("x", fused[::2, :192], slices, lay)
+    assert not order("x", fused[:1, :192].expand(9, -1), slices, lay)
+    assert order("x", torch.zeros(9, 192), new, lay) and order("x", torch.zeros(9 * 192), new, lay)
+    assert order("x", fused[:1, :192], new, lay)                           # a single token has no distance
+    pool = torch.zeros(5, 2, 3, 16, 64)
+    assert order("k", pool[:, 0], new, wide) and order("k", pool[:, 1], new, wide) and order("k", pool, new, wide)
+    assert not order("k", pool[:, 1], new, lay) and not order("k", pool.transpose(2, 3)[:, 0], new, wide)
+    assert order("c", torch.zeros(5, 2, 3, 16, 32)[:, 1], new, wide) and order("s", torch.zeros(5, 2, 3, 16, 2)[:, 1], new, wide)
+    assert order("k", torch.zeros(5, 3, 16, 64), new, lay)
+    table = torch.zeros(2, 7, dtype=torch.int32)
+    assert order("i", table, new, lay) and order("i", table.view(-1), new, lay) and order("i", table[:, :4], new, lay)
+    assert not order("i", torch.zeros(2, 8, dtype=torch.int32), new, lay)
+    assert not order("i", torch.zeros(7, 2, dtype=torch.int32).t(), new, lay)
+    assert not order("q", torch.zeros(4, 4).t(), new, lay)
