@@ -355,7 +355,7 @@ int32_t yoco_kv_append_fp8(const yoco_kv_append_shape* shape, const void* X, con
  *          K_scale, V_scale: d/32 fp16 a row.  The value of a channel is (code - 8) * scale of its 32 channels,
  *          codes 1 .. 15 (0 reads as -8).  4.5 bits a value.  A V scale must stay below 448 in magnitude (append
  *          writes no larger one).
- * Pools start on 16-byte boundaries (scales too).  Pool, table, Q and O are device memory of the current device.
+ * Sequences hold at most 2^30 keys.  Pools start on 16-byte boundaries (scales too).  Pool, table, Q and O are device memory of the current device.
  *
  * Table entries are read on the device, only those that hold a key that some row of the call sees (with a window, pages
  * wholly below every row's window may have been given away); slots of unseen keys may hold anything.  One outside [0, num_pages) is
@@ -387,7 +387,8 @@ typedef struct yoco_paged_append_shape {
  * may be 0) or shape->T.  K_new, V_new: bf16, the tokens of all sequences one after the other (no padding between
  * sequences), heads consecutive inside a token: usually two slices of one projection's output.  With layout->cos_sin
  * every key is first turned by the angles a of its position: a pair becomes (x1 cos a - x2 sin a, x2 cos a + x1 sin a),
- * each of the three operations rounded to fp32.  bf16 rows are rounded once, from that.  kv_len_host: host
+ * each of the three operations rounded to fp32.  bf16 rows are rounded once, from that.  A call recorded into a CUDA graph
+ * keeps its lengths; table, angles and rows are read at every replay.  kv_len_host: host
  * [B], N_i including the new tokens.  Other rows of the pools are not touched.  Two tokens of one call must
  * not land in the same slot. */
 int32_t yoco_paged_append(const yoco_paged_append_shape* shape, const yoco_paged_layout* layout, const void* K_new,

@@ -533,6 +533,9 @@ int32_t no_throw(F f) {
     }
 }
 
+// Longest sequence, and most rows of one append or gather: key numbers a little past the end stay 32-bit integers.
+constexpr int64_t kMaxPagedLen = 1ll << 30;
+
 bool valid_page_size(int32_t P) { return P == 16 || P == 32 || P == 64 || P == 128 || P == 256; }
 
 // Checks the layout against the lengths of a call (kv_len_host null: every N_i = max_kv_len) and fills the map.
@@ -552,6 +555,7 @@ int32_t page_map(const yoco_paged_layout* layout, int32_t B, int32_t Hkv, const 
     for (int32_t i = 0; i < B; ++i) {
         const int64_t n = kv_len_host ? kv_len_host[i] : max_kv_len;
         if (n < 0 || (n + L.page_size - 1) / L.page_size > L.table_stride) return YOCO_ERR_INVALID_ARG;
+        if (n > kMaxPagedLen) return YOCO_ERR_UNSUPPORTED;
     }
     int shift = 4;
     while ((1 << shift) < L.page_size) ++shift;
@@ -596,7 +600,7 @@ int32_t sequence_table(int32_t B, Begin begin, End end, SeqTable* tab, int64_t* 
         tab->pos0[i] = (int32_t)lo;
         tab->tok0[i] = (int32_t)*tokens;
         *tokens += hi - lo;
-        if (*tokens >= (1ll << 31)) return YOCO_ERR_UNSUPPORTED;
+        if (*tokens > kMaxPagedLen) return YOCO_ERR_UNSUPPORTED;
         if (hi - lo != *per_seq) *per_seq = 0;
     }
     tab->tok0[B] = (int32_t)*tokens;

@@ -363,6 +363,46 @@ def test_pages_shared_by_sequences_and_pools_side_by_side(q4):
     assert_lse_close(lse, lref)
 
 
+@pytest.mark.parametrize("q4", [False, True])
+def test_pools_of_more_than_2_to_the_32_elements(q4):
+    """The pages of a small cache at the far end of a pool pair of 34 million rows: the bits of the small pools' calls."""
+    import torch
+    from paper_2405_05254_b200 import binding as bd
+    H, P, d, T, lens, far = 8, 256, 128, 3, np.array([700, 90], np.int32), 16500
+    cache = pr.PagedCache(67, lens, P, H, d, q4, slack_nan=False)
+    small = pr.DevCache(cache, pr.cos_sin(1000, d))
+    near = bd.make_paged_layout(P, cache.num_pages, cache.width, cos_sin=small.cos_sin)
+    big = bd.make_paged_layout(P, far + cache.num_pages, cache.width, cos_sin=small.cos_sin)
+    pools = [torch.empty((far + cache.num_pages) * H * P, t.shape[1] if t.dim() > 1 else t.numel() // (cache.num_pages * H * P), dtype=t.dtype,
+                         device="cuda") for t in small.pools]
+    for t, s in zip(pools, small.pools):
+        t[far * H * P:] = s.view(cache.num_pages * H * P, -1)
+    table = small.table.clone()
+    used = torch.arange(cache.width, device="cuda")[None] < torch.from_numpy(-(-lens // P)).cuda()[:, None]
+    table[used] += far
+    tail = "_q4" if q4 else ""
+    k, v = (torch.randn(4, H * d, device="cuda").to(torch.bfloat16) for _ in range(2))
+    Q = torch.randn(2, 16, T, d, device="cuda").to(torch.bfloat16)
+    out = []
+    for layout, p, t in ((near, small.pools, small.table), (big, pools, table)):
+        bd.prepare_paged("yoco_paged_append" + tail, bd.PagedAppendShape(2, H, d, 2, 0), layout, k, v, *p, t, None, lens).run()
+        G = [torch.empty(int(lens.sum()) * H * d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        bd.prepare_paged("yoco_paged_gather" + tail, bd.PagedAppendShape(2, H, d, 0, 0), layout, *p, t, np.zeros(2, np.int32), lens, *G).run()
+        got = G
+        for mode in ("decode", "chunk"):
+            shape = bd.make_shape(2, 16, H, d, T)
+            ws = torch.empty(bd.yoco_xattn_workspace_size_paged(shape, layout, lens, bd.MODE_DECODE if mode == "decode" else bd.MODE_CHUNK, q4),
+                             dtype=torch.uint8, device="cuda")
+            O = torch.empty_like(Q)
+            bd.prepare_paged(f"yoco_xattn_{mode}_paged{tail}", shape, layout, Q, *p, t, lens, O, None, ws).run()
+            assert bd.yoco_xattn_status(ws) == 0
+            got.append(O)
+        assert bd.yoco_kv_append_status() == 0
+        out.append(got)
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+    assert all(torch.equal(t[far * H * P:].view(torch.uint8), s.view(cache.num_pages * H * P, -1).view(torch.uint8)) for t, s in zip(pools, small.pools))
+
+
 @pytest.mark.parametrize("mode", ["decode", "chunk"])
 @pytest.mark.parametrize("q4", [False, True])
 def test_a_bad_page_is_reported_and_harms_nobody_else(q4, mode):

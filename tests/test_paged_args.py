@@ -55,6 +55,8 @@ def test_attention_refuses_bad_arguments(fn):
     assert attend(fn, lay=layout(pages=2**31 // 128)) == uns         # row numbers pass 32 bits
     assert attend(fn, lay=layout(pages=2, page_rows=2**31)) == uns
     assert attend(fn, lens=(100, -1)) == inv
+    assert attend(fn, lens=(100, 2**30 + 1), lay=layout(P=256, stride=2**23)) == uns
+    assert attend(fn, lens=(100, 2**31 - 1), lay=layout(P=256, stride=2**23)) == uns
     assert attend(fn, lens=(100, 1025)) == inv                       # 17 pages in 16 entries
     assert attend(fn, shape=bd.make_shape(2, 8, 2, 128, 1, kv_head_stride=128 * 2000)) == inv
     assert attend(fn, shape=bd.make_shape(2, 7, 2, 128, 1)) == uns
@@ -107,6 +109,8 @@ def test_append_and_gather_refuse_bad_arguments(fn):
     if fn.endswith("_q4"):
         assert rows_call(fn, s=None) == inv and rows_call(fn, s=vp(4104)) == inv
         assert rows_call(fn, shape=S(2, 2, 64, 1, 0)) == uns
+    assert rows_call(fn, a=(1, 1) if "append" in fn else (0, 0), b=(100, 2**30 + 1), lay=layout(P=256, stride=2**23)) == uns
+    assert rows_call(fn, a=(2**29, 2**30) if "append" in fn else (2**29, 0), b=(2**30, 2**30), lay=layout(P=256, stride=2**23)) == uns
     for d in (0, 32, 96, 256):
         assert rows_call(fn, shape=S(2, 2, d, 1, 0)) == (inv if d == 0 else uns)
     assert rows_call(fn, shape=S(513, 2, 128, 1, 0)) == uns
