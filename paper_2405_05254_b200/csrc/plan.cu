@@ -97,14 +97,21 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
     int64_t num_groups = std::max<int64_t>(1, std::min<int64_t>(target, total_tiles));
     // first flat tile of every group: equal shares, or handfuls that end with their stream (CacheForm)
     std::vector<int64_t> bounds;
-    const int handful = mode != YOCO_MODE_DECODE ? 0 : rows_per_stream <= 8 ? form.side_by_side8 : form.side_by_side16;
+    int64_t handful = mode != YOCO_MODE_DECODE ? 0 : rows_per_stream <= 8 ? form.side_by_side8 : form.side_by_side16;
     if (handful > 0 && total_tiles > 0) {
-        int64_t groups = 0, flat_lo = 0;
-        for (int i = 0; i < s.B; ++i)
-            groups += s.Hkv * (((len_vis[i] + tile_n - 1) / tile_n - tile_lo[i] + handful - 1) / handful);
+        auto tiles_of = [&](int i) { return (len_vis[i] + tile_n - 1) / tile_n - tile_lo[i]; };
+        auto count_groups = [&](int64_t of) {
+            int64_t n = 0;
+            for (int i = 0; i < s.B; ++i) n += s.Hkv * ((tiles_of(i) + of - 1) / of);
+            return n;
+        };
+        int64_t longest = 0, groups = count_groups(handful), flat_lo = 0;
+        for (int i = 0; i < s.B; ++i) longest = std::max(longest, tiles_of(i));
+        if (longest > handful && num_streams <= target && longest <= (groups > target ? 3 : 2) * handful)
+            groups = count_groups(handful = longest);
         if (groups <= target) {
             for (int i = 0; i < s.B; ++i) {
-                const int64_t nt = (len_vis[i] + tile_n - 1) / tile_n - tile_lo[i], k = (nt + handful - 1) / handful;
+                const int64_t nt = tiles_of(i), k = (nt + handful - 1) / handful;
                 for (int c = 0; c < s.Hkv; ++c, flat_lo += nt)
                     for (int64_t j = 0; j < k; ++j) bounds.push_back(flat_lo + j * nt / k);
             }

@@ -110,6 +110,9 @@ struct CacheForm {
     // streams' ends: as many groups per stream as it has such handfuls, each a run of its own.  (Measured, 8
     // sequences of 700 to 1,100 keys, 8 KV heads: groups of equal size, most of them in two streams, 16.1 us;
     // groups that end with their stream 12.8 us, and streams of at most 12 tiles need no merge.)
+    // A merge costs more than a second turn: streams of up to two handfuls stay whole (the call of the case above 15.4 -> 14.4
+    // us, 16 sequences of 1,000 keys 21.6 -> 14.4), and streams of up to three where handfuls would be too many for the
+    // SMs (8 sequences of 2,200 keys 22.1 -> 18.5 us; one such sequence, whose handfuls fit, 15.4 against 17.6).
     int side_by_side8 = 0, side_by_side16 = 0;
     // What going over to another stream costs a group (the warps' unequal last turns, the merge, the first loads), in
     // tiles: shares are equal with it counted in.  (Measured with 0 / 12 / 24 / 40: 16 sequences of 4,001 to 62,000

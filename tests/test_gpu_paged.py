@@ -204,6 +204,9 @@ def attention_on_gpu(cache, dev, Q_bits, T):
     ([150000, 70001], 8, 8, 1, 16),          # small pages: many batches of page numbers per warp
     ([600000], 16, 8, 2, 64),                # more than 32 tiles per warp of the 4-bit kernel
     ([260000], 32, 4, 2, 32),                # 16 query rows per KV head
+    ([700, 1500, 0, 1100, 64], 16, 8, 1, 64),  # whole streams of up to two turns of a CTA's warps
+    ([2200, 2300, 1, 900] * 3, 32, 8, 1, 16),  # ... of three turns
+    ([1000, 1500], 8, 1, 2, 32),               # ... of two and three turns, 16 query rows
     ([40000, 17, 30000, 0, 5000, 1], 16, 8, 1, 64),     # CTAs that go from stream to stream, some of them empty
     ([9000, 2, 130, 7000, 64, 65, 2500, 12000, 300, 5000, 1111, 640], 12, 4, 2, 16),
 ])
