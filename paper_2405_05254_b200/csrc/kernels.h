@@ -220,10 +220,12 @@ cudaError_t kv_append_kernel_setup();
 // ---- rows of a paged cache: append with rotation, read back, rotation of the queries --------------
 constexpr int kQ4Group = 32;            // channels of a 4-bit row that share a scale
 constexpr float kQ4ScaleMax = 448.f;    // largest scale a 4-bit row is given
-struct SeqTable {               // per sequence, as kernel parameters
-    int32_t pos0[kAppendMaxSequences];       // position of the sequence's first token of this call
-    int32_t tok0[kAppendMaxSequences + 1];   // its first token among all tokens of the call
+template <int N>
+struct SeqTableOf {             // per sequence, as kernel parameters
+    int32_t pos0[N];            // position of the sequence's first token of this call
+    int32_t tok0[N + 1];        // its first token among all tokens of the call
 };
+using SeqTable = SeqTableOf<kAppendMaxSequences>;
 struct Rotation {
     const float* cos_sin;       // [max_pos, d]: d/2 cosines, d/2 sines of a position; null = no rotation
     int32_t neighbours;         // 0: channels (c, c + d/2) turn together; 1: (2c, 2c + 1)
