@@ -33,6 +33,9 @@ APPEND = [
     ([257, 256, 16, 1], [257, 100, 16, 1], 16, 3, 128, 1, 0, False),
     ([512], [301], 256, 4, 128, None, 8, True),
     ([90, 0, 55], [90, 0, 55], 128, 5, 64, 0, 0, False),
+    ([3 + i % 37 for i in range(64)], [i % 4 for i in range(64)], 16, 2, 128, 0, 0, False),     # as many as the small table holds
+    ([3 + i % 37 for i in range(65)], [i % 4 for i in range(65)], 16, 2, 128, 1, 0, False),     # ... and one more
+    ([20] * 512, [1] * 512, 16, 1, 64, 0, 0, False),                                            # as many as a call may have
 ]
 
 
@@ -97,7 +100,8 @@ def test_append_q4_bit_for_bit_and_nothing_else_touched(case):
 
 
 @pytest.mark.parametrize("q4", [False, True])
-@pytest.mark.parametrize("lens,lo,P,H,d", [([5], [0], 16, 1, 128), ([200, 33, 64], [50, 33, 0], 32, 4, 64), ([300, 1], [299, 0], 256, 3, 128)])
+@pytest.mark.parametrize("lens,lo,P,H,d", [([5], [0], 16, 1, 128), ([200, 33, 64], [50, 33, 0], 32, 4, 64), ([300, 1], [299, 0], 256, 3, 128),
+                                           ([2 + i % 19 for i in range(70)], [i % 2 for i in range(70)], 16, 2, 128)])
 def test_gather_reads_the_rows_back(q4, lens, lo, P, H, d):
     import torch
     from paper_2405_05254_b200 import binding as bd
@@ -117,7 +121,7 @@ def test_gather_reads_the_rows_back(q4, lens, lo, P, H, d):
 
 
 @pytest.mark.parametrize("pairs", [0, 1])
-@pytest.mark.parametrize("B,Hq,T,d,lens", [(1, 1, 1, 64, [1]), (3, 6, 5, 128, [100, 5, 3])])
+@pytest.mark.parametrize("B,Hq,T,d,lens", [(1, 1, 1, 64, [1]), (3, 6, 5, 128, [100, 5, 3]), (70, 3, 2, 128, [2 + i for i in range(70)])])
 def test_rope_q_bit_for_bit_also_in_place(pairs, B, Hq, T, d, lens):
     import torch
     from paper_2405_05254_b200 import binding as bd
