@@ -492,7 +492,7 @@ int32_t run(const yoco_xattn_shape* shape, int32_t mode, const void* Q, const vo
         // directly behind the attention kernel (no event in between): its launch may overlap
         // that kernel's tail
         const bool chained = plan.info.num_segments > 0 && !timed;
-        YOCO_CUDA_TRY(launch_combine(c, stream, inline_tables ? &ready->combine_tab : nullptr, chained));
+        YOCO_CUDA_TRY(launch_combine(c, stream, inline_tables ? &ready->combine_tab : nullptr, chained, paged != nullptr));
     }
     return YOCO_OK;
 }

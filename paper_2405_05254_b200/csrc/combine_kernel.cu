@@ -16,6 +16,11 @@ namespace {
 constexpr int kCombineWarps = 4;       // warps per CTA of the small shapes
 constexpr int kCombineWarpsMany = 32;  // one 1024-thread CTA per row when a row has very many pieces
 constexpr int kManyPieces = 64;
+// With this many rows, and pieces few enough for one warp, a warp per row fills the GPU by itself, and a CTA per row is mostly
+// launch and synchronisation (the merge's share of a call, a CTA / a warp per row: 9,120 rows of 5 pieces 38 / 10 us, 4,968
+// rows of 6 pieces 23 / 7 us, 3,008 rows of 6 pieces 12 / 4 us).  Asked for by the calls over a paged cache; the
+// order of a row's sums is part of the other calls' results.
+constexpr int kManyRows = 2048, kWarpPieces = 16;
 
 // WPR: warps per output row (1 or WARPS); WARPS: warps per CTA
 template <int WPR, int WARPS>
@@ -192,10 +197,11 @@ combine_kernel_inline(const CombineParams p0, const __grid_constant__ CombineInl
 }  // namespace
 
 cudaError_t launch_combine(const CombineParams& p, cudaStream_t stream, const CombineInlineTables* inline_tab,
-                           bool after_attention) {
+                           bool after_attention, bool warp_per_many_rows) {
     if (p.rows == 0) return cudaSuccess;
     // pieces per row -> shape: a warp per row; a 4-warp CTA per row; a 32-warp CTA per row
-    const int shape = p.max_pieces > kManyPieces ? 2 : p.max_pieces > kCombineWarps ? 1 : 0;
+    const bool by_warps = warp_per_many_rows && p.rows >= kManyRows && p.max_pieces <= kWarpPieces;
+    const int shape = p.max_pieces > kManyPieces ? 2 : p.max_pieces > kCombineWarps && !by_warps ? 1 : 0;
     const int warps = shape == 2 ? kCombineWarpsMany : kCombineWarps;
     const int64_t blocks = shape ? p.rows : (p.rows + kCombineWarps - 1) / kCombineWarps;
     cudaLaunchConfig_t cfg = {};

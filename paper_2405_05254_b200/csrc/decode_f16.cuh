@@ -1,23 +1,12 @@
-// What the decode kernels over narrow caches (8-bit, 4-bit) share: fp16 warp-level products, and the wait of a
-// consumer warp that takes whole tiles in turn.
+// What the decode kernels over narrow caches (8-bit, 4-bit) share around their fp16 products.
 #pragma once
 
 #include <cuda_fp16.h>
 
-#include "kernels.h"
-#include "ptx.cuh"
+#include <cstdint>
 
 namespace yoco {
 
-// D(16x8, f32) += A(16x16, f16, row) * B(16x8, f16, col)
-__device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                              uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
-        "{%0,%1,%2,%3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 // 8 x 8 transpose of 16-bit units across the warp: lane (g, tq) gives row g, columns 2 tq and 2 tq + 1,
 // and receives the same positions of the transposed matrix.
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a) {
@@ -33,30 +22,6 @@ __device__ __forceinline__ float ex2_fast(float x) {   // 2^x, one special-funct
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-
-__device__ __forceinline__ void st_release_shared(uint32_t* p, uint32_t v) {
-    asm volatile("st.release.cta.shared::cta.u32 [%0], %1;" ::"r"(smem_u32(p)), "r"(v) : "memory");
-}
-__device__ __forceinline__ uint32_t ld_acquire_shared(const uint32_t* p) {
-    uint32_t v;
-    asm volatile("ld.acquire.cta.shared::cta.u32 %0, [%1];" : "=r"(v) : "r"(smem_u32(p)) : "memory");
-    return v;
-}
-// Waits (bounded, like every wait) until the producer's count of armed tiles has reached `want`.
-__device__ __forceinline__ bool wait_armed(const uint32_t* armed, uint32_t want, const Abort& ab) {
-    if (ld_acquire_shared(armed) >= want) return true;
-    const uint64_t t0 = global_timer_ns();
-    for (uint32_t i = 1;; ++i) {
-        if (ld_acquire_shared(armed) >= want) return true;
-        if ((i & 63u) == 0) {
-            if (*ab.flag) return false;
-            if ((int64_t)(global_timer_ns() - t0) > ab.limit_ns || i >= kWaitMaxPolls) {
-                report_give_up(ab, kWaitItemQueue);
-                return false;
-            }
-        }
-    }
 }
 
 }  // namespace yoco

@@ -69,9 +69,10 @@ struct CombineParams {
 // inline_tab (host, may be null): stream tables passed as kernel parameters instead of
 // p.stream_base / p.stream_nseg.  after_attention: launched right behind the attention kernel of
 // the same call; the launch is then allowed to overlap that kernel's tail (the merge itself still
-// waits for it).
+// waits for it).  warp_per_many_rows: see kManyRows (combine_kernel.cu).
 cudaError_t launch_combine(const CombineParams& p, cudaStream_t stream,
-                           const CombineInlineTables* inline_tab = nullptr, bool after_attention = false);
+                           const CombineInlineTables* inline_tab = nullptr, bool after_attention = false,
+                           bool warp_per_many_rows = false);
 
 // Where the rows of a paged cache are: row(page, head c, slot) = page * page_rows + c * P + slot, P = 1 << page_shift.
 struct PageMap {

@@ -234,6 +234,8 @@ CHUNK = [
     ([5000, 1300], 16, 4, 65, 256, 0, 128),            # split and merged
     ([2600], 8, 8, 300, 16, 0, 64),
     ([3001, 40], 32, 8, 40, 16, 0, 128),               # 160 rows per KV head, small pages
+    ([4000, 0, 900], 16, 2, 60, 32, 0, 128),           # 2,880 rows in up to 16 pieces: a warp merges a row
+    ([2500], 16, 1, 150, 64, 0, 128),                  # 2,400 rows in more pieces than a warp takes
     ([9000, 2000], 4, 1, 9, 64, 500, 128),             # few rows, window, split
 ]
 
@@ -298,6 +300,7 @@ def test_q4_log_sum_exp_of_few_keys_is_that_of_32_bits(lens, Hq, Hkv, T, P, wind
 
 @pytest.mark.parametrize("T,d", [(5, 64), (60, 128), (90, 64), (110, 128)])
 def test_chunk_bf16_gives_the_bits_of_the_packed_cache(T, d):
+    """(Of fewer than 2,048 rows: with more, a paged call's merge may group its sums differently.)"""
     from helpers import GpuRunner
     lens, H, Hq = [1500, 177], 2, 8
     cache = pr.PagedCache(14, lens, 32, H, d, False)
