@@ -263,8 +263,8 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 const uint32_t entries = k_entries(seg);
                 for (int k0 = seg.k_begin; k0 < seg.k_end; k0 += BN, ++it) {
                     const int row = seg.kv_row0 + (k0 - seg.k_begin);
-                    const uint32_t kb = k_armed % KS;
-                    if (!(ok = wait(&k_empty[kb], ((k_armed / KS) & 1u) ^ 1u))) break;
+                    const uint32_t k_entry = KIND == kPaged4 ? k_armed : it, kb = k_entry % KS, kn = k_entry / KS;
+                    if (!(ok = wait(&k_empty[kb], (kn & 1u) ^ 1u))) break;
                     ++k_armed;
                     if (PAGED) {
                         load_pages(smem + C::OFF_K + kb * C::TILE_BYTES, tmK, tmKs, &k_full[kb], k0);
@@ -324,7 +324,8 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             const uint32_t tmem_o = tmem_base + 2 * BN + r * BN;
             bool ok = true;
             uint32_t it = 0, n_seg = 0;
-            uint32_t ke = 0;              // the K ring entry of the next key tile to be scored
+            uint32_t ke = 0;              // the K ring entry of the next key tile to be scored (if not its number)
+            auto entry_of = [&](uint32_t tile) { return KIND == kPaged4 ? ke : tile; };
 
             // scores of half h of the key tile at `entry` of the K ring (it must have landed)
             auto issue_scores = [&](uint32_t entry, uint32_t entries, int h, bool last_of_segment) {
@@ -365,15 +366,16 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 if (!(ok = warp_wait(q_use, n_seg & 1u, ab, kWaitRingFull))) break;
                 ++n_seg;
                 const uint32_t entries = k_entries(p.segments[si]);
-                if (!(ok = warp_wait(&k_use[ke % KS], (ke / KS) & 1u, ab, kWaitRingFull))) break;
-                issue_scores(ke, entries, 0, n_tiles == 1);
-                issue_scores(ke, entries, 1, n_tiles == 1);
+                if (!(ok = warp_wait(&k_use[entry_of(it) % KS], (entry_of(it) / KS) & 1u, ab, kWaitRingFull))) break;
+                issue_scores(entry_of(it), entries, 0, n_tiles == 1);
+                issue_scores(entry_of(it), entries, 1, n_tiles == 1);
                 for (int t = 0; t < n_tiles && ok; ++t, ++it) {
                     ke += entries;
                     const uint32_t vb = it % VS;
                     if (!(ok = warp_wait(&v_use[vb], (it / VS) & 1u, ab, kWaitRingFull))) break;
                     const bool more = t + 1 < n_tiles;
-                    if (more && !(ok = warp_wait(&k_use[ke % KS], (ke / KS) & 1u, ab, kWaitRingFull))) break;
+                    const uint32_t next = entry_of(it + 1);
+                    if (more && !(ok = warp_wait(&k_use[next % KS], (next / KS) & 1u, ab, kWaitRingFull))) break;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         if (!(ok = warp_wait(&p_full[r * 2 + h], it & 1u, ab, kWaitTensor))) break;
@@ -390,7 +392,7 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                             if (h == 1) umma_commit(&v_empty[vb]);
                         }
                         __syncwarp();
-                        if (more) issue_scores(ke, entries, h, t + 2 == n_tiles);
+                        if (more) issue_scores(next, entries, h, t + 2 == n_tiles);
                     }
                 }
             }
