@@ -396,8 +396,8 @@ int32_t yoco_paged_append(const yoco_paged_append_shape* shape, const yoco_paged
                           const int32_t* new_len_host, const int32_t* kv_len_host, void* stream);
 /* The same into 4-bit pages.  Per 32 channels of a row (a key after its rotation, in fp32):
  *     scale = fp16(min(max|x| * fp32(1/7), 448)),  code = 8 + clamp(rint(x * fp32(1 / scale)), -7, 7)
- * and code 8 throughout where the scale is 0.  Rows should be finite: an infinity is stored as +-7 * 448, a NaN
- * as the code 1. */
+ * and code 8 throughout where the scale is 0.  Rows should be finite: an infinity is stored as +-7 * 448 (and leaves the
+ * group the scale 448), a NaN as the code 1; it does not count for the scale (of 32 NaN the scale is 448). */
 int32_t yoco_paged_append_q4(const yoco_paged_append_shape* shape, const yoco_paged_layout* layout, const void* K_new,
                              const void* V_new, void* K4, void* K_scale, void* V4, void* V_scale,
                              const int32_t* page_table, const int32_t* new_len_host, const int32_t* kv_len_host,

@@ -83,18 +83,31 @@ __device__ __forceinline__ void rotate_chunks(float (&lo)[8], float (&hi)[8], co
     }
 }
 
-// Largest magnitude of a 32-channel group that four neighbouring lanes hold eight channels of each.
+// max of two; a NaN beats everything (fmaxf passes it over)
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// Largest magnitude of a 32-channel group that four neighbouring lanes hold eight channels of each.  KEEP_NAN: a NaN comes
+// out as one, which is how a group that has one is noticed without an instruction more; otherwise it does not count.
+template <bool KEEP_NAN>
 __device__ __forceinline__ float group_max(const float (&x)[8]) {
-    float a = fmaxf(fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3]))),
-                    fmaxf(fmaxf(fabsf(x[4]), fabsf(x[5])), fmaxf(fabsf(x[6]), fabsf(x[7]))));
-    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
-    return fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
+    auto larger = [](float a, float b) { return KEEP_NAN ? max_or_nan(a, b) : fmaxf(a, b); };
+    float a = larger(larger(larger(fabsf(x[0]), fabsf(x[1])), larger(fabsf(x[2]), fabsf(x[3]))),
+                     larger(larger(fabsf(x[4]), fabsf(x[5])), larger(fabsf(x[6]), fabsf(x[7]))));
+    a = larger(a, __shfl_xor_sync(0xffffffffu, a, 1));
+    return larger(a, __shfl_xor_sync(0xffffffffu, a, 2));
 }
-__device__ __forceinline__ __half group_scale(float largest) {
-    return __float2half_rn(fminf(__fmul_rn(largest, 1.0f / 7.0f), kQ4ScaleMax));
+// NaN stays NaN: see group_max
+__device__ __forceinline__ float capped_seventh(float largest) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__fmul_rn(largest, 1.0f / 7.0f)), "f"(kQ4ScaleMax));
+    return r;
 }
-// The codes of eight channels.  CLAMP = false where the scale is a normal number below the limit: it is then within
-// 2^-11 of a seventh of the largest magnitude, and no quotient rounds to more than 7.
+// The codes of eight channels.  CLAMP = false where no channel is NaN and the scale is a normal number below the limit: it is
+// then within 2^-11 of a seventh of the largest magnitude, and no quotient rounds to more than 7.  (A NaN has no place in that
+// sum: its bits would run into the other channels' codes.  The clamp turns it into the code 1.)
 template <bool CLAMP>
 __device__ __forceinline__ uint32_t quantise8(const float (&x)[8], float scale) {
     const float inv = scale > 0.f ? __frcp_rn(scale) : 0.f;
@@ -166,12 +179,16 @@ paged_append_kernel(const PagedRowsParams p, const __grid_constant__ Table tab, 
             float vlo[8], vhi[8];
             unpack8(v0, vlo);
             unpack8(v1, vhi);
-            const __half s[4] = {group_scale(group_max(lo)), group_scale(group_max(hi)), group_scale(group_max(vlo)),
-                                 group_scale(group_max(vhi))};
-            const float f[4] = {__half2float(s[0]), __half2float(s[1]), __half2float(s[2]), __half2float(s[3])};
+            const float largest[4] = {group_max<true>(lo), group_max<true>(hi), group_max<true>(vlo), group_max<true>(vhi)};
+            __half s[4];
+            float f[4];
             bool plain = true;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) plain = plain && f[q] >= 6.103515625e-5f && f[q] < kQ4ScaleMax;
+            for (int q = 0; q < 4; ++q) {
+                s[q] = __float2half_rn(capped_seventh(largest[q]));
+                f[q] = __half2float(s[q]);
+                plain = plain && f[q] >= 6.103515625e-5f && f[q] < kQ4ScaleMax;         // false for a NaN
+            }
             uint32_t w[4];
             if (__all_sync(0xffffffffu, plain)) {
                 w[0] = quantise8<false>(lo, f[0]);
@@ -179,6 +196,12 @@ paged_append_kernel(const PagedRowsParams p, const __grid_constant__ Table tab, 
                 w[2] = quantise8<false>(vlo, f[2]);
                 w[3] = quantise8<false>(vhi, f[3]);
             } else {
+                const float finite[4] = {group_max<false>(lo), group_max<false>(hi), group_max<false>(vlo), group_max<false>(vhi)};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    s[q] = __float2half_rn(fminf(__fmul_rn(finite[q], 1.0f / 7.0f), kQ4ScaleMax));
+                    f[q] = __half2float(s[q]);
+                }
                 w[0] = quantise8<true>(lo, f[0]);
                 w[1] = quantise8<true>(hi, f[1]);
                 w[2] = quantise8<true>(vlo, f[2]);

@@ -1,0 +1,60 @@
+"""The paged cache on the GPU where its operators can go wrong: NaN among ordinary values of a new 4-bit row."""
+import numpy as np
+import pytest
+
+import paged_ref as pr
+import synth_inputs as si
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("neighbour", ["ordinary", "clamped"])
+@pytest.mark.parametrize("tokens,H,rotated", [(1, 1, False), (19, 2, True), (40, 3, False)])
+def test_a_nan_in_a_4_bit_row_is_the_code_1_and_harms_no_other_channel(tokens, H, rotated, neighbour):
+    """Bit for bit, whatever else shares the warp: ordinary rows only (no row needs the clamp), or a row that does."""
+    import torch
+    from paper_2405_05254_b200 import binding as bd
+    P, d, lens = 16, 128, np.array([tokens], np.int32)
+    cache = pr.PagedCache(71, lens, P, H, d, True, slack_nan=False)
+    cs = pr.cos_sin(tokens, d) if rotated else None
+    dev = pr.DevCache(cache, cs)
+    r = np.random.default_rng(71)
+    src = [pr.bf16(r.standard_normal((tokens, H * d)))[0] for _ in range(2)]
+    for w, s in enumerate(src):
+        for t in range(0, tokens, 2):                                  # every other token has one, or two, somewhere
+            s[t, r.integers(0, H * d)] = 0x7FC0
+            s[t, (7 * t + 33 * w) % (H * d)] = [0x7FC0, 0xFFC1][w]
+        if neighbour == "clamped":
+            s[-1, :32] = 0                                             # scale 0
+            s[-1, 32:64] = pr.bf16(np.full(32, 3e38, np.float32))[0]   # scale 448
+    bd.yoco_paged_append_q4(bd.PagedAppendShape(1, H, d, tokens, 0), dev.layout, pr.bits_to_dev(src[0]), pr.bits_to_dev(src[1]),
+                            *dev.pools, dev.table, None, lens)
+    assert bd.yoco_kv_append_status() == 0
+    for w in range(2):
+        codes, s = dev.pools[2 * w].cpu().numpy(), dev.pools[2 * w + 1].cpu().numpy()
+        for h in range(H):
+            x = si.bf16_bits_to_f32(src[w][:, h * d:(h + 1) * d])
+            with np.errstate(invalid="ignore", over="ignore"):
+                x = pr.rotate(x, cs, 0) if rotated and w == 0 else x
+                want_codes, want_s = pr.quantise(x)
+            at = cache.row_numbers(0, h, tokens)
+            assert np.array_equal(s[at].view(np.uint16), want_s.view(np.uint16)), (w, h)
+            assert np.array_equal(codes[at], want_codes), (w, h)
+
+
+def test_a_group_of_nothing_but_nan_gets_a_finite_scale():
+    """Codes 1 and the largest scale (0 * NaN must not reach the results of rows that do not see this one)."""
+    import torch
+    from paper_2405_05254_b200 import binding as bd
+    cache = pr.PagedCache(72, [5], 16, 1, 128, True, slack_nan=False)
+    dev = pr.DevCache(cache)
+    x = pr.bf16(np.random.default_rng(72).standard_normal((5, 128)))[0]
+    x[2, 64:96] = 0x7FC0
+    bd.yoco_paged_append_q4(bd.PagedAppendShape(1, 1, 128, 5, 0), dev.layout, pr.bits_to_dev(x), pr.bits_to_dev(x), *dev.pools, dev.table,
+                            None, cache.lens)
+    want_codes, want_s = pr.quantise(np.where(np.isnan(si.bf16_bits_to_f32(x)), 0, si.bf16_bits_to_f32(x)))
+    want_codes[2, 32:48], want_s[2, 2] = 0x11, np.float16(448)
+    at = cache.row_numbers(0, 0, 5)
+    for w in range(2):
+        assert np.array_equal(dev.pools[2 * w].cpu().numpy()[at], want_codes)
+        assert np.array_equal(dev.pools[2 * w + 1].cpu().numpy()[at], want_s)
