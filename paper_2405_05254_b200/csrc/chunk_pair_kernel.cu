@@ -34,16 +34,20 @@
 // inside the part of the upper half tile that the same warp's fp16 rows will fill, so a warp has read all of its
 // source (one __syncwarp) before it overwrites any of it, and no two warps meet.
 // A value (code - 8) * scale has up to 14 bits, three more than fp16 holds.  V takes one rounding (half a step, 2^-11
-// of the value; O leaves in bf16).  For K that rounding puts a score off by about 3e-4, which the log-sum-exp of a row of
-// many keys averages out and that of a row of few does not: where a CTA has a row that sees fewer than kExactKeys keys,
-// K takes two ring entries, (code - 8) times the upper eight bits of the scale and times its lower three, both
-// exact in fp16, and the scores are the sum of two products.  The polynomial exponentials are quartic (no time lost:
-// 522 us with the cubic, 520 us with the quartic for 391 tokens over 65,927 keys).  Relative error (2-norm) of the log-sum-exp
-// against 64 bits, chunks of 11 to 41 tokens over as many keys: 4e-5 with K rounded once and the cubic, 4e-6 with K in two
-// parts, 1.6e-7 with the quartic as well; above the rule, at most 1.2e-6.  K in two parts everywhere would make that case
-// 812 us; with the rule a whole sequence of 4,096 tokens pays most, 575 us instead of 494.
-// V rows that a window has left behind are zeroed where they are widened; the softmax warps, which zero the rows
-// past the end, have no register left for it (595 us with the test there; 472 us as it is, 890 TFLOP/s).
+// of the value; O leaves in bf16).  K takes none: every key tile becomes two, (code - 8) times the upper eight bits of the
+// scale and times its lower three, both exact in fp16, and the scores are the sum of two products.  (Rounded once, K puts a
+// score off by up to 2^-11 of the sum of its products' magnitudes.  Flat softmax rows of many keys average that out, rows that a
+// few keys lead do not, whatever their length: log-sum-exp 0.035 off, O 0.032, for 6,000 keys with scores of some hundreds.)
+// The second part has a place of its own, written and given back by halves of 64 keys, so that a half's part can be
+// written as soon as both row tiles have scored the same half of the tile before; K's ring is two deep for it.
+// The polynomial exponentials are quartic (no time lost); the log-sum-exp of a few keys is then within 1.6e-7 (2-norm, chunks of
+// 11 to 41 tokens over as many keys) of 64 bits.
+// Bound by the softmax warps (as over a bf16 cache, 407 us) and by 1.5 times the products.  Kernel alone at the full clock, 391
+// tokens over 65,927 keys, 32 query over 8 KV heads: 570 us = 740 TFLOP/s counted once (K rounded: 470; K in two parts
+// through two entries of the three-deep ring: 812); 670 us a call in a loop of seconds, where the power cap takes the clock
+// down (K rounded: 556).  A whole sequence of 4,096 tokens 500 us.
+// V rows that a window has left behind are zeroed where they are widened: the softmax warps, which zero the rows
+// past the end, have no register left for it.
 #include <cuda_fp16.h>
 
 #include "kernels.h"
@@ -71,7 +75,6 @@ constexpr int Q4_OFF_SCALE = 32 * 64;
 constexpr int Q4_ROW_BYTES = 64 + 8;
 constexpr int HALF_BYTES = 128 * 128;          // 128 rows x 64 bf16: one swizzled half tile
 constexpr uint32_t TMEM_COLS = 512;
-constexpr int kExactKeys = 2048;               // 4-bit rows: fewer visible keys are treated more exactly, see above
 constexpr float kRescaleThreshold = 8.f;       // in log2 units: P stays below 2^8
 // Register split after launch.  The CTA starts with what its thread count allows (168 registers per
 // thread for 384 threads, 128 for 512); warpgroup 0 (and the widening warpgroup) give back down to
@@ -93,7 +96,9 @@ struct PCfg {
     static constexpr int OFF_K = OFF_Q + 2 * TILE_BYTES;
     static constexpr int OFF_V = OFF_K + K_STAGES * TILE_BYTES;
     static constexpr int OFF_BAR = OFF_V + V_STAGES * TILE_BYTES;
-    static constexpr int NUM_BARS = 2 + 2 * K_STAGES + 2 * V_STAGES + 12 + 3 + (K_STAGES + V_STAGES + 1);
+    static constexpr int K_STAGES_4BIT = 2;                    // the third place takes the second part of K
+    static constexpr int OFF_K_LOWER = OFF_K + K_STAGES_4BIT * TILE_BYTES;
+    static constexpr int NUM_BARS = 2 + 2 * K_STAGES + 2 * V_STAGES + 12 + 3 + (2 * K_STAGES_4BIT + V_STAGES + 1) + 2;
     static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16;
     static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
 };
@@ -133,7 +138,8 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     static_assert(!FP8 || D == 128, "the narrow cache paths are built for head dimension 128");
     using C = PCfg<D>;
     constexpr int HALVES = C::HALVES;
-    constexpr int KS = C::K_STAGES, VS = C::V_STAGES;
+    constexpr int KS = KIND == kPaged4 ? C::K_STAGES_4BIT : C::K_STAGES, VS = C::V_STAGES;
+    constexpr int K_READY = KIND == kPaged4 ? 2 * KS : KS;      // 4-bit rows: a tile is ready by halves
     constexpr int KSTEPS_QK = D / 16;
     constexpr int KSTEPS_PV = BH / 16;
 
@@ -149,9 +155,10 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     uint64_t* p_full = s_full + 4;           // [2][2]  P_r^h has been written over S_r^h
     uint64_t* pv_done = p_full + 4;          // [2][2]  O_r includes the current half step; P_r^h is dead
     uint64_t* drain_bar = pv_done + 4;       // [3]     everything issuer warp 1 + i started has finished
-    uint64_t* k_ready = drain_bar + 3;       // [KS]    8-bit cache: the K tile has been widened to fp16
-    uint64_t* v_ready = k_ready + KS;        // [VS]    ... the V tile
+    uint64_t* k_ready = drain_bar + 3;       // [KS]    8-bit cache: the K tile has been widened to fp16 (4-bit: [KS][2], by halves)
+    uint64_t* v_ready = k_ready + K_READY;   // [VS]    ... the V tile
     uint64_t* q_ready = v_ready + VS;        //         ... both Q tiles have been converted to fp16
+    uint64_t* low_empty = q_ready + 1;       // [2]     4-bit rows: both row tiles have scored this half of K's second part
     // what the issuers and the softmax warpgroups wait on for an operand tile
     uint64_t* k_use = FP8 ? k_ready : k_full;
     uint64_t* v_use = FP8 ? v_ready : v_full;
@@ -164,14 +171,6 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     const int seg_lo = p.group_begin[group], seg_hi = p.group_begin[group + 1];
     const Abort ab{abort_flag, p.status, kWaitLimitNs};
     constexpr bool PAGED = KIND == kPaged16 || KIND == kPaged4;
-    // whether a row of this CTA sees so few keys of the segment's sequence that they are treated more exactly
-    auto few_keys = [&](const DevSegment& seg) {
-        if (KIND != kPaged4) return false;
-        const int t = (m_tile * 2 * BM) % p.T, visible = seg.n_full + (t + 2 * BM <= p.T ? t : 0);
-        return (p.window > 0 ? min(visible, p.window) : visible) < kExactKeys;
-    };
-    // ring entries of a key tile of the segment
-    auto k_entries = [&](const DevSegment& seg) -> uint32_t { return few_keys(seg) ? 2u : 1u; };
     const bool aligned_ok = (smem_u32(smem) & 1023u) == 0;
 
     if (threadIdx.x == 0) {
@@ -180,7 +179,9 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         mbar_init(q_full, 1);
         mbar_init(q_empty, 2);
         for (int b = 0; b < 3; ++b) mbar_init(&drain_bar[b], 1);
-        for (int b = 0; b < KS + VS + 1; ++b) mbar_init(&k_ready[b], 4);      // the four widening warps
+        for (int b = 0; b < K_READY; ++b) mbar_init(&k_ready[b], KIND == kPaged4 ? 2 : 4);
+        for (int b = 0; b < VS + 1; ++b) mbar_init(&v_ready[b], 4);           // the four widening warps (q_ready follows)
+        for (int b = 0; b < 2; ++b) mbar_init(&low_empty[b], 2);
         for (int b = 0; b < KS; ++b) {
             mbar_init(&k_full[b], 1);
             mbar_init(&k_empty[b], 2);            // released by both issuers
@@ -220,7 +221,7 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             auto wait = [&](uint64_t* bar, uint32_t parity) {
                 return PAGED ? warp_wait(bar, parity, ab, kWaitRingEmpty) : wait_or_abort(bar, parity, ab, kWaitRingEmpty);
             };
-            uint32_t it = 0;                                  // key tile; k_armed counts the entries of the K ring
+            uint32_t it = 0;
             uint32_t q_armed = 0, k_armed = 0, v_armed = 0;   // copies started, for the drain on the way out
             bool ok = true;
             for (int si = seg_lo; si < seg_hi && ok; ++si) {
@@ -260,10 +261,9 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         __syncwarp();
                     }
                 };
-                const uint32_t entries = k_entries(seg);
                 for (int k0 = seg.k_begin; k0 < seg.k_end; k0 += BN, ++it) {
                     const int row = seg.kv_row0 + (k0 - seg.k_begin);
-                    const uint32_t k_entry = KIND == kPaged4 ? k_armed : it, kb = k_entry % KS, kn = k_entry / KS;
+                    const uint32_t kb = it % KS, kn = it / KS;
                     if (!(ok = wait(&k_empty[kb], (kn & 1u) ^ 1u))) break;
                     ++k_armed;
                     if (PAGED) {
@@ -276,12 +276,6 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         for (int h = 0; h < HALVES; ++h)
                             tma_load_2d(smem + C::OFF_K + kb * C::TILE_BYTES + h * HALF_BYTES, &tmK, h * 64, row,
                                         &k_full[kb]);
-                    }
-                    if (entries == 2) {    // nothing lands in the second entry; the widening warps may write it
-                        const uint32_t lb = k_armed % KS;
-                        if (!(ok = wait(&k_empty[lb], ((k_armed / KS) & 1u) ^ 1u))) break;
-                        ++k_armed;
-                        if (lane == 0) mbar_arrive(&k_full[lb]);
                     }
                     const uint32_t vb = it % VS, vn = it / VS;
                     if (!(ok = wait(&v_empty[vb], (vn & 1u) ^ 1u))) break;
@@ -324,35 +318,34 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             const uint32_t tmem_o = tmem_base + 2 * BN + r * BN;
             bool ok = true;
             uint32_t it = 0, n_seg = 0;
-            uint32_t ke = 0;              // the K ring entry of the next key tile to be scored (if not its number)
-            auto entry_of = [&](uint32_t tile) { return KIND == kPaged4 ? ke : tile; };
+            auto k_there = [&](uint32_t tile) {      // the whole key tile
+                return warp_wait(&k_use[tile % KS], (tile / KS) & 1u, ab, kWaitRingFull);
+            };
+            auto k_half_there = [&](uint32_t tile, int h) {      // 4-bit rows
+                return warp_wait(&k_ready[(tile % KS) * 2 + h], (tile / KS) & 1u, ab, kWaitRingFull);
+            };
 
-            // scores of half h of the key tile at `entry` of the K ring (it must have landed)
-            auto issue_scores = [&](uint32_t entry, uint32_t entries, int h, bool last_of_segment) {
-                const uint32_t kb = entry % KS;
+            // scores of half h of a key tile (it must have landed)
+            auto issue_scores = [&](uint32_t tile, int h, bool last_of_segment) {
+                const uint32_t kb = tile % KS;
                 tc_fence_after();
-                const uint32_t k_lo = desc_lo(sbase + C::OFF_K + kb * C::TILE_BYTES + h * BH * 128, 16);
+                // (4-bit rows: ... plus the lower bits of the scales)
+                uint32_t k_lo = desc_lo(sbase + C::OFF_K + kb * C::TILE_BYTES + h * BH * 128, 16);
                 if (elect_one()) {
-#pragma unroll
-                    for (int ks = 0; ks < KSTEPS_QK; ++ks) {
-                        const uint32_t off = ((ks >> 2) * HALF_BYTES + (ks & 3) * 32) >> 4;
-                        umma_ss(tmem_base + r * BN + h * BH, desc_from_lo(q_lo + off, 1024),
-                                desc_from_lo(k_lo + off, 1024), idesc_qk, ks > 0 ? 1u : 0u);
-                    }
-                    if (KIND == kPaged4 && entries == 2) {     // ... plus the lower bits of the scales
-                        const uint32_t lb = (entry + 1) % KS;
-                        const uint32_t l_lo = desc_lo(sbase + C::OFF_K + lb * C::TILE_BYTES + h * BH * 128, 16);
+#pragma unroll 1
+                    for (int part = 0; part < (KIND == kPaged4 ? 2 : 1); ++part) {
 #pragma unroll
                         for (int ks = 0; ks < KSTEPS_QK; ++ks) {
                             const uint32_t off = ((ks >> 2) * HALF_BYTES + (ks & 3) * 32) >> 4;
                             umma_ss(tmem_base + r * BN + h * BH, desc_from_lo(q_lo + off, 1024),
-                                    desc_from_lo(l_lo + off, 1024), idesc_qk, 1u);
+                                    desc_from_lo(k_lo + off, 1024), idesc_qk, part + ks > 0 ? 1u : 0u);
                         }
+                        k_lo = desc_lo(sbase + C::OFF_K_LOWER + h * BH * 128, 16);
                     }
                     umma_commit(&s_full[r * 2 + h]);
+                    if (KIND == kPaged4) umma_commit(&low_empty[h]);
                     if (h == 1) {
                         umma_commit(&k_empty[kb]);
-                        if (KIND == kPaged4 && entries == 2) umma_commit(&k_empty[(entry + 1) % KS]);
                         if (last_of_segment) umma_commit(q_empty);   // this row tile's Q may be replaced
                     }
                 }
@@ -365,18 +358,16 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 // both halves of the first key tile of the segment (its Q and K have to be there)
                 if (!(ok = warp_wait(q_use, n_seg & 1u, ab, kWaitRingFull))) break;
                 ++n_seg;
-                const uint32_t entries = k_entries(p.segments[si]);
-                if (!(ok = warp_wait(&k_use[entry_of(it) % KS], (entry_of(it) / KS) & 1u, ab, kWaitRingFull))) break;
-                issue_scores(entry_of(it), entries, 0, n_tiles == 1);
-                issue_scores(entry_of(it), entries, 1, n_tiles == 1);
+                if (!(ok = KIND == kPaged4 ? k_half_there(it, 0) : k_there(it))) break;
+                issue_scores(it, 0, n_tiles == 1);
+                if (KIND == kPaged4 && !(ok = k_half_there(it, 1))) break;
+                issue_scores(it, 1, n_tiles == 1);
                 for (int t = 0; t < n_tiles && ok; ++t, ++it) {
-                    ke += entries;
                     const uint32_t vb = it % VS;
                     if (!(ok = warp_wait(&v_use[vb], (it / VS) & 1u, ab, kWaitRingFull))) break;
                     const bool more = t + 1 < n_tiles;
-                    const uint32_t next = entry_of(it + 1);
-                    if (more && !(ok = warp_wait(&k_use[next % KS], (next / KS) & 1u, ab, kWaitRingFull))) break;
-#pragma unroll
+                    if (KIND != kPaged4 && more && !(ok = k_there(it + 1))) break;
+#pragma unroll (KIND == kPaged4 ? 1 : 2)     // (4-bit rows: unrolled, the issuers spill)
                     for (int h = 0; h < 2; ++h) {
                         if (!(ok = warp_wait(&p_full[r * 2 + h], it & 1u, ab, kWaitTensor))) break;
                         tc_fence_after();
@@ -392,7 +383,8 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                             if (h == 1) umma_commit(&v_empty[vb]);
                         }
                         __syncwarp();
-                        if (more) issue_scores(next, entries, h, t + 2 == n_tiles);
+                        if (KIND == kPaged4 && more && !(ok = k_half_there(it + 1, h))) break;
+                        if (more) issue_scores(it + 1, h, t + 2 == n_tiles);
                     }
                 }
             }
@@ -417,9 +409,10 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             // The bytes of row r were written by TMA with the 128-byte swizzle (16-byte chunk c at position
             // c ^ (r & 7)); the fp16 row goes out in the same swizzle, channels 0-63 to row r of the lower
             // half tile and 64-127 to row r of the upper one, i.e. over the bytes just read.
-            // lower (4-bit rows): nullptr, or the tile that takes the products with the scales' lower bits
-            // dead (4-bit rows): this lane's row holds anything and must come out as zeros
-            auto widen_tile = [&](uint8_t* tile, uint8_t* lower, bool dead) {
+            // 4-bit rows: in_two, a tile of K becomes two (see the head of this file); dead, this lane's row holds anything
+            // and must come out as zeros.  (Both parts are written from one unpacking: a loop of two keeps the unpacked
+            // row, 64 registers, or unpacks it twice.)
+            auto widen_tile = [&](uint8_t* tile, bool in_two, bool dead) {
                 if (KIND == kPaged4) {
                     const int rr = wq * 32 + lane;
                     const uint8_t* src = tile + HALF_BYTES + wq * Q4_WARP_STRIDE;
@@ -433,33 +426,32 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                                       __byte_perm(sw.y, 0u, 0x1010), __byte_perm(sw.y, 0u, 0x3232)};
                     const uint32_t magic = q4_magic();
                     __syncwarp();          // every lane has its source before any row is written
-                    auto widen_into = [&](uint8_t* out) {
+                    // a key's scales: the upper eight bits, and the three below them
+                    uint32_t lower[4];
+                    if (in_two) {
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            const uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {                // channels 32 c + 8 q .. + 7: one 16-byte chunk
-                                const uint32_t l0 = q4_signed_lo(w[q], magic), h0 = q4_signed_hi(w[q], magic);             // (0, 4), (1, 5)
-                                const uint32_t l1 = q4_signed_lo(w[q] >> 8, magic), h1 = q4_signed_hi(w[q] >> 8, magic);   // (2, 6), (3, 7)
-                                const uint4 f = make_uint4(h2_mul(__byte_perm(l0, h0, 0x5410), s2[c]), h2_mul(__byte_perm(l1, h1, 0x5410), s2[c]),
-                                                           h2_mul(__byte_perm(l0, h0, 0x7632), s2[c]), h2_mul(__byte_perm(l1, h1, 0x7632), s2[c]));
-                                const int c0 = (c & 1) * 4 + q;
-                                *reinterpret_cast<uint4*>(out + (c >> 1) * HALF_BYTES + rr * 128 + ((c0 ^ (rr & 7)) << 4)) = f;
-                            }
+                            const uint32_t upper = s2[c] & 0xFFF8FFF8u;
+                            lower[c] = h2_sub(s2[c], upper);
+                            s2[c] = upper;
                         }
-                    };
-                    if (lower) {           // the scales' lower three bits, then (below) the eight above them
-                        uint32_t upper[4];
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            upper[c] = s2[c] & 0xFFF8FFF8u;
-                            s2[c] = h2_sub(s2[c], upper[c]);
-                        }
-                        widen_into(lower);
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) s2[c] = upper[c];
                     }
-                    widen_into(tile);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {                // channels 32 c + 8 q .. + 7: one 16-byte chunk
+                            const uint32_t l0 = q4_signed_lo(w[q], magic), h0 = q4_signed_hi(w[q], magic);             // (0, 4), (1, 5)
+                            const uint32_t l1 = q4_signed_lo(w[q] >> 8, magic), h1 = q4_signed_hi(w[q] >> 8, magic);   // (2, 6), (3, 7)
+                            const uint32_t n[4] = {__byte_perm(l0, h0, 0x5410), __byte_perm(l1, h1, 0x5410), __byte_perm(l0, h0, 0x7632),
+                                                   __byte_perm(l1, h1, 0x7632)};
+                            const int c0 = (c & 1) * 4 + q, at = (c >> 1) * HALF_BYTES + rr * 128 + ((c0 ^ (rr & 7)) << 4);
+                            *reinterpret_cast<uint4*>(tile + at) = make_uint4(h2_mul(n[0], s2[c]), h2_mul(n[1], s2[c]), h2_mul(n[2], s2[c]), h2_mul(n[3], s2[c]));
+                            if (in_two)
+                                *reinterpret_cast<uint4*>(smem + C::OFF_K_LOWER + at) =
+                                    make_uint4(h2_mul(n[0], lower[c]), h2_mul(n[1], lower[c]), h2_mul(n[2], lower[c]), h2_mul(n[3], lower[c]));
+                        }
+                    }
                 } else {
                     const int rr = wq * 32 + lane;
                     uint8_t* src = tile + HALF_BYTES + rr * 128;
@@ -484,12 +476,11 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 fence_proxy_async_smem();                          // generic writes -> tensor core reads
                 __syncwarp();
             };
-            uint32_t it = 0, ke = 0, n_seg = 0;                     // key tile, entry of the K ring, segment
+            uint32_t it = 0, n_seg = 0;
             bool ok = true;
             for (int si = seg_lo; si < seg_hi && ok; ++si) {
                 const int n_tiles = (p.segments[si].k_end - p.segments[si].k_begin + BN - 1) / BN;
                 if (n_tiles <= 0) continue;
-                const uint32_t entries = k_entries(p.segments[si]);
                 const int k_begin = p.segments[si].k_begin;
                 const int seen = first_seen(p.segments[si].n_full, p.window);
                 // Q: bf16 -> fp16 in place (element by element, so the swizzle does not matter)
@@ -505,17 +496,15 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_ready);
-                for (int t = 0; t < n_tiles && ok; ++t, ++it, ke += entries) {
-                    const uint32_t kb = ke % KS, lb = (ke + 1) % KS, vb = it % VS;
-                    const bool split = KIND == kPaged4 && entries == 2;
-                    if (split && !(ok = warp_wait(&k_full[lb], ((ke + 1) / KS) & 1u, ab, kWaitRingFull))) break;
-                    if (!(ok = warp_wait(&k_full[kb], (ke / KS) & 1u, ab, kWaitRingFull))) break;
-                    widen_tile(smem + C::OFF_K + kb * C::TILE_BYTES, split ? smem + C::OFF_K + lb * C::TILE_BYTES : nullptr, false);
-                    if (lane == 0 && split) mbar_arrive(&k_ready[lb]);      // the issuers wait for the other one alone
-                    if (lane == 0) mbar_arrive(&k_ready[kb]);
+                for (int t = 0; t < n_tiles && ok; ++t, ++it) {
+                    const uint32_t kb = it % KS, vb = it % VS;
+                    if (!(ok = warp_wait(&k_full[kb], (it / KS) & 1u, ab, kWaitRingFull))) break;
+                    if (KIND == kPaged4 && !(ok = warp_wait(&low_empty[wq >> 1], (it & 1u) ^ 1u, ab, kWaitRingEmpty))) break;
+                    widen_tile(smem + C::OFF_K + kb * C::TILE_BYTES, true, false);
+                    if (lane == 0) mbar_arrive(&k_ready[KIND == kPaged4 ? kb * 2 + (wq >> 1) : kb]);
                     if (!(ok = warp_wait(&v_full[vb], (it / VS) & 1u, ab, kWaitRingFull))) break;
                     const int key = k_begin + t * BN + wq * 32 + lane;
-                    widen_tile(smem + C::OFF_V + vb * C::TILE_BYTES, nullptr, KIND == kPaged4 && key < seen);
+                    widen_tile(smem + C::OFF_V + vb * C::TILE_BYTES, false, KIND == kPaged4 && key < seen);
                     if (lane == 0) mbar_arrive(&v_ready[vb]);
                 }
             }

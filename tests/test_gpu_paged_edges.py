@@ -58,3 +58,49 @@ def test_a_group_of_nothing_but_nan_gets_a_finite_scale():
     for w in range(2):
         assert np.array_equal(dev.pools[2 * w].cpu().numpy()[at], want_codes)
         assert np.array_equal(dev.pools[2 * w + 1].cpu().numpy()[at], want_s)
+
+
+def q_bits(seed, B, Hq, T, d, gain=1.0):
+    return pr.bf16(np.random.default_rng(seed).standard_normal((B, Hq, T, d)) * gain)[0]
+
+
+def f64(bits):
+    return si.bf16_bits_to_f32(bits).astype(np.float64)
+
+
+@pytest.mark.parametrize("lens,T,P,k_gain,q_gain,window", [
+    ([6000], 2, 64, 12.0, 3.0, 0),
+    ([2200, 2049], 5, 16, 12.0, 3.0, 0),
+    ([6000], 64, 128, 12.0, 3.0, 0),              # two row tiles
+    ([6000, 1500, 0, 2047], 40, 32, 4.0, 1.0, 0),
+    ([9000], 33, 256, 12.0, 3.0, 4000),
+    ([130], 70, 16, 12.0, 3.0, 0),
+])
+def test_4_bit_chunk_of_peaked_scores(lens, T, P, k_gain, q_gain, window):
+    """Scores of some hundreds, a few keys lead every row: there a rounding of K does not average out, however many keys there
+    are.  No operand of the scores is rounded: what is left of a score is the fp32 summing of 256 exact products (2^-23 a step of 16, of
+    sums up to 2 * 8 s |q| a group, below 3e-4 here), so the log-sum-exp holds the tolerance of the packed cache.  O: its own
+    rounding to bf16, half a step 2^-8 of the value (0.0156 where |O| is 4 and more, as the leading keys' values are here: the
+    packed cache's tolerance 1e-2 is for outputs below 2.56); V and P rounded to fp16, 2^-11 each, of at most the largest value;
+    weights off by twice the scores' 3e-4; the exponentials 2.7e-6."""
+    from helpers import assert_lse_close, errors
+    cache = pr.PagedCache(17, lens, P, 2, 128, True, gain=k_gain)
+    dev = pr.DevCache(cache)
+    Q = q_bits(1017, len(lens), 8, T, 128, gain=q_gain)
+    o, lse, _ = dev.attend(Q, T, mode="chunk", window=window)
+    assert dev.status[0] == 0
+    ref, lref = pr.attention(cache, f64(Q), T, window=window)
+    v = max((np.abs(cache.rows(1, b, h)).max() for b in range(len(lens)) if lens[b] for h in range(2)), default=0.0)
+    assert np.isfinite(o).all()
+    assert (np.abs(o - ref) <= 2.0 ** -8 * np.abs(ref) + v * (2 * 2.0 ** -11 + 2 * 3e-4 + 2 * 2.7e-6)).all()
+    assert errors(o, ref)[1] <= 5e-3
+    assert_lse_close(lse, lref, "LSE")
+
+
+def test_4_bit_decode_and_chunk_agree_on_the_same_cache():
+    """Both take the codes and scales as they are: log-sum-exps of up to some hundreds agree to what fp32 sums leave."""
+    cache = pr.PagedCache(73, [5000, 700], 64, 2, 128, True, gain=12.0)
+    dev = pr.DevCache(cache)
+    Q = q_bits(73, 2, 8, 3, 128, gain=3.0)
+    lse = [dev.attend(Q, 3, mode=m)[1] for m in ("decode", "chunk")]
+    assert np.abs(lse[0].astype(np.float64) - lse[1]).max() <= 2 * 3e-4
