@@ -10,8 +10,9 @@ __device__ __forceinline__ void report_bad_page(int32_t* status) {
 }
 
 // Lowest key that any row of a segment sees: with a window, row 0's first one.  Keys below it in the same tile are read by
-// nobody: their pages may be gone and their rows may hold anything.
-__device__ __forceinline__ int first_seen(int n_full, int window) { return window > 0 ? max(0, n_full - window) : 0; }
+// nobody: their pages may be gone and their rows may hold anything.  (n_full is negative where the first rows see no key, and a
+// window may be as long as an int holds: the difference of the two would leave 32 bits.)
+__device__ __forceinline__ int first_seen(int n_full, int window) { return window > 0 ? max(0, max(n_full, 0) - window) : 0; }
 
 // A producer warp's view of the pages of one (sequence, KV head) stream.  Every lane holds one page, 32 at a time:
 // the pool row of its first slot, so that a tile costs one shuffle per box; the next 32 are already requested, so a

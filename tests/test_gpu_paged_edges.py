@@ -104,3 +104,22 @@ def test_4_bit_decode_and_chunk_agree_on_the_same_cache():
     Q = q_bits(73, 2, 8, 3, 128, gain=3.0)
     lse = [dev.attend(Q, 3, mode=m)[1] for m in ("decode", "chunk")]
     assert np.abs(lse[0].astype(np.float64) - lse[1]).max() <= 2 * 3e-4
+
+
+@pytest.mark.parametrize("window", [2**31 - 1, 2**31 - 4, 2**30 + 1, 3])
+@pytest.mark.parametrize("mode", ["decode", "chunk"])
+@pytest.mark.parametrize("q4", [False, True])
+@pytest.mark.parametrize("lens,T", [([2], 8), ([2, 40, 0, 9], 16), ([1, 300], 200)])
+def test_windows_as_long_as_an_int_and_more_rows_than_keys(q4, mode, window, lens, T):
+    """A window that takes nothing away leaves the plain causal rule, also where the first rows stand before the first key."""
+    from helpers import assert_close, assert_lse_close
+    if mode == "decode" and T > 16:
+        pytest.skip("decode takes 16 rows per KV head")
+    cache = pr.PagedCache(74, lens, 16, 2, 128, q4)
+    dev = pr.DevCache(cache)
+    Q = q_bits(74, len(lens), 2, T, 128)
+    o, lse, _ = dev.attend(Q, T, mode=mode, window=window)
+    assert dev.status[0] == 0
+    ref, lref = pr.attention(cache, f64(Q), T, window=window)
+    assert_close(o, ref, "O")
+    assert_lse_close(lse, lref, "LSE")
