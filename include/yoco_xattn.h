@@ -492,6 +492,15 @@ int32_t yoco_xattn_selftest_wait_expiry_fp8(const yoco_xattn_shape* shape, const
                                             void* workspace, size_t workspace_bytes, int32_t limit_ms,
                                             void* stream);
 
+/* The same for the decode kernels over a paged cache (arguments as for yoco_xattn_decode_paged(_q4); K_scale and V_scale
+ * both NULL: bf16 pages; no counterpart in the paper).  In either the wait that runs out is a warp's first wait for a tile:
+ * YOCO_ERR_TIMEOUT with YOCO_WAIT_RING_FULL. */
+int32_t yoco_xattn_selftest_wait_expiry_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout,
+                                              const void* Q, const void* K, const void* K_scale, const void* V,
+                                              const void* V_scale, const int32_t* page_table, const int32_t* kv_len_host,
+                                              void* O, void* workspace, size_t workspace_bytes, int32_t limit_ms,
+                                              void* stream);
+
 /* Measurement aid (no counterpart in the paper).  After yoco_xattn_profile_enable(n), each of
  * the next n decode/chunk calls records a CUDA event pair on its stream around the attention
  * kernel alone (not the merge, not the table upload).  yoco_xattn_profile_collect waits for the

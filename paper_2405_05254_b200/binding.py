@@ -127,7 +127,8 @@ def lib() -> ctypes.CDLL:
                            ("yoco_xattn_chunk_paged_q4", [ctypes.POINTER(Shape), lay] + attend_q4),
                            ("yoco_paged_append", rows + [vp] * 8), ("yoco_paged_append_q4", rows + [vp] * 10),
                            ("yoco_paged_gather", rows + [vp] * 8), ("yoco_paged_gather_q4", rows + [vp] * 10),
-                           ("yoco_rope_q", [ctypes.POINTER(Shape), lay] + [vp] * 4)):
+                           ("yoco_rope_q", [ctypes.POINTER(Shape), lay] + [vp] * 4),
+                           ("yoco_xattn_selftest_wait_expiry_paged", [ctypes.POINTER(Shape), lay] + [vp] * 9 + [sz, i32, vp])):
             getattr(L, name).argtypes = args
             getattr(L, name).restype = i32
         L.yoco_xattn_workspace_size_paged.restype = i32
@@ -448,6 +449,19 @@ def yoco_xattn_selftest_wait_expiry_fp8(shape: Shape, Q, K8, V8, k_scale, v_scal
                                                    _stream_ptr(stream))
     if rc != OK:
         raise YocoError(rc, "yoco_xattn_selftest_wait_expiry_fp8")
+
+
+def yoco_xattn_selftest_wait_expiry_paged(shape: Shape, layout: PagedLayout, Q, pools, page_table, kv_len, O, workspace,
+                                          limit_ms: int, stream=None) -> None:
+    """The same self-test over a paged cache; ``pools``: (K, V) of a bf16 cache, (K4, K_scale, V4, V_scale) of a 4-bit one.  O
+    is left undefined."""
+    keep_len, p_len = _host_i32(kv_len)
+    K, Ks, V, Vs = pools if len(pools) == 4 else (pools[0], None, pools[1], None)
+    rc = lib().yoco_xattn_selftest_wait_expiry_paged(
+        ctypes.byref(shape), ctypes.byref(layout), _ptr(Q), _ptr(K), _ptr(Ks), _ptr(V), _ptr(Vs), _ptr(page_table), p_len, _ptr(O),
+        _ptr(workspace), workspace.numel() * workspace.element_size(), int(limit_ms), _stream_ptr(stream))
+    if rc != OK:
+        raise YocoError(rc, "yoco_xattn_selftest_wait_expiry_paged")
 
 
 # ---- paged cache -----------------------------------------------------------------------------------

@@ -567,7 +567,7 @@ int32_t page_map(const yoco_paged_layout* layout, int32_t B, int32_t Hkv, const 
 int32_t attend_paged(int32_t mode, const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
                      const void* K, const void* k_scale, const void* V, const void* v_scale, bool q4,
                      const int32_t* page_table, const int32_t* kv_len_host, void* O, float* lse, void* workspace,
-                     size_t workspace_bytes, void* stream) {
+                     size_t workspace_bytes, void* stream, const SelfTest* selftest = nullptr) {
     return no_throw([&]() -> int32_t {
         if (!shape) return YOCO_ERR_INVALID_ARG;
         int32_t rc = validate_shape(*shape, mode);
@@ -582,7 +582,7 @@ int32_t attend_paged(int32_t mode, const yoco_xattn_shape* shape, const yoco_pag
         pc.k_scale = q4 ? k_scale : nullptr;
         pc.v_scale = q4 ? v_scale : nullptr;
         return run(shape, mode, Q, K, V, nullptr, kv_len_host, O, lse, workspace, workspace_bytes, stream, nullptr,
-                   nullptr, kMaxSubItems, nullptr, nullptr, &pc);
+                   nullptr, selftest ? 1 : kMaxSubItems, selftest, nullptr, &pc);
     });
 }
 
@@ -1168,6 +1168,17 @@ int32_t yoco_xattn_selftest_wait_expiry_fp8(const yoco_xattn_shape* shape, const
     const Fp8Scales sc{k_scale_host, v_scale_host};
     return run(shape, YOCO_MODE_DECODE, Q, K8, V8, cu_kv_host, kv_len_host, O, nullptr, workspace, workspace_bytes,
                stream, nullptr, &sc, 1, &st);
+}
+
+int32_t yoco_xattn_selftest_wait_expiry_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout,
+                                              const void* Q, const void* K, const void* K_scale, const void* V,
+                                              const void* V_scale, const int32_t* page_table, const int32_t* kv_len_host,
+                                              void* O, void* workspace, size_t workspace_bytes, int32_t limit_ms,
+                                              void* stream) {
+    if (limit_ms <= 0 || limit_ms > 1000 || (K_scale == nullptr) != (V_scale == nullptr)) return YOCO_ERR_INVALID_ARG;
+    const SelfTest st{(int64_t)limit_ms * 1000000ll};
+    return attend_paged(YOCO_MODE_DECODE, shape, layout, Q, K, K_scale, V, V_scale, K_scale != nullptr, page_table,
+                        kv_len_host, O, nullptr, workspace, workspace_bytes, stream, &st);
 }
 
 int32_t yoco_xattn_profile_enable(int32_t max_records) {

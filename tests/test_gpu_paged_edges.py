@@ -123,3 +123,37 @@ def test_windows_as_long_as_an_int_and_more_rows_than_keys(q4, mode, window, len
     ref, lref = pr.attention(cache, f64(Q), T, window=window)
     assert_close(o, ref, "O")
     assert_lse_close(lse, lref, "LSE")
+
+
+@pytest.mark.parametrize("q4", [False, True])
+@pytest.mark.parametrize("lens,Hq,T,P", [([9000, 2500], 16, 1, 64), ([70000], 16, 1, 16), ([30, 0, 7], 8, 2, 32), ([12000] * 3, 32, 2, 256)])
+def test_an_expired_wait_of_a_paged_decode_is_reported_and_the_next_call_is_correct(q4, lens, Hq, T, P):
+    """Nothing is loaded and the first wait for a tile runs out (limit 20 ms): every CTA leaves, the status names the wait, and the
+    same workspace serves the next call."""
+    import time
+    import torch
+    from helpers import assert_close, assert_lse_close, bf16_dev_to_f64
+    from paper_2405_05254_b200 import binding as bd
+    H = 4
+    cache = pr.PagedCache(75, lens, P, H, 128, q4)
+    dev = pr.DevCache(cache)
+    B = len(lens)
+    Qb = q_bits(75, B, Hq, T, 128)
+    Q = pr.bits_to_dev(Qb)
+    shape = bd.make_shape(B, Hq, H, 128, T)
+    ws = torch.empty(bd.yoco_xattn_workspace_size_paged(shape, dev.layout, cache.lens, bd.MODE_DECODE, q4), dtype=torch.uint8, device="cuda")
+    O, L = torch.zeros(B, Hq, T, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(B, Hq, T, device="cuda")
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    bd.yoco_xattn_selftest_wait_expiry_paged(shape, dev.layout, Q, dev.pools, dev.table, cache.lens, O, ws, limit_ms=20)
+    rc, wait_class, cta = bd.yoco_xattn_status_detail(ws)
+    dt = time.perf_counter() - t0
+    assert (rc, wait_class) == (bd.ERR_TIMEOUT, bd.WAIT_RING_FULL)
+    assert 0 <= cta < 2 * torch.cuda.get_device_properties(0).multi_processor_count
+    assert 0.015 < dt < 2.0, dt
+    name = "yoco_xattn_decode_paged" + ("_q4" if q4 else "")
+    bd.prepare_paged(name, shape, dev.layout, Q, *dev.pools, dev.table, cache.lens, O, L, ws).run()
+    assert bd.yoco_xattn_status_detail(ws) == (bd.OK, 0, -1)
+    ref, lref = pr.attention(cache, f64(Qb), T)
+    assert_close(bf16_dev_to_f64(O).reshape(ref.shape), ref)
+    assert_lse_close(L.cpu().numpy(), lref)
