@@ -303,7 +303,13 @@ __device__ __forceinline__ void decode_fp8_body(const CUtensorMap& tmK, const CU
             // THIS tile: the producer can only have done so after the previous tile of the stage was
             // released, i.e. after its round completed, and the barrier is then in the round asked for.
             const uint32_t stage = it % STAGES, round = it / STAGES;
-            if (!wait_armed(armed, it + 1, ab) || !wait_or_abort(&full_bar[stage], round & 1u, ab, kWaitRingFull)) {
+            // (One answer for the warp, see warp_wait_ready.)
+            bool landed = ld_acquire_shared(armed) >= it + 1 && mbar_try_wait(&full_bar[stage], round & 1u);
+            if (!__all_sync(0xffffffffu, landed)) {
+                landed = wait_armed(armed, it + 1, ab) && wait_or_abort(&full_bar[stage], round & 1u, ab, kWaitRingFull);
+                landed = __all_sync(0xffffffffu, landed);
+            }
+            if (!landed) {
                 ok = false;         // this warp touches no tile any more; it still walks to the barriers below
                 continue;
             }

@@ -270,7 +270,7 @@ __device__ __forceinline__ void decode_body(const CUtensorMap& tmK, const CUtens
             for (int k0 = k_lo; k0 < k_hi; k0 += TILE_N, ++it) {
                 if (!ok) continue;
                 const uint32_t stage = it % STAGES, round = it / STAGES;
-                if (!wait_or_abort(&full_bar[stage], round & 1u, ab, kWaitRingFull)) {
+                if (!warp_wait_ready(&full_bar[stage], round & 1u, ab, kWaitRingFull)) {
                     ok = false;     // this warp touches no tile any more; it still walks to the barriers below
                     continue;
                 }

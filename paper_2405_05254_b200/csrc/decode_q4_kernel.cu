@@ -82,13 +82,6 @@ __device__ __forceinline__ void mma_f16_from(float (&d)[4], const float (&c)[4],
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
-// warp_wait, with the usual case ahead of it: every lane finds the tile there at its first look.  The answer is one for the warp:
-// near the limit lanes that look on their own may differ, and one that left the loop would not come to the shuffles and
-// barriers that the others wait at.  (1M keys: 214.8 us, as with every lane on its own; 218.8 with warp_wait alone.)
-__device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, const Abort& ab) {
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    return warp_wait(bar, parity, ab, kWaitRingFull);
-}
 // D(16x8) = A(16x8) B(8x8), tf32 operands, with A's columns 4 .. 7 the same as 0 .. 3
 __device__ __forceinline__ void mma_tf32_twice(float (&d)[4], const float (&c)[4], float a0, float a1, float b0, float b1) {
     asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%4,%5}, {%6,%7}, "
@@ -338,7 +331,7 @@ __device__ __forceinline__ void decode_q4_body(const CUtensorMap& tmK, const CUt
         for (int m_tile = 0; m_tile < m_count; ++m_tile) {
             const int k0 = run.k_begin + (warp + W * m_tile) * TILE_N;
             const uint32_t count = done_tiles + m_tile, kp = count & (KH - 1), vp = KH + (count & (VH - 1));
-            if (!tile_wait(full_bar + warp * H + kp, (count / KH) & 1u, ab)) {
+            if (!warp_wait_ready(full_bar + warp * H + kp, (count / KH) & 1u, ab, kWaitRingFull)) {
                 ok = false;         // this warp touches no tile any more; it still walks to the barriers below
                 drain(m_tile, m_tile);
                 __syncwarp();
@@ -436,7 +429,7 @@ __device__ __forceinline__ void decode_q4_body(const CUtensorMap& tmK, const CUt
             // K has been read (the scores came out of it): its place takes the tile after next
             __syncwarp();
             issue_k();
-            if (!tile_wait(full_bar + warp * H + vp, (count / VH) & 1u, ab)) {
+            if (!warp_wait_ready(full_bar + warp * H + vp, (count / VH) & 1u, ab, kWaitRingFull)) {
                 ok = false;
                 drain(m_tile + 1, m_tile);
                 __syncwarp();

@@ -352,7 +352,7 @@ kv_append_small_kernel(const __grid_constant__ CUtensorMap tmWk, const __grid_co
         }
         __syncthreads();
         const int stage = c % SK_STAGES;
-        if (ok && !wait_or_abort(&full[stage], (uint32_t)(c / SK_STAGES) & 1u, ab, kWaitRingFull)) ok = false;
+        if (ok && !warp_wait_ready(&full[stage], (uint32_t)(c / SK_STAGES) & 1u, ab, kWaitRingFull)) ok = false;
         if (ok) {
             const uint32_t wbase = smem_u32(smem + stage * HALF_BYTES);
             const int k_l = ((lane >> 3) & 1) * 8 + (lane & 7);      // ldmatrix row inside a 16-k step
