@@ -423,11 +423,17 @@ int32_t yoco_rope_q(const yoco_xattn_shape* shape, const yoco_paged_layout* layo
 /* Attention over a paged cache.  Q, O, lse, workspace, lengths, window and the result are as for yoco_xattn_decode
  * (G*T <= 16) and yoco_xattn_chunk (any T); shape->kv_head_stride must be 0.  Q is taken as given (see yoco_rope_q).
  * The _q4 forms read 4-bit pages; Q is widened to fp16 for the products, |Q| < 65504.
- * The workspace is sized by yoco_xattn_workspace_size_paged (mode: YOCO_MODE_DECODE or YOCO_MODE_CHUNK; q4: 0 or 1).
+ * The workspace is sized by yoco_xattn_workspace_size_paged (mode: YOCO_MODE_DECODE or YOCO_MODE_CHUNK; q4: 0 or 1), for
+ * these lengths exactly: others, shorter ones among them, may take more.  A workspace that serves sequences while they grow is sized by
+ * yoco_xattn_workspace_bound_paged, with the lengths that they may reach: enough for all lengths up to those
+ * (shape, mode and q4 the same).
  * A call recorded into a CUDA graph keeps kv_len as it was; the page table is read at every replay. */
 int32_t yoco_xattn_workspace_size_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout,
                                         const int32_t* kv_len_host, int32_t sm_count, int32_t mode, int32_t q4,
                                         size_t* bytes);
+int32_t yoco_xattn_workspace_bound_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout,
+                                         const int32_t* kv_len_host, int32_t sm_count, int32_t mode, int32_t q4,
+                                         size_t* bytes);
 int32_t yoco_xattn_decode_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout, const void* Q,
                                 const void* K_pages, const void* V_pages, const int32_t* page_table,
                                 const int32_t* kv_len_host, void* O, float* lse, void* workspace,

@@ -132,6 +132,8 @@ def lib() -> ctypes.CDLL:
             getattr(L, name).argtypes = args
             getattr(L, name).restype = i32
         L.yoco_xattn_workspace_size_paged.restype = i32
+        L.yoco_xattn_workspace_bound_paged.argtypes = L.yoco_xattn_workspace_size_paged.argtypes
+        L.yoco_xattn_workspace_bound_paged.restype = i32
         L.yoco_xattn_profile_enable.argtypes = [i32]
         L.yoco_xattn_profile_collect.argtypes = [vp, i32, vp]
         L.yoco_xattn_strerror.argtypes = [i32]
@@ -493,7 +495,8 @@ class PreparedPagedCall:
     """A call of one of the paged-cache functions whose arguments are checked and marshalled once; run() only
     enqueues, on ``stream`` or, without one, on the stream that is current then.  The tensors are kept alive; shape, layout
     and the numbers of rows (``new_len``, ``begin``, ``end``) are copied.  ``kv_len``, if a contiguous int32 array, is read
-    at every run(), so a serving loop may advance its lengths in place."""
+    at every run(), so a serving loop may advance its lengths in place; its workspace is then sized by
+    yoco_xattn_workspace_bound_paged with the lengths that it will reach."""
 
     def __init__(self, fn_name, shape, layout, *args, stream=None):
         import torch
@@ -604,15 +607,25 @@ def prepare_paged(fn_name, shape, layout, *args, stream=None) -> PreparedPagedCa
     return PreparedPagedCall(fn_name, shape, layout, *args, stream=stream)
 
 
-def yoco_xattn_workspace_size_paged(shape: Shape, layout: PagedLayout, kv_len, mode: int, q4: bool = False,
-                                    sm_count: int = 0) -> int:
+def _workspace_paged(name, shape, layout, kv_len, mode, q4, sm_count):
     keep, p_len = _host_i32(kv_len)
     out = ctypes.c_size_t(0)
-    rc = lib().yoco_xattn_workspace_size_paged(ctypes.byref(shape), ctypes.byref(layout), p_len, sm_count, mode, int(q4),
-                                               ctypes.byref(out))
+    rc = getattr(lib(), name)(ctypes.byref(shape), ctypes.byref(layout), p_len, sm_count, mode, int(q4), ctypes.byref(out))
     if rc != OK:
-        raise YocoError(rc, "yoco_xattn_workspace_size_paged")
+        raise YocoError(rc, name)
     return int(out.value)
+
+
+def yoco_xattn_workspace_size_paged(shape: Shape, layout: PagedLayout, kv_len, mode: int, q4: bool = False,
+                                    sm_count: int = 0) -> int:
+    """Workspace bytes for exactly these lengths."""
+    return _workspace_paged("yoco_xattn_workspace_size_paged", shape, layout, kv_len, mode, q4, sm_count)
+
+
+def yoco_xattn_workspace_bound_paged(shape: Shape, layout: PagedLayout, kv_len, mode: int, q4: bool = False,
+                                     sm_count: int = 0) -> int:
+    """Workspace bytes that suffice for all lengths up to these: for a workspace kept while the sequences grow."""
+    return _workspace_paged("yoco_xattn_workspace_bound_paged", shape, layout, kv_len, mode, q4, sm_count)
 
 
 def yoco_xattn_decode_paged(shape: Shape, layout: PagedLayout, Q, K_pages, V_pages, page_table, kv_len, O, lse, workspace,

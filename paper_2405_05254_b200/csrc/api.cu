@@ -989,25 +989,48 @@ int32_t yoco_kv_append_fp8(const yoco_kv_append_shape* shape, const void* X, con
                           stream);
 }
 
+namespace {
+// checks; a zero *sm_count becomes that of the current device
+int32_t paged_workspace_args(const yoco_xattn_shape* shape, const yoco_paged_layout* layout, int32_t* sm_count, int32_t mode,
+                             int32_t q4, const size_t* bytes) {
+    if (!shape || !layout || !bytes || *sm_count < 0) return YOCO_ERR_INVALID_ARG;
+    int32_t rc = validate_shape(*shape, mode);
+    if (rc != YOCO_OK) return rc;
+    if (shape->kv_head_stride != 0) return YOCO_ERR_INVALID_ARG;
+    if ((q4 && shape->d != 128) || !valid_page_size(layout->page_size)) return YOCO_ERR_UNSUPPORTED;
+    if (*sm_count == 0) {
+        DeviceState* dev = nullptr;
+        if ((rc = device_state(&dev)) != YOCO_OK) return rc;
+        *sm_count = dev->sm_count;
+    }
+    return YOCO_OK;
+}
+}  // namespace
+
 int32_t yoco_xattn_workspace_size_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout,
                                         const int32_t* kv_len_host, int32_t sm_count, int32_t mode, int32_t q4,
                                         size_t* bytes) {
     return no_throw([&]() -> int32_t {
-        if (!shape || !layout || !bytes || sm_count < 0) return YOCO_ERR_INVALID_ARG;
-        int32_t rc = validate_shape(*shape, mode);
+        int32_t rc = paged_workspace_args(shape, layout, &sm_count, mode, q4, bytes);
         if (rc != YOCO_OK) return rc;
-        if (shape->kv_head_stride != 0) return YOCO_ERR_INVALID_ARG;
-        if ((q4 && shape->d != 128) || !valid_page_size(layout->page_size)) return YOCO_ERR_UNSUPPORTED;
-        if (sm_count == 0) {
-            DeviceState* dev = nullptr;
-            if ((rc = device_state(&dev)) != YOCO_OK) return rc;
-            sm_count = dev->sm_count;
-        }
         Plan plan;
         rc = make_plan(*shape, nullptr, kv_len_host, sm_count, mode, plan, kMaxSubItems, nullptr, nullptr,
                        q4 ? kPagedQ4Cache : kPagedCache);
         if (rc != YOCO_OK) return rc;
         *bytes = (size_t)plan.info.workspace_bytes;
+        return YOCO_OK;
+    });
+}
+
+int32_t yoco_xattn_workspace_bound_paged(const yoco_xattn_shape* shape, const yoco_paged_layout* layout,
+                                         const int32_t* kv_len_host, int32_t sm_count, int32_t mode, int32_t q4,
+                                         size_t* bytes) {
+    return no_throw([&]() -> int32_t {
+        int32_t rc = paged_workspace_args(shape, layout, &sm_count, mode, q4, bytes);
+        if (rc != YOCO_OK) return rc;
+        int64_t n = 0;
+        if ((rc = workspace_bound(*shape, kv_len_host, sm_count, mode, q4 ? kPagedQ4Cache : kPagedCache, &n)) != YOCO_OK) return rc;
+        *bytes = (size_t)n;
         return YOCO_OK;
     });
 }

@@ -35,6 +35,64 @@ int32_t validate_layout(const yoco_xattn_shape& s, const int32_t* cu_kv_host, co
     return YOCO_OK;
 }
 
+namespace {
+
+// Keys of a tile, and query rows of a CTA.
+int tile_keys(int32_t mode) { return mode == YOCO_MODE_DECODE ? kDecodeTileN : kChunkTileN; }
+int tile_rows(int32_t mode, int rows_per_stream, const CacheForm& form) {
+    return mode == YOCO_MODE_DECODE ? kDecodeTileM
+           : (rows_per_stream > kChunkTileM || form.pair_tiles) ? kChunkPairTileM : kChunkTileM;
+}
+// CTA groups that fill the GPU.
+int64_t groups_wanted(int32_t mode, int32_t sm_count, int m_tiles, const CacheForm& form) {
+    return mode == YOCO_MODE_DECODE ? (int64_t)sm_count * form.groups_per_sm : std::max<int64_t>(1, sm_count / m_tiles);
+}
+
+struct WorkspaceLayout {
+    int64_t table, part_lse, part_o, end;
+};
+WorkspaceLayout workspace_layout(int64_t table_words, int64_t slots, int rows_per_stream, int d) {
+    auto align256 = [](int64_t x) { return (x + 255) / 256 * 256; };
+    WorkspaceLayout w;
+    w.table = kWorkspaceHeaderBytes;
+    w.part_lse = align256(w.table + table_words * 4);
+    w.part_o = align256(w.part_lse + slots * rows_per_stream * 4);
+    w.end = align256(w.part_o + slots * rows_per_stream * d * 4);
+    return w;
+}
+
+}  // namespace
+
+// What a plan takes grows with its segments, its groups and its pieces per group, and none of the three is monotone in the
+// lengths: a stream's end may or may not coincide with a group's, and which rule cuts the streams (CacheForm) depends on
+// them.  But each has a bound that is.  Whatever the rule, segments are cut at the ends of streams and of groups only, and there are
+// at most as many groups as wanted and as tiles; pieces per group follow from tiles per group, and are taken only
+// with at most two segments per group.
+int32_t workspace_bound(const yoco_xattn_shape& s, const int32_t* kv_len_host, int32_t sm_count, int32_t mode,
+                        const CacheForm& form, int64_t* bytes) {
+    int32_t rc = validate_shape(s, mode);
+    if (rc != YOCO_OK) return rc;
+    if (sm_count <= 0) return YOCO_ERR_INVALID_ARG;
+    if ((rc = validate_layout(s, nullptr, kv_len_host)) != YOCO_OK) return rc;
+    const int rows_per_stream = s.Hq / s.Hkv * s.T, tile_n = tile_keys(mode), tile_m = tile_rows(mode, rows_per_stream, form);
+    const int m_tiles = (rows_per_stream + tile_m - 1) / tile_m;
+    const int64_t num_streams = (int64_t)s.B * s.Hkv;
+    int64_t tiles = 0;
+    for (int i = 0; i < s.B; ++i) {
+        int64_t n = (kv_len_host ? kv_len_host[i] : s.max_kv_len);
+        n = (n + tile_n - 1) / tile_n;
+        // with a window, a call's rows see at most T - 1 + window consecutive keys, which may start anywhere in a tile
+        if (s.window > 0) n = std::min<int64_t>(n, ((int64_t)s.T - 1 + s.window + tile_n - 2) / tile_n + 1);
+        tiles += n * s.Hkv;
+    }
+    const int64_t groups = std::max<int64_t>(1, std::min(groups_wanted(mode, sm_count, m_tiles, form), tiles));
+    const int64_t segments = std::min(tiles, groups + std::max<int64_t>(num_streams - 1, 0));
+    const int64_t pieces = mode != YOCO_MODE_DECODE ? 1 : choose_sub_items(tiles / groups / form.piece_divisor, std::min(kMaxSubItems, form.max_pieces));
+    const int64_t slots = std::max(segments, std::min(segments, 2 * groups) * pieces);
+    *bytes = workspace_layout(segments * kSegmentWords + groups + 1 + 2 * num_streams, slots, rows_per_stream, s.d).end;
+    return YOCO_OK;
+}
+
 int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const int32_t* kv_len_host,
                   int32_t sm_count, int32_t mode, Plan& plan, int32_t max_sub_items,
                   const int32_t* key_offset_host, const int32_t* kv_total_host, const CacheForm& form) {
@@ -45,9 +103,8 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
 
     const int G = s.Hq / s.Hkv;
     const int rows_per_stream = G * s.T;
-    const int tile_n = mode == YOCO_MODE_DECODE ? kDecodeTileN : kChunkTileN;
-    const int tile_m = mode == YOCO_MODE_DECODE ? kDecodeTileM
-                       : (rows_per_stream > kChunkTileM || form.pair_tiles) ? kChunkPairTileM : kChunkTileM;
+    const int tile_n = tile_keys(mode);
+    const int tile_m = tile_rows(mode, rows_per_stream, form);
     const int m_tiles = (rows_per_stream + tile_m - 1) / tile_m;
     const int num_streams = s.B * s.Hkv;
 
@@ -89,11 +146,7 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
     }
 
     // number of CTA groups
-    int64_t target;
-    if (mode == YOCO_MODE_DECODE)
-        target = (int64_t)sm_count * form.groups_per_sm;
-    else
-        target = std::max<int64_t>(1, sm_count / m_tiles);
+    const int64_t target = groups_wanted(mode, sm_count, m_tiles, form);
     int64_t num_groups = std::max<int64_t>(1, std::min<int64_t>(target, total_tiles));
     // first flat tile of every group: equal shares, or handfuls that end with their stream (CacheForm)
     std::vector<int64_t> bounds;
@@ -240,12 +293,11 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
     std::copy(stream_base.begin(), stream_base.end(), plan.table.begin() + plan.off_stream_base);
     std::copy(stream_nseg.begin(), stream_nseg.end(), plan.table.begin() + plan.off_stream_nseg);
 
-    auto align256 = [](int64_t x) { return (x + 255) / 256 * 256; };
-    plan.ws_table = kWorkspaceHeaderBytes;
-    plan.ws_part_lse = align256(plan.ws_table + (int64_t)plan.table.size() * 4);
     const int64_t slots = (int64_t)dev.size() * R;
-    plan.ws_part_o = align256(plan.ws_part_lse + slots * rows_per_stream * 4);
-    const int64_t ws_end = align256(plan.ws_part_o + slots * rows_per_stream * s.d * 4);
+    const WorkspaceLayout ws = workspace_layout((int64_t)plan.table.size(), slots, rows_per_stream, s.d);
+    plan.ws_table = ws.table;
+    plan.ws_part_lse = ws.part_lse;
+    plan.ws_part_o = ws.part_o;
 
     yoco_xattn_plan_info& info = plan.info;
     info.mode = mode;
@@ -261,7 +313,7 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
     info.max_splits = max_splits;
     info.needs_combine = needs_combine;
     info.total_tiles = total_tiles;
-    info.workspace_bytes = ws_end;
+    info.workspace_bytes = ws.end;
     return YOCO_OK;
 }
 

@@ -139,6 +139,10 @@ int32_t make_plan(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const in
                   const int32_t* key_offset_host = nullptr, const int32_t* kv_total_host = nullptr,
                   const CacheForm& form = kBf16Cache);
 
+// Bytes that suffice for make_plan's workspace with any lengths up to those given (the rest of the shape, and no shards).
+int32_t workspace_bound(const yoco_xattn_shape& s, const int32_t* kv_len_host, int32_t sm_count, int32_t mode,
+                        const CacheForm& form, int64_t* bytes);
+
 int32_t validate_shape(const yoco_xattn_shape& s, int32_t mode);
 // Lengths, head stride and token offsets must describe sequences that do not overlap (pure host).
 int32_t validate_layout(const yoco_xattn_shape& s, const int32_t* cu_kv_host, const int32_t* kv_len_host);

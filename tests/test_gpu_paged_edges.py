@@ -157,3 +157,32 @@ def test_an_expired_wait_of_a_paged_decode_is_reported_and_the_next_call_is_corr
     ref, lref = pr.attention(cache, f64(Qb), T)
     assert_close(bf16_dev_to_f64(O).reshape(ref.shape), ref)
     assert_lse_close(L.cpu().numpy(), lref)
+
+
+@pytest.mark.parametrize("q4", [False, True])
+def test_one_workspace_serves_a_batch_while_it_grows(q4):
+    """Lengths advanced in place through several ways of cutting the work; the workspace is that of the bound."""
+    import torch
+    from helpers import assert_close, assert_lse_close, bf16_dev_to_f64
+    from paper_2405_05254_b200 import binding as bd
+    B, H, steps = 16, 8, [1, 64, 700, 1536, 1537, 2560, 2688]
+    cache = pr.PagedCache(76, [steps[-1]] * B, 64, H, 128, q4, slack_nan=False)
+    dev = pr.DevCache(cache)
+    Qb = q_bits(76, B, H, 1, 128)
+    Q = pr.bits_to_dev(Qb)
+    shape = bd.make_shape(B, H, H, 128, 1)
+    lens = np.full(B, steps[-1], np.int32)
+    size = bd.yoco_xattn_workspace_bound_paged(shape, dev.layout, lens, bd.MODE_DECODE, q4)
+    buf = torch.full((size + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    O, L = torch.empty_like(Q), torch.empty(B, H, 1, device="cuda")
+    call = bd.prepare_paged("yoco_xattn_decode_paged" + ("_q4" if q4 else ""), shape, dev.layout, Q, *dev.pools, dev.table, lens, O, L, buf[:size])
+    for n in steps:
+        lens[:] = n
+        lens[3] = n // 2
+        call.run()
+        assert bd.yoco_xattn_status(buf) == 0
+        cache.lens = lens.copy()
+        ref, lref = pr.attention(cache, f64(Qb), 1)
+        assert_close(bf16_dev_to_f64(O).reshape(ref.shape), ref)
+        assert_lse_close(L.cpu().numpy(), lref)
+    assert (buf[size:] == 0x5A).all()
