@@ -544,27 +544,33 @@ class PreparedPagedCall:
     @staticmethod
     def _in_order(kind, a, shape, layout):
         """Whether the tensor's strides are those that the call goes by: contiguous, or rows (of all heads of a token, of a
-        page, of a sequence's table) that lie src_stride, page_rows or table_stride apart."""
-        if kind == "i" and a.dim() == 2 and a.shape[0] > 1 and a.stride(0) != layout.table_stride:
-            return False
-        if a.is_contiguous():
+        page, of a sequence's table) that lie src_stride, page_rows or table_stride apart.  Rows that are
+        contiguous, but wider or narrower than that, are not; a tensor without a dimension for the rows lies as the caller says.
+        (A pool's dimension may count parts of the distance between pages, K and V pages in turn say: it is held to its size.)"""
+        if a.numel() == 0:
             return True
         elems = {"k": shape.d, "c": shape.d // 2, "s": shape.d // 32}.get(kind)
         if kind == "x":
             width, apart = shape.Hkv * shape.d, shape.src_stride or shape.Hkv * shape.d
         elif kind == "i":
-            width, apart = a.shape[-1], layout.table_stride
+            width, apart = a.shape[-1] if a.dim() else 1, layout.table_stride
         elif elems:
             width = shape.Hkv * layout.page_size * elems
             apart = layout.page_rows * elems or width
         else:
-            return False
+            return a.is_contiguous()
         n, i = 1, a.dim()
         while i > 0 and n < width:                 # the dimensions of one row, densely
             i -= 1
             if a.shape[i] != 1 and a.stride(i) != n:
                 return False
             n *= a.shape[i]
+        # dimensions between a row and the next one: K and V pages side by side, or a token's K, V and more, in one tensor
+        while i > 1 and n < apart and a.stride(i - 1) == n and n * a.shape[i - 1] <= apart:
+            i -= 1
+            n *= a.shape[i]
+        if elems and i > 0 and apart % n == 0 and a.is_contiguous():
+            return True
         for j in reversed(range(i)):               # the rows, `apart` from one another
             if a.shape[j] != 1 and a.stride(j) != apart:
                 return False

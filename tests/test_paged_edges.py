@@ -98,3 +98,32 @@ def test_the_workspace_bound_refuses_what_the_size_refuses():
         assert call(**kw) == bd.ERR_INVALID_ARG, kw
     assert call(lay=layout(P=48)) == bd.ERR_UNSUPPORTED and call(shape=bd.make_shape(2, 8, 2, 64, 1), q4=1) == bd.ERR_UNSUPPORTED
     assert call(shape=bd.make_shape(2, 8, 2, 128, 5)) == bd.ERR_UNSUPPORTED
+
+
+def test_the_binding_checks_the_strides_of_contiguous_tensors_too():
+    """A contiguous tensor whose rows are wider than the call's would be read at the wrong distance."""
+    import torch
+    order = bd.PreparedPagedCall._in_order
+    lay, wide = layout(P=16, pages=5, stride=7), layout(P=16, pages=5, stride=7, page_rows=2 * 3 * 16)
+    new, fused = bd.PagedAppendShape(2, 3, 64, 1, 0), bd.PagedAppendShape(2, 3, 64, 1, 9 * 64)
+    qkv = torch.zeros(9, 9 * 64)                                    # a projection's whole output
+    assert not order("x", qkv, new, lay) and not order("x", qkv.view(9, 9, 64), new, lay)
+    assert order("x", qkv, fused, lay) and order("x", qkv.view(9, 9, 64), fused, lay) and order("x", qkv.view(9, 3, 3, 64), fused, lay)
+    assert order("x", qkv.view(9, 3, 192)[:, 1], fused, lay) and not order("x", qkv.view(9, 3, 192)[:, 1], new, lay)
+    own = torch.zeros(9, 3 * 64)
+    assert order("x", own, new, lay) and order("x", own.view(9, 3, 64), new, lay) and order("x", own.view(3, 3, 3, 64), new, lay)
+    assert not order("x", own, fused, lay) and not order("x", own.view(9, 3, 64), fused, lay)   # its tokens are 192 apart
+    assert order("x", own[:1], fused, lay)                          # a single token has no distance
+    assert order("x", torch.zeros(0, 192), new, lay) and order("x", torch.zeros(0, 192), fused, lay)
+    for kind, e in (("k", 64), ("c", 32), ("s", 2)):
+        both, one = torch.zeros(5, 2, 3, 16, e), torch.zeros(5, 3, 16, e)
+        assert order(kind, both, new, wide) and order(kind, one, new, lay)
+        assert order(kind, torch.zeros(10, 3, 16, e), new, wide)                                         # K and V pages in turn
+        assert not order(kind, torch.zeros(5, 4, 16, e), new, lay)                                       # pages of four heads
+        assert not order(kind, torch.zeros(5, 3, 32, e), new, lay)                                       # ... of 32 tokens
+        assert order(kind, one.view(-1, e), new, lay) and order(kind, one.view(-1), new, wide)           # flat: as the caller says
+        assert order(kind, torch.zeros(8, 3, 16, e), new, lay)                                           # spare pages
+    table = torch.zeros(2, 7, dtype=torch.int32)
+    assert order("i", table, new, lay) and order("i", table.view(-1), new, lay)
+    assert not order("i", torch.zeros(2, 8, dtype=torch.int32), new, lay) and not order("i", torch.zeros(4, 6, dtype=torch.int32), new, lay)
+    assert order("i", torch.zeros(1, 8, dtype=torch.int32), new, lay)
