@@ -390,7 +390,7 @@ typedef struct yoco_paged_append_shape {
  * each of the three operations rounded to fp32.  bf16 rows are rounded once, from that.  A call recorded into a CUDA graph
  * keeps its lengths; table, angles and rows are read at every replay.  kv_len_host: host
  * [B], N_i including the new tokens.  Other rows of the pools are not touched.  Two tokens of one call must
- * not land in the same slot. */
+ * not land in the same slot.  A call without a new token does nothing (K_new and V_new may be NULL then). */
 int32_t yoco_paged_append(const yoco_paged_append_shape* shape, const yoco_paged_layout* layout, const void* K_new,
                           const void* V_new, void* K_pages, void* V_pages, const int32_t* page_table,
                           const int32_t* new_len_host, const int32_t* kv_len_host, void* stream);

@@ -634,14 +634,14 @@ int32_t paged_rows(const yoco_paged_append_shape* shape, const yoco_paged_layout
         if (!K || !V || !aligned(K, 16) || !aligned(V, 16)) return YOCO_ERR_INVALID_ARG;
         if (q4 && (!k_scale || !v_scale || !aligned(k_scale, 16) || !aligned(v_scale, 16))) return YOCO_ERR_INVALID_ARG;
         if (append) {
-            if (!k_new || !v_new || !aligned(k_new, 16) || !aligned(v_new, 16)) return YOCO_ERR_INVALID_ARG;
+            if (!aligned(k_new, 16) || !aligned(v_new, 16)) return YOCO_ERR_INVALID_ARG;
             p.src_stride = s.src_stride ? s.src_stride : (int64_t)s.Hkv * s.d;
             if (p.src_stride < (int64_t)s.Hkv * s.d) return YOCO_ERR_INVALID_ARG;
             if (p.src_stride % 8 != 0) return YOCO_ERR_UNSUPPORTED;
             if (new_len_host)
                 for (int32_t i = 0; i < s.B; ++i)
                     if (new_len_host[i] < 0) return YOCO_ERR_INVALID_ARG;
-        } else if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16)) {
+        } else if (!aligned(k_out, 16) || !aligned(v_out, 16)) {
             return YOCO_ERR_INVALID_ARG;
         }
         SeqTable tab;
@@ -659,7 +659,8 @@ int32_t paged_rows(const yoco_paged_append_shape* shape, const yoco_paged_layout
             for (int32_t i = 0; i < s.B; ++i) max_len = std::max<int64_t>(max_len, end_host[i]);
             if ((rc = check_rotation(*layout, max_len, &p.rot)) != YOCO_OK) return rc;
         }
-        if (tokens == 0) return YOCO_OK;
+        if (tokens == 0) return YOCO_OK;             // (an empty tensor's address may be null)
+        if (append ? !k_new || !v_new : !k_out || !v_out) return YOCO_ERR_INVALID_ARG;
         DeviceState* dev = nullptr;
         if ((rc = device_state(&dev)) != YOCO_OK) return rc;
         p.k_src = static_cast<const __nv_bfloat16*>(k_new);

@@ -186,3 +186,20 @@ def test_one_workspace_serves_a_batch_while_it_grows(q4):
         assert_close(bf16_dev_to_f64(O).reshape(ref.shape), ref)
         assert_lse_close(L.cpu().numpy(), lref)
     assert (buf[size:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("q4", [False, True])
+def test_a_step_without_a_token_changes_nothing(q4):
+    import torch
+    from paper_2405_05254_b200 import binding as bd
+    cache = pr.PagedCache(77, [20, 0], 16, 2, 128, q4, slack_nan=False)
+    dev = pr.DevCache(cache)
+    before = [t.clone() for t in dev.pools]
+    none = torch.empty(0, 2 * 128, dtype=torch.bfloat16, device="cuda")
+    tail = "_q4" if q4 else ""
+    bd.prepare_paged("yoco_paged_append" + tail, bd.PagedAppendShape(2, 2, 128, 0, 0), dev.layout, none, none, *dev.pools, dev.table,
+                     np.zeros(2, np.int32), cache.lens).run()
+    bd.prepare_paged("yoco_paged_gather" + tail, bd.PagedAppendShape(2, 2, 128, 0, 0), dev.layout, *dev.pools, dev.table, cache.lens, cache.lens,
+                     none, none).run()
+    assert bd.yoco_kv_append_status() == 0
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, dev.pools))

@@ -127,3 +127,18 @@ def test_the_binding_checks_the_strides_of_contiguous_tensors_too():
     assert order("i", table, new, lay) and order("i", table.view(-1), new, lay)
     assert not order("i", torch.zeros(2, 8, dtype=torch.int32), new, lay) and not order("i", torch.zeros(4, 6, dtype=torch.int32), new, lay)
     assert order("i", torch.zeros(1, 8, dtype=torch.int32), new, lay)
+
+
+@pytest.mark.parametrize("fn", ["yoco_paged_append", "yoco_paged_append_q4", "yoco_paged_gather", "yoco_paged_gather_q4"])
+def test_calls_without_a_token_take_empty_tensors(fn):
+    """An empty tensor's address is null: no token to store or read back is no error; with a token a null address is."""
+    from test_paged_args import rows_call
+    none = (0, 0) if "append" in fn else (100, 1000)
+    assert rows_call(fn, a=none, src=None, out=None) == bd.OK
+    if "append" in fn:
+        assert rows_call(fn, a=None, shape=bd.PagedAppendShape(2, 2, 128, 0, 0), src=None) == bd.OK
+        assert rows_call(fn, a=(0, 1), src=None) == bd.ERR_INVALID_ARG
+    else:
+        assert rows_call(fn, a=(100, 999), out=None) == bd.ERR_INVALID_ARG
+    assert rows_call(fn, a=none, src=vp(4104), out=vp(4104)) == bd.ERR_INVALID_ARG
+    assert rows_call(fn, a=none, src=None, out=None, pool=None) == bd.ERR_INVALID_ARG
