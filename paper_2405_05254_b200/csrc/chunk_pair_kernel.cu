@@ -76,6 +76,9 @@ constexpr int Q4_ROW_BYTES = 64 + 8;
 constexpr int HALF_BYTES = 128 * 128;          // 128 rows x 64 bf16: one swizzled half tile
 constexpr uint32_t TMEM_COLS = 512;
 constexpr float kRescaleThreshold = 8.f;       // in log2 units: P stays below 2^8
+// fp16 P is kept 2^7 larger, at most 2^15: the weights of many keys behind one that leads by 16 to 23 octaves, which may be most of a
+// row's sum, would otherwise fall among fp16's subnormals and lose their bits (200,000 keys 20.6 octaves behind: O 2.7 % off).
+__host__ __device__ constexpr float p_shift(CacheKind kind) { return kind == kPaged4 ? 7.f : 0.f; }
 // Register split after launch.  The CTA starts with what its thread count allows (168 registers per
 // thread for 384 threads, 128 for 512); warpgroup 0 (and the widening warpgroup) give back down to
 // kOther / kWiden and the softmax warpgroups grow to kSoftmax.  The total must fit in what the CTA
@@ -623,7 +626,7 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                             }
                         }
                     }
-                    const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;
+                    const float neg_m = m_ref == -INFINITY ? 0.f : p_shift(KIND) - m_ref;
 
                     // keys past the end of the sequence (or before all windows): their V rows may hold anything; zero them so
                     // that 0 * garbage cannot make NaN.  Both warpgroups write the same zeros in
@@ -643,7 +646,7 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         fence_proxy_async_smem();                   // generic writes -> tensor core reads
                     }
 
-                    // P = 2^(s * scale - m_ref), two elements per instruction where the hardware
+                    // P = 2^(s * scale - m_ref + p_shift), two elements per instruction where the hardware
                     // allows; a masked score (-inf) comes out as exactly 0.
                     const uint64_t scale2 = f2_pack(scale_log2, scale_log2), negm2 = f2_pack(neg_m, neg_m);
                     uint64_t ls2[4] = {0ull, 0ull, 0ull, 0ull};            // packed partial row sums
@@ -692,7 +695,7 @@ chunk_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 tc_fence_after();
                 const bool has = l > 0.f;
                 const float inv = has ? out_scale / l : 0.f;
-                const float lse = has ? (m_ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                const float lse = has ? (m_ref - p_shift(KIND) + log2f(l)) * 0.6931471805599453f : -INFINITY;
                 const bool final_out = seg.stream_nseg == 1 && !p.force_partial;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {

@@ -203,3 +203,39 @@ def test_a_step_without_a_token_changes_nothing(q4):
                      none, none).run()
     assert bd.yoco_kv_append_status() == 0
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, dev.pools))
+
+
+@pytest.mark.parametrize("mode", ["chunk", "decode"])
+@pytest.mark.parametrize("n,octaves", [(40000, 17.0), (200000, 19.5), (200000, 20.6), (1000000, 21.6)])
+def test_4_bit_weights_of_many_keys_behind_one_that_leads_keep_their_bits(mode, n, octaves):
+    """All keys are zero but one, which leads by so many octaves and whose value is zero: O is the others' value times their
+    share.  Enough streams that most are one CTA's alone, so that the leader sets the maximum of all its keys.  Bound: the
+    output's half step 2^-8; P's 2^-11 (it is a normal fp16 number, 2^7 times the weight: 2^-14.6 would be the limit of 21.6
+    octaves behind, half a step 2^-25 absolute, 2^-10.4 relative); the row's fp32 sum, 64 keys an addition, each off by half a step 2^-24 of the sum (equal terms do not average
+    out): n / 64 * 2^-24, which is the log-sum-exp's error too, beside 2e-5 for the exponentials and fp32 scores; and the chunk
+    kernel's sums of n equal products on the tensor core, 16 a step, each step cut at 2^-23 of the sum so far, which is half the
+    last one on average: n / 16 * 2^-24."""
+    import torch
+    from paper_2405_05254_b200 import binding as bd
+    B, H, P = 20, 8, 64
+    pages = -(-n // P)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None].expand(B, pages).contiguous()      # one set of pages for all
+    layout = bd.make_paged_layout(P, pages, pages)
+    kc = torch.full((pages, H, P, 64), 0x88, dtype=torch.uint8, device="cuda")
+    ks = torch.ones(pages, H, P, 4, dtype=torch.float16, device="cuda")
+    vc, vs = torch.full_like(kc, 0xCC), torch.full_like(ks, 0.02)
+    kc[1, :, 5, 0], vc[1, :, 5] = 0x8F, 0x88                                                               # 7 in channel 0; zeros
+    q = pr.bf16(np.array([octaves * np.log(2) / 7 * 128 ** 0.5], np.float32))[1][0]
+    Q = torch.zeros(B, H, 1, 128, dtype=torch.bfloat16, device="cuda")
+    Q[..., 0] = float(q)
+    O, L = torch.empty_like(Q), torch.empty(B, H, 1, device="cuda")
+    lens = np.full(B, n, np.int32)
+    shape = bd.make_shape(B, H, H, 128, 1)
+    ws = torch.empty(bd.yoco_xattn_workspace_size_paged(shape, layout, lens, bd.MODE_DECODE if mode == "decode" else bd.MODE_CHUNK, True),
+                     dtype=torch.uint8, device="cuda")
+    bd.prepare_paged(f"yoco_xattn_{mode}_paged_q4", shape, layout, Q, kc, ks, vc, vs, table, lens, O, L, ws).run()
+    assert bd.yoco_xattn_status(ws) == 0
+    lead = np.exp(float(q) * 7 * 128 ** -0.5)
+    want = 4 * float(np.float16(0.02)) * (n - 1) / (n - 1 + lead)
+    assert np.abs(O.double().cpu().numpy() / want - 1).max() <= 2.0 ** -8 + 2.0 ** -10.4 + (n / 16 + n / 64) * 2.0 ** -24
+    assert np.abs(L.double().cpu().numpy() - np.log(n - 1 + lead)).max() <= n / 64 * 2.0 ** -24 + 2e-5
