@@ -77,8 +77,8 @@ constexpr int HALF_BYTES = 128 * 128;          // 128 rows x 64 bf16: one swizzl
 constexpr uint32_t TMEM_COLS = 512;
 constexpr float kRescaleThreshold = 8.f;       // in log2 units: P stays below 2^8
 // fp16 P is kept 2^7 larger, at most 2^15: the weights of many keys behind one that leads by 16 to 23 octaves, which may be most of a
-// row's sum, would otherwise fall among fp16's subnormals and lose their bits (200,000 keys 20.6 octaves behind: O 2.7 % off).
-__host__ __device__ constexpr float p_shift(CacheKind kind) { return kind == kPaged4 ? 7.f : 0.f; }
+// row's sum, would otherwise fall among fp16's subnormals and lose their bits (90,000 keys 20.6 octaves behind: O 2.6 % off).
+__host__ __device__ constexpr float p_shift(CacheKind kind) { return widened(kind) ? 7.f : 0.f; }
 // Register split after launch.  The CTA starts with what its thread count allows (168 registers per
 // thread for 384 threads, 128 for 512); warpgroup 0 (and the widening warpgroup) give back down to
 // kOther / kWiden and the softmax warpgroups grow to kSoftmax.  The total must fit in what the CTA
