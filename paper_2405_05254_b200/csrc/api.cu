@@ -180,9 +180,10 @@ struct MapKey {
     const void* base;
     int64_t rows;
     int32_t row_bytes, box_rows, box_bytes, bf16;
+    CUtensorMapSwizzle swizzle;
     bool operator==(const MapKey& o) const {
         return base == o.base && rows == o.rows && row_bytes == o.row_bytes && box_rows == o.box_rows &&
-               box_bytes == o.box_bytes && bf16 == o.bf16;
+               box_bytes == o.box_bytes && bf16 == o.bf16 && swizzle == o.swizzle;
     }
 };
 struct MapCache {
@@ -211,7 +212,7 @@ thread_local MapCache g_maps;
 // swizzled by the box's width (128 or 64 bytes) or not at all.
 int32_t make_map(CUtensorMap* map, const void* base, int64_t rows, int32_t row_bytes, int32_t box_bytes,
                  int32_t box_rows, bool bf16, CUtensorMapSwizzle swizzle) {
-    const MapKey mk{base, rows, row_bytes, box_rows, box_bytes, bf16 ? 1 : 0};
+    const MapKey mk{base, rows, row_bytes, box_rows, box_bytes, bf16 ? 1 : 0, swizzle};
     if (g_maps.find(mk, map)) return YOCO_OK;
     EncodeTiledFn enc;
     int32_t rc = get_encoder(&enc);
