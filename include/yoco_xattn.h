@@ -353,8 +353,8 @@ int32_t yoco_kv_append_fp8(const yoco_kv_append_shape* shape, const void* X, con
  *   bf16   K_pages, V_pages: d bf16 a row (d = 64 or 128)
  *   4-bit  K4, V4: d/2 bytes a row, channel 2e in the low nibble of byte e, 2e + 1 in the high one (d = 128);
  *          K_scale, V_scale: d/32 fp16 a row.  The value of a channel is (code - 8) * scale of its 32 channels,
- *          codes 1 .. 15 (0 reads as -8).  4.5 bits a value.  A V scale must stay below 448 in magnitude (append
- *          writes no larger one).
+ *          codes 1 .. 15 (0 reads as -8).  4.5 bits a value.  A V scale must not pass 448 in magnitude, a K scale must stay
+ *          below 8,188 (append writes none above 448).
  * Sequences hold at most 2^30 keys.  Pools start on 16-byte boundaries (scales too).  Pool, table, Q and O are device memory of the current device.
  *
  * Table entries are read on the device, only those that hold a key that some row of the call sees (with a window, pages
@@ -422,7 +422,9 @@ int32_t yoco_rope_q(const yoco_xattn_shape* shape, const yoco_paged_layout* layo
 
 /* Attention over a paged cache.  Q, O, lse, workspace, lengths, window and the result are as for yoco_xattn_decode
  * (G*T <= 16) and yoco_xattn_chunk (any T); shape->kv_head_stride must be 0.  Q is taken as given (see yoco_rope_q).
- * The _q4 forms read 4-bit pages; Q is widened to fp16 for the products, |Q| < 65504.
+ * The _q4 forms read 4-bit pages; Q is taken in fp16 for the products: |Q| < 65504, and elements below 2^-14 in magnitude (decode:
+ * 2^-13) are off by up to 2^-25 (decode: 2^-21).  K enters the scores unrounded; V (chunk), P and P times a V scale (decode) are
+ * rounded to fp16.
  * The workspace is sized by yoco_xattn_workspace_size_paged (mode: YOCO_MODE_DECODE or YOCO_MODE_CHUNK; q4: 0 or 1), for
  * these lengths exactly: others, shorter ones among them, may take more.  A workspace that serves sequences while they grow is sized by
  * yoco_xattn_workspace_bound_paged, with the lengths that they may reach: enough for all lengths up to those

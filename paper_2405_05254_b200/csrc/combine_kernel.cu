@@ -72,7 +72,8 @@ __device__ __forceinline__ void combine_body(const CombineParams& p) {
 
     // The partial rows this warp will need do not depend on the weights: ask for the first U of them
     // now, so that they travel while the log-sum-exps are read and reduced (one memory round trip
-    // instead of two or more; U covers all of a warp's pieces in the launch shapes used).
+    // instead of two or more; U covers all of a warp's pieces in the launch shapes used, but for the warp per row of
+    // kManyRows, whose pieces from the fifth on are a second round trip that many rows hide).
     constexpr int U = WPR == 1 ? 4 : (WARPS == kCombineWarpsMany ? 2 : 10);
     const int e0 = lane * 4;
     float4 pre[U][2];

@@ -1,12 +1,14 @@
 // Split-KV decode over a paged 4-bit cache: 64 bytes of codes and four fp16 scales a row (32 channels share a
-// scale, value = (code - 8) * scale), head dimension 128.  Work items, ring protocol, masks and the merge are those
-// of the 8-bit kernel; a 64-key tile is 4 KB of codes and 512 bytes of scales per tensor, 9 KB in all, so at the same
-// HBM bandwidth a key has to be worked off in a little over half of the 8-bit kernel's time.  What this kernel does about
-// that is to spend few instructions per key:
+// scale, value = (code - 8) * scale), head dimension 128.  A CTA works off the segments of its group one after the other; its
+// warps take whole tiles in turn, each loads its own into places that nobody else touches (no producer, no ring, no
+// pieces handed out at run time), and their states are merged at the end of every segment.  A 64-key tile is 4 KB of codes and
+// 512 bytes of scales per tensor, 9 KB in all, so at the same HBM bandwidth a key has to be worked off in a little over half
+// of the 8-bit kernel's time.  What this kernel does about that is to spend few instructions per key:
 //
 //   codes    No conversion instruction.  A code n sits in the low bits of an fp16 word after one AND, where it is
 //            the subnormal n 2^-24 (or 16 n 2^-24 for the nibble next to it): an exact multiple, and tensor-core
-//            operands keep subnormals.  The factor 16 goes into Q (exact), 2^24 into the softmax scale.
+//            operands keep subnormals.  The factor 16 goes into Q, 2^24 into the softmax scale.  (q / 16 in fp16 is exact
+//            where q is a multiple of 2^-20, as a bf16 value from 2^-13 on is; below, it is off by up to 2^-21.)
 //   K        S = sum over groups j of  s_j(key) * 2^24 * (sum_c q_c n_c 2^-24  -  8 * 2^-24 * sum_c q_c).
 //            The inner sums are the two products of a group; the scales are applied to their fp32 result, four
 //            multiply-adds per group and 16 keys; the offsets of all groups are one small product per 16 keys, which
@@ -24,9 +26,11 @@
 // stays below 448, and 2^7 * 448 is below the largest fp16 value.  Towards zero a P s below 2^-25 is lost to O (not to
 // the log-sum-exp, which sums P in fp32): weights below 2^-32 / s of the row's largest.
 //
-// Bound by instructions: 1M keys (32 query over 8 KV heads, pages of 64) take 215 us = 5,620 GB/s, 0.87 of the measured copy
-// rate; 996 instructions a tile, of them 256 ANDs and 64 shifts that bring the codes into place, so the ALU
-// pipe is busy 51 % of the cycles, the tensor pipe 39 %, and one of three warps issues in 58 %.  Sixteen rows (T = 4): 412 us.
+// Bound by latency with three warps a scheduler, none of the units being full: 1M keys (32 query over 8 KV heads, pages of 64), kernel
+// alone in short bursts at the full clock, take 215 us = 5,620 GB/s, 0.87 of the measured copy rate; a call in a loop of
+// seconds, where the power cap takes the clock down, 239 to 257 us.  1,001 instructions a tile, of them 256 ANDs and 64 shifts
+// that bring the codes into place: the ALU pipe is busy 53 % of the cycles, the tensor pipe 39 %, a warp issues in 59 %, and
+// fixed latencies are the most frequent stall.  Sixteen rows (T = 4): 391 us.
 // W = 12 because 168 registers a thread is the least that spills little: 8 / 12 / 16 warps 272 / 219 / 232 us.
 #include "decode_f16.cuh"
 #include "kernels.h"

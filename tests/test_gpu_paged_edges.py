@@ -1,4 +1,5 @@
-"""The paged cache on the GPU where its operators can go wrong: NaN among ordinary values of a new 4-bit row."""
+"""The paged cache on the GPU where its operators can go wrong: NaN among ordinary values of a new 4-bit row, peaked scores and
+long tails, windows near the end of an int, waits that run out, batches that grow, steps without a token."""
 import numpy as np
 import pytest
 
@@ -107,14 +108,12 @@ def test_4_bit_decode_and_chunk_agree_on_the_same_cache():
 
 
 @pytest.mark.parametrize("window", [2**31 - 1, 2**31 - 4, 2**30 + 1, 3])
-@pytest.mark.parametrize("mode", ["decode", "chunk"])
 @pytest.mark.parametrize("q4", [False, True])
-@pytest.mark.parametrize("lens,T", [([2], 8), ([2, 40, 0, 9], 16), ([1, 300], 200)])
+@pytest.mark.parametrize("lens,T,mode", [([2], 8, "decode"), ([2], 8, "chunk"), ([2, 40, 0, 9], 16, "decode"), ([2, 40, 0, 9], 16, "chunk"),
+                                         ([1, 300], 200, "chunk")])
 def test_windows_as_long_as_an_int_and_more_rows_than_keys(q4, mode, window, lens, T):
     """A window that takes nothing away leaves the plain causal rule, also where the first rows stand before the first key."""
     from helpers import assert_close, assert_lse_close
-    if mode == "decode" and T > 16:
-        pytest.skip("decode takes 16 rows per KV head")
     cache = pr.PagedCache(74, lens, 16, 2, 128, q4)
     dev = pr.DevCache(cache)
     Q = q_bits(74, len(lens), 2, T, 128)
