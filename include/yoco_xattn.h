@@ -453,6 +453,89 @@ int32_t yoco_xattn_chunk_paged_q4(const yoco_xattn_shape* shape, const yoco_page
                                   const int32_t* page_table, const int32_t* kv_len_host, void* O, float* lse,
                                   void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Self-decoder with gated retention (Section 3.1) --------------------------------------------------
+ * Per head, with rows q_t, k_t, v_t of d channels and a decay g_t, a state S (d x d) runs along a sequence:
+ *     S_t = g_t S_(t-1) + k_t^T v_t,    o_t = scale * q_t S_t
+ * (the recurrent form; for whole prompts the calls evaluate the chunkwise form, which is the same sums in another order).
+ * Rows are token-major, as a projection leaves them: the tokens of all sequences one after the other (no padding between
+ * sequences), heads consecutive inside a token, `stride` elements from token to token; Q, K, V (and the gate) may be slices of one
+ * fused projection.  They start on 16-byte boundaries, strides are multiples of 8 elements (0 -> H * d).  Rows should be finite: a value that is
+ * not may reach every row of the same 128 tokens of its sequence, and what follows them.
+ *
+ * States live in a pool [num_slots, H, d, d] fp32 (first index after the head: the keys' channel), 16-byte aligned.  Sequence i starts from the
+ * state in slot slot_in_host[i] (-1: from zero; the arrays are host [B], NULL = slot i) and leaves its state in slot
+ * slot_out_host[i] (-1: nowhere).  A slot may be read by several sequences (a common prefix) and may be read and written by the same one; one
+ * that is written by two sequences, or written by one and read by another, is refused.  Other slots are not touched.  A sequence
+ * without tokens hands its state on. */
+typedef struct yoco_gret_shape {
+    int32_t B;               /* sequences (<= 512)                                        */
+    int32_t H;               /* heads (<= 65535)                                          */
+    int32_t d;               /* channels of a head: 64 or 128                             */
+    int32_t T;               /* tokens per sequence when len_host is NULL                 */
+    int32_t num_slots;       /* states in the pool                                        */
+    float   scale;           /* > 0, or 0 -> 1/sqrt(d); negative values are rejected      */
+    float   tau;             /* > 0: decay holds logits z, g = sigmoid(z)^(1/tau); 0: natural logarithms of g.  Logarithms
+                                below -110 (g < 2^-158, which no product in fp32 tells from 0) count as -110 */
+    int32_t decay_bf16;      /* 0: decay is fp32, 1: bf16                                 */
+    int64_t q_stride, k_stride, v_stride, o_stride;   /* elements between two tokens      */
+    int64_t decay_stride;    /* elements between two tokens of decay [tokens, H]; 0 -> H  */
+} yoco_gret_shape;
+
+/* (GroupNorm and swish gate of multi-head gated retention.)  Every head's output row x, and what is done with it before it is stored:
+ *     y = swish(gate) * ((x - mean) / sqrt(var + eps) * gain + bias)        rms = 0
+ *     y = swish(gate) * (x / sqrt(mean(x^2) + eps) * gain + bias)           rms = 1
+ * mean and var over the head's channels, swish(u) = u / (1 + exp(-u)), all in fp32, y rounded to bf16 once. */
+typedef struct yoco_norm_gate {
+    const void* gate;        /* bf16 [tokens, H * d], gate_stride apart, or NULL: no gate */
+    const void* gain;        /* bf16 [H * d] or NULL: ones                                */
+    const void* bias;        /* bf16 [H * d] or NULL: zeros                               */
+    int64_t gate_stride;     /* elements between two tokens; a multiple of 8; 0 -> H * d  */
+    float   eps;             /* >= 0, used as given                                       */
+    int32_t rms;             /* 0: mean and variance, 1: root mean square                 */
+} yoco_norm_gate;
+
+/* One token of every sequence: Q, K, V, O are rows [B, H * d], decay [B, H] (shape->T is not read).  norm may be NULL: O is o rounded
+ * to bf16.  O must not overlap the inputs.  A call recorded into a CUDA graph keeps its slots; rows, decays and states are
+ * read at every replay. */
+int32_t yoco_gret_step(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay,
+                       const yoco_norm_gate* norm, float* state, const int32_t* slot_in_host, const int32_t* slot_out_host,
+                       void* O, void* stream);
+/* Any number of tokens: len_host[i] (host [B], may be 0) or shape->T of sequence i.  The workspace (16-byte aligned) is sized by
+ * yoco_gret_workspace_size, for these lengths exactly; where that is 0, it may be NULL.  A call recorded into a CUDA graph keeps
+ * lengths and slots.  A bounded device-side wait that ran out is reported by yoco_kv_append_status. */
+int32_t yoco_gret_chunk(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay,
+                        const yoco_norm_gate* norm, float* state, const int32_t* slot_in_host, const int32_t* slot_out_host,
+                        const int32_t* len_host, void* O, void* workspace, size_t workspace_bytes, void* stream);
+/* sm_count <= 0: that of the current device. */
+int32_t yoco_gret_workspace_size(const yoco_gret_shape* shape, const int32_t* len_host, int32_t sm_count, size_t* bytes);
+
+/* The normalisation and gate alone: X, Y [tokens, H * d] bf16.  Y may be X (with the same stride). */
+typedef struct yoco_head_norm_shape {
+    int64_t tokens;          /* tokens * H below 2^31                                     */
+    int32_t H;               /* groups per token                                          */
+    int32_t d;               /* channels of a group: a multiple of 8, at most 1024        */
+    int64_t x_stride, y_stride;  /* elements between two tokens; multiples of 8; 0 -> H * d */
+} yoco_head_norm_shape;
+int32_t yoco_head_norm(const yoco_head_norm_shape* shape, const void* X, const yoco_norm_gate* norm, void* Y, void* stream);
+
+/* Queries and keys turned by the angles of their tokens' positions (the factors Theta of gated retention), token-major rows.  Sequence i's
+ * tokens stand at pos_host[i], pos_host[i] + 1, ... (host [B]; positions stay below 2^31); pair j of a head turns by a = position * inv_freq[j]:
+ *     (x1, x2) -> (x1 cos a - x2 sin a, x2 cos a + x1 sin a),  each of the three operations rounded to fp32, the result to bf16.
+ * inv_freq: device [rot / 2], 64-bit, whatever scaling for long contexts already in it; the angle is reduced in 64 bits, so
+ * far positions lose nothing.  Channels rot .. d - 1 of a head are copied.  K may be NULL with Hk = 0.  Q_rot may be Q and K_rot
+ * K (with the same stride); otherwise they must not overlap the inputs. */
+typedef struct yoco_rope_shape {
+    int32_t B;               /* sequences (<= 512)                                        */
+    int32_t Hq, Hk;          /* heads of Q and of K (Hk may be 0)                         */
+    int32_t d;               /* channels of a head: a multiple of 16, at most 512         */
+    int32_t T;               /* tokens per sequence when len_host is NULL                 */
+    int32_t rot;             /* channels that turn: a multiple of 16, at most d; 0 -> d   */
+    int32_t rope_pairs;      /* 0: channels (c, c + rot/2) turn together, 1: (2c, 2c + 1) */
+    int64_t q_stride, k_stride, q_out_stride, k_out_stride;   /* elements between two tokens; multiples of 8; 0 -> heads * d */
+} yoco_rope_shape;
+int32_t yoco_rope(const yoco_rope_shape* shape, const void* Q, const void* K, const double* inv_freq,
+                  const int32_t* pos_host, const int32_t* len_host, void* Q_rot, void* K_rot, void* stream);
+
 /* (No counterpart in the paper.)  Synchronises `stream`; returns YOCO_OK, or YOCO_ERR_TIMEOUT if an
  * append kernel on the current device gave up a wait (YOCO_ERR_BAD_PAGE: a paged append or gather met a bad page)
  * since the last call of this function (which clears the record).  The _detail form also reports which wait and which CTA (see below). */

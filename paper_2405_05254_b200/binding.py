@@ -43,6 +43,29 @@ class PagedAppendShape(ctypes.Structure):
                 ("src_stride", ctypes.c_int64)]
 
 
+class GretShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("d", ctypes.c_int32), ("T", ctypes.c_int32),
+                ("num_slots", ctypes.c_int32), ("scale", ctypes.c_float), ("tau", ctypes.c_float), ("decay_bf16", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("o_stride", ctypes.c_int64), ("decay_stride", ctypes.c_int64)]
+
+
+class NormGate(ctypes.Structure):
+    _fields_ = [("gate", ctypes.c_void_p), ("gain", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("gate_stride", ctypes.c_int64), ("eps", ctypes.c_float), ("rms", ctypes.c_int32)]
+
+
+class HeadNormShape(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("H", ctypes.c_int32), ("d", ctypes.c_int32), ("x_stride", ctypes.c_int64),
+                ("y_stride", ctypes.c_int64)]
+
+
+class RopeShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hk", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("T", ctypes.c_int32), ("rot", ctypes.c_int32), ("rope_pairs", ctypes.c_int32), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64)]
+
+
 class Segment(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("group", "b", "c", "k_begin", "k_end", "slot")]
 
@@ -134,6 +157,11 @@ def lib() -> ctypes.CDLL:
         L.yoco_xattn_workspace_size_paged.restype = i32
         L.yoco_xattn_workspace_bound_paged.argtypes = L.yoco_xattn_workspace_size_paged.argtypes
         L.yoco_xattn_workspace_bound_paged.restype = i32
+        for name, args in (("yoco_gret_step", [vp] * 11), ("yoco_gret_chunk", [vp] * 12 + [sz, vp]),
+                           ("yoco_gret_workspace_size", [vp, vp, i32, ctypes.POINTER(sz)]),
+                           ("yoco_head_norm", [vp] * 5), ("yoco_rope", [vp] * 9)):
+            getattr(L, name).argtypes = args
+            getattr(L, name).restype = i32
         L.yoco_xattn_profile_enable.argtypes = [i32]
         L.yoco_xattn_profile_collect.argtypes = [vp, i32, vp]
         L.yoco_xattn_strerror.argtypes = [i32]
@@ -693,6 +721,190 @@ def yoco_paged_gather_q4(shape: PagedAppendShape, layout: PagedLayout, K4, K_sca
 def yoco_rope_q(shape: Shape, layout: PagedLayout, Q, kv_len, Q_rot, stream=None) -> None:
     """Turn the queries [B, Hq, T, d] by the angles of their rows' positions N_i - T + t."""
     prepare_paged("yoco_rope_q", shape, layout, Q, kv_len, Q_rot, stream=stream).run()
+
+
+# ---- self-decoder: token-major rows -------------------------------------------------------------------
+def make_gret_shape(B, H, d, T=1, num_slots=0, scale=0.0, tau=0.0, decay_bf16=False, q_stride=0, k_stride=0, v_stride=0,
+                    o_stride=0, decay_stride=0) -> GretShape:
+    """``tau`` > 0: the decays are logits z of g = sigmoid(z)^(1/tau); 0: natural logarithms of g.  ``num_slots`` 0: B."""
+    return GretShape(int(B), int(H), int(d), int(T), int(num_slots) or int(B), float(scale), float(tau), int(decay_bf16),
+                     int(q_stride), int(k_stride), int(v_stride), int(o_stride), int(decay_stride))
+
+
+def make_norm_gate(eps, rms=False, gate=None, gain=None, bias=None, gate_stride=None) -> NormGate:
+    """Normalisation of the heads' outputs, gain, bias (bf16 [H * d] or None) and gate (bf16 rows or None; ``gate_stride`` None:
+    the distance of the tensor's tokens).  The tensors are kept alive by the object."""
+    if gate_stride is None:
+        gate_stride = gate.stride(0) if gate is not None and gate.dim() > 1 and gate.shape[0] > 1 else 0
+    norm = NormGate(None if gate is None else gate.data_ptr(), None if gain is None else gain.data_ptr(),
+                    None if bias is None else bias.data_ptr(), int(gate_stride), float(eps), int(rms))
+    norm.tensors = {"gate": gate, "gain": gain, "bias": bias}
+    return norm
+
+
+def make_rope_shape(B, Hq, Hk, d, T=1, rot=0, pairs=0, q_stride=0, k_stride=0, q_out_stride=0, k_out_stride=0) -> RopeShape:
+    """``rot``: channels of a head that turn (0: all); ``pairs``: 0 halves, 1 neighbours."""
+    return RopeShape(int(B), int(Hq), int(Hk), int(d), int(T), int(rot), int(pairs), int(q_stride), int(k_stride),
+                     int(q_out_stride), int(k_out_stride))
+
+
+# The arguments after the shape: rows (bf16, named by their stride in the shape), "decay", "norm" (NormGate or None), "state", "freq" (fp64
+# [rot / 2]), host int32 arrays [B] or None ("slots", "pos": read at every run; "lens": copied), "workspace" bytes.
+_TOKEN_ARGS = {
+    "yoco_gret_step": ("q", "k", "v", "decay", "norm", "state", "slots", "slots", "o"),
+    "yoco_gret_chunk": ("q", "k", "v", "decay", "norm", "state", "slots", "slots", "lens", "o", "workspace"),
+    "yoco_head_norm": ("x", "norm", "y"),
+    "yoco_rope": ("q", "k", "freq", "pos", "lens", "q_out", "k_out"),
+}
+
+
+def _rows_lie(a, width: int, apart: int) -> bool:
+    """Whether the tensor's strides are those of rows of ``width`` elements, ``apart`` from one another (a tensor without
+    a dimension for the rows lies as the caller says)."""
+    n, i = 1, a.dim()
+    while i > 0 and n < width:                     # the dimensions of one row, densely
+        i -= 1
+        if a.shape[i] != 1 and a.stride(i) != n:
+            return False
+        n *= a.shape[i]
+    for j in reversed(range(i)):
+        if a.shape[j] != 1 and a.stride(j) != apart:
+            return False
+        apart *= a.shape[j]
+    return True
+
+
+class PreparedTokensCall:
+    """A call over token-major rows whose arguments are checked and marshalled once; run() only enqueues, on ``stream`` or, without
+    one, on the stream that is current then.  The tensors are kept alive; shape and lengths are copied.  Slots and positions, if contiguous
+    int32 arrays, are read at every run(), so a serving loop may change them in place."""
+
+    def __init__(self, fn_name, shape, *args, stream=None):
+        import torch
+        kinds = _TOKEN_ARGS[fn_name]
+        if len(args) != len(kinds):
+            raise TypeError(f"{fn_name} takes {len(kinds)} arguments after the shape, got {len(args)}")
+        shape = type(shape).from_buffer_copy(shape)
+        device = torch.cuda.current_device()
+        self._keep, out = [shape, stream], [ctypes.addressof(shape)]
+        lens = args[kinds.index("lens")] if "lens" in kinds else None
+        if lens is not None:
+            lens = np.array(lens, dtype=np.int32)
+            if lens.size < shape.B:
+                raise ValueError(f"{fn_name}: {lens.size} lengths for {shape.B} sequences")
+        if fn_name == "yoco_head_norm":
+            tokens = shape.tokens
+        elif "lens" in kinds:
+            tokens = shape.B * shape.T if lens is None else int(lens[:shape.B].sum(dtype=np.int64))
+        else:
+            tokens = shape.B
+        rope = fn_name == "yoco_rope"
+
+        def device_tensor(name, a, dtype, elements, width=0, apart=0):
+            if not a.is_cuda or a.device.index != device:
+                raise ValueError(f"{fn_name}: {name} is on {a.device}, the current device is cuda:{device}")
+            if dtype is not None and a.dtype != dtype:
+                raise ValueError(f"{fn_name}: {name} has type {a.dtype}, not {dtype}")
+            if a.numel() and not (_rows_lie(a, width, apart) if width else a.is_contiguous()):
+                raise ValueError(f"{fn_name}: {name} has strides {a.stride()}, which are not those of the call")
+            have = a.untyped_storage().nbytes() // a.element_size() - a.storage_offset()
+            if have < elements:
+                raise ValueError(f"{fn_name}: {name} holds {have} elements, the call needs {elements}")
+            self._keep.append(a)
+
+        def rows(name, a, width, stride, dtype=torch.bfloat16):
+            apart = stride or width
+            device_tensor(name, a, dtype, (tokens - 1) * apart + width if tokens > 0 else 0, width, apart)
+
+        for kind, a in zip(kinds, args):
+            if kind in ("slots", "pos", "lens"):
+                keep = lens if kind == "lens" else _host_i32(a)[0]
+                if keep is not None and keep.size < shape.B:
+                    raise ValueError(f"{fn_name}: a host array has {keep.size} entries for {shape.B} sequences")
+                self._keep.append(keep)
+                out.append(None if keep is None else keep.ctypes.data)
+                continue
+            if kind == "norm":
+                norm = None if a is None else NormGate.from_buffer_copy(a)
+                if norm is not None:
+                    for name, t in getattr(a, "tensors", {}).items():
+                        if t is not None and name == "gate":
+                            rows(name, t, shape.H * shape.d, norm.gate_stride)
+                        elif t is not None:
+                            device_tensor(name, t, torch.bfloat16, shape.H * shape.d)
+                self._keep.append(norm)
+                out.append(None if norm is None else ctypes.addressof(norm))
+                continue
+            if a is None:
+                if not (kind == "workspace" or (rope and kind in ("k", "k_out") and shape.Hk == 0)):
+                    raise ValueError(f"{fn_name}: {kind} is missing")
+                out += [None, 0] if kind == "workspace" else [None]
+                continue
+            if kind == "decay":
+                rows(kind, a, shape.H, shape.decay_stride, torch.bfloat16 if shape.decay_bf16 else torch.float32)
+            elif kind == "state":
+                device_tensor(kind, a, torch.float32, shape.num_slots * shape.H * shape.d * shape.d)
+            elif kind == "freq":
+                device_tensor(kind, a, torch.float64, (shape.rot or shape.d) // 2)
+            elif kind == "workspace":
+                device_tensor(kind, a, None, 0)
+            else:
+                heads = (shape.Hk if kind in ("k", "k_out") else shape.Hq) if rope else shape.H
+                rows(kind, a, heads * shape.d, getattr(shape, kind + "_stride"))
+            out.append(a.data_ptr())
+            if kind == "workspace":
+                out.append(a.numel() * a.element_size())
+        self._stream = None if stream is None else stream.cuda_stream
+        self._current_stream, self._device = torch._C._cuda_getCurrentRawStream, device
+        self._others = torch.cuda.device_count() > 1
+        proto = ctypes.CFUNCTYPE(ctypes.c_int32, *[ctypes.c_void_p] * (len(out) + 1))
+        self._name, self._fn, self._args = fn_name, proto((fn_name, lib())), tuple(out)
+
+    def run(self) -> None:
+        if self._others:
+            import torch
+            if torch.cuda.current_device() != self._device:
+                raise ValueError(f"{self._name}: prepared for cuda:{self._device}, the current device is cuda:{torch.cuda.current_device()}")
+        stream = self._stream
+        rc = self._fn(*self._args, self._current_stream(self._device) if stream is None else stream)
+        if rc != OK:
+            raise YocoError(rc, self._name)
+
+
+def prepare_tokens(fn_name, shape, *args, stream=None) -> PreparedTokensCall:
+    """``fn_name(shape, *args)`` with its arguments marshalled once; call .run() to enqueue it."""
+    return PreparedTokensCall(fn_name, shape, *args, stream=stream)
+
+
+def yoco_gret_workspace_size(shape: GretShape, lens=None, sm_count: int = 0) -> int:
+    """Workspace bytes of yoco_gret_chunk for exactly these lengths (None: shape.T each); may be 0."""
+    keep, p_len = _host_i32(lens)
+    out = ctypes.c_size_t(0)
+    rc = lib().yoco_gret_workspace_size(ctypes.byref(shape), p_len, sm_count, ctypes.byref(out))
+    if rc != OK:
+        raise YocoError(rc, "yoco_gret_workspace_size")
+    return int(out.value)
+
+
+def yoco_gret_chunk(shape: GretShape, Q, K, V, decay, norm, state, slot_in, slot_out, lens, O, workspace=None, stream=None) -> None:
+    """Enqueue gated retention over whole prompts or chunks of them: ``lens`` [B] tokens (None: shape.T each), states from slots
+    ``slot_in`` (-1: zero) into slots ``slot_out`` (-1: not kept; None: slot i of sequence i)."""
+    prepare_tokens("yoco_gret_chunk", shape, Q, K, V, decay, norm, state, slot_in, slot_out, lens, O, workspace, stream=stream).run()
+
+
+def yoco_gret_step(shape: GretShape, Q, K, V, decay, norm, state, slot_in, slot_out, O, stream=None) -> None:
+    """The same for one token of every sequence."""
+    prepare_tokens("yoco_gret_step", shape, Q, K, V, decay, norm, state, slot_in, slot_out, O, stream=stream).run()
+
+
+def yoco_head_norm(shape: HeadNormShape, X, norm: NormGate, Y, stream=None) -> None:
+    """Normalise every head's channels, gain, bias, swish gate; Y may be X."""
+    prepare_tokens("yoco_head_norm", shape, X, norm, Y, stream=stream).run()
+
+
+def yoco_rope(shape: RopeShape, Q, K, inv_freq, pos, lens, Q_rot, K_rot, stream=None) -> None:
+    """Turn queries and keys (None with Hk = 0) by the angles of their positions pos[i], pos[i] + 1, ..."""
+    prepare_tokens("yoco_rope", shape, Q, K, inv_freq, pos, lens, Q_rot, K_rot, stream=stream).run()
 
 
 def yoco_xattn_profile_enable(max_records: int) -> None:

@@ -10,6 +10,8 @@
 #include <memory>
 #include <mutex>
 #include <new>
+#include <utility>
+#include <vector>
 
 #include "kernels.h"
 #include "plan.h"
@@ -682,6 +684,116 @@ int32_t paged_rows(const yoco_paged_append_shape* shape, const yoco_paged_layout
     });
 }
 
+// ---- self-decoder: gated retention, head norm, rotation ---------------------------------------------
+// Rows of `width` elements, `stride` (0: width) apart.
+int32_t check_rows(const void* ptr, int64_t* stride, int64_t width) {
+    if (*stride == 0) *stride = width;
+    if (*stride < width || !aligned(ptr, 16)) return YOCO_ERR_INVALID_ARG;
+    return *stride % 8 == 0 ? YOCO_OK : YOCO_ERR_UNSUPPORTED;
+}
+
+int32_t check_norm(const yoco_norm_gate* norm, int64_t width, NormGate* out) {
+    *out = NormGate{};
+    if (!norm) return YOCO_OK;
+    if (!(norm->eps >= 0.f) || !std::isfinite(norm->eps) || (norm->rms & ~1) || norm->gate_stride < 0) return YOCO_ERR_INVALID_ARG;
+    int64_t stride = norm->gate_stride;
+    const int32_t rc = check_rows(norm->gate, &stride, width);
+    if (rc != YOCO_OK) return rc;
+    if (!aligned(norm->gain, 16) || !aligned(norm->bias, 16)) return YOCO_ERR_INVALID_ARG;
+    *out = NormGate{static_cast<const __nv_bfloat16*>(norm->gate), static_cast<const __nv_bfloat16*>(norm->gain),
+                    static_cast<const __nv_bfloat16*>(norm->bias), stride, norm->eps, norm->rms, 1};
+    return YOCO_OK;
+}
+
+// Tokens of every sequence; *tokens: their sum.
+int32_t check_lengths(int32_t B, const int32_t* len_host, int32_t T, int64_t* tokens) {
+    if (!len_host && T < 0) return YOCO_ERR_INVALID_ARG;
+    *tokens = 0;
+    for (int32_t i = 0; i < B; ++i) {
+        const int64_t n = len_host ? len_host[i] : T;
+        if (n < 0) return YOCO_ERR_INVALID_ARG;
+        *tokens += n;
+    }
+    return *tokens > kMaxPagedLen ? YOCO_ERR_UNSUPPORTED : YOCO_OK;
+}
+
+int32_t check_gret_shape(const yoco_gret_shape& s) {
+    if (s.B < 0 || s.H <= 0 || s.d <= 0 || !(s.scale >= 0.f) || !std::isfinite(s.scale) || !(s.tau >= 0.f) || !std::isfinite(s.tau) ||
+        (s.decay_bf16 & ~1) || s.q_stride < 0 || s.k_stride < 0 || s.v_stride < 0 || s.o_stride < 0 || s.decay_stride < 0)
+        return YOCO_ERR_INVALID_ARG;
+    return (s.d == 64 || s.d == 128) && s.H <= 65535 && s.B <= kAppendMaxSequences ? YOCO_OK : YOCO_ERR_UNSUPPORTED;
+}
+
+// Slots of the states: in range, none written twice, none written that another sequence reads.
+int32_t check_slots(const yoco_gret_shape& s, const int32_t* in, const int32_t* out, GretTable* tab) {
+    if (s.num_slots <= 0) return YOCO_ERR_INVALID_ARG;
+    std::vector<std::pair<int32_t, int32_t>> written;      // (slot, sequence)
+    written.reserve(s.B);
+    for (int32_t i = 0; i < s.B; ++i) {
+        tab->from[i] = in ? in[i] : i;
+        tab->to[i] = out ? out[i] : i;
+        if (tab->from[i] < -1 || tab->from[i] >= s.num_slots || tab->to[i] < -1 || tab->to[i] >= s.num_slots) return YOCO_ERR_INVALID_ARG;
+        if (tab->to[i] >= 0) written.emplace_back(tab->to[i], i);
+    }
+    std::sort(written.begin(), written.end());
+    for (size_t j = 1; j < written.size(); ++j)
+        if (written[j].first == written[j - 1].first) return YOCO_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < s.B; ++i) {
+        if (tab->from[i] < 0) continue;
+        const auto it = std::lower_bound(written.begin(), written.end(), std::make_pair(tab->from[i], INT32_MIN));
+        if (it != written.end() && it->first == tab->from[i] && it->second != i) return YOCO_ERR_INVALID_ARG;
+    }
+    return YOCO_OK;
+}
+
+int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay, const yoco_norm_gate* norm,
+             float* state, const int32_t* slot_in_host, const int32_t* slot_out_host, const int32_t* len_host, bool step, void* O,
+             void* workspace, size_t workspace_bytes, void* stream) {
+    return no_throw([&]() -> int32_t {
+        if (!shape) return YOCO_ERR_INVALID_ARG;
+        const yoco_gret_shape& s = *shape;
+        int32_t rc = check_gret_shape(s);
+        if (rc != YOCO_OK) return rc;
+        if (s.B == 0) return YOCO_OK;
+        const int64_t width = (int64_t)s.H * s.d;
+        GretParams p{};
+        int64_t tokens = 0;
+        if ((rc = check_lengths(s.B, len_host, step ? 1 : s.T, &tokens)) != YOCO_OK) return rc;
+        p.q_stride = s.q_stride;
+        p.k_stride = s.k_stride;
+        p.v_stride = s.v_stride;
+        p.o_stride = s.o_stride;
+        p.decay_stride = s.decay_stride ? s.decay_stride : s.H;
+        if ((rc = check_rows(Q, &p.q_stride, width)) != YOCO_OK || (rc = check_rows(K, &p.k_stride, width)) != YOCO_OK ||
+            (rc = check_rows(V, &p.v_stride, width)) != YOCO_OK || (rc = check_rows(O, &p.o_stride, width)) != YOCO_OK ||
+            (rc = check_norm(norm, width, &p.norm)) != YOCO_OK)
+            return rc;
+        if (p.decay_stride < s.H || !aligned(decay, s.decay_bf16 ? 2 : 4) || !state || !aligned(state, 16)) return YOCO_ERR_INVALID_ARG;
+        if (tokens > 0 && (!Q || !K || !V || !decay || !O)) return YOCO_ERR_INVALID_ARG;   // (an empty tensor's address may be null)
+        GretTable tab;
+        std::memset(&tab, 0, sizeof tab);
+        if ((rc = check_slots(s, slot_in_host, slot_out_host, &tab)) != YOCO_OK) return rc;
+        for (int32_t i = 0; i < s.B; ++i) tab.tok0[i + 1] = tab.tok0[i] + (len_host ? len_host[i] : step ? 1 : s.T);
+        for (int32_t i = s.B; i < kAppendMaxSequences; ++i) tab.tok0[i + 1] = tab.tok0[i];
+        DeviceState* dev = nullptr;
+        if ((rc = device_state(&dev)) != YOCO_OK) return rc;
+        p.q = static_cast<const __nv_bfloat16*>(Q);
+        p.k = static_cast<const __nv_bfloat16*>(K);
+        p.v = static_cast<const __nv_bfloat16*>(V);
+        p.o = static_cast<__nv_bfloat16*>(O);
+        p.decay = decay;
+        p.state = state;
+        p.scale = s.scale > 0.f ? s.scale : 1.f / std::sqrt((float)s.d);
+        p.tau = s.tau;
+        p.decay_bf16 = s.decay_bf16;
+        p.B = s.B;
+        p.H = s.H;
+        p.d = s.d;
+        YOCO_CUDA_TRY(launch_gret_tokens(p, tab, reinterpret_cast<cudaStream_t>(stream)));
+        return YOCO_OK;
+    });
+}
+
 }  // namespace
 }  // namespace yoco
 
@@ -1123,6 +1235,111 @@ int32_t yoco_rope_q(const yoco_xattn_shape* shape, const yoco_paged_layout* layo
         if ((rc = device_state(&dev)) != YOCO_OK) return rc;
         YOCO_CUDA_TRY(launch_rope_q(static_cast<const __nv_bfloat16*>(Q), static_cast<__nv_bfloat16*>(Q_rot), shape->B,
                                     shape->Hq, shape->T, shape->d, rot, tab, reinterpret_cast<cudaStream_t>(stream)));
+        return YOCO_OK;
+    });
+}
+
+int32_t yoco_gret_step(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay,
+                       const yoco_norm_gate* norm, float* state, const int32_t* slot_in_host, const int32_t* slot_out_host,
+                       void* O, void* stream) {
+    return gret(shape, Q, K, V, decay, norm, state, slot_in_host, slot_out_host, nullptr, true, O, nullptr, 0, stream);
+}
+
+int32_t yoco_gret_chunk(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay,
+                        const yoco_norm_gate* norm, float* state, const int32_t* slot_in_host, const int32_t* slot_out_host,
+                        const int32_t* len_host, void* O, void* workspace, size_t workspace_bytes, void* stream) {
+    return gret(shape, Q, K, V, decay, norm, state, slot_in_host, slot_out_host, len_host, false, O, workspace, workspace_bytes, stream);
+}
+
+int32_t yoco_gret_workspace_size(const yoco_gret_shape* shape, const int32_t* len_host, int32_t sm_count, size_t* bytes) {
+    return no_throw([&]() -> int32_t {
+        if (!shape || !bytes) return YOCO_ERR_INVALID_ARG;
+        int64_t tokens = 0;
+        int32_t rc = check_gret_shape(*shape);
+        if (rc != YOCO_OK || (rc = check_lengths(shape->B, len_host, shape->T, &tokens)) != YOCO_OK) return rc;
+        *bytes = 0;
+        return YOCO_OK;
+    });
+}
+
+int32_t yoco_head_norm(const yoco_head_norm_shape* shape, const void* X, const yoco_norm_gate* norm, void* Y, void* stream) {
+    if (!shape || !norm) return YOCO_ERR_INVALID_ARG;
+    const yoco_head_norm_shape& s = *shape;
+    if (s.tokens < 0 || s.H <= 0 || s.d <= 0 || s.x_stride < 0 || s.y_stride < 0) return YOCO_ERR_INVALID_ARG;
+    if (s.d % 8 != 0 || s.d > 1024 || s.tokens > INT32_MAX / s.H) return YOCO_ERR_UNSUPPORTED;
+    const int64_t width = (int64_t)s.H * s.d;
+    HeadNormParams p{};
+    p.x_stride = s.x_stride;
+    p.y_stride = s.y_stride;
+    int32_t rc;
+    if ((rc = check_rows(X, &p.x_stride, width)) != YOCO_OK || (rc = check_rows(Y, &p.y_stride, width)) != YOCO_OK ||
+        (rc = check_norm(norm, width, &p.norm)) != YOCO_OK)
+        return rc;
+    if (s.tokens == 0) return YOCO_OK;
+    if (!X || !Y) return YOCO_ERR_INVALID_ARG;
+    DeviceState* dev = nullptr;
+    if ((rc = device_state(&dev)) != YOCO_OK) return rc;
+    p.x = static_cast<const __nv_bfloat16*>(X);
+    p.y = static_cast<__nv_bfloat16*>(Y);
+    p.groups = (int32_t)(s.tokens * s.H);
+    p.H = s.H;
+    p.d = s.d;
+    YOCO_CUDA_TRY(launch_head_norm(p, reinterpret_cast<cudaStream_t>(stream)));
+    return YOCO_OK;
+}
+
+int32_t yoco_rope(const yoco_rope_shape* shape, const void* Q, const void* K, const double* inv_freq, const int32_t* pos_host,
+                  const int32_t* len_host, void* Q_rot, void* K_rot, void* stream) {
+    return no_throw([&]() -> int32_t {
+        if (!shape) return YOCO_ERR_INVALID_ARG;
+        const yoco_rope_shape& s = *shape;
+        if (s.B < 0 || s.Hq <= 0 || s.Hk < 0 || s.d <= 0 || s.rot < 0 || s.rot > s.d || (s.rope_pairs & ~1) || s.q_stride < 0 ||
+            s.k_stride < 0 || s.q_out_stride < 0 || s.k_out_stride < 0)
+            return YOCO_ERR_INVALID_ARG;
+        if (s.d % 16 != 0 || s.d > 512 || s.rot % 16 != 0 || s.B > kAppendMaxSequences || (int64_t)s.Hq + s.Hk > 65535)
+            return YOCO_ERR_UNSUPPORTED;
+        int64_t tokens = 0;
+        int32_t rc = check_lengths(s.B, len_host, s.T, &tokens);
+        if (rc != YOCO_OK) return rc;
+        if (s.B == 0) return YOCO_OK;
+        if (!pos_host || !inv_freq || !aligned(inv_freq, 8)) return YOCO_ERR_INVALID_ARG;
+        for (int32_t i = 0; i < s.B; ++i)
+            if (pos_host[i] < 0 || (int64_t)pos_host[i] + (len_host ? len_host[i] : s.T) > (1ll << 31)) return YOCO_ERR_INVALID_ARG;
+        RopeParams p{};
+        p.q_stride = s.q_stride;
+        p.k_stride = s.k_stride;
+        p.q_out_stride = s.q_out_stride;
+        p.k_out_stride = s.k_out_stride;
+        const int64_t wq = (int64_t)s.Hq * s.d, wk = (int64_t)s.Hk * s.d;
+        if ((rc = check_rows(Q, &p.q_stride, wq)) != YOCO_OK || (rc = check_rows(Q_rot, &p.q_out_stride, wq)) != YOCO_OK) return rc;
+        if (s.Hk > 0 && ((rc = check_rows(K, &p.k_stride, wk)) != YOCO_OK || (rc = check_rows(K_rot, &p.k_out_stride, wk)) != YOCO_OK))
+            return rc;
+        if (tokens == 0) return YOCO_OK;
+        if (!Q || !Q_rot || (s.Hk > 0 && (!K || !K_rot))) return YOCO_ERR_INVALID_ARG;
+        SeqTable tab;
+        std::memset(&tab, 0, sizeof tab);
+        p.tokens_per_seq = len_host ? len_host[0] : s.T;
+        for (int32_t i = 0; i < s.B; ++i) {
+            const int32_t n = len_host ? len_host[i] : s.T;
+            tab.pos0[i] = pos_host[i];
+            tab.tok0[i + 1] = tab.tok0[i] + n;
+            if (n != p.tokens_per_seq) p.tokens_per_seq = 0;
+        }
+        DeviceState* dev = nullptr;
+        if ((rc = device_state(&dev)) != YOCO_OK) return rc;
+        p.q = static_cast<const __nv_bfloat16*>(Q);
+        p.k = static_cast<const __nv_bfloat16*>(K);
+        p.q_out = static_cast<__nv_bfloat16*>(Q_rot);
+        p.k_out = static_cast<__nv_bfloat16*>(K_rot);
+        p.inv_freq = inv_freq;
+        p.B = s.B;
+        p.Hq = s.Hq;
+        p.Hk = s.Hk;
+        p.d = s.d;
+        p.rot = s.rot ? s.rot : s.d;
+        p.neighbours = s.rope_pairs;
+        p.tokens = (int32_t)tokens;
+        YOCO_CUDA_TRY(launch_rope(p, tab, dev->sm_count, reinterpret_cast<cudaStream_t>(stream)));
         return YOCO_OK;
     });
 }

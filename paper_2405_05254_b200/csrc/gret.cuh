@@ -1,0 +1,41 @@
+// What the gated-retention kernels share: decays, and the normalisation and gate of a head's output.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "kernels.h"
+#include "ptx.cuh"
+#include "rows.cuh"
+
+namespace yoco {
+
+// Natural logarithm of the decay of (token, head), not below kMinLogDecay; a NaN stays one.
+__device__ __forceinline__ float log_decay(const GretParams& p, int64_t tok, int h) {
+    const int64_t at = tok * p.decay_stride + h;
+    float z = p.decay_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.decay)[at]) : static_cast<const float*>(p.decay)[at];
+    if (p.tau > 0.f) z = (fminf(z, 0.f) - log1pf(expf(-fabsf(z)))) / p.tau;        // log sigmoid(z) / tau, without overflow on either side
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(z), "f"(kMinLogDecay));
+    return r;
+}
+
+__device__ __forceinline__ float swish(float u) { return u / (1.f + __expf(-u)); }
+
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) x += __shfl_xor_sync(0xffffffffu, x, m);
+    return x;
+}
+
+// calls of few sequences take a table of their size (see with_table)
+template <class F>
+void with_gret_table(const GretTable& tab, int B, F launch) {
+    if (B > kFewSequences) return launch(tab);
+    GretTableOf<kFewSequences> few;
+    std::memcpy(few.from, tab.from, sizeof few.from);
+    std::memcpy(few.to, tab.to, sizeof few.to);
+    std::memcpy(few.tok0, tab.tok0, sizeof few.tok0);
+    launch(few);
+}
+
+}  // namespace yoco

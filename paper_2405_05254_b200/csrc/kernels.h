@@ -253,4 +253,61 @@ cudaError_t launch_paged_gather(const PagedRowsParams& p, const SeqTable& tab, b
 cudaError_t launch_rope_q(const __nv_bfloat16* Q, __nv_bfloat16* Qr, int32_t B, int32_t Hq, int32_t T, int32_t d,
                           const Rotation& rot, const SeqTable& tab, cudaStream_t stream);
 
+// ---- token-major rows: rotation by computed angles, normalisation of the heads with a gate -----------
+struct RopeParams {
+    const __nv_bfloat16* q;     // rows q_stride elements apart, Hq heads of d channels
+    const __nv_bfloat16* k;     // null: none
+    __nv_bfloat16* q_out;
+    __nv_bfloat16* k_out;
+    int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+    const double* inv_freq;     // [rot / 2]
+    int32_t B, Hq, Hk, d, rot, neighbours, tokens;
+    int32_t tokens_per_seq;     // > 0: every sequence has so many; 0: see SeqTable::tok0
+};
+cudaError_t launch_rope(const RopeParams& p, const SeqTable& tab, int sm_count, cudaStream_t stream);
+
+struct NormGate {               // y = swish(gate) * (normalised x * gain + bias); see yoco_norm_gate
+    const __nv_bfloat16* gate;  // null: none; heads consecutive, gate_stride elements between tokens
+    const __nv_bfloat16* gain;  // null: ones
+    const __nv_bfloat16* bias;  // null: zeros
+    int64_t gate_stride;
+    float eps;
+    int32_t rms;                // 0: mean and variance, 1: root mean square
+    int32_t on;                 // 0: x as it is
+};
+struct HeadNormParams {
+    const __nv_bfloat16* x;
+    __nv_bfloat16* y;
+    int64_t x_stride, y_stride;
+    NormGate norm;
+    int32_t groups;             // tokens * H
+    int32_t H, d;
+};
+cudaError_t launch_head_norm(const HeadNormParams& p, cudaStream_t stream);
+
+// ---- gated retention -----------------------------------------------------------------------------------
+constexpr float kMinLogDecay = -110.f;      // e^-110 is 0 in fp32
+struct GretParams {
+    const __nv_bfloat16* q;     // token-major rows, heads consecutive
+    const __nv_bfloat16* k;
+    const __nv_bfloat16* v;
+    const void* decay;          // [tokens, H] fp32 or bf16
+    __nv_bfloat16* o;
+    float* state;               // [slots, H, d, d]
+    int64_t q_stride, k_stride, v_stride, o_stride, decay_stride;
+    NormGate norm;
+    float scale;
+    float tau;                  // 0: decay holds natural logarithms
+    int32_t decay_bf16;
+    int32_t B, H, d;
+};
+template <int N>
+struct GretTableOf {            // per sequence, as kernel parameters
+    int32_t from[N], to[N];     // slots, -1: zero state / not kept
+    int32_t tok0[N + 1];        // first token among all tokens of the call
+};
+using GretTable = GretTableOf<kAppendMaxSequences>;
+// One CTA per (sequence, head) walks its tokens with the state in registers.
+cudaError_t launch_gret_tokens(const GretParams& p, const GretTable& tab, cudaStream_t stream);
+
 }  // namespace yoco

@@ -14,12 +14,11 @@
 // read while they are in flight, and nothing is kept in shared memory.  What bounds them at size is instructions, then
 // memory: so a block works on one head (no division to find it), and rounding and conversion of 4-bit codes go through
 // additions to a large constant instead of the conversion instructions, which run at a quarter of the rate.
-#include <cstring>
-
 #include "kernels.h"
 #include "page_map.cuh"
 #include "ptx.cuh"
 #include "q4.cuh"
+#include "rows.cuh"
 
 namespace yoco {
 
@@ -27,35 +26,6 @@ namespace {
 
 constexpr int kRowThreads = 128;
 
-// which sequence a token belongs to, and its number inside it
-template <class Table>
-__device__ __forceinline__ int find_sequence(const Table& tab, int B, int per_seq, int tok) {
-    if (per_seq > 0) return tok / per_seq;
-    int lo = 0, hi = B - 1;                        // last i with tok0[i] <= tok (empty sequences are passed over)
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (tab.tok0[mid] <= tok) lo = mid; else hi = mid - 1;
-    }
-    return lo;
-}
-
-__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-}
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-    return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-}
-
-__device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
-    const float y1 = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s));
-    b = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
-    a = y1;
-}
 // The two chunks of a row that thread i of d / 16 holds: channels 8 i .. 8 i + 7 (lo) and d / 2 + 8 i .. (hi).  Their
 // angles at a position: halves turn together, pair j is (lo[j], hi[j]); neighbours do, pairs 0 .. 3 lie in lo, 4 .. 7 in hi.
 struct Angles {
@@ -319,19 +289,6 @@ dim3 rows_grid(const PagedRowsParams& p, int per_row, int blocks_per_sm, int* he
     *heads = 1;
     while (*heads < p.pages.Hkv && (int64_t)blocks * ((p.pages.Hkv + 2 * *heads - 1) / (2 * *heads)) >= 148 * blocks_per_sm) *heads *= 2;
     return dim3(blocks, (unsigned)((p.pages.Hkv + *heads - 1) / *heads));
-}
-
-// Calls of few sequences take a table of their size: 4 KB of parameters are written for every launch.
-// (Measured, 64 sequences of one token: 20 calls after a synchronisation 8.6 -> 6.4 us each, rows of hundreds 3.9 either way; the
-// kernels themselves take 1.6 us.)
-constexpr int kFewSequences = 64;
-template <class F>
-void with_table(const SeqTable& tab, int B, F launch) {
-    if (B > kFewSequences) return launch(tab);
-    SeqTableOf<kFewSequences> few;
-    std::memcpy(few.pos0, tab.pos0, sizeof few.pos0);
-    std::memcpy(few.tok0, tab.tok0, sizeof few.tok0);
-    launch(few);
 }
 
 }  // namespace
