@@ -64,6 +64,7 @@ int32_t device_state(DeviceState** out) {
         YOCO_CUDA_TRY(kv_append_kernel_setup());
         YOCO_CUDA_TRY(decode_fp8_kernel_setup());
         YOCO_CUDA_TRY(decode_q4_kernel_setup());
+        YOCO_CUDA_TRY(gret_chunk_kernel_setup());
         YOCO_CUDA_TRY(kv_append_status_address(&st.append_status));
         st.ready = true;
     }
@@ -180,11 +181,11 @@ int32_t get_encoder(EncodeTiledFn* fn) {
 // encoded maps are kept per host thread, keyed by everything that goes into the encoding.
 struct MapKey {
     const void* base;
-    int64_t rows;
+    int64_t rows, stride;
     int32_t row_bytes, box_rows, box_bytes, bf16;
     CUtensorMapSwizzle swizzle;
     bool operator==(const MapKey& o) const {
-        return base == o.base && rows == o.rows && row_bytes == o.row_bytes && box_rows == o.box_rows &&
+        return base == o.base && rows == o.rows && stride == o.stride && row_bytes == o.row_bytes && box_rows == o.box_rows &&
                box_bytes == o.box_bytes && bf16 == o.bf16 && swizzle == o.swizzle;
     }
 };
@@ -210,18 +211,19 @@ struct MapCache {
 };
 thread_local MapCache g_maps;
 
-// 2-D map over a row-major matrix of `rows` rows of row_bytes bytes, as bf16 or bytes; box {box_bytes, box_rows},
-// swizzled by the box's width (128 or 64 bytes) or not at all.
+// 2-D map over a row-major matrix of `rows` rows of row_bytes bytes, stride bytes apart (0: row_bytes), as bf16 or bytes; box
+// {box_bytes, box_rows}, swizzled by the box's width (128 or 64 bytes) or not at all.
 int32_t make_map(CUtensorMap* map, const void* base, int64_t rows, int32_t row_bytes, int32_t box_bytes,
-                 int32_t box_rows, bool bf16, CUtensorMapSwizzle swizzle) {
-    const MapKey mk{base, rows, row_bytes, box_rows, box_bytes, bf16 ? 1 : 0, swizzle};
+                 int32_t box_rows, bool bf16, CUtensorMapSwizzle swizzle, int64_t stride = 0) {
+    if (stride == 0) stride = row_bytes;
+    const MapKey mk{base, rows, stride, row_bytes, box_rows, box_bytes, bf16 ? 1 : 0, swizzle};
     if (g_maps.find(mk, map)) return YOCO_OK;
     EncodeTiledFn enc;
     int32_t rc = get_encoder(&enc);
     if (rc != YOCO_OK) return rc;
     const int32_t elem = bf16 ? 2 : 1;
     cuuint64_t gdim[2] = {(cuuint64_t)(row_bytes / elem), (cuuint64_t)rows};
-    cuuint64_t gstride[1] = {(cuuint64_t)row_bytes};
+    cuuint64_t gstride[1] = {(cuuint64_t)stride};
     cuuint32_t box[2] = {(cuuint32_t)(box_bytes / elem), (cuuint32_t)box_rows};
     cuuint32_t estr[2] = {1u, 1u};
     CUresult r = enc(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2,
@@ -746,6 +748,53 @@ int32_t check_slots(const yoco_gret_shape& s, const int32_t* in, const int32_t* 
     return YOCO_OK;
 }
 
+// Sequences of no more tokens than this walk them one by one (one CTA per head, state in registers); longer ones in chunks.
+constexpr int32_t kGretTokens = 16;
+// What a chunk costs in the state-only pass over split streams, and the extra launches, in chunks of the main pass.
+constexpr double kGretStateCost = 0.55, kGretSplitCost = 3.0;
+
+struct GretPlan {
+    GretChunkTable tab;
+    int32_t seqs;               // sequences in tab
+    int64_t total;              // chunks of all heads
+    int32_t groups, split;
+    size_t part_bytes;          // workspace: parts' states, then their decays
+    size_t bytes() const { return split ? part_bytes + (size_t)(groups + 1) * sizeof(float) : 0; }
+};
+
+// Whole streams, one per CTA (longest first), or equal ranges of chunks that cut streams: the latter pay a second pass over K and V.
+void plan_gret(const yoco_gret_shape& s, const int32_t* len_host, const GretTable* slots, int32_t sm_count, GretPlan* out) {
+    std::memset(&out->tab, 0, sizeof out->tab);
+    std::vector<std::pair<int32_t, int32_t>> order;        // (-length, sequence)
+    std::vector<int32_t> tok0(s.B + 1, 0);
+    for (int32_t i = 0; i < s.B; ++i) {
+        const int32_t n = len_host ? len_host[i] : s.T;
+        tok0[i + 1] = tok0[i] + n;
+        if (n > 0) order.emplace_back(-n, i);
+    }
+    std::stable_sort(order.begin(), order.end());
+    out->seqs = (int32_t)order.size();
+    for (int32_t j = 0; j < out->seqs; ++j) {
+        const int32_t i = order[j].second;
+        out->tab.tok0[j] = tok0[i];
+        out->tab.len[j] = -order[j].first;
+        out->tab.from[j] = slots ? slots->from[i] : -1;
+        out->tab.to[j] = slots ? slots->to[i] : -1;
+        out->tab.chunk0[j + 1] = out->tab.chunk0[j] + (out->tab.len[j] + kGretChunk - 1) / kGretChunk;
+    }
+    for (int32_t j = out->seqs; j < kAppendMaxSequences; ++j) out->tab.chunk0[j + 1] = out->tab.chunk0[out->seqs];
+    out->total = (int64_t)out->tab.chunk0[out->seqs] * s.H;
+    const int64_t streams = (int64_t)out->seqs * s.H;
+    // time of whole streams, dealt out longest first: no less than the longest one, and than an equal share in whole streams' steps
+    double whole = 0.0;
+    for (int64_t first = 0; first < streams; first += sm_count) whole += out->tab.chunk0[first / s.H + 1] - out->tab.chunk0[first / s.H];
+    const int64_t cut = std::min<int64_t>(out->total, sm_count);
+    const double share = cut > 0 ? (double)((out->total + cut - 1) / cut) : 0.0;
+    out->split = cut > 1 && share * (1.0 + kGretStateCost) + kGretSplitCost < whole;
+    out->groups = (int32_t)(out->split ? cut : streams);
+    out->part_bytes = (size_t)2 * out->groups * s.d * s.d * sizeof(float);
+}
+
 int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay, const yoco_norm_gate* norm,
              float* state, const int32_t* slot_in_host, const int32_t* slot_out_host, const int32_t* len_host, bool step, void* O,
              void* workspace, size_t workspace_bytes, void* stream) {
@@ -789,7 +838,47 @@ int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const v
         p.B = s.B;
         p.H = s.H;
         p.d = s.d;
-        YOCO_CUDA_TRY(launch_gret_tokens(p, tab, reinterpret_cast<cudaStream_t>(stream)));
+        cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+        int32_t longest = 0;
+        for (int32_t i = 0; i < s.B; ++i) longest = std::max(longest, tab.tok0[i + 1] - tab.tok0[i]);
+        if (longest <= kGretTokens) {
+            YOCO_CUDA_TRY(launch_gret_tokens(p, tab, st));
+            return YOCO_OK;
+        }
+        GretPlan plan;
+        plan_gret(s, len_host, &tab, dev->sm_count, &plan);
+        if (plan.bytes() > 0) {
+            if (!workspace || !aligned(workspace, 16)) return YOCO_ERR_INVALID_ARG;
+            if (workspace_bytes < plan.bytes()) return YOCO_ERR_WORKSPACE_TOO_SMALL;
+        }
+        CUtensorMap tmQ, tmK, tmV;
+        auto map = [&](CUtensorMap* m, const void* base, int64_t stride) {
+            return make_map(m, base, tokens, (int32_t)(width * 2), 128, kGretChunk, true, CU_TENSOR_MAP_SWIZZLE_128B, stride * 2);
+        };
+        if ((rc = map(&tmQ, Q, p.q_stride)) != YOCO_OK || (rc = map(&tmK, K, p.k_stride)) != YOCO_OK || (rc = map(&tmV, V, p.v_stride)) != YOCO_OK)
+            return rc;
+        GretChunkParams cp{};
+        cp.base = p;
+        cp.base.B = plan.seqs;
+        cp.total = plan.total;
+        cp.groups = plan.groups;
+        cp.split = plan.split;
+        cp.part = static_cast<float*>(workspace);
+        cp.part_keep = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + plan.part_bytes);
+        cp.status = dev->append_status;
+        if (plan.seqs < s.B) {           // sequences without tokens hand their states on
+            GretTable idle;
+            std::memset(&idle, 0, sizeof idle);
+            GretParams ip = p;
+            ip.B = 0;
+            for (int32_t i = 0; i < s.B; ++i) {
+                if (tab.tok0[i + 1] > tab.tok0[i] || tab.to[i] < 0 || tab.to[i] == tab.from[i]) continue;
+                idle.from[ip.B] = tab.from[i];
+                idle.to[ip.B++] = tab.to[i];
+            }
+            YOCO_CUDA_TRY(launch_gret_tokens(ip, idle, st));
+        }
+        YOCO_CUDA_TRY(launch_gret_chunk(cp, plan.tab, tmQ, tmK, tmV, st));
         return YOCO_OK;
     });
 }
@@ -1257,7 +1346,20 @@ int32_t yoco_gret_workspace_size(const yoco_gret_shape* shape, const int32_t* le
         int64_t tokens = 0;
         int32_t rc = check_gret_shape(*shape);
         if (rc != YOCO_OK || (rc = check_lengths(shape->B, len_host, shape->T, &tokens)) != YOCO_OK) return rc;
-        *bytes = 0;
+        int32_t longest = 0;
+        for (int32_t i = 0; i < shape->B; ++i) longest = std::max(longest, len_host ? len_host[i] : shape->T);
+        if (longest <= kGretTokens) {
+            *bytes = 0;
+            return YOCO_OK;
+        }
+        if (sm_count <= 0) {
+            DeviceState* dev = nullptr;
+            if ((rc = device_state(&dev)) != YOCO_OK) return rc;
+            sm_count = dev->sm_count;
+        }
+        GretPlan plan;
+        plan_gret(*shape, len_host, nullptr, sm_count, &plan);
+        *bytes = plan.bytes();
         return YOCO_OK;
     });
 }

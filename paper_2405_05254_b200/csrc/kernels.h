@@ -310,4 +310,27 @@ using GretTable = GretTableOf<kAppendMaxSequences>;
 // One CTA per (sequence, head) walks its tokens with the state in registers.
 cudaError_t launch_gret_tokens(const GretParams& p, const GretTable& tab, cudaStream_t stream);
 
+// The chunkwise form.  The flat space of (sequence, head, chunk), in that order, has `total` chunks.
+constexpr int kGretChunk = 128;     // tokens of a chunk
+template <int N>
+struct GretChunkTableOf {       // sequences with at least one token
+    int32_t from[N], to[N];
+    int32_t tok0[N], len[N];
+    int32_t chunk0[N + 1];      // chunks of the sequences before this one (of one head)
+};
+using GretChunkTable = GretChunkTableOf<kAppendMaxSequences>;
+struct GretChunkParams {
+    GretParams base;            // base.B: sequences of the table
+    int64_t total;
+    int32_t groups;             // CTAs
+    int32_t split;              // 1: CTA g walks chunks [g total / groups, (g + 1) total / groups); 0: one stream each
+    float* part;                // split: 2 * groups states
+    float* part_keep;           // split: decay over a CTA's last segment, groups + 1
+    int32_t* status;
+};
+// tmQ, tmK, tmV: bf16 maps over [tokens, H * d], box {64, kGretChunk}, 128-byte swizzle
+cudaError_t launch_gret_chunk(const GretChunkParams& p, const GretChunkTable& tab, const CUtensorMap& tmQ, const CUtensorMap& tmK,
+                              const CUtensorMap& tmV, cudaStream_t stream);
+cudaError_t gret_chunk_kernel_setup();
+
 }  // namespace yoco
