@@ -833,7 +833,7 @@ int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const v
         p.decay = decay;
         p.state = state;
         p.scale = s.scale > 0.f ? s.scale : 1.f / std::sqrt((float)s.d);
-        p.tau = s.tau;
+        p.inv_tau = s.tau > 0.f ? 1.f / s.tau : 0.f;
         p.decay_bf16 = s.decay_bf16;
         p.B = s.B;
         p.H = s.H;
@@ -847,6 +847,7 @@ int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const v
         }
         GretPlan plan;
         plan_gret(s, len_host, &tab, dev->sm_count, &plan);
+        if (plan.total > INT32_MAX) return YOCO_ERR_UNSUPPORTED;
         if (plan.bytes() > 0) {
             if (!workspace || !aligned(workspace, 16)) return YOCO_ERR_INVALID_ARG;
             if (workspace_bytes < plan.bytes()) return YOCO_ERR_WORKSPACE_TOO_SMALL;
@@ -860,9 +861,11 @@ int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const v
         GretChunkParams cp{};
         cp.base = p;
         cp.base.B = plan.seqs;
-        cp.total = plan.total;
+        cp.total = (int32_t)plan.total;
         cp.groups = plan.groups;
         cp.split = plan.split;
+        cp.share = cp.total / cp.groups;
+        cp.extra = cp.total % cp.groups;
         cp.part = static_cast<float*>(workspace);
         cp.part_keep = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + plan.part_bytes);
         cp.status = dev->append_status;

@@ -9,17 +9,19 @@
 
 namespace yoco {
 
-// Natural logarithm of the decay of (token, head), not below kMinLogDecay; a NaN stays one.
-__device__ __forceinline__ float log_decay(const GretParams& p, int64_t tok, int h) {
+__device__ __forceinline__ float read_decay(const GretParams& p, int64_t tok, int h) {
     const int64_t at = tok * p.decay_stride + h;
-    float z = p.decay_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.decay)[at]) : static_cast<const float*>(p.decay)[at];
-    if (p.tau > 0.f) z = (fminf(z, 0.f) - log1pf(expf(-fabsf(z)))) / p.tau;        // log sigmoid(z) / tau, without overflow on either side
+    return p.decay_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.decay)[at]) : static_cast<const float*>(p.decay)[at];
+}
+// Natural logarithm of the decay that z stands for, not below kMinLogDecay; a NaN stays one.
+__device__ __forceinline__ float log_decay(const GretParams& p, float z) {
+    if (p.inv_tau > 0.f) z = (fminf(z, 0.f) - log1pf(expf(-fabsf(z)))) * p.inv_tau;        // log sigmoid(z) / tau, without overflow on either side
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(z), "f"(kMinLogDecay));
     return r;
 }
 
-__device__ __forceinline__ float swish(float u) { return u / (1.f + __expf(-u)); }
+__device__ __forceinline__ float swish(float u) { return __fdividef(u, 1.f + __expf(-u)); }
 
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll

@@ -4,22 +4,23 @@
 //     P_ij = (q_i . k_j) 2^(b_i - b_j)  (j <= i),   o_i = scale (sum_j P_ij v_j + 2^b_i q_i S),
 //     S' = 2^b_C S + sum_j (2^(b_C - b_j) k_j)^T v_j.
 // A CTA walks a contiguous range of chunks, of one (sequence, head) stream or of several one after the other, with the state in the
-// registers of a warpgroup.  512 threads:
+// registers of two warpgroups.  768 threads:
 //   warp 0       TMA producer: K, Q, V tiles (128 tokens x d, 128-byte swizzle) through one ring
 //   warp 1       issuer of all products: Q K^T -> SC;  K'^T V -> DS;  Q S -> OI;  P V -> OA    (tensor memory, fp32)
-//   warp 2       decays: prefix sums of the logarithms in 64 bits, kept as integer part and rest (their differences are what
-//                is used: b_i - b_j stays exact to 2^-24 however strong the decays before j were)
-//   warpgroup 1  thread = token: P (bf16, over the scores' own columns: it goes to P V from tensor memory), then the chunk's output:
-//                scale, normalisation, gate, rounding, store
-//   warpgroup 2  thread = row of the state: S' from S and DS in fp32; S in bf16 to shared memory for the next chunk's Q S
-//   warpgroup 3  K' = 2^(b_C - b_j) k_j, in pieces of 16 tokens
+//   warp 2       decays: prefix sums of the logarithms in 64 bits, kept as integer part and rest (b_i - b_j is the difference of
+//                both: exact to 2^-24 however strong the decays before j were), and the factors that depend on one token alone
+//   warpgroup 1  thread = token: P (bf16, over the scores' own columns: it goes to P V from tensor memory)
+//   warpgroup 2  thread = token: the chunk's output: scale, normalisation, gate, rounding, store
+//   warpgroups 3, 4  thread = half a row of the state: S' from S and DS in fp32; S in bf16 to shared memory for the next chunk's Q S
+//   warpgroup 5  K' = 2^(b_C - b_j) k_j, in pieces of 16 tokens through a ring of their own
+// Decays of P: in the 32 x 32 blocks on the diagonal one exponential per element; below it 2^(b_i - m) 2^(m - b_j), m the value at the
+// end of j's block: both factors are at most 1, and the second is the same for all rows.
 // Roundings: P and the copy of S that multiplies Q go to bf16 (half a step, 2^-9 of the value, like the output's own).  K' goes to
-// the tensor cores as the sum of three bf16, 24 bits of it: the state is handed on in fp32, and with one bf16 it would be 1.7e-3
-// off (2-norm), with two 2.7e-6.
+// the tensor cores as a sum of bf16: where the sums leave the kernel as a state, of three (24 bits; with one it would be 1.7e-3 off (2-norm),
+// with two 2.7e-6), where they only multiply Q inside, of two.
 //
-// Order of the products per chunk: Q K^T (then P is computed), K'^T V (3 products), Q S, P V.  None waits for work that was not begun a
-// product or more earlier: P has K'^T V and Q S to be ready, the state has all of the next Q K^T and K'^T V.  Tensor
-// pipe 6 x 512 cycles a chunk (d = 128).
+// Order of the products per chunk: Q K^T, first half of K'^T V, Q S, second half, P V.  None waits for work that was not begun a product or
+// more earlier: P has K'^T V and Q S to be ready in, the state has P V, the next Q K^T and the half behind it, the output the same.
 #include "gret.cuh"
 #include "kernels.h"
 #include "ptx.cuh"
@@ -31,31 +32,62 @@ namespace yoco {
 namespace {
 
 constexpr int CT = kGretChunk;                 // 128 tokens
-constexpr int kThreads = 512;
+constexpr int kThreads = 768;
 constexpr int HALF_BYTES = CT * 128;           // 128 rows x 64 bf16: one swizzled half tile
-constexpr int PIECE = 16;                      // tokens of a piece of K': one instruction's depth
+constexpr int PIECE = 32;                      // tokens of a piece of K'
 constexpr int PIECES = CT / PIECE;
-constexpr int TERM_BYTES = 2 * PIECE * 128;    // a piece of one of K's three parts: two halves of 64 channels
-constexpr int PIECE_BYTES = 3 * TERM_BYTES;
+constexpr int PIECE_HALF = PIECE * 128;        // 64 channels of a piece of one of K's parts
+constexpr int TERM_BYTES = 2 * PIECE_HALF;
 constexpr uint32_t TMEM_COLS = 512;
 constexpr uint32_t COL_SC = 0, COL_OA = 128, COL_OI = 256, COL_DS = 384;
-// Registers per thread after the split; the CTA starts with 128 each.
-constexpr int kRegsIo = 56, kRegsOut = 192, kRegsState = 192, kRegsKeys = 72;
-static_assert(kRegsIo + kRegsOut + kRegsState + kRegsKeys <= 4 * 128, "register pool of the CTA");
+// Registers per thread after the split; the CTA starts with 80 each.
+constexpr int kRegsIo = 72, kRegsP = 72, kRegsOut = 104, kRegsState = 88, kRegsKeys = 56;
+static_assert(kRegsIo + kRegsP + kRegsOut + 2 * kRegsState + kRegsKeys <= 6 * 80, "register pool of the CTA");
 
-template <int D>
+// What a CTA does: the whole; the whole, where the state pass has the states that leave (K' in two parts); the states alone.
+enum Pass { kWhole, kMain, kStates };
+
+template <int D, Pass PASS>
 struct GCfg {
+    static constexpr bool OUT = PASS != kStates;
     static constexpr int HALVES = D / 64;
     static constexpr int TILE_BYTES = HALVES * HALF_BYTES;
-    static constexpr int STAGES = D == 128 ? 5 : 9;
-    static constexpr int OFF_KP = STAGES * TILE_BYTES;
-    static constexpr int OFF_S = OFF_KP + 2 * PIECE_BYTES;
-    static constexpr int OFF_DEC = OFF_S + D * D * 2;          // two buffers of 128 negated integer parts and 128 negated rests
-    static constexpr int OFF_BAR = OFF_DEC + 2 * 2 * CT * 4;
-    static constexpr int NUM_BARS = 2 * STAGES + 17;
+    static constexpr int TERMS = PASS == kMain ? 2 : 3;
+    static constexpr int PIECE_BYTES = TERMS * TERM_BYTES;
+    // Tiles of K, Q and V in shared memory.  K and Q are given back early (once scored and turned into K', once multiplied by S), V last.
+    static constexpr int KS = D == 64 || !OUT ? 2 : 1, QS = !OUT ? 0 : D == 64 ? 2 : 1, VS = D == 64 ? 3 : 2;
+    static constexpr int KP_STAGES = OUT && PASS == kWhole ? 2 : 3;
+    static constexpr int OFF_K = 0;
+    static constexpr int OFF_Q = OFF_K + KS * TILE_BYTES;
+    static constexpr int OFF_V = OFF_Q + QS * TILE_BYTES;
+    static constexpr int OFF_KP = OFF_V + VS * TILE_BYTES;
+    static constexpr int OFF_S = OFF_KP + KP_STAGES * PIECE_BYTES;
+    static constexpr int OFF_ROWS = OFF_S + (OUT ? D * D * 2 : 0);      // output: 32 rows x 32 channels a warp
+    static constexpr int OFF_DEC = OFF_ROWS + (OUT ? 4 * 2048 : 0);
+    static constexpr int DEC_FLOATS = 4 * CT;          // integer parts and rests of -b_j; 2^(m - b_j); 2^(b_C - b_j)
+    static constexpr int OFF_BAR = OFF_DEC + 2 * DEC_FLOATS * 4;
+    static constexpr int NUM_BARS = 2 * (KS + QS + VS) + 2 * KP_STAGES + 13;
     static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16;
     static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
 };
+
+// The bounded wait of this kernel: one answer for the warp, in few instructions.  The roles' loops together have to stay in the
+// instruction cache of the SM, which is why they are rolled up wherever registers are not indexed by them.  (With everything
+// unrolled, 173 KB instead of 45, a chunk took twice as long.)
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, const Abort& ab, int32_t wait_class) {
+    uint32_t polls = 0, t0 = 0;
+    while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
+        uint32_t t;
+        asm volatile("mov.u32 %0, %globaltimer_lo;" : "=r"(t));
+        if (polls++ == 0) t0 = t;
+        const bool late = (int32_t)(t - t0) > (int32_t)kWaitLimitNs || polls >= kWaitMaxPolls;
+        if (__any_sync(0xffffffffu, late || *ab.flag != 0)) {
+            if (late) report_give_up(ab, wait_class);
+            return false;
+        }
+    }
+    return true;
+}
 
 // A place in a ring of N, and which time round.
 template <int N>
@@ -71,46 +103,53 @@ struct Place {
     }
 };
 
+// The sequence of a place in the flat space.
+template <class Table>
+__device__ __forceinline__ int sequence_at(const GretChunkParams& p, const Table& tab, int pos) {
+    const int per = pos / p.base.H;                // tab.chunk0[b] <= per < tab.chunk0[b + 1]
+    int lo = 0, hi = p.base.B - 1;
+#pragma unroll 1
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (tab.chunk0[mid] <= per) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
 // The segments of a CTA: chunks [c, c_end) of stream (b, h), in the flat space of (sequence, head, chunk).
 template <class Table>
 struct Walk {
     const GretChunkParams& p;
     const Table& tab;
-    int64_t pos, end;
+    int pos, end;
     int b, h, c, c_end, chunks;
     __device__ __forceinline__ Walk(const GretChunkParams& p_, const Table& tab_) : p(p_), tab(tab_) {
-        const int64_t g = blockIdx.x;
+        const int g = blockIdx.x;
         if (p.split) {
-            pos = g * p.total / p.groups;
-            end = (g + 1) * p.total / p.groups;
+            pos = p.first_of(g);
+            end = p.first_of(g + 1);
         } else {                                   // one CTA per stream
-            const int bb = (int)(g / p.base.H), hh = (int)(g - (int64_t)bb * p.base.H), n = tab.chunk0[bb + 1] - tab.chunk0[bb];
-            pos = (int64_t)tab.chunk0[bb] * p.base.H + (int64_t)hh * n;
+            const int bb = g / p.base.H, n = tab.chunk0[bb + 1] - tab.chunk0[bb];
+            pos = tab.chunk0[bb] * p.base.H + (g - bb * p.base.H) * n;
             end = pos + n;
         }
     }
     // Enters the segment at pos; false when there is none left.
     __device__ __forceinline__ bool enter() {
         if (pos >= end) return false;
-        const int64_t per = pos / p.base.H;        // tab.chunk0[b] <= per < tab.chunk0[b + 1]
-        int lo = 0, hi = p.base.B - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (tab.chunk0[mid] <= per) lo = mid; else hi = mid - 1;
-        }
-        b = lo;
+        b = sequence_at(p, tab, pos);
         chunks = tab.chunk0[b + 1] - tab.chunk0[b];
-        const int64_t in = pos - (int64_t)tab.chunk0[b] * p.base.H;
-        h = (int)(in / chunks);
-        c = (int)(in - (int64_t)h * chunks);
-        const int64_t left = end - pos;
-        c_end = left < chunks - c ? c + (int)left : chunks;
+        const int in = pos - tab.chunk0[b] * p.base.H;
+        h = in / chunks;
+        c = in - h * chunks;
+        c_end = min(chunks, c + (end - pos));
         pos += c_end - c;
         return true;
     }
     // State-only pass: straight to the segment that the range ends in, if its stream goes on behind it.
     __device__ __forceinline__ bool enter_open_end() {
         bool any = false;
+#pragma unroll 1
         while (enter()) any = true;
         return any && c_end < chunks;
     }
@@ -118,31 +157,34 @@ struct Walk {
 
 __device__ __forceinline__ float exp2_parts(float whole, float rest) { return exp2f(whole) * exp2f(rest); }
 
-template <int D, bool STATE_ONLY, class Table>
+template <int D, Pass PASS, class Table>
 __global__ void __launch_bounds__(kThreads, 1)
 gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                   const GretChunkParams p, const __grid_constant__ Table tab) {
-    using C = GCfg<D>;
-    constexpr int PER_CHUNK = STATE_ONLY ? 2 : 3;          // tiles a chunk brings: K (Q) V
-    constexpr uint32_t V_AT = PER_CHUNK - 1;
+    using C = GCfg<D, PASS>;
+    constexpr bool OUT = C::OUT;
 
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
-    uint64_t* ring_full = bars;                            // [STAGES]
-    uint64_t* ring_empty = bars + C::STAGES;               // [STAGES]
-    uint64_t* kp_full = bars + 2 * C::STAGES;              // [2]
-    uint64_t* kp_empty = kp_full + 2;                      // [2]
-    uint64_t* dec_full = kp_full + 4;                      // [2]
-    uint64_t* dec_empty = kp_full + 6;                     // [2]
-    uint64_t* sc_full = kp_full + 8;
-    uint64_t* p_full = kp_full + 9;
-    uint64_t* ds_full = kp_full + 10;
-    uint64_t* ds_empty = kp_full + 11;
-    uint64_t* s_full = kp_full + 12;
-    uint64_t* s_empty = kp_full + 13;
-    uint64_t* o_full = kp_full + 14;
-    uint64_t* o_empty = kp_full + 15;
-    uint64_t* drain_bar = kp_full + 16;
+    uint64_t* k_full = bars;                               // [KS]
+    uint64_t* k_empty = k_full + C::KS;
+    uint64_t* q_full = k_empty + C::KS;                    // [QS]
+    uint64_t* q_empty = q_full + C::QS;
+    uint64_t* v_full = q_empty + C::QS;                    // [VS]
+    uint64_t* v_empty = v_full + C::VS;
+    uint64_t* kp_full = v_empty + C::VS;                   // [KP_STAGES]
+    uint64_t* kp_empty = kp_full + C::KP_STAGES;
+    uint64_t* dec_full = kp_empty + C::KP_STAGES;          // [2]
+    uint64_t* dec_empty = dec_full + 2;                    // [2]
+    uint64_t* sc_full = dec_full + 4;
+    uint64_t* p_full = dec_full + 5;
+    uint64_t* ds_full = dec_full + 6;
+    uint64_t* ds_empty = dec_full + 7;
+    uint64_t* s_full = dec_full + 8;
+    uint64_t* s_empty = dec_full + 9;
+    uint64_t* o_full = dec_full + 10;
+    uint64_t* o_empty = dec_full + 11;
+    uint64_t* drain_bar = dec_full + 12;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     float* dec = reinterpret_cast<float*>(smem + C::OFF_DEC);
@@ -154,21 +196,31 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     if (threadIdx.x == 0) {
         *abort_flag = aligned_ok ? 0 : 1;
         if (!aligned_ok) atomicCAS(p.status, 0, status_word(kWaitMisaligned, linear_cta()));
-        for (int i = 0; i < C::STAGES; ++i) {
-            mbar_init(&ring_full[i], 1);
-            mbar_init(&ring_empty[i], 1);
+        for (int i = 0; i < C::KS; ++i) {
+            mbar_init(&k_full[i], 1);
+            mbar_init(&k_empty[i], OUT ? 5 : 4);           // the warps that make K', and Q K^T
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < C::QS; ++i) {
+            mbar_init(&q_full[i], 1);
+            mbar_init(&q_empty[i], 1);
+        }
+        for (int i = 0; i < C::VS; ++i) {
+            mbar_init(&v_full[i], 1);
+            mbar_init(&v_empty[i], 1);
+        }
+        for (int i = 0; i < C::KP_STAGES; ++i) {
             mbar_init(&kp_full[i], 4);
             mbar_init(&kp_empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
             mbar_init(&dec_full[i], 1);
-            mbar_init(&dec_empty[i], STATE_ONLY ? 8 : 12);
+            mbar_init(&dec_empty[i], OUT ? 20 : 12);
         }
         mbar_init(sc_full, 1);
         mbar_init(p_full, 4);
         mbar_init(ds_full, 1);
-        mbar_init(ds_empty, 4);
-        mbar_init(s_full, 4);
+        mbar_init(ds_empty, 8);
+        mbar_init(s_full, 8);
         mbar_init(s_empty, 1);
         mbar_init(o_full, 1);
         mbar_init(o_empty, 4);
@@ -189,7 +241,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     Walk<Table> walk(p, tab);
     bool open_end_done = false;
     auto enter = [&]() -> bool {
-        if (!STATE_ONLY) return walk.enter();
+        if (OUT) return walk.enter();
         if (open_end_done) return false;
         open_end_done = true;
         return walk.enter_open_end();
@@ -202,28 +254,37 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             if (lane == 0 && aligned_ok) {
                 tma_prefetch_desc(&tmK);
                 tma_prefetch_desc(&tmV);
-                if (!STATE_ONLY) tma_prefetch_desc(&tmQ);
-                Place<C::STAGES> at(0);
-                uint32_t armed = 0;
+                if (OUT) tma_prefetch_desc(&tmQ);
+                uint32_t k_armed = 0, q_armed = 0, v_armed = 0;
+                auto load = [&](uint64_t* full, uint64_t* empty, uint32_t places, uint32_t& armed, const CUtensorMap* tm, uint32_t off, int x, int y) {
+                    const uint32_t slot = armed % places;
+                    if (!wait_or_abort(&empty[slot], ((armed / places) & 1u) ^ 1u, ab, kWaitRingEmpty)) return false;
+                    mbar_expect_tx(&full[slot], C::TILE_BYTES);
+                    for (int hf = 0; hf < C::HALVES; ++hf)
+                        tma_load_2d(smem + off + slot * C::TILE_BYTES + hf * HALF_BYTES, tm, x + hf * 64, y, &full[slot]);
+                    ++armed;
+                    return true;
+                };
                 bool ok = true;
                 while (ok && enter()) {
-                    for (int c = walk.c; ok && c < walk.c_end; ++c) {
-                        const int row = tab.tok0[walk.b] + c * CT;
-                        for (int i = 0; i < PER_CHUNK; ++i) {
-                            if (!(ok = wait_or_abort(&ring_empty[at.slot], at.phase ^ 1u, ab, kWaitRingEmpty))) break;
-                            const CUtensorMap* tm = i == 0 ? &tmK : i == (int)V_AT ? &tmV : &tmQ;
-                            mbar_expect_tx(&ring_full[at.slot], C::TILE_BYTES);
-                            for (int hf = 0; hf < C::HALVES; ++hf)
-                                tma_load_2d(smem + at.slot * C::TILE_BYTES + hf * HALF_BYTES, tm, walk.h * D + hf * 64, row, &ring_full[at.slot]);
-                            ++armed;
-                            at.advance(1);
-                        }
+                    const int x = walk.h * D;
+#pragma unroll 1
+                    for (int c = walk.c; c < walk.c_end; ++c) {
+                        const int y = tab.tok0[walk.b] + c * CT;
+                        // (the order in which their places become free)
+                        if (!(ok = load(v_full, v_empty, C::VS, v_armed, &tmV, C::OFF_V, x, y))) break;
+                        if (!(ok = load(k_full, k_empty, C::KS, k_armed, &tmK, C::OFF_K, x, y))) break;
+                        if (OUT && !(ok = load(q_full, q_empty, OUT ? C::QS : 1, q_armed, &tmQ, C::OFF_Q, x, y))) break;
                     }
                 }
-                // no copy may land after the CTA has ended (at once when all went well)
-                bool drained = true;
-                for (uint32_t k = armed > (uint32_t)C::STAGES ? armed - C::STAGES : 0; drained && k < armed; ++k)
-                    drained = drain_wait(&ring_full[k % C::STAGES], (k / C::STAGES) & 1u, ab);
+                // no copy may land after the CTA has ended (at once when all went well): the last ones into every place
+                auto drain = [&](uint64_t* full, uint32_t places, uint32_t armed) {
+                    for (uint32_t k = armed > places ? armed - places : 0; k < armed; ++k)
+                        if (!drain_wait(&full[k % places], (k / places) & 1u, ab)) return;
+                };
+                drain(v_full, C::VS, v_armed);
+                drain(k_full, C::KS, k_armed);
+                if (OUT) drain(q_full, OUT ? C::QS : 1, q_armed);
             }
         } else if (warp == 1) {
             // ======================================= issuer of the products ======================
@@ -231,19 +292,23 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 constexpr uint32_t idesc_qk = make_idesc(CT, false);
                 constexpr uint32_t idesc_mn = make_idesc(D, true);              // B with its columns contiguous: V, S
                 constexpr uint32_t idesc_kv = idesc_mn | (1u << 15);            // and A with its rows contiguous: K'
-                Place<C::STAGES> kat(0), qat(1), vat(V_AT);
-                uint32_t it = 0, pc = 0;
+                Place<C::KS> kat(0);
+                Place<OUT ? C::QS : 1> qat(0);
+                Place<C::VS> vat(0);
+                Place<C::KP_STAGES> pat(0);
+                uint32_t it = 0;
                 bool ok = true;
                 while (ok && enter()) {
+#pragma unroll 1
                     for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                         const uint32_t ph = it & 1u;
-                        const uint64_t q_desc = make_desc(sbase + qat.slot * C::TILE_BYTES, 16, 1024);
-                        const uint64_t v_desc = make_desc(sbase + vat.slot * C::TILE_BYTES, HALF_BYTES, 1024);
-                        if (!(ok = warp_wait(&ring_full[kat.slot], kat.phase, ab, kWaitRingFull))) break;
-                        if (!STATE_ONLY) {
-                            if (!(ok = warp_wait(&ring_full[qat.slot], qat.phase, ab, kWaitRingFull))) break;
+                        const uint64_t q_desc = make_desc(sbase + C::OFF_Q + qat.slot * C::TILE_BYTES, 16, 1024);
+                        const uint64_t v_desc = make_desc(sbase + C::OFF_V + vat.slot * C::TILE_BYTES, HALF_BYTES, 1024);
+                        if (OUT) {
+                            if (!(ok = wait_for(&k_full[kat.slot], kat.phase, ab, kWaitRingFull))) break;
+                            if (!(ok = wait_for(&q_full[qat.slot], qat.phase, ab, kWaitRingFull))) break;
                             tc_fence_after();
-                            const uint64_t k_desc = make_desc(sbase + kat.slot * C::TILE_BYTES, 16, 1024);
+                            const uint64_t k_desc = make_desc(sbase + C::OFF_K + kat.slot * C::TILE_BYTES, 16, 1024);
                             if (elect_one()) {
 #pragma unroll
                                 for (int ks = 0; ks < D / 16; ++ks) {
@@ -251,49 +316,58 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                                     umma_ss(tmem_base + COL_SC, q_desc + (off >> 4), k_desc + (off >> 4), idesc_qk, ks > 0 ? 1u : 0u);
                                 }
                                 umma_commit(sc_full);
+                                umma_commit(&k_empty[kat.slot]);
                             }
                             __syncwarp();
+                            kat.advance(1);
                         }
-                        // ---- K'^T V
-                        if (!(ok = warp_wait(&ring_full[vat.slot], vat.phase, ab, kWaitRingFull))) break;
-                        if (!(ok = warp_wait(ds_empty, ph ^ 1u, ab, kWaitTensor))) break;
-                        for (int e = 0; e < PIECES; ++e, ++pc) {
-                            const uint32_t buf = pc & 1u;
-                            if (!(ok = warp_wait(&kp_full[buf], (pc >> 1) & 1u, ab, kWaitTensor))) break;
+                        if (!(ok = wait_for(&v_full[vat.slot], vat.phase, ab, kWaitRingFull))) break;
+                        if (!(ok = wait_for(ds_empty, ph ^ 1u, ab, kWaitTensor))) break;
+#pragma unroll 1
+                        for (int e = 0; e < PIECES; ++e) {
+                            if (OUT && e == 1) {
+                                // ---- Q S
+                                if (!(ok = wait_for(s_full, ph, ab, kWaitTensor))) break;
+                                if (!(ok = wait_for(o_empty, ph ^ 1u, ab, kWaitTensor))) break;
+                                tc_fence_after();
+                                const uint64_t s_desc = make_desc(sbase + C::OFF_S, D * 128, 1024);
+                                if (elect_one()) {
+#pragma unroll
+                                    for (int ks = 0; ks < D / 16; ++ks) {
+                                        const uint32_t off = (ks >> 2) * HALF_BYTES + (ks & 3) * 32;
+                                        umma_ss(tmem_base + COL_OI, q_desc + (off >> 4), s_desc + ((ks * 16 * 128) >> 4), idesc_mn, ks > 0 ? 1u : 0u);
+                                    }
+                                    umma_commit(s_empty);
+                                    umma_commit(&q_empty[qat.slot]);
+                                }
+                                __syncwarp();
+                                qat.advance(1);
+                            }
+                            // ---- K'^T V, 32 tokens
+                            if (!(ok = wait_for(&kp_full[pat.slot], pat.phase, ab, kWaitTensor))) break;
                             tc_fence_after();
+                            const uint64_t kp_desc = make_desc(sbase + C::OFF_KP + pat.slot * C::PIECE_BYTES, PIECE_HALF, 1024);
+                            const uint64_t vp_desc = v_desc + ((e * PIECE * 128) >> 4);
                             if (elect_one()) {
 #pragma unroll
-                                for (int t = 0; t < 3; ++t)
-                                    umma_ss(tmem_base + COL_DS, make_desc(sbase + C::OFF_KP + buf * PIECE_BYTES + t * TERM_BYTES, PIECE * 128, 1024),
-                                            v_desc + ((e * PIECE * 128) >> 4), idesc_kv, e > 0 || t > 0 ? 1u : 0u);
-                                umma_commit(&kp_empty[buf]);
+                                for (int j = 0; j < PIECE / 16 * C::TERMS; ++j) {
+                                    const uint32_t ks = j / C::TERMS, t = j % C::TERMS;
+                                    umma_ss(tmem_base + COL_DS, kp_desc + ((t * TERM_BYTES + ks * 2048) >> 4), vp_desc + ((ks * 2048) >> 4), idesc_kv,
+                                            e > 0 || j > 0 ? 1u : 0u);
+                                }
+                                umma_commit(&kp_empty[pat.slot]);
                                 if (e == PIECES - 1) {
                                     umma_commit(ds_full);
-                                    umma_commit(&ring_empty[kat.slot]);
-                                    if (STATE_ONLY) umma_commit(&ring_empty[vat.slot]);
+                                    if (!OUT) umma_commit(&v_empty[vat.slot]);
                                 }
                             }
                             __syncwarp();
+                            pat.advance(1);
                         }
                         if (!ok) break;
-                        if (!STATE_ONLY) {
-                            // ---- Q S
-                            if (!(ok = warp_wait(s_full, ph, ab, kWaitTensor))) break;
-                            if (!(ok = warp_wait(o_empty, ph ^ 1u, ab, kWaitTensor))) break;
-                            tc_fence_after();
-                            const uint64_t s_desc = make_desc(sbase + C::OFF_S, D * 128, 1024);
-                            if (elect_one()) {
-#pragma unroll
-                                for (int ks = 0; ks < D / 16; ++ks) {
-                                    const uint32_t off = (ks >> 2) * HALF_BYTES + (ks & 3) * 32;
-                                    umma_ss(tmem_base + COL_OI, q_desc + (off >> 4), s_desc + ((ks * 16 * 128) >> 4), idesc_mn, ks > 0 ? 1u : 0u);
-                                }
-                                umma_commit(s_empty);
-                                umma_commit(&ring_empty[qat.slot]);
-                            }
-                            __syncwarp();
+                        if (OUT) {
                             // ---- P V
-                            if (!(ok = warp_wait(p_full, ph, ab, kWaitTensor))) break;
+                            if (!(ok = wait_for(p_full, ph, ab, kWaitTensor))) break;
                             tc_fence_after();
                             if (elect_one()) {
 #pragma unroll
@@ -301,13 +375,11 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                                     umma_ts(tmem_base + COL_OA, tmem_base + COL_SC + ks * 8, v_desc + ((ks * 16 * 128) >> 4), idesc_mn,
                                             ks > 0 ? 1u : 0u);
                                 umma_commit(o_full);
-                                umma_commit(&ring_empty[vat.slot]);
+                                umma_commit(&v_empty[vat.slot]);
                             }
                             __syncwarp();
                         }
-                        kat.advance(PER_CHUNK);
-                        qat.advance(PER_CHUNK);
-                        vat.advance(PER_CHUNK);
+                        vat.advance(1);
                     }
                 }
                 // nothing issued may still run when tensor memory is released
@@ -324,93 +396,129 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             while (ok && enter()) {
                 const int len = tab.len[walk.b];
                 const int64_t tok0 = tab.tok0[walk.b];
-                auto read = [&](int c, float (&z)[4]) {
+                // a lane has four neighbouring tokens; those of the next chunk are asked for a chunk ahead
+                auto read = [&](int t0, float (&z)[4]) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int t = c * CT + lane * 4 + j;
-                        z[j] = t < len ? log_decay(p.base, tok0 + t, walk.h) : 0.f;
-                    }
+                    for (int j = 0; j < 4; ++j) z[j] = t0 + j < len ? read_decay(p.base, tok0 + t0 + j, walk.h) : 0.f;
                 };
                 float z[4];
-                read(walk.c, z);
+                read(walk.c * CT + lane * 4, z);
+#pragma unroll 1
                 for (int c = walk.c; c < walk.c_end; ++c, ++it) {
-                    float next[4] = {0.f, 0.f, 0.f, 0.f};
-                    if (c + 1 < walk.c_end) read(c + 1, next);
+                    const int t0 = c * CT + lane * 4;
                     double s[4], sum = 0.0;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[j] = sum += (double)z[j] * 1.4426950408889634;
+                    for (int j = 0; j < 4; ++j) {
+                        const double l = (double)log_decay(p.base, z[j]) * 1.4426950408889634;
+                        s[j] = sum += t0 + j < len ? l : 0.0;
+                    }
+                    read(t0 + CT, z);                      // (behind the segment: read for nothing)
                     double before = sum;
-#pragma unroll
+#pragma unroll 1
                     for (int m = 1; m < 32; m <<= 1) {
                         const double o = __shfl_up_sync(0xffffffffu, before, m);
                         if (lane >= m) before += o;
                     }
+                    const double block_end = __shfl_sync(0xffffffffu, before, lane | 7), chunk_end = __shfl_sync(0xffffffffu, before, 31);
                     before -= sum;
                     const uint32_t buf = it & 1u;
-                    if (!(ok = warp_wait(&dec_empty[buf], ((it >> 1) & 1u) ^ 1u, ab, kWaitTensor))) break;
-                    float whole[4], rest[4];
+                    if (!(ok = wait_for(&dec_empty[buf], ((it >> 1) & 1u) ^ 1u, ab, kWaitTensor))) break;
+                    float* dst = dec + buf * C::DEC_FLOATS + lane * 4;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const double x = before + s[j], w = rint(x);
-                        whole[j] = (float)-w;
-                        rest[j] = (float)(w - x);
-                        z[j] = next[j];
+                        const double x = before + s[j], r = rint(x);
+                        dst[j] = (float)-r;
+                        dst[CT + j] = (float)(r - x);
+                        dst[2 * CT + j] = ex2_approx((float)(block_end - x));
+                        dst[3 * CT + j] = ex2_approx((float)(chunk_end - x));
                     }
-                    *reinterpret_cast<float4*>(dec + buf * 2 * CT + lane * 4) = make_float4(whole[0], whole[1], whole[2], whole[3]);
-                    *reinterpret_cast<float4*>(dec + buf * 2 * CT + CT + lane * 4) = make_float4(rest[0], rest[1], rest[2], rest[3]);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&dec_full[buf]);
                 }
             }
         }
+        else if (OUT && p.base.norm.gate && aligned_ok) {
+            // ======================================= the gate's rows, into L2 a chunk ahead ======
+            uint32_t it = 0;
+            bool ok = true;
+            while (ok && enter()) {
+                const int len = tab.len[walk.b];
+                const __nv_bfloat16* gate = p.base.norm.gate + (int64_t)tab.tok0[walk.b] * p.base.norm.gate_stride + walk.h * D;
+#pragma unroll 1
+                for (int c = walk.c; c < walk.c_end; ++c, ++it) {
+                    if (it > 0 && !(ok = wait_for(sc_full, (it - 1) & 1u, ab, kWaitTensor))) break;
+                    for (int r = lane; r < CT * C::HALVES; r += 32) {
+                        const int t = c * CT + r / C::HALVES;
+                        if (t < len)
+                            asm volatile("prefetch.global.L2 [%0];" ::"l"(gate + t * p.base.norm.gate_stride + (r % C::HALVES) * 64));
+                    }
+                }
+            }
+        }
     } else if (warp < 8) {
-        // ======================================= P and the output ================================
-        setmaxnreg_inc<kRegsOut>();
+        // ======================================= P ===============================================
+        setmaxnreg_dec<kRegsP>();
         const int quad = warp & 3, i = quad * 32 + lane;
-        const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
+        const uint32_t sc = tmem_base + COL_SC + ((uint32_t)(quad * 32) << 16);
         uint32_t it = 0;
-        bool ok = aligned_ok && !STATE_ONLY;
+        bool ok = aligned_ok && OUT;
         while (ok && enter()) {
-            const int len = tab.len[walk.b];
-            const int64_t tok0 = tab.tok0[walk.b];
+#pragma unroll 1
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                 const uint32_t buf = it & 1u, ph = it & 1u;
-                if (!(ok = warp_wait(&dec_full[buf], (it >> 1) & 1u, ab, kWaitTensor))) break;
-                const float* whole = dec + buf * 2 * CT;                        // negated
+                if (!(ok = wait_for(&dec_full[buf], (it >> 1) & 1u, ab, kWaitTensor))) break;
+                const float* whole = dec + buf * C::DEC_FLOATS;                 // negated
                 const float* rest = whole + CT;
                 const float wi = -whole[i], ri = -rest[i];
-                if (!(ok = warp_wait(sc_full, ph, ab, kWaitTensor))) break;
+                if (!(ok = wait_for(sc_full, ph, ab, kWaitTensor))) break;
                 tc_fence_after();
-                const uint64_t wi2 = f2_pack(wi, wi), ri2 = f2_pack(ri, ri);
+                uint32_t w[8];
+                float s[16];
+                float r = 0.f;
+#pragma unroll 1
+                for (int blk = 0; blk < 2 * quad; ++blk) {         // 16 columns below the diagonal
+                    tmem_ld16(sc + blk * 16, s);
+                    const int m = blk * 16 | 31;
+                    r = ex2_approx((wi + whole[m]) + (ri + rest[m]));
+                    const uint64_t r2 = f2_pack(r, r);
+                    const ulonglong2* u = reinterpret_cast<const ulonglong2*>(whole + 2 * CT + blk * 16);
+                    tmem_wait_ld();
 #pragma unroll
-                for (int blk = 0; blk < 4; ++blk) {
-                    uint32_t w[16];
-                    if (blk <= quad) {
-                        float s[32];
-                        tmem_ld32(tmem_base + COL_SC + lane_addr + blk * 32, s);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int j = 0; j < 32; j += 4) {
-                            const ulonglong2 wj = *reinterpret_cast<const ulonglong2*>(whole + blk * 32 + j);
-                            const ulonglong2 rj = *reinterpret_cast<const ulonglong2*>(rest + blk * 32 + j);
-                            float x[4];
-                            f2_unpack(f2_add(f2_add(wi2, wj.x), f2_add(ri2, rj.x)), x[0], x[1]);
-                            f2_unpack(f2_add(f2_add(wi2, wj.y), f2_add(ri2, rj.y)), x[2], x[3]);
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                x[q] = s[j + q] * ex2_approx(x[q]);
-                                if (blk == quad) x[q] = j + q <= lane ? x[q] : 0.f;
-                            }
-                            w[j / 2] = pack_bf16x2(x[0], x[1]);
-                            w[j / 2 + 1] = pack_bf16x2(x[2], x[3]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) w[j] = 0u;
+                    for (int j = 0; j < 16; j += 4) {
+                        const ulonglong2 uj = u[j / 4];
+                        float x[4];
+                        f2_unpack(f2_mul(f2_mul(f2_pack(s[j], s[j + 1]), r2), uj.x), x[0], x[1]);
+                        f2_unpack(f2_mul(f2_mul(f2_pack(s[j + 2], s[j + 3]), r2), uj.y), x[2], x[3]);
+                        w[j / 2] = pack_bf16x2(x[0], x[1]);
+                        w[j / 2 + 1] = pack_bf16x2(x[2], x[3]);
                     }
-                    tmem_st16(tmem_base + COL_SC + lane_addr + blk * 16, w);
+                    tmem_st8(sc + blk * 8, w);             // (over columns that have been read)
                 }
-                const float ei = exp2_parts(wi, ri) * p.base.scale;
+                const uint64_t wi2 = f2_pack(wi, wi), ri2 = f2_pack(ri, ri);
+#pragma unroll 1
+                for (int blk = 2 * quad; blk < 2 * quad + 2; ++blk) {
+                    tmem_ld16(sc + blk * 16, s);
+                    const int last = i - blk * 16;         // the row's last column here
+                    const ulonglong2* wj = reinterpret_cast<const ulonglong2*>(whole + blk * 16);
+                    const ulonglong2* rj = reinterpret_cast<const ulonglong2*>(rest + blk * 16);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 16; j += 4) {
+                        const ulonglong2 wq = wj[j / 4], rq = rj[j / 4];
+                        float x[4];
+                        f2_unpack(f2_add(f2_add(wi2, wq.x), f2_add(ri2, rq.x)), x[0], x[1]);
+                        f2_unpack(f2_add(f2_add(wi2, wq.y), f2_add(ri2, rq.y)), x[2], x[3]);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) x[q] = j + q <= last ? s[j + q] * ex2_approx(x[q]) : 0.f;
+                        w[j / 2] = pack_bf16x2(x[0], x[1]);
+                        w[j / 2 + 1] = pack_bf16x2(x[2], x[3]);
+                    }
+                    tmem_st8(sc + blk * 8, w);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = 0u;
+#pragma unroll 1
+                for (int blk = 2 * quad + 2; blk < 8; ++blk) tmem_st8(sc + blk * 8, w);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -418,87 +526,139 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     mbar_arrive(p_full);
                     mbar_arrive(&dec_empty[buf]);
                 }
-                // ---- output
-                if (!(ok = warp_wait(o_full, ph, ab, kWaitTensor))) break;
-                tc_fence_after();
-                float y[D];
-#pragma unroll
-                for (int blk = 0; blk < D / 32; ++blk) {
-                    float x[32];
-                    tmem_ld32(tmem_base + COL_OA + lane_addr + blk * 32, *reinterpret_cast<float(*)[32]>(&y[blk * 32]));
-                    tmem_ld32(tmem_base + COL_OI + lane_addr + blk * 32, x);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) y[blk * 32 + j] = fmaf(ei, x[j], p.base.scale * y[blk * 32 + j]);
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(o_empty);
-                const int t = c * CT + i;
-                const int64_t tok = tok0 + t;
-                if (t < len) {
-                    const NormGate& nm = p.base.norm;
-                    if (nm.on) {
-                        float mean = 0.f, sq = 0.f;
-                        if (!nm.rms) {
-                            float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                            for (int j = 0; j < D; ++j) part[j & 3] += y[j];
-                            mean = ((part[0] + part[1]) + (part[2] + part[3])) * (1.f / D);
-                        }
-                        float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int j = 0; j < D; ++j) {
-                            y[j] -= mean;
-                            part[j & 3] = fmaf(y[j], y[j], part[j & 3]);
-                        }
-                        sq = (part[0] + part[1]) + (part[2] + part[3]);
-                        const float inv = 1.f / sqrtf(sq * (1.f / D) + nm.eps);
-#pragma unroll
-                        for (int j = 0; j < D; ++j) y[j] *= inv;
-                        const int at = walk.h * D;
-                        if (nm.gain) {
-#pragma unroll
-                            for (int j = 0; j < D; j += 8) {
-                                float g[8];
-                                unpack8(__ldg(reinterpret_cast<const uint4*>(nm.gain + at + j)), g);
-#pragma unroll
-                                for (int q = 0; q < 8; ++q) y[j + q] *= g[q];
-                            }
-                        }
-                        if (nm.bias) {
-#pragma unroll
-                            for (int j = 0; j < D; j += 8) {
-                                float g[8];
-                                unpack8(__ldg(reinterpret_cast<const uint4*>(nm.bias + at + j)), g);
-#pragma unroll
-                                for (int q = 0; q < 8; ++q) y[j + q] += g[q];
-                            }
-                        }
-                        if (nm.gate) {
-                            const uint4* src = reinterpret_cast<const uint4*>(nm.gate + tok * nm.gate_stride + at);
-#pragma unroll
-                            for (int j = 0; j < D; j += 8) {
-                                float g[8];
-                                unpack8(__ldg(src + j / 8), g);
-#pragma unroll
-                                for (int q = 0; q < 8; ++q) y[j + q] *= swish(g[q]);
-                            }
-                        }
-                    }
-                    uint4* dst = reinterpret_cast<uint4*>(p.base.o + tok * p.base.o_stride + walk.h * D);
-#pragma unroll
-                    for (int j = 0; j < D; j += 8) dst[j / 8] = pack8(*reinterpret_cast<float(*)[8]>(&y[j]));
-                }
-                __syncwarp();
             }
         }
     } else if (warp < 12) {
+        // ======================================= output ==========================================
+        setmaxnreg_inc<kRegsOut>();
+        const int quad = warp & 3, i = quad * 32 + lane;
+        const uint32_t oa = tmem_base + COL_OA + ((uint32_t)(quad * 32) << 16), oi = oa + (COL_OI - COL_OA);
+        const NormGate& nm = p.base.norm;
+        const float scale = p.base.scale;
+        uint8_t* rows = smem + C::OFF_ROWS + quad * 2048;
+        auto staged = [&](int r, int ch) { return reinterpret_cast<uint4*>(rows + r * 64 + ((ch ^ ((r >> 1) & 3)) << 4)); };   // no bank twice
+        uint32_t it = 0;
+        bool ok = aligned_ok && OUT;
+        while (ok && enter()) {
+            const int len = tab.len[walk.b], at = walk.h * D;
+            const int64_t tok0 = tab.tok0[walk.b];
+#pragma unroll 1
+            for (int c = walk.c; c < walk.c_end; ++c, ++it) {
+                const uint32_t buf = it & 1u, ph = it & 1u;
+                if (!(ok = wait_for(&dec_full[buf], (it >> 1) & 1u, ab, kWaitTensor))) break;
+                const float ei = exp2_parts(-dec[buf * C::DEC_FLOATS + i], -dec[buf * C::DEC_FLOATS + CT + i]) * scale;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&dec_empty[buf]);
+                if (!(ok = wait_for(o_full, ph, ab, kWaitTensor))) break;
+                tc_fence_after();
+                // 16 channels of the row
+                auto channels = [&](int j, float (&y)[16]) {
+                    float x[16];
+                    tmem_ld16(oa + j, y);
+                    tmem_ld16(oi + j, x);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) y[q] = fmaf(ei, x[q], scale * y[q]);
+                };
+                float mean = 0.f, inv = 1.f;
+                if (nm.on) {
+                    // sums of the differences from the row's first channel (rms: from zero) and of their squares: one of d values is at most
+                    // sqrt(d) standard deviations from the mean, so the difference of the two loses at most d roundings
+                    float first = 0.f, s1[2] = {0.f, 0.f}, s2[2] = {0.f, 0.f};
+#pragma unroll 1
+                    for (int j = 0; j < D; j += 16) {
+                        float y[16];
+                        channels(j, y);
+                        if (j == 0 && !nm.rms) first = y[0];
+#pragma unroll
+                        for (int q = 0; q < 16; ++q) {
+                            const float e = y[q] - first;
+                            s1[q & 1] += e;
+                            s2[q & 1] = fmaf(e, e, s2[q & 1]);
+                        }
+                    }
+                    const float m1 = nm.rms ? 0.f : (s1[0] + s1[1]) * (1.f / D);
+                    mean = first + m1;
+                    inv = 1.f / sqrtf(fmaxf(fmaf(-m1, m1, (s2[0] + s2[1]) * (1.f / D)), 0.f) + nm.eps);
+                }
+                // Rows leave (and the gate's come) 32 channels at a time through shared memory, so that a warp's access covers 8 rows, not 32.
+                const int t0 = c * CT + quad * 32, lrow = lane >> 2, lch = lane & 3;
+                __nv_bfloat16* out = p.base.o + (tok0 + t0 + lrow) * p.base.o_stride + at + lch * 8;
+                const __nv_bfloat16* gate = nm.gate + (tok0 + t0 + lrow) * nm.gate_stride + at + lch * 8;
+                uint4 g[4];
+                auto ask = [&](int j) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        g[r] = make_uint4(0u, 0u, 0u, 0u);
+                        if (t0 + lrow + 8 * r < len) g[r] = __ldg(reinterpret_cast<const uint4*>(gate + 8 * r * nm.gate_stride + j));
+                    }
+                };
+                if (nm.gate) ask(0);
+#pragma unroll 1
+                for (int j = 0; j < D; j += 32) {
+                    uint4 mine[4];
+                    if (nm.gate) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) *staged(lrow + 8 * r, lch) = g[r];
+                        __syncwarp();
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) mine[q] = *staged(lane, q);
+                        __syncwarp();
+                        if (j + 32 < D) ask(j + 32);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; e += 16) {
+                        float y[16];
+                        channels(j + e, y);
+                        if (nm.on) {
+#pragma unroll
+                            for (int q = 0; q < 16; ++q) y[q] = (y[q] - mean) * inv;
+                            float f[8];
+                            if (nm.gain) {
+#pragma unroll
+                                for (int q = 0; q < 16; ++q) {
+                                    if (q % 8 == 0) unpack8(__ldg(reinterpret_cast<const uint4*>(nm.gain + at + j + e + q)), f);
+                                    y[q] *= f[q % 8];
+                                }
+                            }
+                            if (nm.bias) {
+#pragma unroll
+                                for (int q = 0; q < 16; ++q) {
+                                    if (q % 8 == 0) unpack8(__ldg(reinterpret_cast<const uint4*>(nm.bias + at + j + e + q)), f);
+                                    y[q] += f[q % 8];
+                                }
+                            }
+                            if (nm.gate) {
+#pragma unroll
+                                for (int q = 0; q < 16; ++q) {
+                                    if (q % 8 == 0) unpack8(mine[(e + q) / 8], f);
+                                    y[q] *= swish(f[q % 8]);
+                                }
+                            }
+                        }
+                        *staged(lane, e / 8) = pack8(*reinterpret_cast<float(*)[8]>(&y[0]));
+                        *staged(lane, e / 8 + 1) = pack8(*reinterpret_cast<float(*)[8]>(&y[8]));
+                    }
+                    if (j + 32 == D) {                     // all of it has been read
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(o_empty);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (t0 + lrow + 8 * r < len)
+                            *reinterpret_cast<uint4*>(out + 8 * r * p.base.o_stride + j) = *staged(lrow + 8 * r, lch);
+                    __syncwarp();
+                }
+            }
+        }
+    } else if (warp < 20) {
         // ======================================= state ===========================================
         setmaxnreg_inc<kRegsState>();
-        constexpr int N = D == 128 ? 128 : 32;             // channels of a thread (d = 64: two threads a row)
-        const int quad = warp & 3, l = quad * 32 + lane, row = l % D, col = (l / D) * N;
-        const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
+        constexpr int N = D * D / 256;                     // channels of a thread: half a row (d = 64: a quarter)
+        const int quad = warp & 3, l = quad * 32 + lane, row = l % D, col = (warp >= 16 ? D / 2 : 0) + (l / D) * N;
+        const uint32_t ds = tmem_base + COL_DS + ((uint32_t)(quad * 32) << 16) + col;
         uint8_t* s_row = smem + C::OFF_S + row * 128;
         uint32_t it = 0;
         bool ok = aligned_ok;
@@ -508,7 +668,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             float s[N];
             // where the segment's first state is: the stream's own, or what the merge left for this CTA
             const float* src = nullptr;
-            if (!STATE_ONLY) {
+            if (OUT) {
                 if (whole_stream)
                     src = tab.from[b] >= 0 ? p.base.state + ((int64_t)tab.from[b] * p.base.H + h) * (D * D) : nullptr;
                 else
@@ -524,10 +684,11 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             }
             float all_whole = 0.f;                         // logarithm of the segment's decay
             double all_rest = 0.0;
+#pragma unroll 1
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                 const uint32_t buf = it & 1u, ph = it & 1u;
-                if (!STATE_ONLY) {
-                    if (!(ok = warp_wait(s_empty, ph ^ 1u, ab, kWaitTensor))) break;
+                if (OUT) {
+                    if (!(ok = wait_for(s_empty, ph ^ 1u, ab, kWaitTensor))) break;
 #pragma unroll
                     for (int j = 0; j < N; j += 8) {
                         const int ch = (col + j) / 8;
@@ -538,24 +699,24 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     __syncwarp();
                     if (lane == 0) mbar_arrive(s_full);
                 }
-                if (!(ok = warp_wait(&dec_full[buf], (it >> 1) & 1u, ab, kWaitTensor))) break;
-                const float whole = -dec[buf * 2 * CT + CT - 1], rest = -dec[buf * 2 * CT + 2 * CT - 1];
+                if (!(ok = wait_for(&dec_full[buf], (it >> 1) & 1u, ab, kWaitTensor))) break;
+                const float whole = -dec[buf * C::DEC_FLOATS + CT - 1], rest = -dec[buf * C::DEC_FLOATS + 2 * CT - 1];
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&dec_empty[buf]);
                 const float keep = exp2_parts(whole, rest);
-                if (STATE_ONLY) {
+                if (!OUT) {
                     all_whole += whole;
                     all_rest += (double)rest;
                 }
-                if (!(ok = warp_wait(ds_full, ph, ab, kWaitTensor))) break;
+                if (!(ok = wait_for(ds_full, ph, ab, kWaitTensor))) break;
                 tc_fence_after();
 #pragma unroll
-                for (int blk = 0; blk < N / 32; ++blk) {
-                    float x[32];
-                    tmem_ld32(tmem_base + COL_DS + lane_addr + col + blk * 32, x);
+                for (int blk = 0; blk < N / 16; ++blk) {
+                    float x[16];
+                    tmem_ld16(ds + blk * 16, x);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) s[blk * 32 + j] = fmaf(keep, s[blk * 32 + j], x[j]);
+                    for (int j = 0; j < 16; ++j) s[blk * 16 + j] = fmaf(keep, s[blk * 16 + j], x[j]);
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -563,7 +724,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             }
             if (!ok) break;
             float* dst = nullptr;
-            if (STATE_ONLY)
+            if (PASS == kStates)
                 dst = p.part + (int64_t)(blockIdx.x + 1) * (D * D);
             else if (walk.c_end == walk.chunks && tab.to[b] >= 0)
                 dst = p.base.state + ((int64_t)tab.to[b] * p.base.H + h) * (D * D);
@@ -572,71 +733,88 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 for (int j = 0; j < N; j += 4)
                     *reinterpret_cast<float4*>(dst + row * D + col + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
             }
-            if (STATE_ONLY && l == 0) p.part_keep[blockIdx.x + 1] = exp2f(all_whole) * (float)exp2(all_rest);
+            if (PASS == kStates && threadIdx.x == 12 * 32) p.part_keep[blockIdx.x + 1] = exp2f(all_whole) * (float)exp2(all_rest);
         }
     } else {
         // ======================================= K' ==============================================
         setmaxnreg_dec<kRegsKeys>();
         const int l = threadIdx.x & 127, row = l >> 3, ch = l & 7;
         const uint32_t at = row * 128 + ((ch ^ (row & 7)) << 4);       // inside a piece's half; the same in a tile's
-        Place<C::STAGES> kat(0), vat(V_AT);
-        uint32_t it = 0, pc = 0;
+        Place<C::KS> kat(0);
+        Place<C::VS> vat(0);
+        Place<C::KP_STAGES> pat(0);
+        uint32_t it = 0;
         bool ok = aligned_ok;
         while (ok && enter()) {
             const int len = tab.len[walk.b];
-            for (int c = walk.c; ok && c < walk.c_end; ++c, ++it) {
+#pragma unroll 1
+            for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                 const uint32_t buf = it & 1u;
                 const int valid = len - c * CT;            // tokens of the sequence from here on
-                if (!(ok = warp_wait(&dec_full[buf], (it >> 1) & 1u, ab, kWaitTensor))) break;
-                const float* whole = dec + buf * 2 * CT;
-                const float* rest = whole + CT;
-                const float w_end = whole[CT - 1], r_end = rest[CT - 1];
-                if (!(ok = warp_wait(&ring_full[kat.slot], kat.phase, ab, kWaitRingFull))) break;
+                if (!(ok = wait_for(&dec_full[buf], (it >> 1) & 1u, ab, kWaitTensor))) break;
+                const float* weight = dec + buf * C::DEC_FLOATS + 3 * CT + row;
+                if (!(ok = wait_for(&k_full[kat.slot], kat.phase, ab, kWaitRingFull))) break;
                 if (valid < CT) {
                     // rows behind the sequence are the next one's, or none: they may hold anything, and 0 times that is not 0
-                    if (!(ok = warp_wait(&ring_full[vat.slot], vat.phase, ab, kWaitRingFull))) break;
+                    if (!(ok = wait_for(&v_full[vat.slot], vat.phase, ab, kWaitRingFull))) break;
                     if (l >= valid) {
-#pragma unroll
+#pragma unroll 1
                         for (int q = 0; q < 8 * C::HALVES; ++q)
-                            *reinterpret_cast<uint4*>(smem + vat.slot * C::TILE_BYTES + (q >> 3) * HALF_BYTES + l * 128 + (q & 7) * 16) =
+                            *reinterpret_cast<uint4*>(smem + C::OFF_V + vat.slot * C::TILE_BYTES + (q >> 3) * HALF_BYTES + l * 128 + (q & 7) * 16) =
                                 make_uint4(0u, 0u, 0u, 0u);
                     }
                 }
-                for (int e = 0; e < PIECES; ++e, ++pc) {
-                    const uint32_t pb = pc & 1u;
-                    const int j = e * PIECE + row;
-                    const float w = exp2_parts(whole[j] - w_end, rest[j] - r_end);
-                    if (!(ok = warp_wait(&kp_empty[pb], ((pc >> 1) & 1u) ^ 1u, ab, kWaitTensor))) break;
-                    const uint8_t* src = smem + kat.slot * C::TILE_BYTES + e * (PIECE * 128) + at;
-                    uint8_t* dst = smem + C::OFF_KP + pb * PIECE_BYTES + at;
+#pragma unroll 1
+                for (int e = 0; e < PIECES; ++e) {
+                    if (!(ok = wait_for(&kp_empty[pat.slot], pat.phase ^ 1u, ab, kWaitTensor))) break;
+                    const uint8_t* src = smem + C::OFF_K + kat.slot * C::TILE_BYTES + e * PIECE_HALF + at;
+                    uint8_t* dst = smem + C::OFF_KP + pat.slot * C::PIECE_BYTES + at;
 #pragma unroll
-                    for (int hf = 0; hf < C::HALVES; ++hf) {
-                        float x[8], y[8];
-                        unpack8(*reinterpret_cast<const uint4*>(src + hf * HALF_BYTES), x);
+                    for (int r = 0; r < PIECE; r += 16) {
+                        const float w = weight[e * PIECE + r];
+                        const bool in = e * PIECE + r + row < valid;
+                        const uint64_t w2 = f2_pack(w, w);
 #pragma unroll
-                        for (int q = 0; q < 8; ++q) x[q] = j < valid ? w * x[q] : 0.f;
+                        for (int hf = 0; hf < C::HALVES; ++hf) {
+                            uint4 raw = *reinterpret_cast<const uint4*>(src + hf * HALF_BYTES + r * 128);
+                            if (!in) raw = make_uint4(0u, 0u, 0u, 0u);
+                            uint32_t part[C::TERMS][4];
+                            const uint32_t kk[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-                        for (int t = 0; t < 3; ++t) {
-                            const uint4 part = pack8(x);
-                            *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + hf * (PIECE * 128)) = part;
-                            // d = 64: the instruction's upper 64 rows are the same ones again (the second threads of the state's rows read them)
-                            if (D == 64) *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + PIECE * 128) = part;
-                            if (t < 2) {
-                                unpack8(part, y);
+                            for (int q = 0; q < 4; ++q) {
+                                uint64_t x = f2_mul(w2, f2_pack(__uint_as_float(kk[q] << 16), __uint_as_float(kk[q] & 0xFFFF0000u)));
 #pragma unroll
-                                for (int q = 0; q < 8; ++q) x[q] -= y[q];
+                                for (int t = 0; t < C::TERMS; ++t) {
+                                    float x0, x1;
+                                    f2_unpack(x, x0, x1);
+                                    const uint32_t h = pack_bf16x2(x0, x1);
+                                    part[t][q] = h;
+                                    if (t + 1 < C::TERMS)
+                                        x = f2_fma(f2_pack(__uint_as_float(h << 16), __uint_as_float(h & 0xFFFF0000u)), f2_pack(-1.f, -1.f), x);
+                                }
+                            }
+#pragma unroll
+                            for (int t = 0; t < C::TERMS; ++t) {
+                                const uint4 v = make_uint4(part[t][0], part[t][1], part[t][2], part[t][3]);
+                                *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + hf * PIECE_HALF + r * 128) = v;
+                                // d = 64: the instruction's upper 64 rows are the same ones again (read by the second threads of the state's rows)
+                                if (D == 64) *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + PIECE_HALF + r * 128) = v;
                             }
                         }
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&kp_full[pb]);
+                    if (lane == 0) mbar_arrive(&kp_full[pat.slot]);
+                    pat.advance(1);
                 }
                 if (!ok) break;
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&dec_empty[buf]);
-                kat.advance(PER_CHUNK);
-                vat.advance(PER_CHUNK);
+                if (lane == 0) {
+                    mbar_arrive(&k_empty[kat.slot]);
+                    mbar_arrive(&dec_empty[buf]);
+                }
+                kat.advance(1);
+                vat.advance(1);
             }
         }
     }
@@ -658,20 +836,15 @@ template <int D, class Table>
 __global__ void __launch_bounds__(kMergeThreads)
 gret_merge_kernel(const GretChunkParams p, const __grid_constant__ Table tab) {
     const int g0 = blockIdx.x + 1;                         // first CTA that starts inside the stream
-    const int64_t H = p.base.H, pos = (int64_t)g0 * p.total / p.groups, per = pos / H;
-    int lo = 0, hi = p.base.B - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (tab.chunk0[mid] <= per) lo = mid; else hi = mid - 1;
-    }
-    const int64_t base = (int64_t)tab.chunk0[lo] * H, chunks = tab.chunk0[lo + 1] - tab.chunk0[lo], h = (pos - base) / chunks;
-    const int64_t begin = base + h * chunks, end = begin + chunks;
-    if (pos == begin || (int64_t)(g0 - 1) * p.total / p.groups > begin) return;       // no cut, or not the stream's first one
+    const int H = p.base.H, pos = p.first_of(g0), lo = sequence_at(p, tab, pos);
+    const int base = tab.chunk0[lo] * H, chunks = tab.chunk0[lo + 1] - tab.chunk0[lo], h = (pos - base) / chunks;
+    const int begin = base + h * chunks, end = begin + chunks;
+    if (pos == begin || p.first_of(g0 - 1) > begin) return;        // no cut, or not the stream's first one
     const int at = (blockIdx.y * kMergeThreads + threadIdx.x) * 4;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (tab.from[lo] >= 0) s = *reinterpret_cast<const float4*>(p.base.state + ((int64_t)tab.from[lo] * H + h) * (D * D) + at);
     *reinterpret_cast<float4*>(p.part + (int64_t)(p.groups + g0 - 1) * (D * D) + at) = s;
-    for (int g = g0; g < p.groups && (int64_t)g * p.total / p.groups < end; ++g) {
+    for (int g = g0; g < p.groups && p.first_of(g) < end; ++g) {
         float4* slot = reinterpret_cast<float4*>(p.part + (int64_t)g * (D * D) + at);
         const float keep = p.part_keep[g];
         const float4 x = *slot;
@@ -683,37 +856,44 @@ gret_merge_kernel(const GretChunkParams p, const __grid_constant__ Table tab) {
     }
 }
 
-template <int D, class Table>
-cudaError_t launch_one(const GretChunkParams& p, const Table& tab, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
-                       cudaStream_t stream) {
-    if (p.split) {
-        gret_chunk_kernel<D, true><<<p.groups, kThreads, GCfg<D>::SMEM_BYTES, stream>>>(tmQ, tmK, tmV, p, tab);
-        cudaError_t e = cudaGetLastError();
-        if (e != cudaSuccess) return e;
-        gret_merge_kernel<D><<<dim3(p.groups - 1, D * D / (4 * kMergeThreads)), kMergeThreads, 0, stream>>>(p, tab);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    }
-    gret_chunk_kernel<D, false><<<p.groups, kThreads, GCfg<D>::SMEM_BYTES, stream>>>(tmQ, tmK, tmV, p, tab);
+template <int D, Pass PASS, class Table>
+cudaError_t launch_pass(const GretChunkParams& p, const Table& tab, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                        cudaStream_t stream) {
+    gret_chunk_kernel<D, PASS><<<p.groups, kThreads, GCfg<D, PASS>::SMEM_BYTES, stream>>>(tmQ, tmK, tmV, p, tab);
     return cudaGetLastError();
 }
 
-template <int D, bool STATE_ONLY>
-cudaError_t setup_one() {
-    cudaError_t e = cudaFuncSetAttribute(gret_chunk_kernel<D, STATE_ONLY, GretChunkTable>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         GCfg<D>::SMEM_BYTES);
+template <int D, class Table>
+cudaError_t launch_one(const GretChunkParams& p, const Table& tab, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                       cudaStream_t stream) {
+    if (!p.split) return launch_pass<D, kWhole>(p, tab, tmQ, tmK, tmV, stream);
+    cudaError_t e = launch_pass<D, kStates>(p, tab, tmQ, tmK, tmV, stream);
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(gret_chunk_kernel<D, STATE_ONLY, GretChunkTableOf<kFewSequences>>,
-                                cudaFuncAttributeMaxDynamicSharedMemorySize, GCfg<D>::SMEM_BYTES);
+    gret_merge_kernel<D><<<dim3(p.groups - 1, D * D / (4 * kMergeThreads)), kMergeThreads, 0, stream>>>(p, tab);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    return launch_pass<D, kMain>(p, tab, tmQ, tmK, tmV, stream);
+}
+
+template <int D, Pass PASS>
+cudaError_t setup_pass() {
+    constexpr int bytes = GCfg<D, PASS>::SMEM_BYTES;
+    cudaError_t e = cudaFuncSetAttribute(gret_chunk_kernel<D, PASS, GretChunkTable>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(gret_chunk_kernel<D, PASS, GretChunkTableOf<kFewSequences>>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+template <int D>
+cudaError_t setup_one() {
+    cudaError_t e = setup_pass<D, kWhole>();
+    if (e != cudaSuccess) return e;
+    if ((e = setup_pass<D, kMain>()) != cudaSuccess) return e;
+    return setup_pass<D, kStates>();
 }
 
 }  // namespace
 
 cudaError_t gret_chunk_kernel_setup() {
-    cudaError_t e = setup_one<128, false>();
-    if (e != cudaSuccess) return e;
-    if ((e = setup_one<128, true>()) != cudaSuccess) return e;
-    if ((e = setup_one<64, false>()) != cudaSuccess) return e;
-    return setup_one<64, true>();
+    const cudaError_t e = setup_one<128>();
+    return e != cudaSuccess ? e : setup_one<64>();
 }
 
 cudaError_t launch_gret_chunk(const GretChunkParams& p, const GretChunkTable& tab, const CUtensorMap& tmQ, const CUtensorMap& tmK,

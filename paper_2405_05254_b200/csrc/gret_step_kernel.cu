@@ -65,7 +65,7 @@ gret_tokens_kernel(const GretParams p, const __grid_constant__ Table tab) {
             dst[0] = make_float4(x[0], x[1], x[2], x[3]);
             dst[1] = make_float4(x[4], x[5], x[6], x[7]);
         }
-        if (tid < m) gamma[tid] = expf(log_decay(p, tok0 + t0 + tid, h));
+        if (tid < m) gamma[tid] = expf(log_decay(p, read_decay(p, tok0 + t0 + tid, h)));
         __syncthreads();
         for (int t = 0; t < m; ++t) {
             const uint64_t g = f2_pack(gamma[t], gamma[t]);

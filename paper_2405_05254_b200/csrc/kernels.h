@@ -297,7 +297,7 @@ struct GretParams {
     int64_t q_stride, k_stride, v_stride, o_stride, decay_stride;
     NormGate norm;
     float scale;
-    float tau;                  // 0: decay holds natural logarithms
+    float inv_tau;              // 0: decay holds natural logarithms; otherwise logits, 1 / tau
     int32_t decay_bf16;
     int32_t B, H, d;
 };
@@ -321,9 +321,11 @@ struct GretChunkTableOf {       // sequences with at least one token
 using GretChunkTable = GretChunkTableOf<kAppendMaxSequences>;
 struct GretChunkParams {
     GretParams base;            // base.B: sequences of the table
-    int64_t total;
+    int32_t total;
     int32_t groups;             // CTAs
-    int32_t split;              // 1: CTA g walks chunks [g total / groups, (g + 1) total / groups); 0: one stream each
+    int32_t split;              // 1: CTA g walks chunks [first_of(g), first_of(g + 1)); 0: one stream each
+    int32_t share, extra;       // total / groups, total % groups
+    __host__ __device__ int32_t first_of(int32_t g) const { return g * share + (g < extra ? g : extra); }
     float* part;                // split: 2 * groups states
     float* part_keep;           // split: decay over a CTA's last segment, groups + 1
     int32_t* status;
