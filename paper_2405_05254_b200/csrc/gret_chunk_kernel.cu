@@ -71,23 +71,25 @@ struct GCfg {
     static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
 };
 
-// The bounded wait of this kernel: one answer for the warp, in few instructions.  The roles' loops together have to stay in the
-// instruction cache of the SM, which is why they are rolled up wherever registers are not indexed by them.  (With everything
-// unrolled, 173 KB instead of 45, a chunk took twice as long.)
-__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, const Abort& ab, int32_t wait_class) {
-    uint32_t polls = 0, t0 = 0;
-    while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
-        uint32_t t;
-        asm volatile("mov.u32 %0, %globaltimer_lo;" : "=r"(t));
-        if (polls++ == 0) t0 = t;
-        const bool late = (int32_t)(t - t0) > (int32_t)kWaitLimitNs || polls >= kWaitMaxPolls;
-        if (__any_sync(0xffffffffu, late || *ab.flag != 0)) {
-            if (late) report_give_up(ab, wait_class);
-            return false;
+// The bounded wait of this kernel: one answer for the warp, in few instructions; what ran out is reported at the role's end.  The roles'
+// loops together have to stay in the instruction cache of the SM, which is why they are rolled up wherever registers are not indexed by
+// them.  (With everything unrolled, 173 KB of code instead of 60, a chunk took twice as long.)
+struct Wait {
+    int32_t what = 0;
+    __device__ __forceinline__ bool operator()(uint64_t* bar, uint32_t parity, int32_t wait_class) {
+        uint32_t polls = 0, t0 = 0;
+        while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
+            uint32_t t;
+            asm volatile("mov.u32 %0, %globaltimer_lo;" : "=r"(t));
+            if (polls == 0) t0 = t;
+            if (__any_sync(0xffffffffu, (int32_t)(t - t0) > (int32_t)kWaitLimitNs || ++polls >= kWaitMaxPolls)) {
+                what = wait_class;
+                return false;
+            }
         }
+        return true;
     }
-    return true;
-}
+};
 
 // A place in a ring of N, and which time round.
 template <int N>
@@ -237,6 +239,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     const uint32_t tmem_base = *tmem_slot;
     const uint32_t sbase = smem_u32(smem);
 
+    Wait wait;
     // every role walks the same segments: `enter` moves to the next one
     Walk<Table> walk(p, tab);
     bool open_end_done = false;
@@ -251,40 +254,47 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         setmaxnreg_dec<kRegsIo>();
         if (warp == 0) {
             // ======================================= TMA producer ================================
-            if (lane == 0 && aligned_ok) {
-                tma_prefetch_desc(&tmK);
-                tma_prefetch_desc(&tmV);
-                if (OUT) tma_prefetch_desc(&tmQ);
-                uint32_t k_armed = 0, q_armed = 0, v_armed = 0;
-                auto load = [&](uint64_t* full, uint64_t* empty, uint32_t places, uint32_t& armed, const CUtensorMap* tm, uint32_t off, int x, int y) {
-                    const uint32_t slot = armed % places;
-                    if (!wait_or_abort(&empty[slot], ((armed / places) & 1u) ^ 1u, ab, kWaitRingEmpty)) return false;
-                    mbar_expect_tx(&full[slot], C::TILE_BYTES);
-                    for (int hf = 0; hf < C::HALVES; ++hf)
-                        tma_load_2d(smem + off + slot * C::TILE_BYTES + hf * HALF_BYTES, tm, x + hf * 64, y, &full[slot]);
-                    ++armed;
-                    return true;
-                };
+            if (aligned_ok) {
+                if (lane == 0) {
+                    tma_prefetch_desc(&tmK);
+                    tma_prefetch_desc(&tmV);
+                    if (OUT) tma_prefetch_desc(&tmQ);
+                }
+                uint32_t armed[3] = {0u, 0u, 0u};          // copies of V, K, Q (the order in which their places become free)
                 bool ok = true;
                 while (ok && enter()) {
                     const int x = walk.h * D;
 #pragma unroll 1
                     for (int c = walk.c; c < walk.c_end; ++c) {
                         const int y = tab.tok0[walk.b] + c * CT;
-                        // (the order in which their places become free)
-                        if (!(ok = load(v_full, v_empty, C::VS, v_armed, &tmV, C::OFF_V, x, y))) break;
-                        if (!(ok = load(k_full, k_empty, C::KS, k_armed, &tmK, C::OFF_K, x, y))) break;
-                        if (OUT && !(ok = load(q_full, q_empty, OUT ? C::QS : 1, q_armed, &tmQ, C::OFF_Q, x, y))) break;
+#pragma unroll
+                        for (int i = 0; i < (OUT ? 3 : 2); ++i) {
+                            const uint32_t places = i == 0 ? C::VS : i == 1 ? C::KS : OUT ? C::QS : 1;
+                            const uint32_t slot = armed[i] % places;
+                            uint64_t* full = (i == 0 ? v_full : i == 1 ? k_full : q_full) + slot;
+                            if (!(ok = wait((i == 0 ? v_empty : i == 1 ? k_empty : q_empty) + slot, ((armed[i] / places) & 1u) ^ 1u, kWaitRingEmpty))) break;
+                            ++armed[i];
+                            if (lane == 0) {
+                                const CUtensorMap* tm = i == 0 ? &tmV : i == 1 ? &tmK : &tmQ;
+                                uint8_t* dst = smem + (i == 0 ? C::OFF_V : i == 1 ? C::OFF_K : C::OFF_Q) + slot * C::TILE_BYTES;
+                                mbar_expect_tx(full, C::TILE_BYTES);
+                                for (int hf = 0; hf < C::HALVES; ++hf) tma_load_2d(dst + hf * HALF_BYTES, tm, x + hf * 64, y, full);
+                            }
+                            __syncwarp();
+                        }
+                        if (!ok) break;
                     }
                 }
                 // no copy may land after the CTA has ended (at once when all went well): the last ones into every place
-                auto drain = [&](uint64_t* full, uint32_t places, uint32_t armed) {
-                    for (uint32_t k = armed > places ? armed - places : 0; k < armed; ++k)
-                        if (!drain_wait(&full[k % places], (k / places) & 1u, ab)) return;
-                };
-                drain(v_full, C::VS, v_armed);
-                drain(k_full, C::KS, k_armed);
-                if (OUT) drain(q_full, OUT ? C::QS : 1, q_armed);
+                if (lane == 0) {
+#pragma unroll
+                    for (int i = 0; i < (OUT ? 3 : 2); ++i) {
+                        const uint32_t places = i == 0 ? C::VS : i == 1 ? C::KS : OUT ? C::QS : 1, n = armed[i];
+#pragma unroll 1
+                        for (uint32_t k = n > places ? n - places : 0; k < n; ++k)
+                            if (!drain_wait((i == 0 ? v_full : i == 1 ? k_full : q_full) + k % places, (k / places) & 1u, ab)) break;
+                    }
+                }
             }
         } else if (warp == 1) {
             // ======================================= issuer of the products ======================
@@ -305,12 +315,12 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         const uint64_t q_desc = make_desc(sbase + C::OFF_Q + qat.slot * C::TILE_BYTES, 16, 1024);
                         const uint64_t v_desc = make_desc(sbase + C::OFF_V + vat.slot * C::TILE_BYTES, HALF_BYTES, 1024);
                         if (OUT) {
-                            if (!(ok = wait_for(&k_full[kat.slot], kat.phase, ab, kWaitRingFull))) break;
-                            if (!(ok = wait_for(&q_full[qat.slot], qat.phase, ab, kWaitRingFull))) break;
+                            if (!(ok = wait(&k_full[kat.slot], kat.phase, kWaitRingFull))) break;
+                            if (!(ok = wait(&q_full[qat.slot], qat.phase, kWaitRingFull))) break;
                             tc_fence_after();
                             const uint64_t k_desc = make_desc(sbase + C::OFF_K + kat.slot * C::TILE_BYTES, 16, 1024);
                             if (elect_one()) {
-#pragma unroll
+#pragma unroll 1
                                 for (int ks = 0; ks < D / 16; ++ks) {
                                     const uint32_t off = (ks >> 2) * HALF_BYTES + (ks & 3) * 32;
                                     umma_ss(tmem_base + COL_SC, q_desc + (off >> 4), k_desc + (off >> 4), idesc_qk, ks > 0 ? 1u : 0u);
@@ -321,18 +331,18 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                             __syncwarp();
                             kat.advance(1);
                         }
-                        if (!(ok = wait_for(&v_full[vat.slot], vat.phase, ab, kWaitRingFull))) break;
-                        if (!(ok = wait_for(ds_empty, ph ^ 1u, ab, kWaitTensor))) break;
+                        if (!(ok = wait(&v_full[vat.slot], vat.phase, kWaitRingFull))) break;
+                        if (!(ok = wait(ds_empty, ph ^ 1u, kWaitTensor))) break;
 #pragma unroll 1
                         for (int e = 0; e < PIECES; ++e) {
                             if (OUT && e == 1) {
                                 // ---- Q S
-                                if (!(ok = wait_for(s_full, ph, ab, kWaitTensor))) break;
-                                if (!(ok = wait_for(o_empty, ph ^ 1u, ab, kWaitTensor))) break;
+                                if (!(ok = wait(s_full, ph, kWaitTensor))) break;
+                                if (!(ok = wait(o_empty, ph ^ 1u, kWaitTensor))) break;
                                 tc_fence_after();
                                 const uint64_t s_desc = make_desc(sbase + C::OFF_S, D * 128, 1024);
                                 if (elect_one()) {
-#pragma unroll
+#pragma unroll 1
                                     for (int ks = 0; ks < D / 16; ++ks) {
                                         const uint32_t off = (ks >> 2) * HALF_BYTES + (ks & 3) * 32;
                                         umma_ss(tmem_base + COL_OI, q_desc + (off >> 4), s_desc + ((ks * 16 * 128) >> 4), idesc_mn, ks > 0 ? 1u : 0u);
@@ -344,7 +354,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                                 qat.advance(1);
                             }
                             // ---- K'^T V, 32 tokens
-                            if (!(ok = wait_for(&kp_full[pat.slot], pat.phase, ab, kWaitTensor))) break;
+                            if (!(ok = wait(&kp_full[pat.slot], pat.phase, kWaitTensor))) break;
                             tc_fence_after();
                             const uint64_t kp_desc = make_desc(sbase + C::OFF_KP + pat.slot * C::PIECE_BYTES, PIECE_HALF, 1024);
                             const uint64_t vp_desc = v_desc + ((e * PIECE * 128) >> 4);
@@ -367,10 +377,10 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         if (!ok) break;
                         if (OUT) {
                             // ---- P V
-                            if (!(ok = wait_for(p_full, ph, ab, kWaitTensor))) break;
+                            if (!(ok = wait(p_full, ph, kWaitTensor))) break;
                             tc_fence_after();
                             if (elect_one()) {
-#pragma unroll
+#pragma unroll 1
                                 for (int ks = 0; ks < CT / 16; ++ks)
                                     umma_ts(tmem_base + COL_OA, tmem_base + COL_SC + ks * 8, v_desc + ((ks * 16 * 128) >> 4), idesc_mn,
                                             ks > 0 ? 1u : 0u);
@@ -422,7 +432,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     const double block_end = __shfl_sync(0xffffffffu, before, lane | 7), chunk_end = __shfl_sync(0xffffffffu, before, 31);
                     before -= sum;
                     const uint32_t buf = it & 1u;
-                    if (!(ok = wait_for(&dec_empty[buf], ((it >> 1) & 1u) ^ 1u, ab, kWaitTensor))) break;
+                    if (!(ok = wait(&dec_empty[buf], ((it >> 1) & 1u) ^ 1u, kWaitTensor))) break;
                     float* dst = dec + buf * C::DEC_FLOATS + lane * 4;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -446,7 +456,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 const __nv_bfloat16* gate = p.base.norm.gate + (int64_t)tab.tok0[walk.b] * p.base.norm.gate_stride + walk.h * D;
 #pragma unroll 1
                 for (int c = walk.c; c < walk.c_end; ++c, ++it) {
-                    if (it > 0 && !(ok = wait_for(sc_full, (it - 1) & 1u, ab, kWaitTensor))) break;
+                    if (it > 0 && !(ok = wait(sc_full, (it - 1) & 1u, kWaitTensor))) break;
                     for (int r = lane; r < CT * C::HALVES; r += 32) {
                         const int t = c * CT + r / C::HALVES;
                         if (t < len)
@@ -466,11 +476,11 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll 1
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                 const uint32_t buf = it & 1u, ph = it & 1u;
-                if (!(ok = wait_for(&dec_full[buf], (it >> 1) & 1u, ab, kWaitTensor))) break;
+                if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
                 const float* whole = dec + buf * C::DEC_FLOATS;                 // negated
                 const float* rest = whole + CT;
                 const float wi = -whole[i], ri = -rest[i];
-                if (!(ok = wait_for(sc_full, ph, ab, kWaitTensor))) break;
+                if (!(ok = wait(sc_full, ph, kWaitTensor))) break;
                 tc_fence_after();
                 uint32_t w[8];
                 float s[16];
@@ -545,41 +555,54 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll 1
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                 const uint32_t buf = it & 1u, ph = it & 1u;
-                if (!(ok = wait_for(&dec_full[buf], (it >> 1) & 1u, ab, kWaitTensor))) break;
+                if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
                 const float ei = exp2_parts(-dec[buf * C::DEC_FLOATS + i], -dec[buf * C::DEC_FLOATS + CT + i]) * scale;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&dec_empty[buf]);
-                if (!(ok = wait_for(o_full, ph, ab, kWaitTensor))) break;
+                if (!(ok = wait(o_full, ph, kWaitTensor))) break;
                 tc_fence_after();
-                // 16 channels of the row
-                auto channels = [&](int j, float (&y)[16]) {
-                    float x[16];
-                    tmem_ld16(oa + j, y);
+                // 16 channels of the row: by * (state's part) + a * (chunk's part) + add
+                auto channels = [&](int j, float by, float a, float add, uint64_t (&y)[8]) {
+                    float x[16], z[16];
+                    tmem_ld16(oa + j, z);
                     tmem_ld16(oi + j, x);
+                    const uint64_t by2 = f2_pack(by, by), a2 = f2_pack(a, a), add2 = f2_pack(add, add);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int q = 0; q < 16; ++q) y[q] = fmaf(ei, x[q], scale * y[q]);
+                    for (int q = 0; q < 8; ++q)
+                        y[q] = f2_fma(by2, f2_pack(x[2 * q], x[2 * q + 1]), f2_fma(a2, f2_pack(z[2 * q], z[2 * q + 1]), add2));
                 };
-                float mean = 0.f, inv = 1.f;
+                float by = ei, of = scale, add = 0.f;      // what the row's channels are made of: the normalisation goes into it
                 if (nm.on) {
                     // sums of the differences from the row's first channel (rms: from zero) and of their squares: one of d values is at most
                     // sqrt(d) standard deviations from the mean, so the difference of the two loses at most d roundings
-                    float first = 0.f, s1[2] = {0.f, 0.f}, s2[2] = {0.f, 0.f};
+                    float first = 0.f;
+                    if (!nm.rms) {
+                        float x, z;
+                        tmem_ld1(oa, z);
+                        tmem_ld1(oi, x);
+                        tmem_wait_ld();
+                        first = fmaf(ei, x, scale * z);
+                    }
+                    uint64_t s1 = 0ull, s2 = 0ull;
 #pragma unroll 1
                     for (int j = 0; j < D; j += 16) {
-                        float y[16];
-                        channels(j, y);
-                        if (j == 0 && !nm.rms) first = y[0];
+                        uint64_t y[8];
+                        channels(j, ei, scale, -first, y);
 #pragma unroll
-                        for (int q = 0; q < 16; ++q) {
-                            const float e = y[q] - first;
-                            s1[q & 1] += e;
-                            s2[q & 1] = fmaf(e, e, s2[q & 1]);
+                        for (int q = 0; q < 8; ++q) {
+                            s1 = f2_add(s1, y[q]);
+                            s2 = f2_fma(y[q], y[q], s2);
                         }
                     }
-                    const float m1 = nm.rms ? 0.f : (s1[0] + s1[1]) * (1.f / D);
-                    mean = first + m1;
-                    inv = 1.f / sqrtf(fmaxf(fmaf(-m1, m1, (s2[0] + s2[1]) * (1.f / D)), 0.f) + nm.eps);
+                    float a0, a1, b0, b1;
+                    f2_unpack(s1, a0, a1);
+                    f2_unpack(s2, b0, b1);
+                    const float m1 = nm.rms ? 0.f : (a0 + a1) * (1.f / D);
+                    const float inv = 1.f / sqrtf(fmaxf(fmaf(-m1, m1, (b0 + b1) * (1.f / D)), 0.f) + nm.eps);
+                    by *= inv;
+                    of *= inv;
+                    add = -(first + m1) * inv;
                 }
                 // Rows leave (and the gate's come) 32 channels at a time through shared memory, so that a warp's access covers 8 rows, not 32.
                 const int t0 = c * CT + quad * 32, lrow = lane >> 2, lch = lane & 3;
@@ -596,48 +619,51 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 if (nm.gate) ask(0);
 #pragma unroll 1
                 for (int j = 0; j < D; j += 32) {
-                    uint4 mine[4];
                     if (nm.gate) {
 #pragma unroll
                         for (int r = 0; r < 4; ++r) *staged(lrow + 8 * r, lch) = g[r];
                         __syncwarp();
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) mine[q] = *staged(lane, q);
-                        __syncwarp();
                         if (j + 32 < D) ask(j + 32);
                     }
-#pragma unroll
-                    for (int e = 0; e < 32; e += 16) {
-                        float y[16];
-                        channels(j + e, y);
+#pragma unroll 1
+                    for (int e = 0; e < 32; e += 16) {     // (a thread's row of the gate gives way to its row of the output)
+                        uint64_t y[8];
+                        channels(j + e, by, of, add, y);
                         if (nm.on) {
+                            uint64_t f[8];
+                            auto eight = [&](const uint4& v, int at8) {
+                                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                            for (int q = 0; q < 16; ++q) y[q] = (y[q] - mean) * inv;
-                            float f[8];
+                                for (int q = 0; q < 4; ++q) f[at8 + q] = f2_pack(__uint_as_float(w[q] << 16), __uint_as_float(w[q] & 0xFFFF0000u));
+                            };
                             if (nm.gain) {
+                                eight(__ldg(reinterpret_cast<const uint4*>(nm.gain + at + j + e)), 0);
+                                eight(__ldg(reinterpret_cast<const uint4*>(nm.gain + at + j + e) + 1), 4);
 #pragma unroll
-                                for (int q = 0; q < 16; ++q) {
-                                    if (q % 8 == 0) unpack8(__ldg(reinterpret_cast<const uint4*>(nm.gain + at + j + e + q)), f);
-                                    y[q] *= f[q % 8];
-                                }
+                                for (int q = 0; q < 8; ++q) y[q] = f2_mul(y[q], f[q]);
                             }
                             if (nm.bias) {
+                                eight(__ldg(reinterpret_cast<const uint4*>(nm.bias + at + j + e)), 0);
+                                eight(__ldg(reinterpret_cast<const uint4*>(nm.bias + at + j + e) + 1), 4);
 #pragma unroll
-                                for (int q = 0; q < 16; ++q) {
-                                    if (q % 8 == 0) unpack8(__ldg(reinterpret_cast<const uint4*>(nm.bias + at + j + e + q)), f);
-                                    y[q] += f[q % 8];
-                                }
+                                for (int q = 0; q < 8; ++q) y[q] = f2_add(y[q], f[q]);
                             }
                             if (nm.gate) {
+                                eight(*staged(lane, e / 8), 0);
+                                eight(*staged(lane, e / 8 + 1), 4);
 #pragma unroll
-                                for (int q = 0; q < 16; ++q) {
-                                    if (q % 8 == 0) unpack8(mine[(e + q) / 8], f);
-                                    y[q] *= swish(f[q % 8]);
-                                }
+                                for (int q = 0; q < 8; ++q) y[q] = f2_swish_mul(f[q], y[q]);
                             }
                         }
-                        *staged(lane, e / 8) = pack8(*reinterpret_cast<float(*)[8]>(&y[0]));
-                        *staged(lane, e / 8 + 1) = pack8(*reinterpret_cast<float(*)[8]>(&y[8]));
+                        uint32_t w[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            float y0, y1;
+                            f2_unpack(y[q], y0, y1);
+                            w[q] = pack_bf16x2(y0, y1);
+                        }
+                        *staged(lane, e / 8) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *staged(lane, e / 8 + 1) = make_uint4(w[4], w[5], w[6], w[7]);
                     }
                     if (j + 32 == D) {                     // all of it has been read
                         tc_fence_before();
@@ -688,7 +714,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                 const uint32_t buf = it & 1u, ph = it & 1u;
                 if (OUT) {
-                    if (!(ok = wait_for(s_empty, ph ^ 1u, ab, kWaitTensor))) break;
+                    if (!(ok = wait(s_empty, ph ^ 1u, kWaitTensor))) break;
 #pragma unroll
                     for (int j = 0; j < N; j += 8) {
                         const int ch = (col + j) / 8;
@@ -699,7 +725,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     __syncwarp();
                     if (lane == 0) mbar_arrive(s_full);
                 }
-                if (!(ok = wait_for(&dec_full[buf], (it >> 1) & 1u, ab, kWaitTensor))) break;
+                if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
                 const float whole = -dec[buf * C::DEC_FLOATS + CT - 1], rest = -dec[buf * C::DEC_FLOATS + 2 * CT - 1];
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&dec_empty[buf]);
@@ -708,7 +734,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     all_whole += whole;
                     all_rest += (double)rest;
                 }
-                if (!(ok = wait_for(ds_full, ph, ab, kWaitTensor))) break;
+                if (!(ok = wait(ds_full, ph, kWaitTensor))) break;
                 tc_fence_after();
 #pragma unroll
                 for (int blk = 0; blk < N / 16; ++blk) {
@@ -751,12 +777,12 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                 const uint32_t buf = it & 1u;
                 const int valid = len - c * CT;            // tokens of the sequence from here on
-                if (!(ok = wait_for(&dec_full[buf], (it >> 1) & 1u, ab, kWaitTensor))) break;
+                if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
                 const float* weight = dec + buf * C::DEC_FLOATS + 3 * CT + row;
-                if (!(ok = wait_for(&k_full[kat.slot], kat.phase, ab, kWaitRingFull))) break;
+                if (!(ok = wait(&k_full[kat.slot], kat.phase, kWaitRingFull))) break;
                 if (valid < CT) {
                     // rows behind the sequence are the next one's, or none: they may hold anything, and 0 times that is not 0
-                    if (!(ok = wait_for(&v_full[vat.slot], vat.phase, ab, kWaitRingFull))) break;
+                    if (!(ok = wait(&v_full[vat.slot], vat.phase, kWaitRingFull))) break;
                     if (l >= valid) {
 #pragma unroll 1
                         for (int q = 0; q < 8 * C::HALVES; ++q)
@@ -766,15 +792,15 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 }
 #pragma unroll 1
                 for (int e = 0; e < PIECES; ++e) {
-                    if (!(ok = wait_for(&kp_empty[pat.slot], pat.phase ^ 1u, ab, kWaitTensor))) break;
+                    if (!(ok = wait(&kp_empty[pat.slot], pat.phase ^ 1u, kWaitTensor))) break;
                     const uint8_t* src = smem + C::OFF_K + kat.slot * C::TILE_BYTES + e * PIECE_HALF + at;
                     uint8_t* dst = smem + C::OFF_KP + pat.slot * C::PIECE_BYTES + at;
-#pragma unroll
+#pragma unroll 1
                     for (int r = 0; r < PIECE; r += 16) {
                         const float w = weight[e * PIECE + r];
                         const bool in = e * PIECE + r + row < valid;
                         const uint64_t w2 = f2_pack(w, w);
-#pragma unroll
+#pragma unroll 1
                         for (int hf = 0; hf < C::HALVES; ++hf) {
                             uint4 raw = *reinterpret_cast<const uint4*>(src + hf * HALF_BYTES + r * 128);
                             if (!in) raw = make_uint4(0u, 0u, 0u, 0u);
@@ -819,6 +845,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
     }
 
+    if (wait.what != 0 && lane == 0) report_give_up(ab, wait.what);
     tc_fence_before();
     __syncthreads();
     if (warp == 1) {
