@@ -759,7 +759,7 @@ struct GretPlan {
     int64_t total;              // chunks of all heads
     int32_t groups, split;
     size_t part_bytes;          // workspace: parts' states, then their decays
-    size_t bytes() const { return split ? part_bytes + (size_t)(groups + 1) * sizeof(float) : 0; }
+    size_t bytes() const { return split ? part_bytes + (size_t)3 * groups * sizeof(float) : 0; }
 };
 
 // Whole streams, one per CTA (longest first), or equal ranges of chunks that cut streams: the latter pay a second pass over K and V.
@@ -792,7 +792,7 @@ void plan_gret(const yoco_gret_shape& s, const int32_t* len_host, const GretTabl
     const double share = cut > 0 ? (double)((out->total + cut - 1) / cut) : 0.0;
     out->split = cut > 1 && share * (1.0 + kGretStateCost) + kGretSplitCost < whole;
     out->groups = (int32_t)(out->split ? cut : streams);
-    out->part_bytes = (size_t)2 * out->groups * s.d * s.d * sizeof(float);
+    out->part_bytes = (size_t)3 * out->groups * s.d * s.d * sizeof(float);
 }
 
 int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay, const yoco_norm_gate* norm,

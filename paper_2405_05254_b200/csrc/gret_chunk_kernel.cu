@@ -5,22 +5,22 @@
 //     S' = 2^b_C S + sum_j (2^(b_C - b_j) k_j)^T v_j.
 // A CTA walks a contiguous range of chunks, of one (sequence, head) stream or of several one after the other, with the state in the
 // registers of two warpgroups.  768 threads:
-//   warp 0       TMA producer: K, Q, V tiles (128 tokens x d, 128-byte swizzle) through one ring
-//   warp 1       issuer of all products: Q K^T -> SC;  K'^T V -> DS;  Q S -> OI;  P V -> OA    (tensor memory, fp32)
+//   warp 0       TMA producer: K, Q, V tiles (128 tokens x d, 128-byte swizzle)
+//   warp 1       issuer of all products: Q K^T -> SC;  K'^T V -> DS;  Q S and P V -> O[n & 1]    (tensor memory, fp32)
 //   warp 2       decays: prefix sums of the logarithms in 64 bits, kept as integer part and rest (b_i - b_j is the difference of
 //                both: exact to 2^-24 however strong the decays before j were), and the factors that depend on one token alone
-//   warpgroup 1  thread = token: P (bf16, over the scores' own columns: it goes to P V from tensor memory)
-//   warpgroup 2  thread = token: the chunk's output: scale, normalisation, gate, rounding, store
-//   warpgroups 3, 4  thread = half a row of the state: S' from S and DS in fp32; S in bf16 to shared memory for the next chunk's Q S
-//   warpgroup 5  K' = 2^(b_C - b_j) k_j, in pieces of 16 tokens through a ring of their own
+//   warp 3       asks for the gate's rows, a chunk ahead
+//   warpgroup 1  thread = token: P (bf16, over the scores' own columns: it goes to P V from tensor memory); 2^b_i times Q S, in place
+//   warpgroups 2, 5  thread = token, every other chunk each: the output: scale, normalisation, gate, rounding, store
+//   warpgroups 3, 4  K' = 2^(b_C - b_j) k_j, in pieces of 32 tokens; thread = half a row of the state: S' from S and DS in fp32,
+//                S in bf16 to shared memory for Q S
 // Decays of P: in the 32 x 32 blocks on the diagonal one exponential per element; below it 2^(b_i - m) 2^(m - b_j), m the value at the
 // end of j's block: both factors are at most 1, and the second is the same for all rows.
 // Roundings: P and the copy of S that multiplies Q go to bf16 (half a step, 2^-9 of the value, like the output's own).  K' goes to
 // the tensor cores as a sum of bf16: where the sums leave the kernel as a state, of three (24 bits; with one it would be 1.7e-3 off (2-norm),
-// with two 2.7e-6), where they only multiply Q inside, of two.
+// with two 2e-6), where they only multiply Q inside, of two.
 //
-// Order of the products per chunk: Q K^T, first half of K'^T V, Q S, second half, P V.  None waits for work that was not begun a product or
-// more earlier: P has K'^T V and Q S to be ready in, the state has P V, the next Q K^T and the half behind it, the output the same.
+// Order of the products per chunk: Q K^T, a quarter of K'^T V, Q S, the other three, P V.
 #include "gret.cuh"
 #include "kernels.h"
 #include "ptx.cuh"
@@ -39,34 +39,32 @@ constexpr int PIECES = CT / PIECE;
 constexpr int PIECE_HALF = PIECE * 128;        // 64 channels of a piece of one of K's parts
 constexpr int TERM_BYTES = 2 * PIECE_HALF;
 constexpr uint32_t TMEM_COLS = 512;
-constexpr uint32_t COL_SC = 0, COL_OA = 128, COL_OI = 256, COL_DS = 384;
+constexpr uint32_t COL_SC = 0, COL_O = 128, COL_DS = 384;     // two buffers of O
 // Registers per thread after the split; the CTA starts with 80 each.
-constexpr int kRegsIo = 72, kRegsP = 72, kRegsOut = 104, kRegsState = 88, kRegsKeys = 56;
-static_assert(kRegsIo + kRegsP + kRegsOut + 2 * kRegsState + kRegsKeys <= 6 * 80, "register pool of the CTA");
+constexpr int kRegsIo = 64, kRegsP = 64, kRegsOut = 64, kRegsState = 112;
+static_assert(kRegsIo + kRegsP + 2 * kRegsOut + 2 * kRegsState <= 6 * 80, "register pool of the CTA");
+constexpr int kTerms = 3;                      // parts of K', where a state leaves; otherwise kTermsInside
+constexpr int kTermsInside = 2;
 
-// What a CTA does: the whole; the whole, where the state pass has the states that leave (K' in two parts); the states alone.
-enum Pass { kWhole, kMain, kStates };
-
-template <int D, Pass PASS>
+// STATES: only the states, of the segments that streams are cut into.
+template <int D, bool STATES>
 struct GCfg {
-    static constexpr bool OUT = PASS != kStates;
     static constexpr int HALVES = D / 64;
     static constexpr int TILE_BYTES = HALVES * HALF_BYTES;
-    static constexpr int TERMS = PASS == kMain ? 2 : 3;
-    static constexpr int PIECE_BYTES = TERMS * TERM_BYTES;
+    static constexpr int PIECE_BYTES = kTerms * TERM_BYTES;
     // Tiles of K, Q and V in shared memory.  K and Q are given back early (once scored and turned into K', once multiplied by S), V last.
-    static constexpr int KS = D == 64 || !OUT ? 2 : 1, QS = !OUT ? 0 : D == 64 ? 2 : 1, VS = D == 64 ? 3 : 2;
-    static constexpr int KP_STAGES = OUT && PASS == kWhole ? 2 : 3;
+    static constexpr int KS = D == 64 || STATES ? 2 : 1, QS = STATES ? 0 : D == 64 ? 2 : 1, VS = D == 64 ? 4 : 2;
+    static constexpr int KP_STAGES = 2;                // (pieces of a chunk: 4, so piece e always goes to place e % 2)
     static constexpr int OFF_K = 0;
     static constexpr int OFF_Q = OFF_K + KS * TILE_BYTES;
     static constexpr int OFF_V = OFF_Q + QS * TILE_BYTES;
     static constexpr int OFF_KP = OFF_V + VS * TILE_BYTES;
     static constexpr int OFF_S = OFF_KP + KP_STAGES * PIECE_BYTES;
-    static constexpr int OFF_ROWS = OFF_S + (OUT ? D * D * 2 : 0);      // output: 32 rows x 32 channels a warp
-    static constexpr int OFF_DEC = OFF_ROWS + (OUT ? 4 * 2048 : 0);
+    static constexpr int OFF_ROWS = OFF_S + (STATES ? 0 : D * D * 2);    // output: 32 rows x 16 channels a warp
+    static constexpr int OFF_DEC = OFF_ROWS + (STATES ? 0 : 8 * 1024);
     static constexpr int DEC_FLOATS = 4 * CT;          // integer parts and rests of -b_j; 2^(m - b_j); 2^(b_C - b_j)
     static constexpr int OFF_BAR = OFF_DEC + 2 * DEC_FLOATS * 4;
-    static constexpr int NUM_BARS = 2 * (KS + QS + VS) + 2 * KP_STAGES + 13;
+    static constexpr int NUM_BARS = 2 * (KS + QS + VS) + 2 * KP_STAGES + 16;
     static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16;
     static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
 };
@@ -91,19 +89,11 @@ struct Wait {
     }
 };
 
-// A place in a ring of N, and which time round.
+// The place of use n in a ring of N (a power of two), and the parity of its time round.
 template <int N>
-struct Place {
-    uint32_t slot, phase;
-    __device__ __forceinline__ explicit Place(uint32_t first) : slot(first % N), phase((first / N) & 1u) {}
-    __device__ __forceinline__ void advance(uint32_t by) {
-        slot += by;
-        if (slot >= (uint32_t)N) {
-            slot -= N;
-            phase ^= 1u;
-        }
-    }
-};
+__device__ __forceinline__ uint32_t place(uint32_t n) { return n & (uint32_t)(N - 1); }
+template <int N>
+__device__ __forceinline__ uint32_t round_of(uint32_t n) { return (n / (uint32_t)N) & 1u; }
 
 // The sequence of a place in the flat space.
 template <class Table>
@@ -148,23 +138,17 @@ struct Walk {
         pos += c_end - c;
         return true;
     }
-    // State-only pass: straight to the segment that the range ends in, if its stream goes on behind it.
-    __device__ __forceinline__ bool enter_open_end() {
-        bool any = false;
-#pragma unroll 1
-        while (enter()) any = true;
-        return any && c_end < chunks;
-    }
+    __device__ __forceinline__ bool whole_stream() const { return c == 0 && c_end == chunks; }
 };
 
 __device__ __forceinline__ float exp2_parts(float whole, float rest) { return exp2f(whole) * exp2f(rest); }
 
-template <int D, Pass PASS, class Table>
+template <int D, bool STATES, class Table>
 __global__ void __launch_bounds__(kThreads, 1)
 gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                   const GretChunkParams p, const __grid_constant__ Table tab) {
-    using C = GCfg<D, PASS>;
-    constexpr bool OUT = C::OUT;
+    using C = GCfg<D, STATES>;
+    constexpr int QS = STATES ? 1 : C::QS;
 
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
@@ -178,15 +162,16 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     uint64_t* kp_empty = kp_full + C::KP_STAGES;
     uint64_t* dec_full = kp_empty + C::KP_STAGES;          // [2]
     uint64_t* dec_empty = dec_full + 2;                    // [2]
-    uint64_t* sc_full = dec_full + 4;
-    uint64_t* p_full = dec_full + 5;
-    uint64_t* ds_full = dec_full + 6;
-    uint64_t* ds_empty = dec_full + 7;
-    uint64_t* s_full = dec_full + 8;
-    uint64_t* s_empty = dec_full + 9;
-    uint64_t* o_full = dec_full + 10;
-    uint64_t* o_empty = dec_full + 11;
-    uint64_t* drain_bar = dec_full + 12;
+    uint64_t* o_full = dec_full + 4;                       // [2]
+    uint64_t* o_empty = dec_full + 6;                      // [2]
+    uint64_t* sc_full = dec_full + 8;
+    uint64_t* qs_full = dec_full + 9;
+    uint64_t* p_full = dec_full + 10;
+    uint64_t* ds_full = dec_full + 11;
+    uint64_t* ds_empty = dec_full + 12;
+    uint64_t* s_full = dec_full + 13;
+    uint64_t* s_empty = dec_full + 14;
+    uint64_t* drain_bar = dec_full + 15;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     float* dec = reinterpret_cast<float*>(smem + C::OFF_DEC);
@@ -200,7 +185,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         if (!aligned_ok) atomicCAS(p.status, 0, status_word(kWaitMisaligned, linear_cta()));
         for (int i = 0; i < C::KS; ++i) {
             mbar_init(&k_full[i], 1);
-            mbar_init(&k_empty[i], OUT ? 5 : 4);           // the warps that make K', and Q K^T
+            mbar_init(&k_empty[i], STATES ? 8 : 9);        // the warps that make K', and Q K^T
         }
         for (int i = 0; i < C::QS; ++i) {
             mbar_init(&q_full[i], 1);
@@ -211,21 +196,22 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             mbar_init(&v_empty[i], 1);
         }
         for (int i = 0; i < C::KP_STAGES; ++i) {
-            mbar_init(&kp_full[i], 4);
+            mbar_init(&kp_full[i], 8);
             mbar_init(&kp_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&dec_full[i], 1);
-            mbar_init(&dec_empty[i], OUT ? 20 : 12);
+            mbar_init(&dec_empty[i], STATES ? 8 : 12);
+            mbar_init(&o_full[i], 1);
+            mbar_init(&o_empty[i], 4);
         }
         mbar_init(sc_full, 1);
+        mbar_init(qs_full, 1);
         mbar_init(p_full, 4);
         mbar_init(ds_full, 1);
         mbar_init(ds_empty, 8);
         mbar_init(s_full, 8);
         mbar_init(s_empty, 1);
-        mbar_init(o_full, 1);
-        mbar_init(o_empty, 4);
         mbar_init(drain_bar, 1);
         mbar_fence_init();
     }
@@ -242,13 +228,13 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     Wait wait;
     // every role walks the same segments: `enter` moves to the next one
     Walk<Table> walk(p, tab);
-    bool open_end_done = false;
     auto enter = [&]() -> bool {
-        if (OUT) return walk.enter();
-        if (open_end_done) return false;
-        open_end_done = true;
-        return walk.enter_open_end();
+        while (walk.enter())
+            if (!STATES || !walk.whole_stream()) return true;
+        return false;
     };
+    // parts of K': the state of a whole stream leaves with this kernel, those of cut ones come from the state-only pass
+    auto terms_of = [&]() { return STATES || walk.whole_stream() ? kTerms : kTermsInside; };
 
     if (warp < 4) {
         setmaxnreg_dec<kRegsIo>();
@@ -258,7 +244,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 if (lane == 0) {
                     tma_prefetch_desc(&tmK);
                     tma_prefetch_desc(&tmV);
-                    if (OUT) tma_prefetch_desc(&tmQ);
+                    if (!STATES) tma_prefetch_desc(&tmQ);
                 }
                 uint32_t armed[3] = {0u, 0u, 0u};          // copies of V, K, Q (the order in which their places become free)
                 bool ok = true;
@@ -268,9 +254,9 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     for (int c = walk.c; c < walk.c_end; ++c) {
                         const int y = tab.tok0[walk.b] + c * CT;
 #pragma unroll
-                        for (int i = 0; i < (OUT ? 3 : 2); ++i) {
-                            const uint32_t places = i == 0 ? C::VS : i == 1 ? C::KS : OUT ? C::QS : 1;
-                            const uint32_t slot = armed[i] % places;
+                        for (int i = 0; i < (STATES ? 2 : 3); ++i) {
+                            const uint32_t places = i == 0 ? C::VS : i == 1 ? C::KS : QS;
+                            const uint32_t slot = armed[i] & (places - 1);
                             uint64_t* full = (i == 0 ? v_full : i == 1 ? k_full : q_full) + slot;
                             if (!(ok = wait((i == 0 ? v_empty : i == 1 ? k_empty : q_empty) + slot, ((armed[i] / places) & 1u) ^ 1u, kWaitRingEmpty))) break;
                             ++armed[i];
@@ -288,8 +274,8 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 // no copy may land after the CTA has ended (at once when all went well): the last ones into every place
                 if (lane == 0) {
 #pragma unroll
-                    for (int i = 0; i < (OUT ? 3 : 2); ++i) {
-                        const uint32_t places = i == 0 ? C::VS : i == 1 ? C::KS : OUT ? C::QS : 1, n = armed[i];
+                    for (int i = 0; i < (STATES ? 2 : 3); ++i) {
+                        const uint32_t places = i == 0 ? C::VS : i == 1 ? C::KS : QS, n = armed[i];
 #pragma unroll 1
                         for (uint32_t k = n > places ? n - places : 0; k < n; ++k)
                             if (!drain_wait((i == 0 ? v_full : i == 1 ? k_full : q_full) + k % places, (k / places) & 1u, ab)) break;
@@ -302,23 +288,21 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 constexpr uint32_t idesc_qk = make_idesc(CT, false);
                 constexpr uint32_t idesc_mn = make_idesc(D, true);              // B with its columns contiguous: V, S
                 constexpr uint32_t idesc_kv = idesc_mn | (1u << 15);            // and A with its rows contiguous: K'
-                Place<C::KS> kat(0);
-                Place<OUT ? C::QS : 1> qat(0);
-                Place<C::VS> vat(0);
-                Place<C::KP_STAGES> pat(0);
                 uint32_t it = 0;
                 bool ok = true;
                 while (ok && enter()) {
+                    const int terms = terms_of();
 #pragma unroll 1
                     for (int c = walk.c; c < walk.c_end; ++c, ++it) {
-                        const uint32_t ph = it & 1u;
-                        const uint64_t q_desc = make_desc(sbase + C::OFF_Q + qat.slot * C::TILE_BYTES, 16, 1024);
-                        const uint64_t v_desc = make_desc(sbase + C::OFF_V + vat.slot * C::TILE_BYTES, HALF_BYTES, 1024);
-                        if (OUT) {
-                            if (!(ok = wait(&k_full[kat.slot], kat.phase, kWaitRingFull))) break;
-                            if (!(ok = wait(&q_full[qat.slot], qat.phase, kWaitRingFull))) break;
+                        const uint32_t ph = it & 1u, o_ph = (it >> 1) & 1u;
+                        const uint32_t o_cols = tmem_base + COL_O + ph * 128;
+                        const uint64_t q_desc = make_desc(sbase + C::OFF_Q + place<QS>(it) * C::TILE_BYTES, 16, 1024);
+                        const uint64_t v_desc = make_desc(sbase + C::OFF_V + place<C::VS>(it) * C::TILE_BYTES, HALF_BYTES, 1024);
+                        if (!STATES) {
+                            if (!(ok = wait(&k_full[place<C::KS>(it)], round_of<C::KS>(it), kWaitRingFull))) break;
+                            if (!(ok = wait(&q_full[place<QS>(it)], round_of<QS>(it), kWaitRingFull))) break;
                             tc_fence_after();
-                            const uint64_t k_desc = make_desc(sbase + C::OFF_K + kat.slot * C::TILE_BYTES, 16, 1024);
+                            const uint64_t k_desc = make_desc(sbase + C::OFF_K + place<C::KS>(it) * C::TILE_BYTES, 16, 1024);
                             if (elect_one()) {
 #pragma unroll 1
                                 for (int ks = 0; ks < D / 16; ++ks) {
@@ -326,70 +310,66 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                                     umma_ss(tmem_base + COL_SC, q_desc + (off >> 4), k_desc + (off >> 4), idesc_qk, ks > 0 ? 1u : 0u);
                                 }
                                 umma_commit(sc_full);
-                                umma_commit(&k_empty[kat.slot]);
+                                umma_commit(&k_empty[place<C::KS>(it)]);
                             }
                             __syncwarp();
-                            kat.advance(1);
                         }
-                        if (!(ok = wait(&v_full[vat.slot], vat.phase, kWaitRingFull))) break;
+                        if (!(ok = wait(&v_full[place<C::VS>(it)], round_of<C::VS>(it), kWaitRingFull))) break;
                         if (!(ok = wait(ds_empty, ph ^ 1u, kWaitTensor))) break;
 #pragma unroll 1
                         for (int e = 0; e < PIECES; ++e) {
-                            if (OUT && e == 1) {
+                            if (!STATES && e == 1) {
                                 // ---- Q S
                                 if (!(ok = wait(s_full, ph, kWaitTensor))) break;
-                                if (!(ok = wait(o_empty, ph ^ 1u, kWaitTensor))) break;
+                                if (!(ok = wait(&o_empty[ph], o_ph ^ 1u, kWaitTensor))) break;
                                 tc_fence_after();
                                 const uint64_t s_desc = make_desc(sbase + C::OFF_S, D * 128, 1024);
                                 if (elect_one()) {
 #pragma unroll 1
                                     for (int ks = 0; ks < D / 16; ++ks) {
                                         const uint32_t off = (ks >> 2) * HALF_BYTES + (ks & 3) * 32;
-                                        umma_ss(tmem_base + COL_OI, q_desc + (off >> 4), s_desc + ((ks * 16 * 128) >> 4), idesc_mn, ks > 0 ? 1u : 0u);
+                                        umma_ss(o_cols, q_desc + (off >> 4), s_desc + ((ks * 16 * 128) >> 4), idesc_mn, ks > 0 ? 1u : 0u);
                                     }
+                                    umma_commit(qs_full);
                                     umma_commit(s_empty);
-                                    umma_commit(&q_empty[qat.slot]);
+                                    umma_commit(&q_empty[place<QS>(it)]);
                                 }
                                 __syncwarp();
-                                qat.advance(1);
                             }
                             // ---- K'^T V, 32 tokens
-                            if (!(ok = wait(&kp_full[pat.slot], pat.phase, kWaitTensor))) break;
+                            if (!(ok = wait(&kp_full[(e & 1)], ((uint32_t)(e >> 1) & 1u), kWaitTensor))) break;
                             tc_fence_after();
-                            const uint64_t kp_desc = make_desc(sbase + C::OFF_KP + pat.slot * C::PIECE_BYTES, PIECE_HALF, 1024);
+                            const uint64_t kp_desc = make_desc(sbase + C::OFF_KP + (e & 1) * C::PIECE_BYTES, PIECE_HALF, 1024);
                             const uint64_t vp_desc = v_desc + ((e * PIECE * 128) >> 4);
                             if (elect_one()) {
+#pragma unroll 1
+                                for (int t = 0; t < terms; ++t)
 #pragma unroll
-                                for (int j = 0; j < PIECE / 16 * C::TERMS; ++j) {
-                                    const uint32_t ks = j / C::TERMS, t = j % C::TERMS;
-                                    umma_ss(tmem_base + COL_DS, kp_desc + ((t * TERM_BYTES + ks * 2048) >> 4), vp_desc + ((ks * 2048) >> 4), idesc_kv,
-                                            e > 0 || j > 0 ? 1u : 0u);
-                                }
-                                umma_commit(&kp_empty[pat.slot]);
+                                    for (int ks = 0; ks < PIECE / 16; ++ks)
+                                        umma_ss(tmem_base + COL_DS, kp_desc + ((t * TERM_BYTES + ks * 2048) >> 4), vp_desc + ((ks * 2048) >> 4), idesc_kv,
+                                                e > 0 || t > 0 || ks > 0 ? 1u : 0u);
+                                umma_commit(&kp_empty[(e & 1)]);
                                 if (e == PIECES - 1) {
                                     umma_commit(ds_full);
-                                    if (!OUT) umma_commit(&v_empty[vat.slot]);
+                                    if (STATES) umma_commit(&v_empty[place<C::VS>(it)]);
                                 }
                             }
                             __syncwarp();
-                            pat.advance(1);
                         }
                         if (!ok) break;
-                        if (OUT) {
-                            // ---- P V
+                        if (!STATES) {
+                            // ---- P V, on top of Q S
                             if (!(ok = wait(p_full, ph, kWaitTensor))) break;
                             tc_fence_after();
                             if (elect_one()) {
 #pragma unroll 1
                                 for (int ks = 0; ks < CT / 16; ++ks)
-                                    umma_ts(tmem_base + COL_OA, tmem_base + COL_SC + ks * 8, v_desc + ((ks * 16 * 128) >> 4), idesc_mn,
-                                            ks > 0 ? 1u : 0u);
-                                umma_commit(o_full);
-                                umma_commit(&v_empty[vat.slot]);
+                                    umma_ts(o_cols, tmem_base + COL_SC + ks * 8, v_desc + ((ks * 16 * 128) >> 4), idesc_mn, 1u);
+                                umma_commit(&o_full[ph]);
+                                umma_commit(&v_empty[place<C::VS>(it)]);
                             }
                             __syncwarp();
                         }
-                        vat.advance(1);
                     }
                 }
                 // nothing issued may still run when tensor memory is released
@@ -446,8 +426,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     if (lane == 0) mbar_arrive(&dec_full[buf]);
                 }
             }
-        }
-        else if (OUT && p.base.norm.gate && aligned_ok) {
+        } else if (!STATES && p.base.norm.gate && aligned_ok) {
             // ======================================= the gate's rows, into L2 a chunk ahead ======
             uint32_t it = 0;
             bool ok = true;
@@ -457,6 +436,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll 1
                 for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                     if (it > 0 && !(ok = wait(sc_full, (it - 1) & 1u, kWaitTensor))) break;
+#pragma unroll 1
                     for (int r = lane; r < CT * C::HALVES; r += 32) {
                         const int t = c * CT + r / C::HALVES;
                         if (t < len)
@@ -471,7 +451,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         const int quad = warp & 3, i = quad * 32 + lane;
         const uint32_t sc = tmem_base + COL_SC + ((uint32_t)(quad * 32) << 16);
         uint32_t it = 0;
-        bool ok = aligned_ok && OUT;
+        bool ok = aligned_ok && !STATES;
         while (ok && enter()) {
 #pragma unroll 1
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
@@ -484,12 +464,11 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 tc_fence_after();
                 uint32_t w[8];
                 float s[16];
-                float r = 0.f;
 #pragma unroll 1
                 for (int blk = 0; blk < 2 * quad; ++blk) {         // 16 columns below the diagonal
                     tmem_ld16(sc + blk * 16, s);
                     const int m = blk * 16 | 31;
-                    r = ex2_approx((wi + whole[m]) + (ri + rest[m]));
+                    const float r = ex2_approx((wi + whole[m]) + (ri + rest[m]));
                     const uint64_t r2 = f2_pack(r, r);
                     const ulonglong2* u = reinterpret_cast<const ulonglong2*>(whole + 2 * CT + blk * 16);
                     tmem_wait_ld();
@@ -529,66 +508,93 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 for (int j = 0; j < 8; ++j) w[j] = 0u;
 #pragma unroll 1
                 for (int blk = 2 * quad + 2; blk < 8; ++blk) tmem_st8(sc + blk * 8, w);
+                // ---- 2^b_i q_i S
+                const float ei = exp2_parts(wi, ri);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&dec_empty[buf]);
+                if (!(ok = wait(qs_full, ph, kWaitTensor))) break;
+                tc_fence_after();
+                const uint32_t o = tmem_base + COL_O + ph * 128 + ((uint32_t)(quad * 32) << 16);
+                const uint64_t ei2 = f2_pack(ei, ei);
+#pragma unroll 1
+                for (int j = 0; j < D; j += 16) {
+                    uint32_t x[16];
+                    tmem_ld16(o + j, *reinterpret_cast<float(*)[16]>(&x));
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int q = 0; q < 16; q += 2) {
+                        float y0, y1;
+                        f2_unpack(f2_mul(ei2, f2_pack(__uint_as_float(x[q]), __uint_as_float(x[q + 1]))), y0, y1);
+                        x[q] = __float_as_uint(y0);
+                        x[q + 1] = __float_as_uint(y1);
+                    }
+                    tmem_st16(o + j, x);
+                }
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(p_full);
-                    mbar_arrive(&dec_empty[buf]);
-                }
+                if (lane == 0) mbar_arrive(p_full);
             }
         }
-    } else if (warp < 12) {
+    } else if (warp < 12 || warp >= 20) {
         // ======================================= output ==========================================
-        setmaxnreg_inc<kRegsOut>();
-        const int quad = warp & 3, i = quad * 32 + lane;
-        const uint32_t oa = tmem_base + COL_OA + ((uint32_t)(quad * 32) << 16), oi = oa + (COL_OI - COL_OA);
+        setmaxnreg_dec<kRegsOut>();
+        const int quad = warp & 3;
+        const uint32_t mine = warp < 12 ? 0u : 1u;             // chunks of this warpgroup: even, odd
+        const uint32_t o = tmem_base + COL_O + mine * 128 + ((uint32_t)(quad * 32) << 16);
         const NormGate& nm = p.base.norm;
         const float scale = p.base.scale;
-        uint8_t* rows = smem + C::OFF_ROWS + quad * 2048;
-        auto staged = [&](int r, int ch) { return reinterpret_cast<uint4*>(rows + r * 64 + ((ch ^ ((r >> 1) & 3)) << 4)); };   // no bank twice
+        uint8_t* rows = smem + C::OFF_ROWS + (mine * 4 + quad) * 1024;
+        auto staged = [&](int r, int ch) { return reinterpret_cast<uint4*>(rows + r * 32 + ((ch ^ ((r >> 2) & 1)) << 4)); };   // no bank twice
         uint32_t it = 0;
-        bool ok = aligned_ok && OUT;
+        bool ok = aligned_ok && !STATES;
         while (ok && enter()) {
             const int len = tab.len[walk.b], at = walk.h * D;
             const int64_t tok0 = tab.tok0[walk.b];
 #pragma unroll 1
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
-                const uint32_t buf = it & 1u, ph = it & 1u;
-                if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
-                const float ei = exp2_parts(-dec[buf * C::DEC_FLOATS + i], -dec[buf * C::DEC_FLOATS + CT + i]) * scale;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&dec_empty[buf]);
-                if (!(ok = wait(o_full, ph, kWaitTensor))) break;
+                if ((it & 1u) != mine) continue;
+                // Rows leave (and the gate's come) 16 channels at a time through shared memory, so that a warp's access covers whole sectors.
+                const int t0 = c * CT + quad * 32, lrow = lane >> 1, lch = lane & 1;
+                const bool live0 = t0 + lrow < len, live1 = t0 + lrow + 16 < len;
+                __nv_bfloat16* out = p.base.o + (tok0 + t0 + lrow) * p.base.o_stride + at + lch * 8;
+                const __nv_bfloat16* gate = nm.gate + (tok0 + t0 + lrow) * nm.gate_stride + at + lch * 8;
+                uint4 g0, g1, n0, n1;                          // the gate's next 16 channels, and the ones behind
+                auto ask = [&](int j, uint4& a, uint4& b) {
+                    a = b = make_uint4(0u, 0u, 0u, 0u);
+                    if (live0) a = __ldg(reinterpret_cast<const uint4*>(gate + j));
+                    if (live1) b = __ldg(reinterpret_cast<const uint4*>(gate + 16 * nm.gate_stride + j));
+                };
+                if (nm.gate) {
+                    ask(0, g0, g1);
+                    ask(16, n0, n1);
+                }
+                if (!(ok = wait(&o_full[mine], (it >> 1) & 1u, kWaitTensor))) break;
                 tc_fence_after();
-                // 16 channels of the row: by * (state's part) + a * (chunk's part) + add
-                auto channels = [&](int j, float by, float a, float add, uint64_t (&y)[8]) {
-                    float x[16], z[16];
-                    tmem_ld16(oa + j, z);
-                    tmem_ld16(oi + j, x);
-                    const uint64_t by2 = f2_pack(by, by), a2 = f2_pack(a, a), add2 = f2_pack(add, add);
+                // 16 channels of the row: a * x + add
+                auto channels = [&](int j, float a, float add, uint64_t (&y)[8]) {
+                    float x[16];
+                    tmem_ld16(o + j, x);
+                    const uint64_t a2 = f2_pack(a, a), add2 = f2_pack(add, add);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        y[q] = f2_fma(by2, f2_pack(x[2 * q], x[2 * q + 1]), f2_fma(a2, f2_pack(z[2 * q], z[2 * q + 1]), add2));
+                    for (int q = 0; q < 8; ++q) y[q] = f2_fma(a2, f2_pack(x[2 * q], x[2 * q + 1]), add2);
                 };
-                float by = ei, of = scale, add = 0.f;      // what the row's channels are made of: the normalisation goes into it
+                float of = scale, add = 0.f;
                 if (nm.on) {
                     // sums of the differences from the row's first channel (rms: from zero) and of their squares: one of d values is at most
                     // sqrt(d) standard deviations from the mean, so the difference of the two loses at most d roundings
                     float first = 0.f;
                     if (!nm.rms) {
-                        float x, z;
-                        tmem_ld1(oa, z);
-                        tmem_ld1(oi, x);
+                        tmem_ld1(o, first);
                         tmem_wait_ld();
-                        first = fmaf(ei, x, scale * z);
+                        first *= scale;
                     }
                     uint64_t s1 = 0ull, s2 = 0ull;
 #pragma unroll 1
                     for (int j = 0; j < D; j += 16) {
                         uint64_t y[8];
-                        channels(j, ei, scale, -first, y);
+                        channels(j, scale, -first, y);
 #pragma unroll
                         for (int q = 0; q < 8; ++q) {
                             s1 = f2_add(s1, y[q]);
@@ -600,101 +606,86 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     f2_unpack(s2, b0, b1);
                     const float m1 = nm.rms ? 0.f : (a0 + a1) * (1.f / D);
                     const float inv = 1.f / sqrtf(fmaxf(fmaf(-m1, m1, (b0 + b1) * (1.f / D)), 0.f) + nm.eps);
-                    by *= inv;
-                    of *= inv;
+                    of = scale * inv;
                     add = -(first + m1) * inv;
                 }
-                // Rows leave (and the gate's come) 32 channels at a time through shared memory, so that a warp's access covers 8 rows, not 32.
-                const int t0 = c * CT + quad * 32, lrow = lane >> 2, lch = lane & 3;
-                __nv_bfloat16* out = p.base.o + (tok0 + t0 + lrow) * p.base.o_stride + at + lch * 8;
-                const __nv_bfloat16* gate = nm.gate + (tok0 + t0 + lrow) * nm.gate_stride + at + lch * 8;
-                uint4 g[4];
-                auto ask = [&](int j) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        g[r] = make_uint4(0u, 0u, 0u, 0u);
-                        if (t0 + lrow + 8 * r < len) g[r] = __ldg(reinterpret_cast<const uint4*>(gate + 8 * r * nm.gate_stride + j));
-                    }
-                };
-                if (nm.gate) ask(0);
 #pragma unroll 1
-                for (int j = 0; j < D; j += 32) {
+                for (int j = 0; j < D; j += 16) {
                     if (nm.gate) {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) *staged(lrow + 8 * r, lch) = g[r];
+                        *staged(lrow, lch) = g0;
+                        *staged(lrow + 16, lch) = g1;
+                        g0 = n0;
+                        g1 = n1;
+                        if (j + 32 < D) ask(j + 32, n0, n1);
                         __syncwarp();
-                        if (j + 32 < D) ask(j + 32);
                     }
-#pragma unroll 1
-                    for (int e = 0; e < 32; e += 16) {     // (a thread's row of the gate gives way to its row of the output)
-                        uint64_t y[8];
-                        channels(j + e, by, of, add, y);
-                        if (nm.on) {
-                            uint64_t f[8];
-                            auto eight = [&](const uint4& v, int at8) {
-                                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                                for (int q = 0; q < 4; ++q) f[at8 + q] = f2_pack(__uint_as_float(w[q] << 16), __uint_as_float(w[q] & 0xFFFF0000u));
-                            };
-                            if (nm.gain) {
-                                eight(__ldg(reinterpret_cast<const uint4*>(nm.gain + at + j + e)), 0);
-                                eight(__ldg(reinterpret_cast<const uint4*>(nm.gain + at + j + e) + 1), 4);
-#pragma unroll
-                                for (int q = 0; q < 8; ++q) y[q] = f2_mul(y[q], f[q]);
-                            }
-                            if (nm.bias) {
-                                eight(__ldg(reinterpret_cast<const uint4*>(nm.bias + at + j + e)), 0);
-                                eight(__ldg(reinterpret_cast<const uint4*>(nm.bias + at + j + e) + 1), 4);
-#pragma unroll
-                                for (int q = 0; q < 8; ++q) y[q] = f2_add(y[q], f[q]);
-                            }
-                            if (nm.gate) {
-                                eight(*staged(lane, e / 8), 0);
-                                eight(*staged(lane, e / 8 + 1), 4);
-#pragma unroll
-                                for (int q = 0; q < 8; ++q) y[q] = f2_swish_mul(f[q], y[q]);
-                            }
-                        }
-                        uint32_t w[8];
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) {
-                            float y0, y1;
-                            f2_unpack(y[q], y0, y1);
-                            w[q] = pack_bf16x2(y0, y1);
-                        }
-                        *staged(lane, e / 8) = make_uint4(w[0], w[1], w[2], w[3]);
-                        *staged(lane, e / 8 + 1) = make_uint4(w[4], w[5], w[6], w[7]);
-                    }
-                    if (j + 32 == D) {                     // all of it has been read
+                    uint64_t y[8];
+                    channels(j, of, add, y);
+                    if (j + 16 == D) {                     // all of it has been read
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(o_empty);
+                        if (lane == 0) mbar_arrive(&o_empty[mine]);
                     }
-                    __syncwarp();
+                    if (nm.on) {
+                        uint64_t f[8];
+                        auto eight = [&](const uint4& v, int at8) {
+                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (t0 + lrow + 8 * r < len)
-                            *reinterpret_cast<uint4*>(out + 8 * r * p.base.o_stride + j) = *staged(lrow + 8 * r, lch);
+                            for (int q = 0; q < 4; ++q) f[at8 + q] = f2_pack(__uint_as_float(w[q] << 16), __uint_as_float(w[q] & 0xFFFF0000u));
+                        };
+                        if (nm.gain) {
+                            eight(__ldg(reinterpret_cast<const uint4*>(nm.gain + at + j)), 0);
+                            eight(__ldg(reinterpret_cast<const uint4*>(nm.gain + at + j) + 1), 4);
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) y[q] = f2_mul(y[q], f[q]);
+                        }
+                        if (nm.bias) {
+                            eight(__ldg(reinterpret_cast<const uint4*>(nm.bias + at + j)), 0);
+                            eight(__ldg(reinterpret_cast<const uint4*>(nm.bias + at + j) + 1), 4);
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) y[q] = f2_add(y[q], f[q]);
+                        }
+                        if (nm.gate) {                     // (a thread's row of the gate gives way to its row of the output)
+                            eight(*staged(lane, 0), 0);
+                            eight(*staged(lane, 1), 4);
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) y[q] = f2_swish_mul(f[q], y[q]);
+                        }
+                    }
+                    uint32_t w[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        float y0, y1;
+                        f2_unpack(y[q], y0, y1);
+                        w[q] = pack_bf16x2(y0, y1);
+                    }
+                    *staged(lane, 0) = make_uint4(w[0], w[1], w[2], w[3]);
+                    *staged(lane, 1) = make_uint4(w[4], w[5], w[6], w[7]);
+                    __syncwarp();
+                    if (live0) *reinterpret_cast<uint4*>(out + j) = *staged(lrow, lch);
+                    if (live1) *reinterpret_cast<uint4*>(out + 16 * p.base.o_stride + j) = *staged(lrow + 16, lch);
                     __syncwarp();
                 }
             }
         }
-    } else if (warp < 20) {
-        // ======================================= state ===========================================
+    } else {
+        // ======================================= K', state =======================================
         setmaxnreg_inc<kRegsState>();
-        constexpr int N = D * D / 256;                     // channels of a thread: half a row (d = 64: a quarter)
+        constexpr int N = D * D / 256;                     // channels of a thread: half a row of the state (d = 64: a quarter)
         const int quad = warp & 3, l = quad * 32 + lane, row = l % D, col = (warp >= 16 ? D / 2 : 0) + (l / D) * N;
         const uint32_t ds = tmem_base + COL_DS + ((uint32_t)(quad * 32) << 16) + col;
         uint8_t* s_row = smem + C::OFF_S + row * 128;
+        const int tid = threadIdx.x - 12 * 32, k_row = tid >> 3;
+        const uint32_t k_at = k_row * 128 + (((tid & 7) ^ (k_row & 7)) << 4);      // inside a piece's half; the same in a tile's
         uint32_t it = 0;
         bool ok = aligned_ok;
         while (ok && enter()) {
-            const int b = walk.b, h = walk.h;
-            const bool whole_stream = walk.c == 0 && walk.c_end == walk.chunks;
+            const int b = walk.b, h = walk.h, len = tab.len[b], terms = terms_of();
+            const bool whole_stream = walk.whole_stream();
             float s[N];
             // where the segment's first state is: the stream's own, or what the merge left for this CTA
             const float* src = nullptr;
-            if (OUT) {
+            if (!STATES) {
                 if (whole_stream)
                     src = tab.from[b] >= 0 ? p.base.state + ((int64_t)tab.from[b] * p.base.H + h) * (D * D) : nullptr;
                 else
@@ -708,31 +699,88 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 s[j + 2] = x.z;
                 s[j + 3] = x.w;
             }
-            float all_whole = 0.f;                         // logarithm of the segment's decay
-            double all_rest = 0.0;
+            float all_whole = 0.f, all_rest = 0.f;         // logarithm of the segment's decay
 #pragma unroll 1
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                 const uint32_t buf = it & 1u, ph = it & 1u;
-                if (OUT) {
-                    if (!(ok = wait(s_empty, ph ^ 1u, kWaitTensor))) break;
+                const int valid = len - c * CT;            // tokens of the sequence from here on
+                if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
+                const float* decays = dec + buf * C::DEC_FLOATS;
+                const float whole = -decays[CT - 1], rest = -decays[2 * CT - 1];
+                if (!(ok = wait(&k_full[place<C::KS>(it)], round_of<C::KS>(it), kWaitRingFull))) break;
+                if (valid < CT) {
+                    // rows behind the sequence are the next one's, or none: they may hold anything, and 0 times that is not 0
+                    if (!(ok = wait(&v_full[place<C::VS>(it)], round_of<C::VS>(it), kWaitRingFull))) break;
+                    const int r = tid >> 1;
+                    if (r >= valid) {
+#pragma unroll 1
+                        for (int q = tid & 1; q < 8 * C::HALVES; q += 2)
+                            *reinterpret_cast<uint4*>(smem + C::OFF_V + place<C::VS>(it) * C::TILE_BYTES + (q >> 3) * HALF_BYTES + r * 128 + (q & 7) * 16) =
+                                make_uint4(0u, 0u, 0u, 0u);
+                    }
+                }
+#pragma unroll 1
+                for (int e = 0; e < PIECES; ++e) {
+                    if (!STATES && e == 1) {
+                        // ---- S in bf16
+                        if (!(ok = wait(s_empty, ph ^ 1u, kWaitTensor))) break;
 #pragma unroll
-                    for (int j = 0; j < N; j += 8) {
-                        const int ch = (col + j) / 8;
-                        *reinterpret_cast<uint4*>(s_row + (ch >> 3) * (D * 128) + (((ch & 7) ^ (row & 7)) << 4)) =
-                            pack8(*reinterpret_cast<float(*)[8]>(&s[j]));
+                        for (int j = 0; j < N; j += 8) {
+                            const int ch = (col + j) / 8;
+                            *reinterpret_cast<uint4*>(s_row + (ch >> 3) * (D * 128) + (((ch & 7) ^ (row & 7)) << 4)) =
+                                pack8(*reinterpret_cast<float(*)[8]>(&s[j]));
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(s_full);
+                    }
+                    // ---- 32 tokens of K'
+                    const float w = decays[3 * CT + e * PIECE + k_row];
+                    const uint64_t w2 = f2_pack(w, w);
+                    const bool in = e * PIECE + k_row < valid;
+                    if (!(ok = wait(&kp_empty[(e & 1)], ((uint32_t)(e >> 1) & 1u) ^ 1u, kWaitTensor))) break;
+                    uint8_t* dst = smem + C::OFF_KP + (e & 1) * C::PIECE_BYTES + k_at;
+#pragma unroll 1
+                    for (int hf = 0; hf < C::HALVES; ++hf) {
+                        uint4 raw = *reinterpret_cast<const uint4*>(smem + C::OFF_K + place<C::KS>(it) * C::TILE_BYTES + e * PIECE_HALF + hf * HALF_BYTES + k_at);
+                        if (!in) raw = make_uint4(0u, 0u, 0u, 0u);
+                        const uint32_t kk[4] = {raw.x, raw.y, raw.z, raw.w};
+                        uint64_t x[4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) x[q] = f2_mul(w2, f2_pack(__uint_as_float(kk[q] << 16), __uint_as_float(kk[q] & 0xFFFF0000u)));
+#pragma unroll
+                        for (int t = 0; t < kTerms; ++t) {
+                            if (t >= kTermsInside && t >= terms) break;
+                            uint32_t part[4];
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                float x0, x1;
+                                f2_unpack(x[q], x0, x1);
+                                part[q] = pack_bf16x2(x0, x1);
+                                if (t + 1 < kTerms)
+                                    x[q] = f2_fma(f2_pack(__uint_as_float(part[q] << 16), __uint_as_float(part[q] & 0xFFFF0000u)), f2_pack(-1.f, -1.f), x[q]);
+                            }
+                            const uint4 v = make_uint4(part[0], part[1], part[2], part[3]);
+                            *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + hf * PIECE_HALF) = v;
+                            // d = 64: the instruction's upper 64 rows are the same ones again (read by the second threads of the state's rows)
+                            if (D == 64) *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + PIECE_HALF) = v;
+                        }
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(s_full);
+                    if (lane == 0) mbar_arrive(&kp_full[(e & 1)]);
                 }
-                if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
-                const float whole = -dec[buf * C::DEC_FLOATS + CT - 1], rest = -dec[buf * C::DEC_FLOATS + 2 * CT - 1];
+                if (!ok) break;
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&dec_empty[buf]);
+                if (lane == 0) {
+                    mbar_arrive(&k_empty[place<C::KS>(it)]);
+                    mbar_arrive(&dec_empty[buf]);
+                }
+                // ---- S'
                 const float keep = exp2_parts(whole, rest);
-                if (!OUT) {
+                if (STATES) {
                     all_whole += whole;
-                    all_rest += (double)rest;
+                    all_rest += rest;
                 }
                 if (!(ok = wait(ds_full, ph, kWaitTensor))) break;
                 tc_fence_after();
@@ -749,99 +797,19 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 if (lane == 0) mbar_arrive(ds_empty);
             }
             if (!ok) break;
+            // a state-only segment that ends inside its stream: the next CTA's start; one that ends it: the last part of the final state
+            const int64_t slot = walk.c_end < walk.chunks ? blockIdx.x + 1 : 2 * (int64_t)p.groups + blockIdx.x;
             float* dst = nullptr;
-            if (PASS == kStates)
-                dst = p.part + (int64_t)(blockIdx.x + 1) * (D * D);
-            else if (walk.c_end == walk.chunks && tab.to[b] >= 0)
+            if (STATES)
+                dst = p.part + slot * (D * D);
+            else if (whole_stream && tab.to[b] >= 0)
                 dst = p.base.state + ((int64_t)tab.to[b] * p.base.H + h) * (D * D);
             if (dst) {
 #pragma unroll
                 for (int j = 0; j < N; j += 4)
                     *reinterpret_cast<float4*>(dst + row * D + col + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
             }
-            if (PASS == kStates && threadIdx.x == 12 * 32) p.part_keep[blockIdx.x + 1] = exp2f(all_whole) * (float)exp2(all_rest);
-        }
-    } else {
-        // ======================================= K' ==============================================
-        setmaxnreg_dec<kRegsKeys>();
-        const int l = threadIdx.x & 127, row = l >> 3, ch = l & 7;
-        const uint32_t at = row * 128 + ((ch ^ (row & 7)) << 4);       // inside a piece's half; the same in a tile's
-        Place<C::KS> kat(0);
-        Place<C::VS> vat(0);
-        Place<C::KP_STAGES> pat(0);
-        uint32_t it = 0;
-        bool ok = aligned_ok;
-        while (ok && enter()) {
-            const int len = tab.len[walk.b];
-#pragma unroll 1
-            for (int c = walk.c; c < walk.c_end; ++c, ++it) {
-                const uint32_t buf = it & 1u;
-                const int valid = len - c * CT;            // tokens of the sequence from here on
-                if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
-                const float* weight = dec + buf * C::DEC_FLOATS + 3 * CT + row;
-                if (!(ok = wait(&k_full[kat.slot], kat.phase, kWaitRingFull))) break;
-                if (valid < CT) {
-                    // rows behind the sequence are the next one's, or none: they may hold anything, and 0 times that is not 0
-                    if (!(ok = wait(&v_full[vat.slot], vat.phase, kWaitRingFull))) break;
-                    if (l >= valid) {
-#pragma unroll 1
-                        for (int q = 0; q < 8 * C::HALVES; ++q)
-                            *reinterpret_cast<uint4*>(smem + C::OFF_V + vat.slot * C::TILE_BYTES + (q >> 3) * HALF_BYTES + l * 128 + (q & 7) * 16) =
-                                make_uint4(0u, 0u, 0u, 0u);
-                    }
-                }
-#pragma unroll 1
-                for (int e = 0; e < PIECES; ++e) {
-                    if (!(ok = wait(&kp_empty[pat.slot], pat.phase ^ 1u, kWaitTensor))) break;
-                    const uint8_t* src = smem + C::OFF_K + kat.slot * C::TILE_BYTES + e * PIECE_HALF + at;
-                    uint8_t* dst = smem + C::OFF_KP + pat.slot * C::PIECE_BYTES + at;
-#pragma unroll 1
-                    for (int r = 0; r < PIECE; r += 16) {
-                        const float w = weight[e * PIECE + r];
-                        const bool in = e * PIECE + r + row < valid;
-                        const uint64_t w2 = f2_pack(w, w);
-#pragma unroll 1
-                        for (int hf = 0; hf < C::HALVES; ++hf) {
-                            uint4 raw = *reinterpret_cast<const uint4*>(src + hf * HALF_BYTES + r * 128);
-                            if (!in) raw = make_uint4(0u, 0u, 0u, 0u);
-                            uint32_t part[C::TERMS][4];
-                            const uint32_t kk[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                uint64_t x = f2_mul(w2, f2_pack(__uint_as_float(kk[q] << 16), __uint_as_float(kk[q] & 0xFFFF0000u)));
-#pragma unroll
-                                for (int t = 0; t < C::TERMS; ++t) {
-                                    float x0, x1;
-                                    f2_unpack(x, x0, x1);
-                                    const uint32_t h = pack_bf16x2(x0, x1);
-                                    part[t][q] = h;
-                                    if (t + 1 < C::TERMS)
-                                        x = f2_fma(f2_pack(__uint_as_float(h << 16), __uint_as_float(h & 0xFFFF0000u)), f2_pack(-1.f, -1.f), x);
-                                }
-                            }
-#pragma unroll
-                            for (int t = 0; t < C::TERMS; ++t) {
-                                const uint4 v = make_uint4(part[t][0], part[t][1], part[t][2], part[t][3]);
-                                *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + hf * PIECE_HALF + r * 128) = v;
-                                // d = 64: the instruction's upper 64 rows are the same ones again (read by the second threads of the state's rows)
-                                if (D == 64) *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + PIECE_HALF + r * 128) = v;
-                            }
-                        }
-                    }
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&kp_full[pat.slot]);
-                    pat.advance(1);
-                }
-                if (!ok) break;
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(&k_empty[kat.slot]);
-                    mbar_arrive(&dec_empty[buf]);
-                }
-                kat.advance(1);
-                vat.advance(1);
-            }
+            if (STATES && tid == 0) p.part_keep[slot] = exp2_parts(all_whole, all_rest);
         }
     }
 
@@ -854,73 +822,73 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     }
 }
 
-// States at the cuts of a stream that several CTAs share.  A block owns some elements of one such stream: from the stream's first state on, every
+// States of the streams that several CTAs share.  A block owns some elements of one such stream: from the stream's first state on, every
 // CTA's part (its local state, from zero) is added to what decays from before, in the order of the CTAs.  Slot g: the state that CTA g
 // starts from (the state-only pass left CTA g - 1's part there); slot groups + g: a copy of the first state of the stream
-// that begins in CTA g (the pool's may be overwritten while others still run).
+// that begins in CTA g (the pool's is overwritten here, if it is the slot the stream ends in); slot 2 groups + g: CTA g's part of a stream that ends in it.
 constexpr int kMergeThreads = 256;
 template <int D, class Table>
 __global__ void __launch_bounds__(kMergeThreads)
 gret_merge_kernel(const GretChunkParams p, const __grid_constant__ Table tab) {
     const int g0 = blockIdx.x + 1;                         // first CTA that starts inside the stream
-    const int H = p.base.H, pos = p.first_of(g0), lo = sequence_at(p, tab, pos);
-    const int base = tab.chunk0[lo] * H, chunks = tab.chunk0[lo + 1] - tab.chunk0[lo], h = (pos - base) / chunks;
+    const int H = p.base.H, pos = p.first_of(g0), b = sequence_at(p, tab, pos);
+    const int base = tab.chunk0[b] * H, chunks = tab.chunk0[b + 1] - tab.chunk0[b], h = (pos - base) / chunks;
     const int begin = base + h * chunks, end = begin + chunks;
     if (pos == begin || p.first_of(g0 - 1) > begin) return;        // no cut, or not the stream's first one
     const int at = (blockIdx.y * kMergeThreads + threadIdx.x) * 4;
+    auto part = [&](int64_t slot) { return reinterpret_cast<float4*>(p.part + slot * (D * D) + at); };
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (tab.from[lo] >= 0) s = *reinterpret_cast<const float4*>(p.base.state + ((int64_t)tab.from[lo] * H + h) * (D * D) + at);
-    *reinterpret_cast<float4*>(p.part + (int64_t)(p.groups + g0 - 1) * (D * D) + at) = s;
-    for (int g = g0; g < p.groups && p.first_of(g) < end; ++g) {
-        float4* slot = reinterpret_cast<float4*>(p.part + (int64_t)g * (D * D) + at);
-        const float keep = p.part_keep[g];
-        const float4 x = *slot;
-        s.x = fmaf(keep, s.x, x.x);
-        s.y = fmaf(keep, s.y, x.y);
-        s.z = fmaf(keep, s.z, x.z);
-        s.w = fmaf(keep, s.w, x.w);
-        *slot = s;
+    if (tab.from[b] >= 0) s = *reinterpret_cast<const float4*>(p.base.state + ((int64_t)tab.from[b] * H + h) * (D * D) + at);
+    *part(p.groups + g0 - 1) = s;
+    auto add = [&](int64_t slot) {
+        const float keep = p.part_keep[slot];
+        const float4 x = *part(slot);
+        s = make_float4(fmaf(keep, s.x, x.x), fmaf(keep, s.y, x.y), fmaf(keep, s.z, x.z), fmaf(keep, s.w, x.w));
+    };
+    int g = g0;
+    for (; g < p.groups && p.first_of(g) < end; ++g) {
+        add(g);
+        *part(g) = s;
     }
+    add(2 * (int64_t)p.groups + g - 1);
+    if (tab.to[b] >= 0) *reinterpret_cast<float4*>(p.base.state + ((int64_t)tab.to[b] * H + h) * (D * D) + at) = s;
 }
 
-template <int D, Pass PASS, class Table>
+template <int D, bool STATES, class Table>
 cudaError_t launch_pass(const GretChunkParams& p, const Table& tab, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
                         cudaStream_t stream) {
-    gret_chunk_kernel<D, PASS><<<p.groups, kThreads, GCfg<D, PASS>::SMEM_BYTES, stream>>>(tmQ, tmK, tmV, p, tab);
+    gret_chunk_kernel<D, STATES><<<p.groups, kThreads, GCfg<D, STATES>::SMEM_BYTES, stream>>>(tmQ, tmK, tmV, p, tab);
     return cudaGetLastError();
 }
 
 template <int D, class Table>
 cudaError_t launch_one(const GretChunkParams& p, const Table& tab, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
                        cudaStream_t stream) {
-    if (!p.split) return launch_pass<D, kWhole>(p, tab, tmQ, tmK, tmV, stream);
-    cudaError_t e = launch_pass<D, kStates>(p, tab, tmQ, tmK, tmV, stream);
-    if (e != cudaSuccess) return e;
-    gret_merge_kernel<D><<<dim3(p.groups - 1, D * D / (4 * kMergeThreads)), kMergeThreads, 0, stream>>>(p, tab);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    return launch_pass<D, kMain>(p, tab, tmQ, tmK, tmV, stream);
+    if (p.split) {
+        cudaError_t e = launch_pass<D, true>(p, tab, tmQ, tmK, tmV, stream);
+        if (e != cudaSuccess) return e;
+        gret_merge_kernel<D><<<dim3(p.groups - 1, D * D / (4 * kMergeThreads)), kMergeThreads, 0, stream>>>(p, tab);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    }
+    return launch_pass<D, false>(p, tab, tmQ, tmK, tmV, stream);
 }
 
-template <int D, Pass PASS>
+template <int D, bool STATES>
 cudaError_t setup_pass() {
-    constexpr int bytes = GCfg<D, PASS>::SMEM_BYTES;
-    cudaError_t e = cudaFuncSetAttribute(gret_chunk_kernel<D, PASS, GretChunkTable>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    constexpr int bytes = GCfg<D, STATES>::SMEM_BYTES;
+    cudaError_t e = cudaFuncSetAttribute(gret_chunk_kernel<D, STATES, GretChunkTable>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(gret_chunk_kernel<D, PASS, GretChunkTableOf<kFewSequences>>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-}
-template <int D>
-cudaError_t setup_one() {
-    cudaError_t e = setup_pass<D, kWhole>();
-    if (e != cudaSuccess) return e;
-    if ((e = setup_pass<D, kMain>()) != cudaSuccess) return e;
-    return setup_pass<D, kStates>();
+    return cudaFuncSetAttribute(gret_chunk_kernel<D, STATES, GretChunkTableOf<kFewSequences>>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
 }  // namespace
 
 cudaError_t gret_chunk_kernel_setup() {
-    const cudaError_t e = setup_one<128>();
-    return e != cudaSuccess ? e : setup_one<64>();
+    cudaError_t e = setup_pass<128, false>();
+    if (e != cudaSuccess) return e;
+    if ((e = setup_pass<128, true>()) != cudaSuccess) return e;
+    if ((e = setup_pass<64, false>()) != cudaSuccess) return e;
+    return setup_pass<64, true>();
 }
 
 cudaError_t launch_gret_chunk(const GretChunkParams& p, const GretChunkTable& tab, const CUtensorMap& tmQ, const CUtensorMap& tmK,

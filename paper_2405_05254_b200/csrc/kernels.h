@@ -326,8 +326,8 @@ struct GretChunkParams {
     int32_t split;              // 1: CTA g walks chunks [first_of(g), first_of(g + 1)); 0: one stream each
     int32_t share, extra;       // total / groups, total % groups
     __host__ __device__ int32_t first_of(int32_t g) const { return g * share + (g < extra ? g : extra); }
-    float* part;                // split: 2 * groups states
-    float* part_keep;           // split: decay over a CTA's last segment, groups + 1
+    float* part;                // split: 3 * groups states
+    float* part_keep;           // split: decays over the segments that left them, 3 * groups
     int32_t* status;
 };
 // tmQ, tmK, tmV: bf16 maps over [tokens, H * d], box {64, kGretChunk}, 128-byte swizzle
