@@ -4,7 +4,7 @@
 //     P_ij = (q_i . k_j) 2^(b_i - b_j)  (j <= i),   o_i = scale (sum_j P_ij v_j + 2^b_i q_i S),
 //     S' = 2^b_C S + sum_j (2^(b_C - b_j) k_j)^T v_j.
 // A CTA walks a contiguous range of chunks, of one (sequence, head) stream or of several one after the other, with the state in the
-// registers of two warpgroups.  768 threads:
+// registers of two warpgroups.  1,024 threads:
 //   warp 0       TMA producer: K, Q, V tiles (128 tokens x d, 128-byte swizzle)
 //   warp 1       issuer of all products: Q K^T -> SC;  K'^T V -> DS;  Q S and P V -> O[n & 1]    (tensor memory, fp32)
 //   warp 2       decays: prefix sums of the logarithms in 64 bits, kept as integer part and rest (b_i - b_j is the difference of
@@ -12,8 +12,8 @@
 //   warp 3       asks for the gate's rows, a chunk ahead
 //   warpgroup 1  thread = token: P (bf16, over the scores' own columns: it goes to P V from tensor memory); 2^b_i times Q S, in place
 //   warpgroups 2, 5  thread = token, every other chunk each: the output: scale, normalisation, gate, rounding, store
-//   warpgroups 3, 4  K' = 2^(b_C - b_j) k_j, in pieces of 32 tokens; thread = half a row of the state: S' from S and DS in fp32,
-//                S in bf16 to shared memory for Q S
+//   warpgroups 3, 4  thread = half a row of the state: S' from S and DS in fp32, S in bf16 to shared memory for Q S
+//   warpgroups 6, 7  K' = 2^(b_C - b_j) k_j, in pieces of 32 tokens
 // Decays of P: in the 32 x 32 blocks on the diagonal one exponential per element; below it 2^(b_i - m) 2^(m - b_j), m the value at the
 // end of j's block: both factors are at most 1, and the second is the same for all rows.
 // Roundings: P and the copy of S that multiplies Q go to bf16 (half a step, 2^-9 of the value, like the output's own).  K' goes to
@@ -21,6 +21,8 @@
 // with two 2e-6), where they only multiply Q inside, of two.
 //
 // Order of the products per chunk: Q K^T, a quarter of K'^T V, Q S, the other three, P V.
+#include <type_traits>
+
 #include "gret.cuh"
 #include "kernels.h"
 #include "ptx.cuh"
@@ -32,7 +34,7 @@ namespace yoco {
 namespace {
 
 constexpr int CT = kGretChunk;                 // 128 tokens
-constexpr int kThreads = 768;
+constexpr int kThreads = 1024;
 constexpr int HALF_BYTES = CT * 128;           // 128 rows x 64 bf16: one swizzled half tile
 constexpr int PIECE = 32;                      // tokens of a piece of K'
 constexpr int PIECES = CT / PIECE;
@@ -40,9 +42,9 @@ constexpr int PIECE_HALF = PIECE * 128;        // 64 channels of a piece of one 
 constexpr int TERM_BYTES = 2 * PIECE_HALF;
 constexpr uint32_t TMEM_COLS = 512;
 constexpr uint32_t COL_SC = 0, COL_O = 128, COL_DS = 384;     // two buffers of O
-// Registers per thread after the split; the CTA starts with 80 each.
-constexpr int kRegsIo = 64, kRegsP = 64, kRegsOut = 64, kRegsState = 112;
-static_assert(kRegsIo + kRegsP + 2 * kRegsOut + 2 * kRegsState <= 6 * 80, "register pool of the CTA");
+// Registers per thread after the split; the CTA starts with 64 each.
+constexpr int kRegsIo = 56, kRegsP = 56, kRegsOut = 64, kRegsState = 88, kRegsKeys = 48;
+static_assert(kRegsIo + kRegsP + 2 * kRegsOut + 2 * kRegsState + 2 * kRegsKeys <= 8 * 64, "register pool of the CTA");
 constexpr int kTerms = 3;                      // parts of K', where a state leaves; otherwise kTermsInside
 constexpr int kTermsInside = 2;
 
@@ -51,22 +53,25 @@ template <int D, bool STATES>
 struct GCfg {
     static constexpr int HALVES = D / 64;
     static constexpr int TILE_BYTES = HALVES * HALF_BYTES;
-    static constexpr int PIECE_BYTES = kTerms * TERM_BYTES;
     // Tiles of K, Q and V in shared memory.  K and Q are given back early (once scored and turned into K', once multiplied by S), V last.
     static constexpr int KS = D == 64 || STATES ? 2 : 1, QS = STATES ? 0 : D == 64 ? 2 : 1, VS = D == 64 ? 4 : 2;
-    static constexpr int KP_STAGES = 2;                // (pieces of a chunk: 4, so piece e always goes to place e % 2)
+    // K' pieces: places of three parts each, or in the same memory (not STATES) half as many again of two.
+    static constexpr int KP_WIDE = STATES ? 4 : 2, KP_NARROW = 3, KP_STAGES = STATES ? 4 : 3;
     static constexpr int OFF_K = 0;
     static constexpr int OFF_Q = OFF_K + KS * TILE_BYTES;
     static constexpr int OFF_V = OFF_Q + QS * TILE_BYTES;
     static constexpr int OFF_KP = OFF_V + VS * TILE_BYTES;
-    static constexpr int OFF_S = OFF_KP + KP_STAGES * PIECE_BYTES;
+    static constexpr int OFF_S = OFF_KP + KP_WIDE * kTerms * TERM_BYTES;
     static constexpr int OFF_ROWS = OFF_S + (STATES ? 0 : D * D * 2);    // output: 32 rows x 16 channels a warp
     static constexpr int OFF_DEC = OFF_ROWS + (STATES ? 0 : 8 * 1024);
-    static constexpr int DEC_FLOATS = 4 * CT;          // integer parts and rests of -b_j; 2^(m - b_j); 2^(b_C - b_j)
+    // Of a chunk: 2^(b_C - b_j); whole part and rest of b_C; and where there is output: whole parts and rests of -b_j; 2^(m - b_j).
+    static constexpr int DEC_END = CT, DEC_WHOLE = CT + 4, DEC_REST = DEC_WHOLE + CT, DEC_U = DEC_REST + CT;
+    static constexpr int DEC_FLOATS = STATES ? DEC_WHOLE : DEC_U + CT;
     static constexpr int OFF_BAR = OFF_DEC + 2 * DEC_FLOATS * 4;
     static constexpr int NUM_BARS = 2 * (KS + QS + VS) + 2 * KP_STAGES + 16;
     static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16;
-    static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
+    static_assert(SMEM_BYTES <= 227 * 1024 && OFF_DEC % 16 == 0 && OFF_BAR % 8 == 0, "shared memory");
+    static_assert(KP_NARROW * kTermsInside <= KP_WIDE * kTerms, "places of K'");
 };
 
 // The bounded wait of this kernel: one answer for the warp, in few instructions; what ran out is reported at the role's end.  The roles'
@@ -185,7 +190,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         if (!aligned_ok) atomicCAS(p.status, 0, status_word(kWaitMisaligned, linear_cta()));
         for (int i = 0; i < C::KS; ++i) {
             mbar_init(&k_full[i], 1);
-            mbar_init(&k_empty[i], STATES ? 8 : 9);        // the warps that make K', and Q K^T
+            mbar_init(&k_empty[i], STATES ? 16 : 9);       // the warps that make K', and Q K^T
         }
         for (int i = 0; i < C::QS; ++i) {
             mbar_init(&q_full[i], 1);
@@ -196,12 +201,12 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             mbar_init(&v_empty[i], 1);
         }
         for (int i = 0; i < C::KP_STAGES; ++i) {
-            mbar_init(&kp_full[i], 8);
+            mbar_init(&kp_full[i], STATES ? 4 : 8);
             mbar_init(&kp_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&dec_full[i], 1);
-            mbar_init(&dec_empty[i], STATES ? 8 : 12);
+            mbar_init(&dec_empty[i], STATES ? 24 : 20);
             mbar_init(&o_full[i], 1);
             mbar_init(&o_empty[i], 4);
         }
@@ -232,6 +237,98 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         while (walk.enter())
             if (!STATES || !walk.whole_stream()) return true;
         return false;
+    };
+    // Places of K': their number and size go by the segment's number of parts; bit i of `par` is the parity of place i's uses.
+    struct Pieces {
+        uint32_t at = 0, par = 0, count = 0, bytes = 0;
+        __device__ __forceinline__ void segment(int terms) {
+            at = 0;
+            count = terms == kTerms ? C::KP_WIDE : C::KP_NARROW;
+            bytes = terms * TERM_BYTES;
+        }
+        __device__ __forceinline__ uint32_t parity(uint32_t i) const { return (par >> i) & 1u; }
+        __device__ __forceinline__ uint32_t offset() const { return C::OFF_KP + at * bytes; }
+        __device__ __forceinline__ void next() {
+            par ^= 1u << at;
+            at = at + 1 == count ? 0 : at + 1;
+        }
+    } pieces;
+    // the makers of K', before a segment's first piece: all places have been given back (they may lie differently from now on)
+    auto all_given_back = [&]() {
+#pragma unroll 1
+        for (uint32_t i = 0; i < C::KP_STAGES; ++i)
+            if (!wait(&kp_empty[i], pieces.parity(i) ^ 1u, kWaitTensor)) return false;
+        return true;
+    };
+    // One thread's share of a piece of K': THREADS threads, `tid` of them, rows 8 at a time per 64 of them.
+    auto make_piece = [&](auto threads, int tid, uint32_t it, int e, const float* weight, int valid, int terms) {
+        constexpr int ROWS = decltype(threads)::value / 8;                         // rows that are done at a time
+        const int row = tid >> 3;
+        const uint32_t at = row * 128 + (((tid & 7) ^ (row & 7)) << 4);            // inside a piece's half; the same in a tile's
+        const uint8_t* src = smem + C::OFF_K + place<C::KS>(it) * C::TILE_BYTES + e * PIECE_HALF + at;
+        uint8_t* dst = smem + pieces.offset() + at;
+        auto put = [&](int t, int off, const uint32_t (&v)[4]) {
+            *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + off) = make_uint4(v[0], v[1], v[2], v[3]);
+            // d = 64: the instruction's upper 64 rows are the same ones again (read by the second threads of the state's rows)
+            if (D == 64) *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + off + PIECE_HALF) = make_uint4(v[0], v[1], v[2], v[3]);
+        };
+#pragma unroll 1
+        for (int r = 0; r < PIECE; r += ROWS) {
+            const float w = weight[e * PIECE + r + row];
+            const bool in = e * PIECE + r + row < valid;
+#pragma unroll 1
+            for (int hf = 0; hf < C::HALVES; ++hf) {
+                uint4 raw = *reinterpret_cast<const uint4*>(src + hf * HALF_BYTES + r * 128);
+                if (!in) raw = make_uint4(0u, 0u, 0u, 0u);
+                const int off = hf * PIECE_HALF + r * 128;
+                const uint32_t kk[4] = {raw.x, raw.y, raw.z, raw.w};
+                if (!STATES && terms == kTermsInside) {
+                    // w = w1 + w2 to 16 bits, and all of it in bf16 pairs: w1 k rounded, what that rounding left out (exact), w2 k on top of that
+                    const uint32_t w1 = pack_bf16x2(w, w), w2 = pack_bf16x2(w - __uint_as_float(w1 << 16), w - __uint_as_float(w1 << 16));
+                    uint32_t a[4], b[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        a[q] = bf2_mul(w1, kk[q]);
+                        b[q] = bf2_fma(w2, kk[q], bf2_fma(w1, kk[q], a[q] ^ 0x80008000u));
+                    }
+                    put(0, off, a);
+                    put(1, off, b);
+                } else {
+                    const uint64_t w2 = f2_pack(w, w);
+                    uint64_t x[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) x[q] = f2_mul(w2, f2_pack(__uint_as_float(kk[q] << 16), __uint_as_float(kk[q] & 0xFFFF0000u)));
+#pragma unroll
+                    for (int t = 0; t < kTerms; ++t) {
+                        uint32_t part[4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            float x0, x1;
+                            f2_unpack(x[q], x0, x1);
+                            part[q] = pack_bf16x2(x0, x1);
+                            if (t + 1 < kTerms)
+                                x[q] = f2_fma(f2_pack(__uint_as_float(part[q] << 16), __uint_as_float(part[q] & 0xFFFF0000u)), f2_pack(-1.f, -1.f), x[q]);
+                        }
+                        put(t, off, part);
+                    }
+                }
+            }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&kp_full[pieces.at]);
+    };
+    // rows behind the sequence are the next one's, or none: they may hold anything, and 0 times that is not 0
+    auto clear_tail = [&](int threads, int tid, uint32_t it, int valid) {
+        if (!wait(&v_full[place<C::VS>(it)], round_of<C::VS>(it), kWaitRingFull)) return false;
+#pragma unroll 1
+        for (int i = tid; i < CT * 8 * C::HALVES; i += threads) {
+            const int r = i & (CT - 1), q = i / CT;
+            if (r >= valid)
+                *reinterpret_cast<uint4*>(smem + C::OFF_V + place<C::VS>(it) * C::TILE_BYTES + (q >> 3) * HALF_BYTES + r * 128 + (q & 7) * 16) =
+                    make_uint4(0u, 0u, 0u, 0u);
+        }
+        return true;
     };
     // parts of K': the state of a whole stream leaves with this kernel, those of cut ones come from the state-only pass
     auto terms_of = [&]() { return STATES || walk.whole_stream() ? kTerms : kTermsInside; };
@@ -292,6 +389,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 bool ok = true;
                 while (ok && enter()) {
                     const int terms = terms_of();
+                    pieces.segment(terms);
 #pragma unroll 1
                     for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                         const uint32_t ph = it & 1u, o_ph = (it >> 1) & 1u;
@@ -337,9 +435,9 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                                 __syncwarp();
                             }
                             // ---- K'^T V, 32 tokens
-                            if (!(ok = wait(&kp_full[(e & 1)], ((uint32_t)(e >> 1) & 1u), kWaitTensor))) break;
+                            if (!(ok = wait(&kp_full[pieces.at], pieces.parity(pieces.at), kWaitTensor))) break;
                             tc_fence_after();
-                            const uint64_t kp_desc = make_desc(sbase + C::OFF_KP + (e & 1) * C::PIECE_BYTES, PIECE_HALF, 1024);
+                            const uint64_t kp_desc = make_desc(sbase + pieces.offset(), PIECE_HALF, 1024);
                             const uint64_t vp_desc = v_desc + ((e * PIECE * 128) >> 4);
                             if (elect_one()) {
 #pragma unroll 1
@@ -348,13 +446,14 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                                     for (int ks = 0; ks < PIECE / 16; ++ks)
                                         umma_ss(tmem_base + COL_DS, kp_desc + ((t * TERM_BYTES + ks * 2048) >> 4), vp_desc + ((ks * 2048) >> 4), idesc_kv,
                                                 e > 0 || t > 0 || ks > 0 ? 1u : 0u);
-                                umma_commit(&kp_empty[(e & 1)]);
+                                umma_commit(&kp_empty[pieces.at]);
                                 if (e == PIECES - 1) {
                                     umma_commit(ds_full);
                                     if (STATES) umma_commit(&v_empty[place<C::VS>(it)]);
                                 }
                             }
                             __syncwarp();
+                            pieces.next();
                         }
                         if (!ok) break;
                         if (!STATES) {
@@ -416,11 +515,19 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     float* dst = dec + buf * C::DEC_FLOATS + lane * 4;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const double x = before + s[j], r = rint(x);
-                        dst[j] = (float)-r;
-                        dst[CT + j] = (float)(r - x);
-                        dst[2 * CT + j] = ex2_approx((float)(block_end - x));
-                        dst[3 * CT + j] = ex2_approx((float)(chunk_end - x));
+                        const double x = before + s[j];
+                        dst[j] = ex2_approx((float)(chunk_end - x));
+                        if (!STATES) {
+                            const double r = rint(x);
+                            dst[C::DEC_WHOLE + j] = (float)-r;
+                            dst[C::DEC_REST + j] = (float)(r - x);
+                            dst[C::DEC_U + j] = ex2_approx((float)(block_end - x));
+                        }
+                    }
+                    if (lane == 0) {
+                        const double r = rint(chunk_end);
+                        dst[C::DEC_END] = (float)r;
+                        dst[C::DEC_END + 1] = (float)(chunk_end - r);
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&dec_full[buf]);
@@ -445,6 +552,45 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 }
             }
         }
+    } else if (warp >= 24 || (STATES && warp < 12)) {
+        // ======================================= K' ==============================================
+        // 256 threads make a piece together; in the state-only pass four warpgroups make a piece each, in turn (no more teams than places:
+        // a team that waits for a place has seen the use before the last one of it given back).
+        if (warp >= 24) setmaxnreg_dec<kRegsKeys>(); else if (warp < 8) setmaxnreg_dec<kRegsP>(); else setmaxnreg_dec<kRegsOut>();
+        constexpr int TEAM = STATES ? 128 : 256;
+        constexpr uint32_t TEAMS = STATES ? 4 : 1;
+        const uint32_t team = !STATES ? 0u : warp < 12 ? (uint32_t)(warp >> 2) - 1u : (uint32_t)(warp >> 2) - 4u;
+        const int tid = threadIdx.x & (TEAM - 1);
+        uint32_t it = 0, turn = 0;
+        bool ok = aligned_ok;
+        while (ok && enter()) {
+            const int len = tab.len[walk.b], terms = terms_of();
+            if (!(ok = all_given_back())) break;
+            pieces.segment(terms);
+#pragma unroll 1
+            for (int c = walk.c; c < walk.c_end; ++c, ++it) {
+                const uint32_t buf = it & 1u;
+                const int valid = len - c * CT;            // tokens of the sequence from here on
+                if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
+                if (!(ok = wait(&k_full[place<C::KS>(it)], round_of<C::KS>(it), kWaitRingFull))) break;
+                if (valid < CT && turn == team && !(ok = clear_tail(TEAM, tid, it, valid))) break;     // (before piece 0)
+#pragma unroll 1
+                for (int e = 0; e < PIECES; ++e) {
+                    if (turn == team) {
+                        if (!(ok = wait(&kp_empty[pieces.at], pieces.parity(pieces.at) ^ 1u, kWaitTensor))) break;
+                        make_piece(std::integral_constant<int, TEAM>{}, tid, it, e, dec + buf * C::DEC_FLOATS, valid, terms);
+                    }
+                    pieces.next();
+                    turn = turn + 1u == TEAMS ? 0u : turn + 1u;
+                }
+                if (!ok) break;
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&k_empty[place<C::KS>(it)]);
+                    mbar_arrive(&dec_empty[buf]);
+                }
+            }
+        }
     } else if (warp < 8) {
         // ======================================= P ===============================================
         setmaxnreg_dec<kRegsP>();
@@ -457,7 +603,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                 const uint32_t buf = it & 1u, ph = it & 1u;
                 if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
-                const float* whole = dec + buf * C::DEC_FLOATS;                 // negated
+                const float* whole = dec + buf * C::DEC_FLOATS + C::DEC_WHOLE;   // negated
                 const float* rest = whole + CT;
                 const float wi = -whole[i], ri = -rest[i];
                 if (!(ok = wait(sc_full, ph, kWaitTensor))) break;
@@ -559,16 +705,13 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 const bool live0 = t0 + lrow < len, live1 = t0 + lrow + 16 < len;
                 __nv_bfloat16* out = p.base.o + (tok0 + t0 + lrow) * p.base.o_stride + at + lch * 8;
                 const __nv_bfloat16* gate = nm.gate + (tok0 + t0 + lrow) * nm.gate_stride + at + lch * 8;
-                uint4 g0, g1, n0, n1;                          // the gate's next 16 channels, and the ones behind
-                auto ask = [&](int j, uint4& a, uint4& b) {
-                    a = b = make_uint4(0u, 0u, 0u, 0u);
-                    if (live0) a = __ldg(reinterpret_cast<const uint4*>(gate + j));
-                    if (live1) b = __ldg(reinterpret_cast<const uint4*>(gate + 16 * nm.gate_stride + j));
+                uint4 g0, g1;                                  // the gate's next 16 channels
+                auto ask = [&](int j) {
+                    g0 = g1 = make_uint4(0u, 0u, 0u, 0u);
+                    if (live0) g0 = __ldg(reinterpret_cast<const uint4*>(gate + j));
+                    if (live1) g1 = __ldg(reinterpret_cast<const uint4*>(gate + 16 * nm.gate_stride + j));
                 };
-                if (nm.gate) {
-                    ask(0, g0, g1);
-                    ask(16, n0, n1);
-                }
+                if (nm.gate) ask(0);
                 if (!(ok = wait(&o_full[mine], (it >> 1) & 1u, kWaitTensor))) break;
                 tc_fence_after();
                 // 16 channels of the row: a * x + add
@@ -614,9 +757,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     if (nm.gate) {
                         *staged(lrow, lch) = g0;
                         *staged(lrow + 16, lch) = g1;
-                        g0 = n0;
-                        g1 = n1;
-                        if (j + 32 < D) ask(j + 32, n0, n1);
+                        if (j + 16 < D) ask(j + 16);
                         __syncwarp();
                     }
                     uint64_t y[8];
@@ -627,29 +768,29 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         if (lane == 0) mbar_arrive(&o_empty[mine]);
                     }
                     if (nm.on) {
-                        uint64_t f[8];
-                        auto eight = [&](const uint4& v, int at8) {
-                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                            for (int q = 0; q < 4; ++q) f[at8 + q] = f2_pack(__uint_as_float(w[q] << 16), __uint_as_float(w[q] & 0xFFFF0000u));
-                        };
-                        if (nm.gain) {
-                            eight(__ldg(reinterpret_cast<const uint4*>(nm.gain + at + j)), 0);
-                            eight(__ldg(reinterpret_cast<const uint4*>(nm.gain + at + j) + 1), 4);
+                        for (int e = 0; e < 2; ++e) {          // eight channels
+                            uint64_t f[4];
+                            auto eight = [&](const uint4& v) {
+                                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                            for (int q = 0; q < 8; ++q) y[q] = f2_mul(y[q], f[q]);
-                        }
-                        if (nm.bias) {
-                            eight(__ldg(reinterpret_cast<const uint4*>(nm.bias + at + j)), 0);
-                            eight(__ldg(reinterpret_cast<const uint4*>(nm.bias + at + j) + 1), 4);
+                                for (int q = 0; q < 4; ++q) f[q] = f2_pack(__uint_as_float(w[q] << 16), __uint_as_float(w[q] & 0xFFFF0000u));
+                            };
+                            if (nm.gain) {
+                                eight(__ldg(reinterpret_cast<const uint4*>(nm.gain + at + j) + e));
 #pragma unroll
-                            for (int q = 0; q < 8; ++q) y[q] = f2_add(y[q], f[q]);
-                        }
-                        if (nm.gate) {                     // (a thread's row of the gate gives way to its row of the output)
-                            eight(*staged(lane, 0), 0);
-                            eight(*staged(lane, 1), 4);
+                                for (int q = 0; q < 4; ++q) y[4 * e + q] = f2_mul(y[4 * e + q], f[q]);
+                            }
+                            if (nm.bias) {
+                                eight(__ldg(reinterpret_cast<const uint4*>(nm.bias + at + j) + e));
 #pragma unroll
-                            for (int q = 0; q < 8; ++q) y[q] = f2_swish_mul(f[q], y[q]);
+                                for (int q = 0; q < 4; ++q) y[4 * e + q] = f2_add(y[4 * e + q], f[q]);
+                            }
+                            if (nm.gate) {                     // (a thread's row of the gate gives way to its row of the output)
+                                eight(*staged(lane, e));
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) y[4 * e + q] = f2_swish_mul(f[q], y[4 * e + q]);
+                            }
                         }
                     }
                     uint32_t w[8];
@@ -669,18 +810,16 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             }
         }
     } else {
-        // ======================================= K', state =======================================
+        // ======================================= state ===========================================
         setmaxnreg_inc<kRegsState>();
         constexpr int N = D * D / 256;                     // channels of a thread: half a row of the state (d = 64: a quarter)
         const int quad = warp & 3, l = quad * 32 + lane, row = l % D, col = (warp >= 16 ? D / 2 : 0) + (l / D) * N;
         const uint32_t ds = tmem_base + COL_DS + ((uint32_t)(quad * 32) << 16) + col;
         uint8_t* s_row = smem + C::OFF_S + row * 128;
-        const int tid = threadIdx.x - 12 * 32, k_row = tid >> 3;
-        const uint32_t k_at = k_row * 128 + (((tid & 7) ^ (k_row & 7)) << 4);      // inside a piece's half; the same in a tile's
         uint32_t it = 0;
         bool ok = aligned_ok;
         while (ok && enter()) {
-            const int b = walk.b, h = walk.h, len = tab.len[b], terms = terms_of();
+            const int b = walk.b, h = walk.h;
             const bool whole_stream = walk.whole_stream();
             float s[N];
             // where the segment's first state is: the stream's own, or what the merge left for this CTA
@@ -703,79 +842,23 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll 1
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                 const uint32_t buf = it & 1u, ph = it & 1u;
-                const int valid = len - c * CT;            // tokens of the sequence from here on
-                if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
-                const float* decays = dec + buf * C::DEC_FLOATS;
-                const float whole = -decays[CT - 1], rest = -decays[2 * CT - 1];
-                if (!(ok = wait(&k_full[place<C::KS>(it)], round_of<C::KS>(it), kWaitRingFull))) break;
-                if (valid < CT) {
-                    // rows behind the sequence are the next one's, or none: they may hold anything, and 0 times that is not 0
-                    if (!(ok = wait(&v_full[place<C::VS>(it)], round_of<C::VS>(it), kWaitRingFull))) break;
-                    const int r = tid >> 1;
-                    if (r >= valid) {
-#pragma unroll 1
-                        for (int q = tid & 1; q < 8 * C::HALVES; q += 2)
-                            *reinterpret_cast<uint4*>(smem + C::OFF_V + place<C::VS>(it) * C::TILE_BYTES + (q >> 3) * HALF_BYTES + r * 128 + (q & 7) * 16) =
-                                make_uint4(0u, 0u, 0u, 0u);
-                    }
-                }
-#pragma unroll 1
-                for (int e = 0; e < PIECES; ++e) {
-                    if (!STATES && e == 1) {
-                        // ---- S in bf16
-                        if (!(ok = wait(s_empty, ph ^ 1u, kWaitTensor))) break;
+                if (!STATES) {
+                    // ---- S in bf16
+                    if (!(ok = wait(s_empty, ph ^ 1u, kWaitTensor))) break;
 #pragma unroll
-                        for (int j = 0; j < N; j += 8) {
-                            const int ch = (col + j) / 8;
-                            *reinterpret_cast<uint4*>(s_row + (ch >> 3) * (D * 128) + (((ch & 7) ^ (row & 7)) << 4)) =
-                                pack8(*reinterpret_cast<float(*)[8]>(&s[j]));
-                        }
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(s_full);
-                    }
-                    // ---- 32 tokens of K'
-                    const float w = decays[3 * CT + e * PIECE + k_row];
-                    const uint64_t w2 = f2_pack(w, w);
-                    const bool in = e * PIECE + k_row < valid;
-                    if (!(ok = wait(&kp_empty[(e & 1)], ((uint32_t)(e >> 1) & 1u) ^ 1u, kWaitTensor))) break;
-                    uint8_t* dst = smem + C::OFF_KP + (e & 1) * C::PIECE_BYTES + k_at;
-#pragma unroll 1
-                    for (int hf = 0; hf < C::HALVES; ++hf) {
-                        uint4 raw = *reinterpret_cast<const uint4*>(smem + C::OFF_K + place<C::KS>(it) * C::TILE_BYTES + e * PIECE_HALF + hf * HALF_BYTES + k_at);
-                        if (!in) raw = make_uint4(0u, 0u, 0u, 0u);
-                        const uint32_t kk[4] = {raw.x, raw.y, raw.z, raw.w};
-                        uint64_t x[4];
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) x[q] = f2_mul(w2, f2_pack(__uint_as_float(kk[q] << 16), __uint_as_float(kk[q] & 0xFFFF0000u)));
-#pragma unroll
-                        for (int t = 0; t < kTerms; ++t) {
-                            if (t >= kTermsInside && t >= terms) break;
-                            uint32_t part[4];
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                float x0, x1;
-                                f2_unpack(x[q], x0, x1);
-                                part[q] = pack_bf16x2(x0, x1);
-                                if (t + 1 < kTerms)
-                                    x[q] = f2_fma(f2_pack(__uint_as_float(part[q] << 16), __uint_as_float(part[q] & 0xFFFF0000u)), f2_pack(-1.f, -1.f), x[q]);
-                            }
-                            const uint4 v = make_uint4(part[0], part[1], part[2], part[3]);
-                            *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + hf * PIECE_HALF) = v;
-                            // d = 64: the instruction's upper 64 rows are the same ones again (read by the second threads of the state's rows)
-                            if (D == 64) *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + PIECE_HALF) = v;
-                        }
+                    for (int j = 0; j < N; j += 8) {
+                        const int ch = (col + j) / 8;
+                        *reinterpret_cast<uint4*>(s_row + (ch >> 3) * (D * 128) + (((ch & 7) ^ (row & 7)) << 4)) =
+                            pack8(*reinterpret_cast<float(*)[8]>(&s[j]));
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&kp_full[(e & 1)]);
+                    if (lane == 0) mbar_arrive(s_full);
                 }
-                if (!ok) break;
+                if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
+                const float whole = dec[buf * C::DEC_FLOATS + C::DEC_END], rest = dec[buf * C::DEC_FLOATS + C::DEC_END + 1];
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(&k_empty[place<C::KS>(it)]);
-                    mbar_arrive(&dec_empty[buf]);
-                }
+                if (lane == 0) mbar_arrive(&dec_empty[buf]);
                 // ---- S'
                 const float keep = exp2_parts(whole, rest);
                 if (STATES) {
@@ -809,7 +892,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 for (int j = 0; j < N; j += 4)
                     *reinterpret_cast<float4*>(dst + row * D + col + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
             }
-            if (STATES && tid == 0) p.part_keep[slot] = exp2_parts(all_whole, all_rest);
+            if (STATES && threadIdx.x == 12 * 32) p.part_keep[slot] = exp2_parts(all_whole, all_rest);
         }
     }
 
