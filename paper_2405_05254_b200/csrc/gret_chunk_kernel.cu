@@ -5,22 +5,21 @@
 //     S' = 2^b_C S + sum_j (2^(b_C - b_j) k_j)^T v_j.
 // A CTA walks a contiguous range of chunks, of one (sequence, head) stream or of several one after the other, with the state in the
 // registers of two warpgroups.  1,024 threads:
-//   warp 0       TMA producer: K, Q, V tiles (128 tokens x d, 128-byte swizzle)
-//   warp 1       issuer of all products: Q K^T -> SC;  K'^T V -> DS;  Q S and P V -> O[n & 1]    (tensor memory, fp32)
+//   warp 0       TMA producer: K, Q, V tiles (128 tokens x d, 128-byte swizzle); asks for the gate's rows
+//   warp 1       issuer of Q K^T -> SC, Q S -> O[n & 1], P V on top of it      (tensor memory, fp32)
+//   warp 3       issuer of K'^T V -> DS
 //   warp 2       decays: prefix sums of the logarithms in 64 bits, kept as integer part and rest (b_i - b_j is the difference of
 //                both: exact to 2^-24 however strong the decays before j were), and the factors that depend on one token alone
-//   warp 3       asks for the gate's rows, a chunk ahead
-//   warpgroup 1  thread = token: P (bf16, over the scores' own columns: it goes to P V from tensor memory); 2^b_i times Q S, in place
+//   warpgroup 1  thread = token: P (bf16, over the scores' own columns: it goes to P V from tensor memory)
 //   warpgroups 2, 5  thread = token, every other chunk each: the output: scale, normalisation, gate, rounding, store
-//   warpgroups 3, 4  thread = half a row of the state: S' from S and DS in fp32, S in bf16 to shared memory for Q S
+//   warpgroups 3, 4  thread = half a row of the state: S' from S and DS in fp32, S in bf16 to shared memory for Q S; 2^b_i times
+//                Q S, in place
 //   warpgroups 6, 7  K' = 2^(b_C - b_j) k_j, in pieces of 32 tokens
 // Decays of P: in the 32 x 32 blocks on the diagonal one exponential per element; below it 2^(b_i - m) 2^(m - b_j), m the value at the
 // end of j's block: both factors are at most 1, and the second is the same for all rows.
 // Roundings: P and the copy of S that multiplies Q go to bf16 (half a step, 2^-9 of the value, like the output's own).  K' goes to
 // the tensor cores as a sum of bf16: where the sums leave the kernel as a state, of three (24 bits; with one it would be 1.7e-3 off (2-norm),
 // with two 2e-6), where they only multiply Q inside, of two.
-//
-// Order of the products per chunk: Q K^T, a quarter of K'^T V, Q S, the other three, P V.
 #include <type_traits>
 
 #include "gret.cuh"
@@ -68,7 +67,7 @@ struct GCfg {
     static constexpr int DEC_END = CT, DEC_WHOLE = CT + 4, DEC_REST = DEC_WHOLE + CT, DEC_U = DEC_REST + CT;
     static constexpr int DEC_FLOATS = STATES ? DEC_WHOLE : DEC_U + CT;
     static constexpr int OFF_BAR = OFF_DEC + 2 * DEC_FLOATS * 4;
-    static constexpr int NUM_BARS = 2 * (KS + QS + VS) + 2 * KP_STAGES + 16;
+    static constexpr int NUM_BARS = 2 * (KS + QS + VS) + 2 * KP_STAGES + 19;
     static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16;
     static_assert(SMEM_BYTES <= 227 * 1024 && OFF_DEC % 16 == 0 && OFF_BAR % 8 == 0, "shared memory");
     static_assert(KP_NARROW * kTermsInside <= KP_WIDE * kTerms, "places of K'");
@@ -172,11 +171,11 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     uint64_t* sc_full = dec_full + 8;
     uint64_t* qs_full = dec_full + 9;
     uint64_t* p_full = dec_full + 10;
-    uint64_t* ds_full = dec_full + 11;
-    uint64_t* ds_empty = dec_full + 12;
-    uint64_t* s_full = dec_full + 13;
-    uint64_t* s_empty = dec_full + 14;
-    uint64_t* drain_bar = dec_full + 15;
+    uint64_t* s_full = dec_full + 11;
+    uint64_t* s_empty = dec_full + 12;
+    uint64_t* ds_full = dec_full + 13;                     // [2], the state-only pass has two buffers of DS
+    uint64_t* ds_empty = dec_full + 15;                    // [2]
+    uint64_t* drain_bar = dec_full + 17;                   // [2]
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     float* dec = reinterpret_cast<float*>(smem + C::OFF_DEC);
@@ -198,7 +197,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
         for (int i = 0; i < C::VS; ++i) {
             mbar_init(&v_full[i], 1);
-            mbar_init(&v_empty[i], 1);
+            mbar_init(&v_empty[i], STATES ? 1 : 2);        // K'^T V, and P V
         }
         for (int i = 0; i < C::KP_STAGES; ++i) {
             mbar_init(&kp_full[i], STATES ? 4 : 8);
@@ -212,12 +211,15 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
         mbar_init(sc_full, 1);
         mbar_init(qs_full, 1);
-        mbar_init(p_full, 4);
-        mbar_init(ds_full, 1);
-        mbar_init(ds_empty, 8);
+        mbar_init(p_full, 12);                             // P, and the scaled Q S
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&ds_full[i], 1);
+            mbar_init(&ds_empty[i], 8);
+        }
         mbar_init(s_full, 8);
         mbar_init(s_empty, 1);
-        mbar_init(drain_bar, 1);
+        mbar_init(&drain_bar[0], 1);
+        mbar_init(&drain_bar[1], 1);
         mbar_fence_init();
     }
     if (warp == 1) {
@@ -366,6 +368,16 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                             __syncwarp();
                         }
                         if (!ok) break;
+                        if (!STATES && p.base.norm.gate) {     // the gate's rows, into L2
+                            const int len = tab.len[walk.b];
+#pragma unroll 1
+                            for (int r = lane; r < CT * C::HALVES; r += 32) {
+                                const int t = c * CT + r / C::HALVES;
+                                if (t < len)
+                                    asm volatile("prefetch.global.L2 [%0];" ::"l"(p.base.norm.gate + (tab.tok0[walk.b] + (int64_t)t) * p.base.norm.gate_stride +
+                                                                                  x + (r % C::HALVES) * 64));
+                            }
+                        }
                     }
                 }
                 // no copy may land after the CTA has ended (at once when all went well): the last ones into every place
@@ -380,11 +392,73 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 }
             }
         } else if (warp == 1) {
-            // ======================================= issuer of the products ======================
+            // ======================================= issuer of Q S, Q K^T, P V ===================
             if (aligned_ok) {
                 constexpr uint32_t idesc_qk = make_idesc(CT, false);
                 constexpr uint32_t idesc_mn = make_idesc(D, true);              // B with its columns contiguous: V, S
-                constexpr uint32_t idesc_kv = idesc_mn | (1u << 15);            // and A with its rows contiguous: K'
+                const uint64_t s_desc = make_desc(sbase + C::OFF_S, D * 128, 1024);
+                uint32_t it = 0;
+                bool ok = !STATES;
+                while (ok && enter()) {
+#pragma unroll 1
+                    for (int c = walk.c; c < walk.c_end; ++c, ++it) {
+                        const uint32_t ph = it & 1u;
+                        const uint32_t o_cols = tmem_base + COL_O + ph * 128;
+                        const uint64_t q_desc = make_desc(sbase + C::OFF_Q + place<QS>(it) * C::TILE_BYTES, 16, 1024);
+                        const uint64_t k_desc = make_desc(sbase + C::OFF_K + place<C::KS>(it) * C::TILE_BYTES, 16, 1024);
+                        const uint64_t v_desc = make_desc(sbase + C::OFF_V + place<C::VS>(it) * C::TILE_BYTES, HALF_BYTES, 1024);
+                        if (!(ok = wait(&k_full[place<C::KS>(it)], round_of<C::KS>(it), kWaitRingFull))) break;
+                        if (!(ok = wait(&q_full[place<QS>(it)], round_of<QS>(it), kWaitRingFull))) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int ks = 0; ks < D / 16; ++ks) {
+                                const uint32_t off = (ks >> 2) * HALF_BYTES + (ks & 3) * 32;
+                                umma_ss(tmem_base + COL_SC, q_desc + (off >> 4), k_desc + (off >> 4), idesc_qk, ks > 0 ? 1u : 0u);
+                            }
+                            umma_commit(sc_full);
+                            umma_commit(&k_empty[place<C::KS>(it)]);
+                        }
+                        __syncwarp();
+                        if (!(ok = wait(s_full, ph, kWaitTensor))) break;
+                        if (!(ok = wait(&o_empty[ph], ((it >> 1) & 1u) ^ 1u, kWaitTensor))) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int ks = 0; ks < D / 16; ++ks) {
+                                const uint32_t off = (ks >> 2) * HALF_BYTES + (ks & 3) * 32;
+                                umma_ss(o_cols, q_desc + (off >> 4), s_desc + ((ks * 16 * 128) >> 4), idesc_mn, ks > 0 ? 1u : 0u);
+                            }
+                            umma_commit(qs_full);
+                            umma_commit(s_empty);
+                            umma_commit(&q_empty[place<QS>(it)]);
+                        }
+                        __syncwarp();
+                        // P V, on top of Q S
+                        if (!(ok = wait(&v_full[place<C::VS>(it)], round_of<C::VS>(it), kWaitRingFull))) break;
+                        if (!(ok = wait(p_full, ph, kWaitTensor))) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int ks = 0; ks < CT / 16; ++ks)
+                                umma_ts(o_cols, tmem_base + COL_SC + ks * 8, v_desc + ((ks * 16 * 128) >> 4), idesc_mn, 1u);
+                            umma_commit(&o_full[ph]);
+                            umma_commit(&v_empty[place<C::VS>(it)]);
+                        }
+                        __syncwarp();
+                    }
+                }
+                // nothing issued may still run when tensor memory is released
+                if (elect_one()) {
+                    umma_commit(&drain_bar[0]);
+                    drain_wait(&drain_bar[0], 0u, ab);
+                }
+                __syncwarp();
+            }
+        } else if (warp == 3) {
+            // ======================================= issuer of K'^T V ============================
+            if (aligned_ok) {
+                constexpr uint32_t idesc_kv = make_idesc(D, true) | (1u << 15); // both operands with their columns contiguous
                 uint32_t it = 0;
                 bool ok = true;
                 while (ok && enter()) {
@@ -392,89 +466,41 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     pieces.segment(terms);
 #pragma unroll 1
                     for (int c = walk.c; c < walk.c_end; ++c, ++it) {
-                        const uint32_t ph = it & 1u, o_ph = (it >> 1) & 1u;
-                        const uint32_t o_cols = tmem_base + COL_O + ph * 128;
-                        const uint64_t q_desc = make_desc(sbase + C::OFF_Q + place<QS>(it) * C::TILE_BYTES, 16, 1024);
+                        const uint32_t buf = STATES ? it & 1u : 0u, round = STATES ? (it >> 1) & 1u : it & 1u;
+                        const uint32_t d_cols = tmem_base + (buf ? COL_SC : COL_DS);
                         const uint64_t v_desc = make_desc(sbase + C::OFF_V + place<C::VS>(it) * C::TILE_BYTES, HALF_BYTES, 1024);
-                        if (!STATES) {
-                            if (!(ok = wait(&k_full[place<C::KS>(it)], round_of<C::KS>(it), kWaitRingFull))) break;
-                            if (!(ok = wait(&q_full[place<QS>(it)], round_of<QS>(it), kWaitRingFull))) break;
-                            tc_fence_after();
-                            const uint64_t k_desc = make_desc(sbase + C::OFF_K + place<C::KS>(it) * C::TILE_BYTES, 16, 1024);
-                            if (elect_one()) {
-#pragma unroll 1
-                                for (int ks = 0; ks < D / 16; ++ks) {
-                                    const uint32_t off = (ks >> 2) * HALF_BYTES + (ks & 3) * 32;
-                                    umma_ss(tmem_base + COL_SC, q_desc + (off >> 4), k_desc + (off >> 4), idesc_qk, ks > 0 ? 1u : 0u);
-                                }
-                                umma_commit(sc_full);
-                                umma_commit(&k_empty[place<C::KS>(it)]);
-                            }
-                            __syncwarp();
-                        }
                         if (!(ok = wait(&v_full[place<C::VS>(it)], round_of<C::VS>(it), kWaitRingFull))) break;
-                        if (!(ok = wait(ds_empty, ph ^ 1u, kWaitTensor))) break;
+                        if (!(ok = wait(&ds_empty[buf], round ^ 1u, kWaitTensor))) break;
 #pragma unroll 1
                         for (int e = 0; e < PIECES; ++e) {
-                            if (!STATES && e == 1) {
-                                // ---- Q S
-                                if (!(ok = wait(s_full, ph, kWaitTensor))) break;
-                                if (!(ok = wait(&o_empty[ph], o_ph ^ 1u, kWaitTensor))) break;
-                                tc_fence_after();
-                                const uint64_t s_desc = make_desc(sbase + C::OFF_S, D * 128, 1024);
-                                if (elect_one()) {
-#pragma unroll 1
-                                    for (int ks = 0; ks < D / 16; ++ks) {
-                                        const uint32_t off = (ks >> 2) * HALF_BYTES + (ks & 3) * 32;
-                                        umma_ss(o_cols, q_desc + (off >> 4), s_desc + ((ks * 16 * 128) >> 4), idesc_mn, ks > 0 ? 1u : 0u);
-                                    }
-                                    umma_commit(qs_full);
-                                    umma_commit(s_empty);
-                                    umma_commit(&q_empty[place<QS>(it)]);
-                                }
-                                __syncwarp();
-                            }
-                            // ---- K'^T V, 32 tokens
                             if (!(ok = wait(&kp_full[pieces.at], pieces.parity(pieces.at), kWaitTensor))) break;
                             tc_fence_after();
                             const uint64_t kp_desc = make_desc(sbase + pieces.offset(), PIECE_HALF, 1024);
                             const uint64_t vp_desc = v_desc + ((e * PIECE * 128) >> 4);
                             if (elect_one()) {
-#pragma unroll 1
-                                for (int t = 0; t < terms; ++t)
+#pragma unroll
+                                for (int t = 0; t < kTerms; ++t) {
+                                    if (t >= kTermsInside && t >= terms) break;
 #pragma unroll
                                     for (int ks = 0; ks < PIECE / 16; ++ks)
-                                        umma_ss(tmem_base + COL_DS, kp_desc + ((t * TERM_BYTES + ks * 2048) >> 4), vp_desc + ((ks * 2048) >> 4), idesc_kv,
-                                                e > 0 || t > 0 || ks > 0 ? 1u : 0u);
+                                        umma_ss(d_cols, kp_desc + ((t * TERM_BYTES + ks * 2048) >> 4), vp_desc + ((ks * 2048) >> 4), idesc_kv,
+                                                t > 0 || ks > 0 ? 1u : e > 0 ? 1u : 0u);
+                                }
                                 umma_commit(&kp_empty[pieces.at]);
                                 if (e == PIECES - 1) {
-                                    umma_commit(ds_full);
-                                    if (STATES) umma_commit(&v_empty[place<C::VS>(it)]);
+                                    umma_commit(&ds_full[buf]);
+                                    umma_commit(&v_empty[place<C::VS>(it)]);
                                 }
                             }
                             __syncwarp();
                             pieces.next();
                         }
                         if (!ok) break;
-                        if (!STATES) {
-                            // ---- P V, on top of Q S
-                            if (!(ok = wait(p_full, ph, kWaitTensor))) break;
-                            tc_fence_after();
-                            if (elect_one()) {
-#pragma unroll 1
-                                for (int ks = 0; ks < CT / 16; ++ks)
-                                    umma_ts(o_cols, tmem_base + COL_SC + ks * 8, v_desc + ((ks * 16 * 128) >> 4), idesc_mn, 1u);
-                                umma_commit(&o_full[ph]);
-                                umma_commit(&v_empty[place<C::VS>(it)]);
-                            }
-                            __syncwarp();
-                        }
                     }
                 }
-                // nothing issued may still run when tensor memory is released
                 if (elect_one()) {
-                    umma_commit(drain_bar);
-                    drain_wait(drain_bar, 0u, ab);
+                    umma_commit(&drain_bar[1]);
+                    drain_wait(&drain_bar[1], 0u, ab);
                 }
                 __syncwarp();
             }
@@ -531,24 +557,6 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&dec_full[buf]);
-                }
-            }
-        } else if (!STATES && p.base.norm.gate && aligned_ok) {
-            // ======================================= the gate's rows, into L2 a chunk ahead ======
-            uint32_t it = 0;
-            bool ok = true;
-            while (ok && enter()) {
-                const int len = tab.len[walk.b];
-                const __nv_bfloat16* gate = p.base.norm.gate + (int64_t)tab.tok0[walk.b] * p.base.norm.gate_stride + walk.h * D;
-#pragma unroll 1
-                for (int c = walk.c; c < walk.c_end; ++c, ++it) {
-                    if (it > 0 && !(ok = wait(sc_full, (it - 1) & 1u, kWaitTensor))) break;
-#pragma unroll 1
-                    for (int r = lane; r < CT * C::HALVES; r += 32) {
-                        const int t = c * CT + r / C::HALVES;
-                        if (t < len)
-                            asm volatile("prefetch.global.L2 [%0];" ::"l"(gate + t * p.base.norm.gate_stride + (r % C::HALVES) * 64));
-                    }
                 }
             }
         }
@@ -654,31 +662,10 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 for (int j = 0; j < 8; ++j) w[j] = 0u;
 #pragma unroll 1
                 for (int blk = 2 * quad + 2; blk < 8; ++blk) tmem_st8(sc + blk * 8, w);
-                // ---- 2^b_i q_i S
-                const float ei = exp2_parts(wi, ri);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&dec_empty[buf]);
-                if (!(ok = wait(qs_full, ph, kWaitTensor))) break;
-                tc_fence_after();
-                const uint32_t o = tmem_base + COL_O + ph * 128 + ((uint32_t)(quad * 32) << 16);
-                const uint64_t ei2 = f2_pack(ei, ei);
-#pragma unroll 1
-                for (int j = 0; j < D; j += 16) {
-                    uint32_t x[16];
-                    tmem_ld16(o + j, *reinterpret_cast<float(*)[16]>(&x));
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int q = 0; q < 16; q += 2) {
-                        float y0, y1;
-                        f2_unpack(f2_mul(ei2, f2_pack(__uint_as_float(x[q]), __uint_as_float(x[q + 1]))), y0, y1);
-                        x[q] = __float_as_uint(y0);
-                        x[q + 1] = __float_as_uint(y1);
-                    }
-                    tmem_st16(o + j, x);
-                }
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
+                if (lane == 0) mbar_arrive(&dec_empty[buf]);
                 if (lane == 0) mbar_arrive(p_full);
             }
         }
@@ -814,7 +801,6 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         setmaxnreg_inc<kRegsState>();
         constexpr int N = D * D / 256;                     // channels of a thread: half a row of the state (d = 64: a quarter)
         const int quad = warp & 3, l = quad * 32 + lane, row = l % D, col = (warp >= 16 ? D / 2 : 0) + (l / D) * N;
-        const uint32_t ds = tmem_base + COL_DS + ((uint32_t)(quad * 32) << 16) + col;
         uint8_t* s_row = smem + C::OFF_S + row * 128;
         uint32_t it = 0;
         bool ok = aligned_ok;
@@ -857,6 +843,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 }
                 if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
                 const float whole = dec[buf * C::DEC_FLOATS + C::DEC_END], rest = dec[buf * C::DEC_FLOATS + C::DEC_END + 1];
+                const float ei = STATES ? 0.f : exp2_parts(-dec[buf * C::DEC_FLOATS + C::DEC_WHOLE + l], -dec[buf * C::DEC_FLOATS + C::DEC_REST + l]);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&dec_empty[buf]);
                 // ---- S'
@@ -865,8 +852,30 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     all_whole += whole;
                     all_rest += rest;
                 }
-                if (!(ok = wait(ds_full, ph, kWaitTensor))) break;
+                if (!STATES) {
+                    // ---- 2^b_i q_i S, in place: this thread's token, half of the channels
+                    if (!(ok = wait(qs_full, ph, kWaitTensor))) break;
+                    tc_fence_after();
+                    const uint32_t o = tmem_base + COL_O + ph * 128 + ((uint32_t)(quad * 32) << 16) + (warp >= 16 ? D / 2 : 0);
+                    const uint64_t ei2 = f2_pack(ei, ei);
+#pragma unroll 1
+                    for (int j = 0; j < D / 2; j += 16) {
+                        float x[16];
+                        tmem_ld16(o + j, x);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int q = 0; q < 16; q += 2) f2_unpack(f2_mul(ei2, f2_pack(x[q], x[q + 1])), x[q], x[q + 1]);
+                        tmem_st16(o + j, *reinterpret_cast<uint32_t(*)[16]>(&x));
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full);
+                }
+                const uint32_t ds_buf = STATES ? it & 1u : 0u;
+                if (!(ok = wait(&ds_full[ds_buf], STATES ? (it >> 1) & 1u : ph, kWaitTensor))) break;
                 tc_fence_after();
+                const uint32_t ds = tmem_base + (ds_buf ? COL_SC : COL_DS) + ((uint32_t)(quad * 32) << 16) + col;
 #pragma unroll
                 for (int blk = 0; blk < N / 16; ++blk) {
                     float x[16];
@@ -877,7 +886,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(ds_empty);
+                if (lane == 0) mbar_arrive(&ds_empty[ds_buf]);
             }
             if (!ok) break;
             // a state-only segment that ends inside its stream: the next CTA's start; one that ends it: the last part of the final state
