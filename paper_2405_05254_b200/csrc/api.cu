@@ -748,8 +748,10 @@ int32_t check_slots(const yoco_gret_shape& s, const int32_t* in, const int32_t* 
     return YOCO_OK;
 }
 
-// Sequences of no more tokens than this walk them one by one (one CTA per head, state in registers); longer ones in chunks.
-constexpr int32_t kGretTokens = 16;
+// Calls whose sequences all have no more tokens than this walk them one by one (one CTA per head, state in registers); longer ones in chunks.
+// (Measured, 32 heads of 128: one sequence of 17 / 32 / 64 tokens 12.9 / 17.1 / 35 us token by token, 17 in chunks; 32 sequences of 17 / 32
+// tokens 68 / 103 us, in chunks 83 / 84.)
+constexpr int32_t kGretTokens = 24;
 // What a chunk costs in the state-only pass over split streams, and the extra launches, in chunks of the main pass.
 constexpr double kGretStateCost = 0.55, kGretSplitCost = 3.0;
 
@@ -762,7 +764,7 @@ struct GretPlan {
     size_t bytes() const { return split ? part_bytes + (size_t)3 * groups * sizeof(float) : 0; }
 };
 
-// Whole streams, one per CTA (longest first), or equal ranges of chunks that cut streams: the latter pay a second pass over K and V.
+// Whole streams, dealt out to the CTAs (longest first), or equal ranges of chunks that cut streams: the latter pay a second pass over K and V.
 void plan_gret(const yoco_gret_shape& s, const int32_t* len_host, const GretTable* slots, int32_t sm_count, GretPlan* out) {
     std::memset(&out->tab, 0, sizeof out->tab);
     std::vector<std::pair<int32_t, int32_t>> order;        // (-length, sequence)
@@ -791,7 +793,7 @@ void plan_gret(const yoco_gret_shape& s, const int32_t* len_host, const GretTabl
     const int64_t cut = std::min<int64_t>(out->total, sm_count);
     const double share = cut > 0 ? (double)((out->total + cut - 1) / cut) : 0.0;
     out->split = cut > 1 && share * (1.0 + kGretStateCost) + kGretSplitCost < whole;
-    out->groups = (int32_t)(out->split ? cut : streams);
+    out->groups = (int32_t)(out->split ? cut : std::min<int64_t>(streams, sm_count));
     out->part_bytes = (size_t)3 * out->groups * s.d * s.d * sizeof(float);
 }
 
@@ -1351,10 +1353,8 @@ int32_t yoco_gret_workspace_size(const yoco_gret_shape* shape, const int32_t* le
         if (rc != YOCO_OK || (rc = check_lengths(shape->B, len_host, shape->T, &tokens)) != YOCO_OK) return rc;
         int32_t longest = 0;
         for (int32_t i = 0; i < shape->B; ++i) longest = std::max(longest, len_host ? len_host[i] : shape->T);
-        if (longest <= kGretTokens) {
-            *bytes = 0;
-            return YOCO_OK;
-        }
+        *bytes = 0;
+        if (longest <= kGretTokens) return YOCO_OK;
         if (sm_count <= 0) {
             DeviceState* dev = nullptr;
             if ((rc = device_state(&dev)) != YOCO_OK) return rc;

@@ -24,18 +24,14 @@ __device__ __forceinline__ float log_decay(const GretParams& p, float z) {
 
 __device__ __forceinline__ float swish(float u) { return __fdividef(u, 1.f + __expf(-u)); }
 
-// y * swish(u) for two at a time, with one reciprocal for both: 1 / a = b / (a b).  Below -40, where swish is within
-// 1.7e-16 of 0, u counts as -40, so that the product keeps its reciprocal a normal number; a NaN stays one.
+// y * swish(u) for two at a time: u y / (1 + 2^(-u log2 e))
 __device__ __forceinline__ uint64_t f2_swish_mul(uint64_t u, uint64_t y) {
-    float u0, u1, e0, e1, r;
-    f2_unpack(u, u0, u1);
-    asm("max.NaN.f32 %0, %0, 0fC2200000;" : "+f"(u0));
-    asm("max.NaN.f32 %0, %0, 0fC2200000;" : "+f"(u1));
-    u = f2_pack(u0, u1);
+    float e0, e1;
     f2_unpack(f2_mul(u, f2_pack(-1.4426950408889634f, -1.4426950408889634f)), e0, e1);
     f2_unpack(f2_add(f2_pack(ex2_approx(e0), ex2_approx(e1)), f2_pack(1.f, 1.f)), e0, e1);
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e0 * e1));
-    return f2_mul(f2_mul(u, y), f2_mul(f2_pack(r, r), f2_pack(e1, e0)));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e0));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e1));
+    return f2_mul(f2_mul(u, y), f2_pack(e0, e1));
 }
 
 __device__ __forceinline__ float warp_sum(float x) {

@@ -112,27 +112,30 @@ __device__ __forceinline__ int sequence_at(const GretChunkParams& p, const Table
     return lo;
 }
 
-// The segments of a CTA: chunks [c, c_end) of stream (b, h), in the flat space of (sequence, head, chunk).
+// The segments of a CTA: chunks [c, c_end) of stream (b, h).  Split: a range of the flat space of (sequence, head, chunk); otherwise whole
+// streams, every gridDim.x-th one (they are sorted by length).
 template <class Table>
 struct Walk {
     const GretChunkParams& p;
     const Table& tab;
-    int pos, end;
+    int pos, end;                                  // split: chunks of the flat space; otherwise streams
     int b, h, c, c_end, chunks;
     __device__ __forceinline__ Walk(const GretChunkParams& p_, const Table& tab_) : p(p_), tab(tab_) {
         const int g = blockIdx.x;
-        if (p.split) {
-            pos = p.first_of(g);
-            end = p.first_of(g + 1);
-        } else {                                   // one CTA per stream
-            const int bb = g / p.base.H, n = tab.chunk0[bb + 1] - tab.chunk0[bb];
-            pos = tab.chunk0[bb] * p.base.H + (g - bb * p.base.H) * n;
-            end = pos + n;
-        }
+        pos = p.split ? p.first_of(g) : g;
+        end = p.split ? p.first_of(g + 1) : p.base.B * p.base.H;
     }
     // Enters the segment at pos; false when there is none left.
     __device__ __forceinline__ bool enter() {
         if (pos >= end) return false;
+        if (!p.split) {
+            b = pos / p.base.H;
+            h = pos - b * p.base.H;
+            c = 0;
+            c_end = chunks = tab.chunk0[b + 1] - tab.chunk0[b];
+            pos += gridDim.x;
+            return true;
+        }
         b = sequence_at(p, tab, pos);
         chunks = tab.chunk0[b + 1] - tab.chunk0[b];
         const int in = pos - tab.chunk0[b] * p.base.H;
@@ -848,6 +851,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 if (lane == 0) mbar_arrive(&dec_empty[buf]);
                 // ---- S'
                 const float keep = exp2_parts(whole, rest);
+                const uint64_t keep2 = f2_pack(keep, keep);
                 if (STATES) {
                     all_whole += whole;
                     all_rest += rest;
@@ -882,7 +886,8 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     tmem_ld16(ds + blk * 16, x);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) s[blk * 16 + j] = fmaf(keep, s[blk * 16 + j], x[j]);
+                    for (int j = 0; j < 16; j += 2)
+                        f2_unpack(f2_fma(keep2, f2_pack(s[blk * 16 + j], s[blk * 16 + j + 1]), f2_pack(x[j], x[j + 1])), s[blk * 16 + j], s[blk * 16 + j + 1]);
                 }
                 tc_fence_before();
                 __syncwarp();

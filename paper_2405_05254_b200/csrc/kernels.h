@@ -323,7 +323,7 @@ struct GretChunkParams {
     GretParams base;            // base.B: sequences of the table
     int32_t total;
     int32_t groups;             // CTAs
-    int32_t split;              // 1: CTA g walks chunks [first_of(g), first_of(g + 1)); 0: one stream each
+    int32_t split;              // 1: CTA g walks chunks [first_of(g), first_of(g + 1)); 0: every groups-th stream
     int32_t share, extra;       // total / groups, total % groups
     __host__ __device__ int32_t first_of(int32_t g) const { return g * share + (g < extra ? g : extra); }
     float* part;                // split: 3 * groups states
