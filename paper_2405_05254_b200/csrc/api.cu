@@ -720,7 +720,7 @@ int32_t check_lengths(int32_t B, const int32_t* len_host, int32_t T, int64_t* to
 }
 
 int32_t check_gret_shape(const yoco_gret_shape& s) {
-    if (s.B < 0 || s.H <= 0 || s.d <= 0 || !(s.scale >= 0.f) || !std::isfinite(s.scale) || !(s.tau >= 0.f) || !std::isfinite(s.tau) ||
+    if (s.B < 0 || s.H <= 0 || s.d <= 0 || !(s.scale >= 0.f) || !std::isfinite(s.scale) || !(s.tau >= 0.f) || !std::isfinite(s.tau) || (s.tau > 0.f && !std::isfinite(1.f / s.tau)) ||
         (s.decay_bf16 & ~1) || s.q_stride < 0 || s.k_stride < 0 || s.v_stride < 0 || s.o_stride < 0 || s.decay_stride < 0)
         return YOCO_ERR_INVALID_ARG;
     return (s.d == 64 || s.d == 128) && s.H <= 65535 && s.B <= kAppendMaxSequences ? YOCO_OK : YOCO_ERR_UNSUPPORTED;
