@@ -729,21 +729,35 @@ int32_t check_gret_shape(const yoco_gret_shape& s) {
 // Slots of the states: in range, none written twice, none written that another sequence reads.
 int32_t check_slots(const yoco_gret_shape& s, const int32_t* in, const int32_t* out, GretTable* tab) {
     if (s.num_slots <= 0) return YOCO_ERR_INVALID_ARG;
-    std::vector<std::pair<int32_t, int32_t>> written;      // (slot, sequence)
-    written.reserve(s.B);
     for (int32_t i = 0; i < s.B; ++i) {
         tab->from[i] = in ? in[i] : i;
         tab->to[i] = out ? out[i] : i;
         if (tab->from[i] < -1 || tab->from[i] >= s.num_slots || tab->to[i] < -1 || tab->to[i] >= s.num_slots) return YOCO_ERR_INVALID_ARG;
-        if (tab->to[i] >= 0) written.emplace_back(tab->to[i], i);
     }
-    std::sort(written.begin(), written.end());
-    for (size_t j = 1; j < written.size(); ++j)
-        if (written[j].first == written[j - 1].first) return YOCO_ERR_INVALID_ARG;
+    // One sequence may write a slot; only that one may read it then.  A bit per slot for pools of usual sizes, a sorted list beyond.
+    constexpr int32_t kBits = 8192;
+    uint64_t bits[kBits / 64];
+    std::vector<int32_t> sorted;
+    const bool few = s.num_slots <= kBits;
+    if (few) {
+        std::memset(bits, 0, (size_t)(s.num_slots + 63) / 64 * 8);
+        for (int32_t i = 0; i < s.B; ++i) {
+            if (tab->to[i] < 0) continue;
+            uint64_t& w = bits[tab->to[i] / 64];
+            const uint64_t bit = 1ull << (tab->to[i] % 64);
+            if (w & bit) return YOCO_ERR_INVALID_ARG;
+            w |= bit;
+        }
+    } else {
+        for (int32_t i = 0; i < s.B; ++i)
+            if (tab->to[i] >= 0) sorted.push_back(tab->to[i]);
+        std::sort(sorted.begin(), sorted.end());
+        if (std::adjacent_find(sorted.begin(), sorted.end()) != sorted.end()) return YOCO_ERR_INVALID_ARG;
+    }
     for (int32_t i = 0; i < s.B; ++i) {
-        if (tab->from[i] < 0) continue;
-        const auto it = std::lower_bound(written.begin(), written.end(), std::make_pair(tab->from[i], INT32_MIN));
-        if (it != written.end() && it->first == tab->from[i] && it->second != i) return YOCO_ERR_INVALID_ARG;
+        const int32_t f = tab->from[i];
+        if (f < 0 || f == tab->to[i]) continue;
+        if (few ? (bits[f / 64] >> (f % 64) & 1) != 0 : std::binary_search(sorted.begin(), sorted.end(), f)) return YOCO_ERR_INVALID_ARG;
     }
     return YOCO_OK;
 }
@@ -752,8 +766,9 @@ int32_t check_slots(const yoco_gret_shape& s, const int32_t* in, const int32_t* 
 // (Measured, 32 heads of 128: one sequence of 17 / 32 / 64 tokens 12.9 / 17.1 / 35 us token by token, 17 in chunks; 32 sequences of 17 / 32
 // tokens 68 / 103 us, in chunks 83 / 84.)
 constexpr int32_t kGretTokens = 24;
-// What a chunk costs in the state-only pass over split streams, and the extra launches, in chunks of the main pass.
-constexpr double kGretStateCost = 0.55, kGretSplitCost = 3.0;
+// What a chunk costs in the state-only pass over split streams, and the extra launches, in chunks of the main pass.  (Measured, 32 heads of 128
+// on 148 SMs: whole streams 4.7 us a chunk, split 6.1 us a chunk for both passes, and 40 us more for the launches, their starts and ends.)
+constexpr double kGretStateCost = 0.35, kGretSplitCost = 8.0;
 
 struct GretPlan {
     GretChunkTable tab;
@@ -821,11 +836,10 @@ int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const v
             return rc;
         if (p.decay_stride < s.H || !aligned(decay, s.decay_bf16 ? 2 : 4) || !state || !aligned(state, 16)) return YOCO_ERR_INVALID_ARG;
         if (tokens > 0 && (!Q || !K || !V || !decay || !O)) return YOCO_ERR_INVALID_ARG;   // (an empty tensor's address may be null)
-        GretTable tab;
-        std::memset(&tab, 0, sizeof tab);
+        GretTable tab;                                     // (entries behind the last sequence are not read)
+        tab.tok0[0] = 0;
         if ((rc = check_slots(s, slot_in_host, slot_out_host, &tab)) != YOCO_OK) return rc;
         for (int32_t i = 0; i < s.B; ++i) tab.tok0[i + 1] = tab.tok0[i] + (len_host ? len_host[i] : step ? 1 : s.T);
-        for (int32_t i = s.B; i < kAppendMaxSequences; ++i) tab.tok0[i + 1] = tab.tok0[i];
         DeviceState* dev = nullptr;
         if ((rc = device_state(&dev)) != YOCO_OK) return rc;
         p.q = static_cast<const __nv_bfloat16*>(Q);

@@ -45,9 +45,9 @@ template <class F>
 void with_gret_table(const GretTable& tab, int B, F launch) {
     if (B > kFewSequences) return launch(tab);
     GretTableOf<kFewSequences> few;
-    std::memcpy(few.from, tab.from, sizeof few.from);
-    std::memcpy(few.to, tab.to, sizeof few.to);
-    std::memcpy(few.tok0, tab.tok0, sizeof few.tok0);
+    std::memcpy(few.from, tab.from, B * sizeof few.from[0]);
+    std::memcpy(few.to, tab.to, B * sizeof few.to[0]);
+    std::memcpy(few.tok0, tab.tok0, (B + 1) * sizeof few.tok0[0]);
     launch(few);
 }
 

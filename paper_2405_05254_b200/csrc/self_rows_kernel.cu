@@ -1,5 +1,7 @@
 // Token-major rows of a self-decoder: rotation of queries and keys by computed angles, normalisation of the heads' outputs with a gate.
 // Both move bytes: rows are read and written once in 16-byte pieces.
+#include <type_traits>
+
 #include "gret.cuh"
 #include "kernels.h"
 #include "ptx.cuh"
@@ -15,10 +17,10 @@ namespace {
 // fp32: at position 10^6 an fp32 angle would be off by 0.06.  Then a thread takes units of 16 channels of a (token, head) row: eight pairs
 // (halves: channels 8 u .. and rot / 2 + 8 u ..; neighbours: 16 u ..), or 16 channels that are copied.
 constexpr int kRopeThreads = 256;
-constexpr int kRopeRows = 4;            // rows that a thread has in flight
+constexpr int kRopeRows = 2;            // rows that a thread has in flight
 
 template <class Table>
-__global__ void __launch_bounds__(kRopeThreads)
+__global__ void __launch_bounds__(kRopeThreads, 4)
 rope_kernel(const RopeParams p, const __grid_constant__ Table tab, const int tb) {
     extern __shared__ __align__(16) float angles[];                 // [tb][2][rot / 2]: cosines, sines
     const int half = p.rot / 2, tid = threadIdx.x, tok0 = blockIdx.x * tb, n_tok = min(tb, p.tokens - tok0);
@@ -165,7 +167,8 @@ head_norm_kernel(const HeadNormParams p) {
         if (gate) {
             unpack8(gr[c], w);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[c][j] *= swish(w[j]);
+            for (int j = 0; j < 8; j += 2)
+                f2_unpack(f2_swish_mul(f2_pack(w[j], w[j + 1]), f2_pack(x[c][j], x[c][j + 1])), x[c][j], x[c][j + 1]);
         }
         *reinterpret_cast<uint4*>(dst + at) = pack8(x[c]);
     }
@@ -191,17 +194,28 @@ cudaError_t launch_rope(const RopeParams& p, const SeqTable& tab, int sm_count, 
     return cudaGetLastError();
 }
 
+// Lanes of a group: the fewest (a power of two) that need no more than five pieces each.  A thread then has its loads in flight side by
+// side, few shuffles, and groups of sizes like 80 leave no lane idle.  (Measured, 16,001 tokens of 40 groups of 80 with gain, bias and gate:
+// ten pieces over 16 lanes 134 us, over two 64 us.)
 cudaError_t launch_head_norm(const HeadNormParams& p, cudaStream_t stream) {
     if (p.groups <= 0) return cudaSuccess;
     const int pieces = p.d / 8;
-    if (pieces == 1) return norm_one<1, 1>(p, stream);
-    if (pieces == 2) return norm_one<2, 1>(p, stream);
-    if (pieces <= 4) return norm_one<4, 1>(p, stream);
-    if (pieces <= 8) return norm_one<8, 1>(p, stream);
-    if (pieces <= 16) return norm_one<16, 1>(p, stream);
-    if (pieces <= 32) return norm_one<32, 1>(p, stream);
-    if (pieces <= 64) return norm_one<32, 2>(p, stream);
-    return norm_one<32, 4>(p, stream);
+    auto lanes = [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        switch ((pieces + W - 1) / W) {
+            case 1: return norm_one<W, 1>(p, stream);
+            case 2: return norm_one<W, 2>(p, stream);
+            case 3: return norm_one<W, 3>(p, stream);
+            case 4: return norm_one<W, 4>(p, stream);
+            default: return norm_one<W, 5>(p, stream);
+        }
+    };
+    if (pieces <= 5) return lanes(std::integral_constant<int, 1>{});
+    if (pieces <= 10) return lanes(std::integral_constant<int, 2>{});
+    if (pieces <= 20) return lanes(std::integral_constant<int, 4>{});
+    if (pieces <= 40) return lanes(std::integral_constant<int, 8>{});
+    if (pieces <= 80) return lanes(std::integral_constant<int, 16>{});
+    return lanes(std::integral_constant<int, 32>{});
 }
 
 }  // namespace yoco
