@@ -869,10 +869,11 @@ int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const v
             if (workspace_bytes < plan.bytes()) return YOCO_ERR_WORKSPACE_TOO_SMALL;
         }
         CUtensorMap tmQ, tmK, tmV;
-        auto map = [&](CUtensorMap* m, const void* base, int64_t stride) {
-            return make_map(m, base, tokens, (int32_t)(width * 2), 128, kGretChunk, true, CU_TENSOR_MAP_SWIZZLE_128B, stride * 2);
+        auto map = [&](CUtensorMap* m, const void* base, int64_t stride, int32_t rows) {
+            return make_map(m, base, tokens, (int32_t)(width * 2), 128, rows, true, CU_TENSOR_MAP_SWIZZLE_128B, stride * 2);
         };
-        if ((rc = map(&tmQ, Q, p.q_stride)) != YOCO_OK || (rc = map(&tmK, K, p.k_stride)) != YOCO_OK || (rc = map(&tmV, V, p.v_stride)) != YOCO_OK)
+        if ((rc = map(&tmQ, Q, p.q_stride, kGretChunk)) != YOCO_OK || (rc = map(&tmK, K, p.k_stride, kGretChunk / 2)) != YOCO_OK ||
+            (rc = map(&tmV, V, p.v_stride, kGretChunk / 2)) != YOCO_OK)
             return rc;
         GretChunkParams cp{};
         cp.base = p;

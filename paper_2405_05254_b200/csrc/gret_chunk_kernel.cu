@@ -34,7 +34,9 @@ namespace {
 
 constexpr int CT = kGretChunk;                 // 128 tokens
 constexpr int kThreads = 1024;
-constexpr int HALF_BYTES = CT * 128;           // 128 rows x 64 bf16: one swizzled half tile
+constexpr int HALF_BYTES = CT * 128;           // Q: 128 rows x 64 bf16, one swizzled half of a tile
+constexpr int HT = CT / 2;                     // K and V come by halves of a chunk: 64 tokens
+constexpr int SUB_BYTES = HT * 128;            // 64 rows x 64 bf16
 constexpr int PIECE = 32;                      // tokens of a piece of K'
 constexpr int PIECES = CT / PIECE;
 constexpr int PIECE_HALF = PIECE * 128;        // 64 channels of a piece of one of K's parts
@@ -51,15 +53,18 @@ constexpr int kTermsInside = 2;
 template <int D, bool STATES>
 struct GCfg {
     static constexpr int HALVES = D / 64;
-    static constexpr int TILE_BYTES = HALVES * HALF_BYTES;
-    // Tiles of K, Q and V in shared memory.  K and Q are given back early (once scored and turned into K', once multiplied by S), V last.
-    static constexpr int KS = D == 64 || STATES ? 2 : 1, QS = STATES ? 0 : D == 64 ? 2 : 1, VS = D == 64 ? 4 : 2;
+    static constexpr int TILE_BYTES = HALVES * HALF_BYTES;     // Q
+    static constexpr int KV_BYTES = HALVES * SUB_BYTES;        // 64 tokens of K or V
+    // Places in shared memory: half chunks of K and V (three: one and a half chunks, so that the next one's first half is there before
+    // this one's second half has gone), chunks of Q.  (With whole chunks, one place for K and two for V, K came 1.3 us after it could:
+    // MEASURED.)
+    static constexpr int KS = D == 64 || STATES ? 4 : 3, VS = KS, QS = STATES ? 0 : D == 64 ? 2 : 1;
     // K' pieces: places of three parts each, or in the same memory (not STATES) half as many again of two.
     static constexpr int KP_WIDE = STATES ? 4 : 2, KP_NARROW = 3, KP_STAGES = STATES ? 4 : 3;
     static constexpr int OFF_K = 0;
-    static constexpr int OFF_Q = OFF_K + KS * TILE_BYTES;
+    static constexpr int OFF_Q = OFF_K + KS * KV_BYTES;
     static constexpr int OFF_V = OFF_Q + QS * TILE_BYTES;
-    static constexpr int OFF_KP = OFF_V + VS * TILE_BYTES;
+    static constexpr int OFF_KP = OFF_V + VS * KV_BYTES;
     static constexpr int OFF_S = OFF_KP + KP_WIDE * kTerms * TERM_BYTES;
     static constexpr int OFF_ROWS = OFF_S + (STATES ? 0 : D * D * 2);    // output: 32 rows x 16 channels a warp
     static constexpr int OFF_DEC = OFF_ROWS + (STATES ? 0 : 8 * 1024);
@@ -93,6 +98,17 @@ struct Wait {
     }
 };
 
+// Places of half chunks, used in turn, and the parity of the time round.
+template <int N>
+struct Turn {
+    uint32_t at = 0, round = 0;
+    __device__ __forceinline__ void next() {
+        if (++at == (uint32_t)N) {
+            at = 0;
+            round ^= 1u;
+        }
+    }
+};
 // The place of use n in a ring of N (a power of two), and the parity of its time round.
 template <int N>
 __device__ __forceinline__ uint32_t place(uint32_t n) { return n & (uint32_t)(N - 1); }
@@ -192,7 +208,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         if (!aligned_ok) atomicCAS(p.status, 0, status_word(kWaitMisaligned, linear_cta()));
         for (int i = 0; i < C::KS; ++i) {
             mbar_init(&k_full[i], 1);
-            mbar_init(&k_empty[i], STATES ? 16 : 9);       // the warps that make K', and Q K^T
+            mbar_init(&k_empty[i], STATES ? 8 : 9);        // the warps that make K' of it, and Q K^T
         }
         for (int i = 0; i < C::QS; ++i) {
             mbar_init(&q_full[i], 1);
@@ -266,11 +282,11 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         return true;
     };
     // One thread's share of a piece of K': THREADS threads, `tid` of them, rows 8 at a time per 64 of them.
-    auto make_piece = [&](auto threads, int tid, uint32_t it, int e, const float* weight, int valid, int terms) {
+    auto make_piece = [&](auto threads, int tid, uint32_t k_place, int e, const float* weight, int valid, int terms) {
         constexpr int ROWS = decltype(threads)::value / 8;                         // rows that are done at a time
         const int row = tid >> 3;
         const uint32_t at = row * 128 + (((tid & 7) ^ (row & 7)) << 4);            // inside a piece's half; the same in a tile's
-        const uint8_t* src = smem + C::OFF_K + place<C::KS>(it) * C::TILE_BYTES + e * PIECE_HALF + at;
+        const uint8_t* src = smem + C::OFF_K + k_place * C::KV_BYTES + (e & 1) * PIECE_HALF + at;
         uint8_t* dst = smem + pieces.offset() + at;
         auto put = [&](int t, int off, const uint32_t (&v)[4]) {
             *reinterpret_cast<uint4*>(dst + t * TERM_BYTES + off) = make_uint4(v[0], v[1], v[2], v[3]);
@@ -283,7 +299,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             const bool in = e * PIECE + r + row < valid;
 #pragma unroll 1
             for (int hf = 0; hf < C::HALVES; ++hf) {
-                uint4 raw = *reinterpret_cast<const uint4*>(src + hf * HALF_BYTES + r * 128);
+                uint4 raw = *reinterpret_cast<const uint4*>(src + hf * SUB_BYTES + r * 128);
                 if (!in) raw = make_uint4(0u, 0u, 0u, 0u);
                 const int off = hf * PIECE_HALF + r * 128;
                 const uint32_t kk[4] = {raw.x, raw.y, raw.z, raw.w};
@@ -324,14 +340,16 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         if (lane == 0) mbar_arrive(&kp_full[pieces.at]);
     };
     // rows behind the sequence are the next one's, or none: they may hold anything, and 0 times that is not 0
-    auto clear_tail = [&](int threads, int tid, uint32_t it, int valid) {
-        if (!wait(&v_full[place<C::VS>(it)], round_of<C::VS>(it), kWaitRingFull)) return false;
+    auto clear_tail = [&](int threads, int tid, Turn<C::VS> vat, int valid) {
+        for (int half = 0; half < 2; ++half, vat.next()) {
+            if (!wait(&v_full[vat.at], vat.round, kWaitRingFull)) return false;
 #pragma unroll 1
-        for (int i = tid; i < CT * 8 * C::HALVES; i += threads) {
-            const int r = i & (CT - 1), q = i / CT;
-            if (r >= valid)
-                *reinterpret_cast<uint4*>(smem + C::OFF_V + place<C::VS>(it) * C::TILE_BYTES + (q >> 3) * HALF_BYTES + r * 128 + (q & 7) * 16) =
-                    make_uint4(0u, 0u, 0u, 0u);
+            for (int i = tid; i < HT * 8 * C::HALVES; i += threads) {
+                const int r = i & (HT - 1), q = i / HT;
+                if (half * HT + r >= valid)
+                    *reinterpret_cast<uint4*>(smem + C::OFF_V + vat.at * C::KV_BYTES + (q >> 3) * SUB_BYTES + r * 128 + (q & 7) * 16) =
+                        make_uint4(0u, 0u, 0u, 0u);
+            }
         }
         return true;
     };
@@ -348,27 +366,35 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     tma_prefetch_desc(&tmV);
                     if (!STATES) tma_prefetch_desc(&tmQ);
                 }
-                uint32_t armed[3] = {0u, 0u, 0u};          // copies of V, K, Q (the order in which their places become free)
+                Turn<C::KS> kat;
+                Turn<C::VS> vat;
+                uint32_t chunks = 0, k_armed = 0, v_armed = 0, q_armed = 0;
                 bool ok = true;
                 while (ok && enter()) {
                     const int x = walk.h * D;
 #pragma unroll 1
-                    for (int c = walk.c; c < walk.c_end; ++c) {
+                    for (int c = walk.c; c < walk.c_end; ++c, ++chunks) {
                         const int y = tab.tok0[walk.b] + c * CT;
-#pragma unroll
-                        for (int i = 0; i < (STATES ? 2 : 3); ++i) {
-                            const uint32_t places = i == 0 ? C::VS : i == 1 ? C::KS : QS;
-                            const uint32_t slot = armed[i] & (places - 1);
-                            uint64_t* full = (i == 0 ? v_full : i == 1 ? k_full : q_full) + slot;
-                            if (!(ok = wait((i == 0 ? v_empty : i == 1 ? k_empty : q_empty) + slot, ((armed[i] / places) & 1u) ^ 1u, kWaitRingEmpty))) break;
-                            ++armed[i];
+                        // in the order in which their places become free: V first half, K both, Q, V second half
+#pragma unroll 1
+                        for (int i = 0; i < (STATES ? 4 : 5); ++i) {
+                            const bool is_q = !STATES && i == 3, is_k = i == 1 || i == 2;
+                            const int half = i == 2 || i == (STATES ? 3 : 4);
+                            const uint32_t at = is_q ? place<QS>(chunks) : is_k ? kat.at : vat.at;
+                            const uint32_t round = is_q ? round_of<QS>(chunks) : is_k ? kat.round : vat.round;
+                            uint64_t* full = (is_q ? q_full : is_k ? k_full : v_full) + at;
+                            if (!(ok = wait((is_q ? q_empty : is_k ? k_empty : v_empty) + at, round ^ 1u, kWaitRingEmpty))) break;
                             if (lane == 0) {
-                                const CUtensorMap* tm = i == 0 ? &tmV : i == 1 ? &tmK : &tmQ;
-                                uint8_t* dst = smem + (i == 0 ? C::OFF_V : i == 1 ? C::OFF_K : C::OFF_Q) + slot * C::TILE_BYTES;
-                                mbar_expect_tx(full, C::TILE_BYTES);
-                                for (int hf = 0; hf < C::HALVES; ++hf) tma_load_2d(dst + hf * HALF_BYTES, tm, x + hf * 64, y, full);
+                                const uint32_t off = is_q ? C::OFF_Q + at * C::TILE_BYTES : (is_k ? C::OFF_K : C::OFF_V) + at * C::KV_BYTES;
+                                const CUtensorMap* tm = is_q ? &tmQ : is_k ? &tmK : &tmV;
+                                mbar_expect_tx(full, is_q ? C::TILE_BYTES : C::KV_BYTES);
+                                for (int hf = 0; hf < C::HALVES; ++hf)
+                                    tma_load_2d(smem + off + hf * (is_q ? HALF_BYTES : SUB_BYTES), tm, x + hf * 64, y + half * HT, full);
                             }
                             __syncwarp();
+                            if (is_q) ++q_armed;
+                            else if (is_k) { kat.next(); ++k_armed; }
+                            else { vat.next(); ++v_armed; }
                         }
                         if (!ok) break;
                         if (!STATES && p.base.norm.gate) {     // the gate's rows, into L2
@@ -385,21 +411,24 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 }
                 // no copy may land after the CTA has ended (at once when all went well): the last ones into every place
                 if (lane == 0) {
-#pragma unroll
-                    for (int i = 0; i < (STATES ? 2 : 3); ++i) {
-                        const uint32_t places = i == 0 ? C::VS : i == 1 ? C::KS : QS, n = armed[i];
+                    auto drain = [&](uint64_t* full, uint32_t places, uint32_t n) {
 #pragma unroll 1
                         for (uint32_t k = n > places ? n - places : 0; k < n; ++k)
-                            if (!drain_wait((i == 0 ? v_full : i == 1 ? k_full : q_full) + k % places, (k / places) & 1u, ab)) break;
-                    }
+                            if (!drain_wait(full + k % places, (k / places) & 1u, ab)) return;
+                    };
+                    drain(v_full, C::VS, v_armed);
+                    drain(k_full, C::KS, k_armed);
+                    if (!STATES) drain(q_full, QS, q_armed);
                 }
             }
         } else if (warp == 1) {
             // ======================================= issuer of Q S, Q K^T, P V ===================
             if (aligned_ok) {
-                constexpr uint32_t idesc_qk = make_idesc(CT, false);
+                constexpr uint32_t idesc_qk = make_idesc(HT, false);
                 constexpr uint32_t idesc_mn = make_idesc(D, true);              // B with its columns contiguous: V, S
                 const uint64_t s_desc = make_desc(sbase + C::OFF_S, D * 128, 1024);
+                Turn<C::KS> kat;
+                Turn<C::VS> vat;
                 uint32_t it = 0;
                 bool ok = !STATES;
                 while (ok && enter()) {
@@ -408,21 +437,24 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         const uint32_t ph = it & 1u;
                         const uint32_t o_cols = tmem_base + COL_O + ph * 128;
                         const uint64_t q_desc = make_desc(sbase + C::OFF_Q + place<QS>(it) * C::TILE_BYTES, 16, 1024);
-                        const uint64_t k_desc = make_desc(sbase + C::OFF_K + place<C::KS>(it) * C::TILE_BYTES, 16, 1024);
-                        const uint64_t v_desc = make_desc(sbase + C::OFF_V + place<C::VS>(it) * C::TILE_BYTES, HALF_BYTES, 1024);
-                        if (!(ok = wait(&k_full[place<C::KS>(it)], round_of<C::KS>(it), kWaitRingFull))) break;
                         if (!(ok = wait(&q_full[place<QS>(it)], round_of<QS>(it), kWaitRingFull))) break;
-                        tc_fence_after();
-                        if (elect_one()) {
+#pragma unroll 1
+                        for (int half = 0; half < 2; ++half) {
+                            if (!(ok = wait(&k_full[kat.at], kat.round, kWaitRingFull))) break;
+                            tc_fence_after();
+                            const uint64_t k_desc = make_desc(sbase + C::OFF_K + kat.at * C::KV_BYTES, 16, 1024);
+                            if (elect_one()) {
 #pragma unroll
-                            for (int ks = 0; ks < D / 16; ++ks) {
-                                const uint32_t off = (ks >> 2) * HALF_BYTES + (ks & 3) * 32;
-                                umma_ss(tmem_base + COL_SC, q_desc + (off >> 4), k_desc + (off >> 4), idesc_qk, ks > 0 ? 1u : 0u);
+                                for (int ks = 0; ks < D / 16; ++ks)
+                                    umma_ss(tmem_base + COL_SC + half * HT, q_desc + (((ks >> 2) * HALF_BYTES + (ks & 3) * 32) >> 4),
+                                            k_desc + (((ks >> 2) * SUB_BYTES + (ks & 3) * 32) >> 4), idesc_qk, ks > 0 ? 1u : 0u);
+                                umma_commit(&k_empty[kat.at]);
+                                if (half) umma_commit(sc_full);
                             }
-                            umma_commit(sc_full);
-                            umma_commit(&k_empty[place<C::KS>(it)]);
+                            __syncwarp();
+                            kat.next();
                         }
-                        __syncwarp();
+                        if (!ok) break;
                         if (!(ok = wait(s_full, ph, kWaitTensor))) break;
                         if (!(ok = wait(&o_empty[ph], ((it >> 1) & 1u) ^ 1u, kWaitTensor))) break;
                         tc_fence_after();
@@ -438,17 +470,23 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         }
                         __syncwarp();
                         // P V, on top of Q S
-                        if (!(ok = wait(&v_full[place<C::VS>(it)], round_of<C::VS>(it), kWaitRingFull))) break;
                         if (!(ok = wait(p_full, ph, kWaitTensor))) break;
-                        tc_fence_after();
-                        if (elect_one()) {
+#pragma unroll 1
+                        for (int half = 0; half < 2; ++half) {
+                            if (!(ok = wait(&v_full[vat.at], vat.round, kWaitRingFull))) break;
+                            tc_fence_after();
+                            const uint64_t v_desc = make_desc(sbase + C::OFF_V + vat.at * C::KV_BYTES, SUB_BYTES, 1024);
+                            if (elect_one()) {
 #pragma unroll
-                            for (int ks = 0; ks < CT / 16; ++ks)
-                                umma_ts(o_cols, tmem_base + COL_SC + ks * 8, v_desc + ((ks * 16 * 128) >> 4), idesc_mn, 1u);
-                            umma_commit(&o_full[ph]);
-                            umma_commit(&v_empty[place<C::VS>(it)]);
+                                for (int ks = 0; ks < HT / 16; ++ks)
+                                    umma_ts(o_cols, tmem_base + COL_SC + half * (HT / 2) + ks * 8, v_desc + ((ks * 16 * 128) >> 4), idesc_mn, 1u);
+                                umma_commit(&v_empty[vat.at]);
+                                if (half) umma_commit(&o_full[ph]);
+                            }
+                            __syncwarp();
+                            vat.next();
                         }
-                        __syncwarp();
+                        if (!ok) break;
                     }
                 }
                 // nothing issued may still run when tensor memory is released
@@ -462,6 +500,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             // ======================================= issuer of K'^T V ============================
             if (aligned_ok) {
                 constexpr uint32_t idesc_kv = make_idesc(D, true) | (1u << 15); // both operands with their columns contiguous
+                Turn<C::VS> vat;
                 uint32_t it = 0;
                 bool ok = true;
                 while (ok && enter()) {
@@ -471,15 +510,14 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                         const uint32_t buf = STATES ? it & 1u : 0u, round = STATES ? (it >> 1) & 1u : it & 1u;
                         const uint32_t d_cols = tmem_base + (buf ? COL_SC : COL_DS);
-                        const uint64_t v_desc = make_desc(sbase + C::OFF_V + place<C::VS>(it) * C::TILE_BYTES, HALF_BYTES, 1024);
-                        if (!(ok = wait(&v_full[place<C::VS>(it)], round_of<C::VS>(it), kWaitRingFull))) break;
                         if (!(ok = wait(&ds_empty[buf], round ^ 1u, kWaitTensor))) break;
 #pragma unroll 1
                         for (int e = 0; e < PIECES; ++e) {
+                            if ((e & 1) == 0 && !(ok = wait(&v_full[vat.at], vat.round, kWaitRingFull))) break;
                             if (!(ok = wait(&kp_full[pieces.at], pieces.parity(pieces.at), kWaitTensor))) break;
                             tc_fence_after();
                             const uint64_t kp_desc = make_desc(sbase + pieces.offset(), PIECE_HALF, 1024);
-                            const uint64_t vp_desc = v_desc + ((e * PIECE * 128) >> 4);
+                            const uint64_t vp_desc = make_desc(sbase + C::OFF_V + vat.at * C::KV_BYTES + (e & 1) * (PIECE * 128), SUB_BYTES, 1024);
                             if (elect_one()) {
 #pragma unroll
                                 for (int t = 0; t < kTerms; ++t) {
@@ -490,13 +528,12 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                                                 t > 0 || ks > 0 ? 1u : e > 0 ? 1u : 0u);
                                 }
                                 umma_commit(&kp_empty[pieces.at]);
-                                if (e == PIECES - 1) {
-                                    umma_commit(&ds_full[buf]);
-                                    umma_commit(&v_empty[place<C::VS>(it)]);
-                                }
+                                if (e & 1) umma_commit(&v_empty[vat.at]);
+                                if (e == PIECES - 1) umma_commit(&ds_full[buf]);
                             }
                             __syncwarp();
                             pieces.next();
+                            if (e & 1) vat.next();
                         }
                         if (!ok) break;
                     }
@@ -565,14 +602,16 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
     } else if (warp >= 24 || (STATES && warp < 12)) {
         // ======================================= K' ==============================================
-        // 256 threads make a piece together; in the state-only pass four warpgroups make a piece each, in turn (no more teams than places:
-        // a team that waits for a place has seen the use before the last one of it given back).
+        // 256 threads make a piece together; in the state-only pass four warpgroups make one of a chunk's pieces each (no more teams than
+        // places: a team that waits for a place has seen the use before the last one of it given back).
         if (warp >= 24) setmaxnreg_dec<kRegsKeys>(); else if (warp < 8) setmaxnreg_dec<kRegsP>(); else setmaxnreg_dec<kRegsOut>();
         constexpr int TEAM = STATES ? 128 : 256;
         constexpr uint32_t TEAMS = STATES ? 4 : 1;
         const uint32_t team = !STATES ? 0u : warp < 12 ? (uint32_t)(warp >> 2) - 1u : (uint32_t)(warp >> 2) - 4u;
         const int tid = threadIdx.x & (TEAM - 1);
-        uint32_t it = 0, turn = 0;
+        Turn<C::KS> kat;
+        Turn<C::VS> vat;
+        uint32_t it = 0;
         bool ok = aligned_ok;
         while (ok && enter()) {
             const int len = tab.len[walk.b], terms = terms_of();
@@ -583,23 +622,24 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 const uint32_t buf = it & 1u;
                 const int valid = len - c * CT;            // tokens of the sequence from here on
                 if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
-                if (!(ok = wait(&k_full[place<C::KS>(it)], round_of<C::KS>(it), kWaitRingFull))) break;
-                if (valid < CT && turn == team && !(ok = clear_tail(TEAM, tid, it, valid))) break;     // (before piece 0)
+                if (valid < CT && team == 0 && !(ok = clear_tail(TEAM, tid, vat, valid))) break;       // (this team makes piece 0)
 #pragma unroll 1
                 for (int e = 0; e < PIECES; ++e) {
-                    if (turn == team) {
+                    if (TEAMS == 1 || (uint32_t)e == team) {
+                        if (!(ok = wait(&k_full[kat.at], kat.round, kWaitRingFull))) break;
                         if (!(ok = wait(&kp_empty[pieces.at], pieces.parity(pieces.at) ^ 1u, kWaitTensor))) break;
-                        make_piece(std::integral_constant<int, TEAM>{}, tid, it, e, dec + buf * C::DEC_FLOATS, valid, terms);
+                        make_piece(std::integral_constant<int, TEAM>{}, tid, kat.at, e, dec + buf * C::DEC_FLOATS, valid, terms);
+                        if (lane == 0 && (TEAMS > 1 || (e & 1))) mbar_arrive(&k_empty[kat.at]);
                     }
                     pieces.next();
-                    turn = turn + 1u == TEAMS ? 0u : turn + 1u;
+                    if (e & 1) {
+                        kat.next();
+                        vat.next();
+                    }
                 }
                 if (!ok) break;
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(&k_empty[place<C::KS>(it)]);
-                    mbar_arrive(&dec_empty[buf]);
-                }
+                if (lane == 0) mbar_arrive(&dec_empty[buf]);
             }
         }
     } else if (warp < 8) {

@@ -330,7 +330,7 @@ struct GretChunkParams {
     float* part_keep;           // split: decays over the segments that left them, 3 * groups
     int32_t* status;
 };
-// tmQ, tmK, tmV: bf16 maps over [tokens, H * d], box {64, kGretChunk}, 128-byte swizzle
+// tmQ, tmK, tmV: bf16 maps over [tokens, H * d], box {64, kGretChunk} (K and V: kGretChunk / 2), 128-byte swizzle
 cudaError_t launch_gret_chunk(const GretChunkParams& p, const GretChunkTable& tab, const CUtensorMap& tmQ, const CUtensorMap& tmK,
                               const CUtensorMap& tmV, cudaStream_t stream);
 cudaError_t gret_chunk_kernel_setup();
