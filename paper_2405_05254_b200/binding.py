@@ -758,6 +758,9 @@ _TOKEN_ARGS = {
 }
 
 
+_token_fns = {}
+
+
 def _rows_lie(a, width: int, apart: int) -> bool:
     """Whether the tensor's strides are those of rows of ``width`` elements, ``apart`` from one another (a tensor without
     a dimension for the rows lies as the caller says)."""
@@ -857,8 +860,9 @@ class PreparedTokensCall:
         self._stream = None if stream is None else stream.cuda_stream
         self._current_stream, self._device = torch._C._cuda_getCurrentRawStream, device
         self._others = torch.cuda.device_count() > 1
-        proto = ctypes.CFUNCTYPE(ctypes.c_int32, *[ctypes.c_void_p] * (len(out) + 1))
-        self._name, self._fn, self._args = fn_name, proto((fn_name, lib())), tuple(out)
+        if fn_name not in _token_fns:              # integers as arguments, see PreparedPagedCall
+            _token_fns[fn_name] = ctypes.CFUNCTYPE(ctypes.c_int32, *[ctypes.c_void_p] * (len(out) + 1))((fn_name, lib()))
+        self._name, self._fn, self._args = fn_name, _token_fns[fn_name], tuple(out)
 
     def run(self) -> None:
         if self._others:
