@@ -72,7 +72,7 @@ struct GCfg {
     static constexpr int DEC_END = CT, DEC_WHOLE = CT + 4, DEC_REST = DEC_WHOLE + CT, DEC_U = DEC_REST + CT;
     static constexpr int DEC_FLOATS = STATES ? DEC_WHOLE : DEC_U + CT;
     static constexpr int OFF_BAR = OFF_DEC + 2 * DEC_FLOATS * 4;
-    static constexpr int NUM_BARS = 2 * (KS + QS + VS) + 2 * KP_STAGES + 19;
+    static constexpr int NUM_BARS = 2 * (KS + QS + VS) + 2 * KP_STAGES + 20;
     static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16;
     static_assert(SMEM_BYTES <= 227 * 1024 && OFF_DEC % 16 == 0 && OFF_BAR % 8 == 0, "shared memory");
     static_assert(KP_NARROW * kTermsInside <= KP_WIDE * kTerms, "places of K'");
@@ -195,6 +195,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     uint64_t* ds_full = dec_full + 13;                     // [2], the state-only pass has two buffers of DS
     uint64_t* ds_empty = dec_full + 15;                    // [2]
     uint64_t* drain_bar = dec_full + 17;                   // [2]
+    uint64_t* s_staged = dec_full + 19;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     float* dec = reinterpret_cast<float*>(smem + C::OFF_DEC);
@@ -236,6 +237,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             mbar_init(&ds_empty[i], 8);
         }
         mbar_init(s_full, 8);
+        mbar_init(s_staged, 8);
         mbar_init(s_empty, 1);
         mbar_init(&drain_bar[0], 1);
         mbar_init(&drain_bar[1], 1);
@@ -845,7 +847,29 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         constexpr int N = D * D / 256;                     // channels of a thread: half a row of the state (d = 64: a quarter)
         const int quad = warp & 3, l = quad * 32 + lane, row = l % D, col = (warp >= 16 ? D / 2 : 0) + (l / D) * N;
         uint8_t* s_row = smem + C::OFF_S + row * 128;
-        uint32_t it = 0;
+        // A warp's part of the state is 32 rows of N channels, a row a lane.  On the way from and to memory it goes through the warp's share of the place
+        // of S, SL channels at a time, so that an access covers whole sectors of few rows (a lane's own row: 32 lines an access).
+        constexpr int SL = D == 128 ? 16 : 8, CH = SL / 4;
+        uint8_t* stage = smem + C::OFF_S + (warp - 12) * (32 * SL * 4);
+        const int row0 = row - lane;
+        auto through_rows = [&](auto&& by_lines, auto&& by_rows, bool rows_first) {
+            auto at = [&](int r, int ch) { return reinterpret_cast<uint4*>(stage + r * (SL * 4) + ((ch ^ ((CH == 4 ? r >> 1 : r >> 2) & (CH - 1))) << 4)); };
+#pragma unroll
+            for (int j = 0; j < N; j += SL) {
+                auto rows = [&]() {
+#pragma unroll
+                    for (int ch = 0; ch < CH; ++ch) by_rows(j, ch, at(lane, ch));
+                };
+                if (rows_first) rows();
+                if (rows_first) __syncwarp();
+#pragma unroll
+                for (int i = 0; i < CH; ++i) by_lines(col + j, row0 + (i * 32 + lane) / CH, lane % CH, at((i * 32 + lane) / CH, lane % CH));
+                __syncwarp();
+                if (!rows_first) rows();
+                if (!rows_first) __syncwarp();
+            }
+        };
+        uint32_t it = 0, segments = 0;
         bool ok = aligned_ok;
         while (ok && enter()) {
             const int b = walk.b, h = walk.h;
@@ -859,13 +883,24 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 else
                     src = p.part + (int64_t)(walk.c > 0 ? blockIdx.x : p.groups + blockIdx.x) * (D * D);
             }
+            if (STATES || !src) {
 #pragma unroll
-            for (int j = 0; j < N; j += 4) {
-                const float4 x = src ? *reinterpret_cast<const float4*>(src + row * D + col + j) : make_float4(0.f, 0.f, 0.f, 0.f);
-                s[j] = x.x;
-                s[j + 1] = x.y;
-                s[j + 2] = x.z;
-                s[j + 3] = x.w;
+                for (int j = 0; j < N; ++j) s[j] = 0.f;
+            } else {
+                through_rows([&](int j, int r, int ch, uint4* place) { *place = *reinterpret_cast<const uint4*>(src + r * D + j + ch * 4); },
+                             [&](int j, int ch, uint4* place) {
+                                 const float4 x = *reinterpret_cast<const float4*>(place);
+                                 s[j + ch * 4] = x.x;
+                                 s[j + ch * 4 + 1] = x.y;
+                                 s[j + ch * 4 + 2] = x.z;
+                                 s[j + ch * 4 + 3] = x.w;
+                             }, false);
+            }
+            if (!STATES) {       // S takes the place of the rows that all eight warps have come through
+                __syncwarp();
+                if (lane == 0) mbar_arrive(s_staged);
+                if (!(ok = wait(s_staged, segments & 1u, kWaitTensor))) break;
+                ++segments;
             }
             float all_whole = 0.f, all_rest = 0.f;         // logarithm of the segment's decay
 #pragma unroll 1
@@ -941,10 +976,15 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 dst = p.part + slot * (D * D);
             else if (whole_stream && tab.to[b] >= 0)
                 dst = p.base.state + ((int64_t)tab.to[b] * p.base.H + h) * (D * D);
-            if (dst) {
+            if (STATES) {
 #pragma unroll
                 for (int j = 0; j < N; j += 4)
                     *reinterpret_cast<float4*>(dst + row * D + col + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
+            } else if (dst) {
+                through_rows([&](int j, int r, int ch, uint4* place) { *reinterpret_cast<uint4*>(dst + r * D + j + ch * 4) = *place; },
+                             [&](int j, int ch, uint4* place) {
+                                 *reinterpret_cast<float4*>(place) = make_float4(s[j + ch * 4], s[j + ch * 4 + 1], s[j + ch * 4 + 2], s[j + ch * 4 + 3]);
+                             }, true);
             }
             if (STATES && threadIdx.x == 12 * 32) p.part_keep[slot] = exp2_parts(all_whole, all_rest);
         }
