@@ -763,12 +763,12 @@ int32_t check_slots(const yoco_gret_shape& s, const int32_t* in, const int32_t* 
 }
 
 // Calls whose sequences all have no more tokens than this walk them one by one (one CTA per head, state in registers); longer ones in chunks.
-// (Measured, 32 heads of 128: one sequence of 17 / 32 / 64 tokens 12.9 / 17.1 / 35 us token by token, 17 in chunks; 32 sequences of 17 / 32
-// tokens 68 / 103 us, in chunks 83 / 84.)
-constexpr int32_t kGretTokens = 24;
+// (Measured, 32 heads of 128: one sequence of 18 / 24 tokens 12.7 / 14.7 us token by token, 13.5 in chunks; eight 19.9 / 24.9, 22.8 in chunks;
+// 32 sequences 70 / 84, 64 in chunks.)
+constexpr int32_t kGretTokens = 18;
 // What a chunk costs in the state-only pass over split streams, and the extra launches, in chunks of the main pass.  (Measured, 32 heads of 128
-// on 148 SMs: whole streams 4.7 us a chunk, split 6.1 us a chunk for both passes, and 40 us more for the launches, their starts and ends.)
-constexpr double kGretStateCost = 0.35, kGretSplitCost = 8.0;
+// on 148 SMs: whole streams 4.5 us a chunk, split 5.5 us a chunk for both passes, and 33 us more for the launches, their starts and ends.)
+constexpr double kGretStateCost = 0.25, kGretSplitCost = 7.0;
 
 struct GretPlan {
     GretChunkTable tab;

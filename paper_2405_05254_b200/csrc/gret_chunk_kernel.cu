@@ -17,6 +17,15 @@
 //   warpgroups 6, 7  K' = 2^(b_C - b_j) k_j, in pieces of 32 tokens
 // Decays of P: in the 32 x 32 blocks on the diagonal one exponential per element; below it 2^(b_i - m) 2^(m - b_j), m the value at the
 // end of j's block: both factors are at most 1, and the second is the same for all rows.
+// With few streams a first pass over K and V (STATES) leaves the state of each CTA's range, a merge puts those in order, and the main
+// pass starts every range from its own: all SMs work, K and V are read twice.  In that first pass warpgroups 1, 2, 6 and 7 make K', a piece each, in
+// tensor memory.
+// What bounds it: not the bytes (measured: 45% and 51% of the memory's rate in the two passes), but what goes through the SM's shared
+// memory.  A chunk's matrix products read 320 KB of operands there, the copies write 96 KB, K' and S take another 130 KB: with the traffic of
+// tensor memory's loads and stores some 6,600 of the 6,900 cycles that a chunk takes.  What took load off it made it faster (output and gate
+// past it, K' of the first pass to tensor memory), what shortened the chain from Q K^T over P to P V did not.
+// Measured (bf16, d = 128, no gate): one sequence of 32,768 tokens, 32 heads 358 us (1.08 GB needed: 165 us at 6.56 TB/s); 4,096 tokens 72 us;
+// four of 4,096 tokens, 37 heads, whole streams 143 us (0.68 of that rate); one chunk 13 us.
 // Roundings: P and the copy of S that multiplies Q go to bf16 (half a step, 2^-9 of the value, like the output's own).  K' goes to
 // the tensor cores as a sum of bf16: where the sums leave the kernel as a state, of three (24 bits; with one it would be 1.7e-3 off (2-norm),
 // with two 2e-6), where they only multiply Q inside, of two.
@@ -43,9 +52,13 @@ constexpr int PIECE_HALF = PIECE * 128;        // 64 channels of a piece of one 
 constexpr int TERM_BYTES = 2 * PIECE_HALF;
 constexpr uint32_t TMEM_COLS = 512;
 constexpr uint32_t COL_SC = 0, COL_O = 128, COL_DS = 384;     // two buffers of O
+// The state-only pass has the first 128 columns for a second buffer of DS, and the four pieces of K' where O is otherwise.
+constexpr uint32_t COL_KP = COL_O, KP_COLS = PIECE / 2;       // of each part
 // Registers per thread after the split; the CTA starts with 64 each.
 constexpr int kRegsIo = 56, kRegsP = 56, kRegsOut = 64, kRegsState = 88, kRegsKeys = 48;
 static_assert(kRegsIo + kRegsP + 2 * kRegsOut + 2 * kRegsState + 2 * kRegsKeys <= 8 * 64, "register pool of the CTA");
+constexpr int kRegsAcross = 64, kRegsIdle = 24;               // the state-only pass: four warpgroups make K', one has nothing to do
+static_assert(kRegsIo + 4 * kRegsAcross + kRegsIdle + 2 * kRegsState <= 8 * 64, "register pool of the CTA");
 constexpr int kTerms = 3;                      // parts of K', where a state leaves; otherwise kTermsInside
 constexpr int kTermsInside = 2;
 
@@ -56,23 +69,21 @@ struct GCfg {
     static constexpr int TILE_BYTES = HALVES * HALF_BYTES;     // Q
     static constexpr int KV_BYTES = HALVES * SUB_BYTES;        // 64 tokens of K or V
     // Places in shared memory: half chunks of K and V (three: one and a half chunks, so that the next one's first half is there before
-    // this one's second half has gone), chunks of Q.  (With whole chunks, one place for K and two for V, K came 1.3 us after it could:
-    // MEASURED.)
-    static constexpr int KS = D == 64 || STATES ? 4 : 3, VS = KS, QS = STATES ? 0 : D == 64 ? 2 : 1;
+    // this one's second half has gone), chunks of Q.  The state-only pass, with K' in tensor memory, has room for three chunks.
+    static constexpr int KS = STATES ? 6 : D == 64 ? 4 : 3, VS = KS, QS = STATES ? 0 : D == 64 ? 2 : 1;
     // K' pieces: places of three parts each, or in the same memory (not STATES) half as many again of two.
     static constexpr int KP_WIDE = STATES ? 4 : 2, KP_NARROW = 3, KP_STAGES = STATES ? 4 : 3;
     static constexpr int OFF_K = 0;
     static constexpr int OFF_Q = OFF_K + KS * KV_BYTES;
     static constexpr int OFF_V = OFF_Q + QS * TILE_BYTES;
     static constexpr int OFF_KP = OFF_V + VS * KV_BYTES;
-    static constexpr int OFF_S = OFF_KP + KP_WIDE * kTerms * TERM_BYTES;
-    static constexpr int OFF_ROWS = OFF_S + (STATES ? 0 : D * D * 2);    // output: 32 rows x 16 channels a warp
-    static constexpr int OFF_DEC = OFF_ROWS + (STATES ? 0 : 8 * 1024);
+    static constexpr int OFF_S = OFF_KP + (STATES ? 0 : KP_WIDE * kTerms * TERM_BYTES);
+    static constexpr int OFF_DEC = OFF_S + (STATES ? 0 : D * D * 2);
     // Of a chunk: 2^(b_C - b_j); whole part and rest of b_C; and where there is output: whole parts and rests of -b_j; 2^(m - b_j).
     static constexpr int DEC_END = CT, DEC_WHOLE = CT + 4, DEC_REST = DEC_WHOLE + CT, DEC_U = DEC_REST + CT;
     static constexpr int DEC_FLOATS = STATES ? DEC_WHOLE : DEC_U + CT;
     static constexpr int OFF_BAR = OFF_DEC + 2 * DEC_FLOATS * 4;
-    static constexpr int NUM_BARS = 2 * (KS + QS + VS) + 2 * KP_STAGES + 20;
+    static constexpr int NUM_BARS = 2 * (KS + QS + VS) + 2 * KP_STAGES + 22;
     static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16;
     static_assert(SMEM_BYTES <= 227 * 1024 && OFF_DEC % 16 == 0 && OFF_BAR % 8 == 0, "shared memory");
     static_assert(KP_NARROW * kTermsInside <= KP_WIDE * kTerms, "places of K'");
@@ -164,6 +175,26 @@ struct Walk {
     __device__ __forceinline__ bool whole_stream() const { return c == 0 && c_end == chunks; }
 };
 
+// 16 channels of a row, on 16 or (wide) on 32 bytes.
+__device__ __forceinline__ void load_row16(const __nv_bfloat16* p, bool wide, uint32_t (&v)[8]) {
+    if (wide) {
+        asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(p));
+    } else {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p)), b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    }
+}
+__device__ __forceinline__ void store_row16(__nv_bfloat16* p, bool wide, const uint32_t (&v)[8]) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+                     "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+    } else {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<uint4*>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+    }
+}
+
 __device__ __forceinline__ float exp2_parts(float whole, float rest) { return exp2f(whole) * exp2f(rest); }
 
 template <int D, bool STATES, class Table>
@@ -172,6 +203,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                   const GretChunkParams p, const __grid_constant__ Table tab) {
     using C = GCfg<D, STATES>;
     constexpr int QS = STATES ? 1 : C::QS;
+    if (STATES) asm volatile("griddepcontrol.launch_dependents;");
 
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
@@ -196,6 +228,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     uint64_t* ds_empty = dec_full + 15;                    // [2]
     uint64_t* drain_bar = dec_full + 17;                   // [2]
     uint64_t* s_staged = dec_full + 19;
+    uint64_t* v_cleared = dec_full + 20;                   // [2], by sequences' last chunks
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NUM_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     float* dec = reinterpret_cast<float*>(smem + C::OFF_DEC);
@@ -228,6 +261,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             mbar_init(&dec_empty[i], STATES ? 24 : 20);
             mbar_init(&o_full[i], 1);
             mbar_init(&o_empty[i], 4);
+            mbar_init(&v_cleared[i], 8);
         }
         mbar_init(sc_full, 1);
         mbar_init(qs_full, 1);
@@ -283,9 +317,9 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             if (!wait(&kp_empty[i], pieces.parity(i) ^ 1u, kWaitTensor)) return false;
         return true;
     };
-    // One thread's share of a piece of K': THREADS threads, `tid` of them, rows 8 at a time per 64 of them.
-    auto make_piece = [&](auto threads, int tid, uint32_t k_place, int e, const float* weight, int valid, int terms) {
-        constexpr int ROWS = decltype(threads)::value / 8;                         // rows that are done at a time
+    // One thread's share of a piece of K': all of its rows at a time, eight channels a thread.
+    auto make_piece = [&](int tid, uint32_t k_place, int e, const float* weight, int valid, int terms) {
+        constexpr int ROWS = 256 / 8;
         const int row = tid >> 3;
         const uint32_t at = row * 128 + (((tid & 7) ^ (row & 7)) << 4);            // inside a piece's half; the same in a tile's
         const uint8_t* src = smem + C::OFF_K + k_place * C::KV_BYTES + (e & 1) * PIECE_HALF + at;
@@ -341,6 +375,51 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         __syncwarp();
         if (lane == 0) mbar_arrive(&kp_full[pieces.at]);
     };
+    // The state-only pass: a piece goes to tensor memory, where the product's first operand has a row (a channel) to a thread; it is read down
+    // the columns of K.  (Shared memory's bandwidth is what bounds this pass: parts that are written to it and read from it are two thirds
+    // of what goes through it.)
+    auto make_piece_across = [&](uint32_t k_place, int e, const float* weight, int valid) {
+        const int ch = ((warp & 3) * 32 + lane) % D;       // d = 64: the upper 64 rows are the same ones again
+        uint8_t* src = smem + C::OFF_K + k_place * C::KV_BYTES + (ch >> 6) * SUB_BYTES + (e & 1) * PIECE_HALF + (ch & 7) * 2;
+        auto key = [&](int t) { return reinterpret_cast<uint16_t*>(src + t * 128 + ((((ch >> 3) & 7) ^ (t & 7)) << 4)); };
+        const uint32_t dst = tmem_base + COL_KP + pieces.at * (kTerms * KP_COLS) + ((uint32_t)((warp & 3) * 32) << 16);
+        if (e * PIECE + PIECE > valid) {                   // tokens behind the sequence: anything, and 0 times that is not 0
+#pragma unroll 1
+            for (int t = max(valid - e * PIECE, 0); t < PIECE; ++t) *key(t) = 0;
+            fence_proxy_async_smem();                      // (before the next copy comes into this place)
+        }
+#pragma unroll 1
+        for (int t = 0; t < PIECE; t += 16) {
+            uint64_t x[8];
+            const ulonglong2* w = reinterpret_cast<const ulonglong2*>(weight + e * PIECE + t);
+#pragma unroll
+            for (int q = 0; q < 8; q += 2) {
+                const ulonglong2 w2 = w[q / 2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t k0 = *key(t + 2 * (q + i)), k1 = *key(t + 2 * (q + i) + 1);
+                    x[q + i] = f2_mul(i ? w2.y : w2.x, f2_pack(__uint_as_float(k0 << 16), __uint_as_float(k1 << 16)));
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < kTerms; ++p) {
+                uint32_t part[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    float x0, x1;
+                    f2_unpack(x[q], x0, x1);
+                    part[q] = pack_bf16x2(x0, x1);
+                    if (p + 1 < kTerms)
+                        x[q] = f2_fma(f2_pack(__uint_as_float(part[q] << 16), __uint_as_float(part[q] & 0xFFFF0000u)), f2_pack(-1.f, -1.f), x[q]);
+                }
+                tmem_st8(dst + p * KP_COLS + t / 2, part);
+            }
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&kp_full[pieces.at]);
+    };
     // rows behind the sequence are the next one's, or none: they may hold anything, and 0 times that is not 0
     auto clear_tail = [&](int threads, int tid, Turn<C::VS> vat, int valid) {
         for (int half = 0; half < 2; ++half, vat.next()) {
@@ -353,6 +432,8 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         make_uint4(0u, 0u, 0u, 0u);
             }
         }
+        fence_proxy_async_smem();
+        __syncwarp();
         return true;
     };
     // parts of K': the state of a whole stream leaves with this kernel, those of cut ones come from the state-only pass
@@ -501,7 +582,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         } else if (warp == 3) {
             // ======================================= issuer of K'^T V ============================
             if (aligned_ok) {
-                constexpr uint32_t idesc_kv = make_idesc(D, true) | (1u << 15); // both operands with their columns contiguous
+                constexpr uint32_t idesc_kv = make_idesc(D, true) | (STATES ? 0u : 1u << 15);    // K' from shared memory: its columns are contiguous too
                 Turn<C::VS> vat;
                 uint32_t it = 0;
                 bool ok = true;
@@ -525,9 +606,14 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                                 for (int t = 0; t < kTerms; ++t) {
                                     if (t >= kTermsInside && t >= terms) break;
 #pragma unroll
-                                    for (int ks = 0; ks < PIECE / 16; ++ks)
-                                        umma_ss(d_cols, kp_desc + ((t * TERM_BYTES + ks * 2048) >> 4), vp_desc + ((ks * 2048) >> 4), idesc_kv,
-                                                t > 0 || ks > 0 ? 1u : e > 0 ? 1u : 0u);
+                                    for (int ks = 0; ks < PIECE / 16; ++ks) {
+                                        const uint32_t more = t > 0 || ks > 0 ? 1u : e > 0 ? 1u : 0u;
+                                        if (STATES)
+                                            umma_ts(d_cols, tmem_base + COL_KP + (pieces.at * kTerms + t) * KP_COLS + ks * 8, vp_desc + ((ks * 2048) >> 4),
+                                                    idesc_kv, more);
+                                        else
+                                            umma_ss(d_cols, kp_desc + ((t * TERM_BYTES + ks * 2048) >> 4), vp_desc + ((ks * 2048) >> 4), idesc_kv, more);
+                                    }
                                 }
                                 umma_commit(&kp_empty[pieces.at]);
                                 if (e & 1) umma_commit(&v_empty[vat.at]);
@@ -606,14 +692,14 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         // ======================================= K' ==============================================
         // 256 threads make a piece together; in the state-only pass four warpgroups make one of a chunk's pieces each (no more teams than
         // places: a team that waits for a place has seen the use before the last one of it given back).
-        if (warp >= 24) setmaxnreg_dec<kRegsKeys>(); else if (warp < 8) setmaxnreg_dec<kRegsP>(); else setmaxnreg_dec<kRegsOut>();
+        setmaxnreg_dec<STATES ? kRegsAcross : kRegsKeys>();
         constexpr int TEAM = STATES ? 128 : 256;
         constexpr uint32_t TEAMS = STATES ? 4 : 1;
         const uint32_t team = !STATES ? 0u : warp < 12 ? (uint32_t)(warp >> 2) - 1u : (uint32_t)(warp >> 2) - 4u;
         const int tid = threadIdx.x & (TEAM - 1);
         Turn<C::KS> kat;
         Turn<C::VS> vat;
-        uint32_t it = 0;
+        uint32_t it = 0, tails = 0;
         bool ok = aligned_ok;
         while (ok && enter()) {
             const int len = tab.len[walk.b], terms = terms_of();
@@ -624,13 +710,20 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 const uint32_t buf = it & 1u;
                 const int valid = len - c * CT;            // tokens of the sequence from here on
                 if (!(ok = wait(&dec_full[buf], (it >> 1) & 1u, kWaitTensor))) break;
-                if (valid < CT && team == 0 && !(ok = clear_tail(TEAM, tid, vat, valid))) break;       // (this team makes piece 0)
+                if (valid < CT && team == 0) {             // (this team makes piece 0)
+                    if (!(ok = clear_tail(TEAM, tid, vat, valid))) break;
+                    if (!STATES && lane == 0) mbar_arrive(&v_cleared[tails & 1u]);
+                    ++tails;
+                }
 #pragma unroll 1
                 for (int e = 0; e < PIECES; ++e) {
                     if (TEAMS == 1 || (uint32_t)e == team) {
                         if (!(ok = wait(&k_full[kat.at], kat.round, kWaitRingFull))) break;
                         if (!(ok = wait(&kp_empty[pieces.at], pieces.parity(pieces.at) ^ 1u, kWaitTensor))) break;
-                        make_piece(std::integral_constant<int, TEAM>{}, tid, kat.at, e, dec + buf * C::DEC_FLOATS, valid, terms);
+                        if (STATES)
+                            make_piece_across(kat.at, e, dec + buf * C::DEC_FLOATS, valid);
+                        else
+                            make_piece(tid, kat.at, e, dec + buf * C::DEC_FLOATS, valid, terms);
                         if (lane == 0 && (TEAMS > 1 || (e & 1))) mbar_arrive(&k_empty[kat.at]);
                     }
                     pieces.next();
@@ -649,9 +742,10 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         setmaxnreg_dec<kRegsP>();
         const int quad = warp & 3, i = quad * 32 + lane;
         const uint32_t sc = tmem_base + COL_SC + ((uint32_t)(quad * 32) << 16);
-        uint32_t it = 0;
+        uint32_t it = 0, tails = 0;
         bool ok = aligned_ok && !STATES;
         while (ok && enter()) {
+            const int len = tab.len[walk.b];
 #pragma unroll 1
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                 const uint32_t buf = it & 1u, ph = it & 1u;
@@ -711,19 +805,27 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&dec_empty[buf]);
+                // V's rows behind the sequence have been cleared (of the two barriers' next uses the later one comes behind this chunk's P V)
+                if (len - c * CT < CT) {
+                    if (!(ok = wait(&v_cleared[tails & 1u], (tails >> 1) & 1u, kWaitTensor))) break;
+                    ++tails;
+                }
                 if (lane == 0) mbar_arrive(p_full);
             }
         }
     } else if (warp < 12 || warp >= 20) {
         // ======================================= output ==========================================
-        setmaxnreg_dec<kRegsOut>();
+        setmaxnreg_dec<STATES ? kRegsIdle : kRegsOut>();
         const int quad = warp & 3;
         const uint32_t mine = warp < 12 ? 0u : 1u;             // chunks of this warpgroup: even, odd
         const uint32_t o = tmem_base + COL_O + mine * 128 + ((uint32_t)(quad * 32) << 16);
         const NormGate& nm = p.base.norm;
         const float scale = p.base.scale;
-        uint8_t* rows = smem + C::OFF_ROWS + (mine * 4 + quad) * 1024;
-        auto staged = [&](int r, int ch) { return reinterpret_cast<uint4*>(rows + r * 32 + ((ch ^ ((r >> 2) & 1)) << 4)); };   // no bank twice
+        // A thread's row comes and goes 16 channels at a time: 32 bytes, a whole sector, in one access where rows start on 32 bytes.  (Through
+        // shared memory, eight rows to an access, was slower: the operands of the matrix products keep that busy.  One / four sequences
+        // of 4,096 tokens, 32 / 37 heads: 76.5 / 149 us against 74.1 / 140, with gate 92.7 / 204 against 85.6 / 182.)
+        const bool wide_out = (((uintptr_t)p.base.o | (uintptr_t)(p.base.o_stride * 2)) & 31) == 0;
+        const bool wide_gate = (((uintptr_t)nm.gate | (uintptr_t)(nm.gate_stride * 2)) & 31) == 0;
         uint32_t it = 0;
         bool ok = aligned_ok && !STATES;
         while (ok && enter()) {
@@ -732,16 +834,13 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll 1
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
                 if ((it & 1u) != mine) continue;
-                // Rows leave (and the gate's come) 16 channels at a time through shared memory, so that a warp's access covers whole sectors.
-                const int t0 = c * CT + quad * 32, lrow = lane >> 1, lch = lane & 1;
-                const bool live0 = t0 + lrow < len, live1 = t0 + lrow + 16 < len;
-                __nv_bfloat16* out = p.base.o + (tok0 + t0 + lrow) * p.base.o_stride + at + lch * 8;
-                const __nv_bfloat16* gate = nm.gate + (tok0 + t0 + lrow) * nm.gate_stride + at + lch * 8;
-                uint4 g0, g1;                                  // the gate's next 16 channels
+                const bool live = c * CT + quad * 32 + lane < len;
+                const int64_t token = tok0 + c * CT + quad * 32 + lane;
+                __nv_bfloat16* out = p.base.o + token * p.base.o_stride + at;
+                const __nv_bfloat16* gate = nm.gate + token * nm.gate_stride + at;
+                uint32_t g[8] = {};                            // the gate's next 16 channels
                 auto ask = [&](int j) {
-                    g0 = g1 = make_uint4(0u, 0u, 0u, 0u);
-                    if (live0) g0 = __ldg(reinterpret_cast<const uint4*>(gate + j));
-                    if (live1) g1 = __ldg(reinterpret_cast<const uint4*>(gate + 16 * nm.gate_stride + j));
+                    if (live) load_row16(gate + j, wide_gate, g);
                 };
                 if (nm.gate) ask(0);
                 if (!(ok = wait(&o_full[mine], (it >> 1) & 1u, kWaitTensor))) break;
@@ -786,12 +885,6 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 }
 #pragma unroll 1
                 for (int j = 0; j < D; j += 16) {
-                    if (nm.gate) {
-                        *staged(lrow, lch) = g0;
-                        *staged(lrow + 16, lch) = g1;
-                        if (j + 16 < D) ask(j + 16);
-                        __syncwarp();
-                    }
                     uint64_t y[8];
                     channels(j, of, add, y);
                     if (j + 16 == D) {                     // all of it has been read
@@ -819,7 +912,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                                 for (int q = 0; q < 4; ++q) y[4 * e + q] = f2_add(y[4 * e + q], f[q]);
                             }
                             if (nm.gate) {                     // (a thread's row of the gate gives way to its row of the output)
-                                eight(*staged(lane, e));
+                                eight(make_uint4(g[4 * e], g[4 * e + 1], g[4 * e + 2], g[4 * e + 3]));
 #pragma unroll
                                 for (int q = 0; q < 4; ++q) y[4 * e + q] = f2_swish_mul(f[q], y[4 * e + q]);
                             }
@@ -832,12 +925,8 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         f2_unpack(y[q], y0, y1);
                         w[q] = pack_bf16x2(y0, y1);
                     }
-                    *staged(lane, 0) = make_uint4(w[0], w[1], w[2], w[3]);
-                    *staged(lane, 1) = make_uint4(w[4], w[5], w[6], w[7]);
-                    __syncwarp();
-                    if (live0) *reinterpret_cast<uint4*>(out + j) = *staged(lrow, lch);
-                    if (live1) *reinterpret_cast<uint4*>(out + 16 * p.base.o_stride + j) = *staged(lrow + 16, lch);
-                    __syncwarp();
+                    if (live) store_row16(out + j, wide_out, w);
+                    if (nm.gate && j + 16 < D) ask(j + 16);
                 }
             }
         }
@@ -871,6 +960,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         };
         uint32_t it = 0, segments = 0;
         bool ok = aligned_ok;
+        if (!STATES) asm volatile("griddepcontrol.wait;" ::: "memory");       // (the merge: nothing else here reads what it wrote)
         while (ok && enter()) {
             const int b = walk.b, h = walk.h;
             const bool whole_stream = walk.whole_stream();
@@ -1007,6 +1097,7 @@ constexpr int kMergeThreads = 256;
 template <int D, class Table>
 __global__ void __launch_bounds__(kMergeThreads)
 gret_merge_kernel(const GretChunkParams p, const __grid_constant__ Table tab) {
+    asm volatile("griddepcontrol.launch_dependents;");
     const int g0 = blockIdx.x + 1;                         // first CTA that starts inside the stream
     const int H = p.base.H, pos = p.first_of(g0), b = sequence_at(p, tab, pos);
     const int base = tab.chunk0[b] * H, chunks = tab.chunk0[b + 1] - tab.chunk0[b], h = (pos - base) / chunks;
@@ -1014,40 +1105,68 @@ gret_merge_kernel(const GretChunkParams p, const __grid_constant__ Table tab) {
     if (pos == begin || p.first_of(g0 - 1) > begin) return;        // no cut, or not the stream's first one
     const int at = (blockIdx.y * kMergeThreads + threadIdx.x) * 4;
     auto part = [&](int64_t slot) { return reinterpret_cast<float4*>(p.part + slot * (D * D) + at); };
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (tab.from[b] >= 0) s = *reinterpret_cast<const float4*>(p.base.state + ((int64_t)tab.from[b] * H + h) * (D * D) + at);
-    *part(p.groups + g0 - 1) = s;
-    auto add = [&](int64_t slot) {
-        const float keep = p.part_keep[slot];
-        const float4 x = *part(slot);
-        s = make_float4(fmaf(keep, s.x, x.x), fmaf(keep, s.y, x.y), fmaf(keep, s.z, x.z), fmaf(keep, s.w, x.w));
-    };
-    int g = g0;
-    for (; g < p.groups && p.first_of(g) < end; ++g) {
-        add(g);
-        *part(g) = s;
+    // the parts are asked for kAhead at a time: one at a time, each behind the store of the one before, every CTA of the stream would cost a
+    // way to memory and back
+    constexpr int kAhead = 4;
+    bool first = true;
+    for (int g = g0;; g += kAhead) {
+        float4 x[kAhead];
+        float keep[kAhead];
+        int n = 0;                                         // CTAs that start inside the stream, of these
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (n < i) continue;
+            const bool inside = g + i < p.groups && p.first_of(g + i) < end;
+            const int64_t slot = inside ? g + i : 2 * (int64_t)p.groups + g + i - 1;
+            x[i] = *part(slot);
+            keep[i] = p.part_keep[slot];
+            if (inside) ++n;
+        }
+        if (first) *part(p.groups + g0 - 1) = s;
+        first = false;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (n < i) continue;
+            s = make_float4(fmaf(keep[i], s.x, x[i].x), fmaf(keep[i], s.y, x[i].y), fmaf(keep[i], s.z, x[i].z), fmaf(keep[i], s.w, x[i].w));
+            if (i < n) *part(g + i) = s;
+        }
+        if (n < kAhead) break;
     }
-    add(2 * (int64_t)p.groups + g - 1);
     if (tab.to[b] >= 0) *reinterpret_cast<float4*>(p.base.state + ((int64_t)tab.to[b] * H + h) * (D * D) + at) = s;
 }
 
-template <int D, bool STATES, class Table>
-cudaError_t launch_pass(const GretChunkParams& p, const Table& tab, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
-                        cudaStream_t stream) {
-    gret_chunk_kernel<D, STATES><<<p.groups, kThreads, GCfg<D, STATES>::SMEM_BYTES, stream>>>(tmQ, tmK, tmV, p, tab);
-    return cudaGetLastError();
+// The three kernels of cut streams follow one another with programmatic stream serialisation: each may be launched while the one before it
+// ends, and waits for it before it reads what that one wrote.
+template <class... Params, class... Args>
+cudaError_t launch_behind(bool early, void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t stream, const Args&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = early ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 template <int D, class Table>
 cudaError_t launch_one(const GretChunkParams& p, const Table& tab, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
                        cudaStream_t stream) {
     if (p.split) {
-        cudaError_t e = launch_pass<D, true>(p, tab, tmQ, tmK, tmV, stream);
+        cudaError_t e = launch_behind(false, gret_chunk_kernel<D, true, Table>, dim3(p.groups), kThreads, GCfg<D, true>::SMEM_BYTES, stream, tmQ, tmK,
+                                      tmV, p, tab);
         if (e != cudaSuccess) return e;
-        gret_merge_kernel<D><<<dim3(p.groups - 1, D * D / (4 * kMergeThreads)), kMergeThreads, 0, stream>>>(p, tab);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        e = launch_behind(true, gret_merge_kernel<D, Table>, dim3(p.groups - 1, D * D / (4 * kMergeThreads)), kMergeThreads, 0, stream, p, tab);
+        if (e != cudaSuccess) return e;
     }
-    return launch_pass<D, false>(p, tab, tmQ, tmK, tmV, stream);
+    return launch_behind(p.split, gret_chunk_kernel<D, false, Table>, dim3(p.groups), kThreads, GCfg<D, false>::SMEM_BYTES, stream, tmQ, tmK, tmV, p,
+                         tab);
 }
 
 template <int D, bool STATES>
