@@ -100,7 +100,7 @@ rope_kernel(const RopeParams p, const __grid_constant__ Table tab, const int tb)
 
 // ---- normalisation of a group, gain, bias, gate -------------------------------------------------------
 // W neighbouring lanes hold a group's channels, 8 C each; mean first, then the sum of squares of the differences.
-constexpr int kNormThreads = 256;
+constexpr int kNormThreads = 128;
 
 template <int W, int C>
 __global__ void __launch_bounds__(kNormThreads)
@@ -194,28 +194,33 @@ cudaError_t launch_rope(const RopeParams& p, const SeqTable& tab, int sm_count, 
     return cudaGetLastError();
 }
 
-// Lanes of a group: the fewest (a power of two) that need no more than five pieces each.  A thread then has its loads in flight side by
-// side, few shuffles, and groups of sizes like 80 leave no lane idle.  (Measured, 16,001 tokens of 40 groups of 80 with gain, bias and gate:
-// ten pieces over 16 lanes 134 us, over two 64 us.)
+// Lanes of a group: the fewest (a power of two) that need no more than five pieces each, but four rather than two, and two rather than one,
+// where that leaves no lane idle and at least two pieces to each: a thread then has its loads in flight side by side, with few shuffles, and
+// neighbouring lanes read 64 bytes.  Small blocks, because a block goes through its loads, sums and stores in step.
+// (Measured, 16,001 tokens of 3,200 channels with gain, bias and gate, 307 MB: groups of 64 over two / four / eight lanes 70 / 58 / 68 us; of 80 over
+// two / four / eight 59 / 60 / 84; of 128 over four / eight / sixteen 56 / 58 / 70, and in blocks of 256 instead of 128 threads 61 over four.)
 cudaError_t launch_head_norm(const HeadNormParams& p, cudaStream_t stream) {
     if (p.groups <= 0) return cudaSuccess;
     const int pieces = p.d / 8;
     auto lanes = [&](auto w) {
         constexpr int W = decltype(w)::value;
         switch ((pieces + W - 1) / W) {
-            case 1: return norm_one<W, 1>(p, stream);
-            case 2: return norm_one<W, 2>(p, stream);
             case 3: return norm_one<W, 3>(p, stream);
             case 4: return norm_one<W, 4>(p, stream);
             default: return norm_one<W, 5>(p, stream);
         }
     };
-    if (pieces <= 5) return lanes(std::integral_constant<int, 1>{});
+    if (pieces == 1) return norm_one<1, 1>(p, stream);
+    if (pieces == 2) return norm_one<1, 2>(p, stream);
+    if (pieces == 3) return norm_one<1, 3>(p, stream);
+    if (pieces == 4) return norm_one<2, 2>(p, stream);
+    if (pieces == 5) return norm_one<1, 5>(p, stream);
+    if (pieces == 8) return norm_one<4, 2>(p, stream);
     if (pieces <= 10) return lanes(std::integral_constant<int, 2>{});
     if (pieces <= 20) return lanes(std::integral_constant<int, 4>{});
     if (pieces <= 40) return lanes(std::integral_constant<int, 8>{});
     if (pieces <= 80) return lanes(std::integral_constant<int, 16>{});
-    return lanes(std::integral_constant<int, 32>{});
+    return pieces <= 96 ? norm_one<32, 3>(p, stream) : norm_one<32, 4>(p, stream);
 }
 
 }  // namespace yoco

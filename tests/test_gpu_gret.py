@@ -132,6 +132,33 @@ def test_streams_are_cut_when_there_are_few(d):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+def test_ranges_of_chunks_that_hold_several_streams(d):
+    """Few streams, more chunks than SMs: a CTA's range begins and ends inside streams and has whole ones, and last chunks, in between."""
+    p = Problem([2600, 777, 3, 1900], 6, d, seed=6, norm="group")
+    assert p.workspace()[1] > 0
+    p.chunk().check()
+    Problem([130] * 9 + [9000], 5, d, seed=7, in_place=True).chunk().check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_that_start_on_16_bytes(d):
+    """Output and gate may start on any 16 bytes; rows that start on 32 go another way."""
+    import torch
+    for lens in ([300, 25], [200] * 3):
+        p = Problem(lens, 2, d, seed=8, norm="rms")
+        n, W = sum(lens), 2 * d
+        p.o_buf = torch.full((n + 2, W + 40), 768.0, dtype=torch.bfloat16, device="cuda")
+        p.o = p.o_buf[1:n + 1, :W]
+        gate = torch.zeros(n, W + 24, dtype=torch.bfloat16, device="cuda")
+        gate[:, 8:8 + W] = p.gate
+        p.gate = gate[:, 8:8 + W]
+        assert p.o.data_ptr() % 32 == 16 and p.gate.data_ptr() % 32 == 16
+        p.shape.o_stride = W + 40
+        p.ng = p.yx.make_norm_gate(1e-5, rms=True, gate=p.gate, gate_stride=W + 24)
+        p.chunk().check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("kw", [dict(tau=0.0), dict(tau=0.0, fused=False), dict(tau=1.0), dict(tau=16.0, decay_dtype="bfloat16"), dict(scale=0.7, fresh=(0, 2)),
                                 dict(in_place=True), dict(fresh=(0, 1, 2), in_place=True)], ids=str)
 def test_forms_of_decays_slots_and_rows(kw, d):

@@ -47,6 +47,14 @@ def test_head_norm_sizes(d, rms):
         assert (np.abs(got - want) <= 2.0 ** -8 * size).all(), (n, H, float((np.abs(got - want) / size).max()))
 
 
+@pytest.mark.parametrize("d", [40, 48, 56, 72, 104, 136, 160, 168, 248, 320, 328, 640, 648, 768, 776, 1016])
+def test_head_norm_lanes_of_a_group(d):
+    """Sizes around the borders between the numbers of lanes that share a group, and of pieces that a lane has."""
+    for n, H in ((3, 1), (67, 5)):
+        got, want = norm_case(n, H, d, 0, 1, 1, seed=d + n)
+        assert (np.abs(got - want) <= 2.0 ** -8 * (np.abs(want) + 2.0 ** -10)).all(), (n, H)
+
+
 def test_head_norm_in_place_empty_and_extreme_rows():
     import torch
     got, want = norm_case(33, 4, 128, 0, 1, 0, seed=1, in_place=True)
