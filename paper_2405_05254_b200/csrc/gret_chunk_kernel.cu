@@ -382,6 +382,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         const int ch = ((warp & 3) * 32 + lane) % D;       // d = 64: the upper 64 rows are the same ones again
         uint8_t* src = smem + C::OFF_K + k_place * C::KV_BYTES + (ch >> 6) * SUB_BYTES + (e & 1) * PIECE_HALF + (ch & 7) * 2;
         auto key = [&](int t) { return reinterpret_cast<uint16_t*>(src + t * 128 + ((((ch >> 3) & 7) ^ (t & 7)) << 4)); };
+        tc_fence_after();                                  // (the product that read this place before)
         const uint32_t dst = tmem_base + COL_KP + pieces.at * (kTerms * KP_COLS) + ((uint32_t)((warp & 3) * 32) << 16);
         if (e * PIECE + PIECE > valid) {                   // tokens behind the sequence: anything, and 0 times that is not 0
 #pragma unroll 1

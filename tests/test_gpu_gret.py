@@ -285,6 +285,58 @@ def test_recorded_calls_and_calls_on_another_stream():
         del graph
 
 
+def test_cut_streams_recorded_in_a_row_and_at_once():
+    """The three kernels of cut streams start early behind one another, but never ahead of the call before: one workspace serves calls in a row, in a
+    recorded graph too, and two streams with a workspace each do not meet."""
+    import torch
+    ps = [Problem([2100, 900], 3, d, seed=97 + d, norm="group", in_place=True) for d in (64, 128)]
+    wss = [torch.empty(p.workspace()[1], dtype=torch.uint8, device="cuda") for p in ps]
+    assert all(ws.numel() > 0 for ws in wss)
+    calls = [p.yx.prepare_tokens("yoco_gret_chunk", p.shape, p.q, p.k, p.v, p.decay, p.ng, p.state, p.slot_in, p.slot_out, p.lens, p.o, ws)
+             for p, ws in zip(ps, wss)]
+    start = [p.state.clone() for p in ps]
+    want = []
+    for p, call in zip(ps, calls):
+        for _ in range(4):                                   # each goes on from the state that the one before left
+            call.run()
+            torch.cuda.synchronize()
+        want.append((p.o.clone(), p.state.clone()))
+
+    def begin():
+        for p, s0 in zip(ps, start):
+            p.o.zero_()
+            p.state.copy_(s0)
+        torch.cuda.synchronize()
+
+    def same():
+        torch.cuda.synchronize()
+        for p, (o, s) in zip(ps, want):
+            assert torch.equal(p.o, o) and torch.equal(p.state, s)
+
+    begin()
+    for call in calls:
+        for _ in range(4):
+            call.run()
+    same()
+    begin()
+    sides = [torch.cuda.Stream() for _ in ps]
+    for _ in range(4):
+        for call, side in zip(calls, sides):
+            with torch.cuda.stream(side):
+                call.run()
+    same()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for call in calls:
+            for _ in range(4):
+                call.run()
+    for _ in range(3):
+        begin()
+        graph.replay()
+        same()
+    del graph
+
+
 def test_two_calls_at_once():
     import torch
     ps = [Problem([700, 260], 6, d, seed=90 + d) for d in (64, 128)]
