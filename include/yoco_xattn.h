@@ -474,8 +474,9 @@ typedef struct yoco_gret_shape {
     int32_t T;               /* tokens per sequence when len_host is NULL                 */
     int32_t num_slots;       /* states in the pool                                        */
     float   scale;           /* > 0, or 0 -> 1/sqrt(d); negative values are rejected      */
-    float   tau;             /* > 0: decay holds logits z, g = sigmoid(z)^(1/tau); 0: natural logarithms of g.  Logarithms
-                                below -110 (g < 2^-158, which no product in fp32 tells from 0) count as -110 */
+    float   tau;             /* > 0: decay holds logits z, g = sigmoid(z)^(1/tau); 0: natural logarithms of g, at most 0 (a
+                                state does not grow by itself).  Logarithms below -110 (g < 2^-158, which no product in fp32
+                                tells from 0) count as -110 */
     int32_t decay_bf16;      /* 0: decay is fp32, 1: bf16                                 */
     int64_t q_stride, k_stride, v_stride, o_stride;   /* elements between two tokens      */
     int64_t decay_stride;    /* elements between two tokens of decay [tokens, H]; 0 -> H  */
@@ -501,8 +502,8 @@ int32_t yoco_gret_step(const yoco_gret_shape* shape, const void* Q, const void* 
                        const yoco_norm_gate* norm, float* state, const int32_t* slot_in_host, const int32_t* slot_out_host,
                        void* O, void* stream);
 /* Any number of tokens: len_host[i] (host [B], may be 0) or shape->T of sequence i.  The workspace (16-byte aligned) is sized by
- * yoco_gret_workspace_size, for these lengths exactly; where that is 0, it may be NULL.  A call recorded into a CUDA graph keeps
- * lengths and slots.  A bounded device-side wait that ran out is reported by yoco_kv_append_status. */
+ * yoco_gret_workspace_size, for these lengths exactly; where that is 0, it may be NULL.  Nothing in it outlives the call, but calls
+ * (or recorded graphs) that may run at the same time need one each.  A call recorded into a CUDA graph keeps lengths and slots.  A bounded device-side wait that ran out is reported by yoco_kv_append_status. */
 int32_t yoco_gret_chunk(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay,
                         const yoco_norm_gate* norm, float* state, const int32_t* slot_in_host, const int32_t* slot_out_host,
                         const int32_t* len_host, void* O, void* workspace, size_t workspace_bytes, void* stream);

@@ -1396,7 +1396,7 @@ int32_t yoco_head_norm(const yoco_head_norm_shape* shape, const void* X, const y
         (rc = check_norm(norm, width, &p.norm)) != YOCO_OK)
         return rc;
     if (s.tokens == 0) return YOCO_OK;
-    if (!X || !Y) return YOCO_ERR_INVALID_ARG;
+    if (!X || !Y || (Y == X && s.tokens > 1 && p.y_stride != p.x_stride)) return YOCO_ERR_INVALID_ARG;
     DeviceState* dev = nullptr;
     if ((rc = device_state(&dev)) != YOCO_OK) return rc;
     p.x = static_cast<const __nv_bfloat16*>(X);
@@ -1436,6 +1436,9 @@ int32_t yoco_rope(const yoco_rope_shape* shape, const void* Q, const void* K, co
             return rc;
         if (tokens == 0) return YOCO_OK;
         if (!Q || !Q_rot || (s.Hk > 0 && (!K || !K_rot))) return YOCO_ERR_INVALID_ARG;
+        // in place: rows of the same distance, or one token would be written over another that is still to be read
+        if (tokens > 1 && ((Q_rot == Q && p.q_out_stride != p.q_stride) || (s.Hk > 0 && K_rot == K && p.k_out_stride != p.k_stride)))
+            return YOCO_ERR_INVALID_ARG;
         SeqTable tab;
         std::memset(&tab, 0, sizeof tab);
         p.tokens_per_seq = len_host ? len_host[0] : s.T;

@@ -35,14 +35,14 @@ __device__ __forceinline__ float log_decay(const GretParams& p, float z) {
 
 __device__ __forceinline__ float swish(float u) { return __fdividef(u, 1.f + __expf(-u)); }
 
-// y * swish(u) for two at a time: u y / (1 + 2^(-u log2 e))
+// y * swish(u) for two at a time, swish(u) = u / (1 + 2^(-u log2 e)) first: u y may overflow where swish(u) is 0.
 __device__ __forceinline__ uint64_t f2_swish_mul(uint64_t u, uint64_t y) {
     float e0, e1;
     f2_unpack(f2_mul(u, f2_pack(-1.4426950408889634f, -1.4426950408889634f)), e0, e1);
     f2_unpack(f2_add(f2_pack(ex2_approx(e0), ex2_approx(e1)), f2_pack(1.f, 1.f)), e0, e1);
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e0));
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e1));
-    return f2_mul(f2_mul(u, y), f2_pack(e0, e1));
+    return f2_mul(f2_mul(u, f2_pack(e0, e1)), y);
 }
 
 __device__ __forceinline__ float warp_sum(float x) {

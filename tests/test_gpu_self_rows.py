@@ -126,6 +126,40 @@ def rope_case(lens, Hq, Hk, d, rot, pairs, pos, seed, base=640000.0, in_place=Fa
         assert np.array_equal(got[..., rot:], s[..., rot:])
 
 
+@pytest.mark.parametrize("way", ["norm", "chunk", "step"])
+def test_gate_that_closes_against_large_values(way):
+    """swish(u) is 0 for u far below zero, and 0 times any finite value is 0, also where u times that value would overflow."""
+    import torch
+    from paper_2405_05254_b200 import binding as yx
+    d, n = 128, 1 if way == "step" else 40
+    x = torch.zeros(n, d, dtype=torch.bfloat16, device="cuda")
+    x[:, ::8] = 4.0                                          # rms 2^0.5: normalised values 2^1.5; with the gain up to 2^11.5
+    gain = torch.full((d,), 1024.0, dtype=torch.bfloat16, device="cuda")
+    gate = torch.full((n, d), -3e38, dtype=torch.bfloat16, device="cuda")
+    gate[:, 64:] = 1.0
+    ng = yx.make_norm_gate(0.0, rms=True, gate=gate, gain=gain)
+    y = torch.full((n, d), 768.0, dtype=torch.bfloat16, device="cuda")
+    if way == "norm":
+        yx.yoco_head_norm(yx.HeadNormShape(n, 1, d, 0, 0), x, ng, y)
+    else:
+        # k = (1, 0, ..), q = k, no decay before the first token: the first output is v = x, the others multiples of it
+        k = torch.zeros_like(x)
+        k[:, 0] = 1.0
+        state = torch.zeros(1, 1, d, d, device="cuda")
+        shape = yx.make_gret_shape(1, 1, d, T=n, scale=1.0)
+        slot, begin = np.array([0], np.int32), np.array([-1], np.int32)
+        args = (shape, k, k, x, torch.full((n, 1), -0.5, device="cuda"), ng, state, begin, slot)
+        if way == "chunk":
+            yx.yoco_gret_chunk(*args, None, y, torch.empty(yx.yoco_gret_workspace_size(shape), dtype=torch.uint8, device="cuda"))
+        else:
+            yx.yoco_gret_step(*args, y)
+    got = y.double().cpu().numpy()
+    want = np.zeros((n, d))
+    want[:, 64::8] = 2 ** 1.5 * 1024 / (1 + np.exp(-1.0))
+    # step's and norm's roundings: the output's half step 2^-8; chunk: P and its sum as well, but they leave the norm with the row's size
+    assert np.isfinite(got).all() and (np.abs(got - want) <= 2.0 ** -7 * np.abs(want)).all()
+
+
 @pytest.mark.parametrize("pairs", [0, 1])
 @pytest.mark.parametrize("d,rot", [(64, 64), (128, 128), (128, 64), (128, 32), (80, 16), (80, 80), (112, 96), (512, 512), (16, 16)])
 def test_rotation_sizes(d, rot, pairs):

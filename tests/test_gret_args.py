@@ -149,6 +149,16 @@ def test_rotation_refuses_bad_arguments():
     assert bd.lib().yoco_rope(None, A, A, A, None, None, A, A, None) == INV
 
 
+def test_in_place_needs_rows_of_one_distance():
+    B = vp(1 << 20)
+    ok = norm_call()
+    assert norm_call(xs=392) == INV and norm_call(ys=392) == INV and norm_call(xs=392, ys=392) == ok and norm_call(xs=392, Y=B) == ok
+    assert norm_call(n=1, xs=392) == ok
+    ok = rope_call()
+    assert rope_call(q_stride=520) == INV and rope_call(k_out_stride=264) == INV and rope_call(q_stride=520, q_out_stride=520) == ok
+    assert rope_call(q_stride=520, Qr=B) == ok and rope_call(k_stride=264, Kr=B) == ok and rope_call(lens=(1, 0), q_stride=520) == ok
+
+
 def test_structures_have_the_sizes_of_the_header():
     assert ctypes.sizeof(bd.GretShape) == 72 and ctypes.sizeof(bd.NormGate) == 40 and ctypes.sizeof(bd.HeadNormShape) == 32
     assert ctypes.sizeof(bd.RopeShape) == 64
