@@ -503,7 +503,8 @@ int32_t yoco_gret_step(const yoco_gret_shape* shape, const void* Q, const void* 
                        void* O, void* stream);
 /* Any number of tokens: len_host[i] (host [B], may be 0) or shape->T of sequence i.  The workspace (16-byte aligned) is sized by
  * yoco_gret_workspace_size, for these lengths exactly; where that is 0, it may be NULL.  Nothing in it outlives the call, but calls
- * (or recorded graphs) that may run at the same time need one each.  A call recorded into a CUDA graph keeps lengths and slots.  A bounded device-side wait that ran out is reported by yoco_kv_append_status. */
+ * (or recorded graphs) that may run at the same time need one each.  A call recorded into a CUDA graph keeps lengths and slots.
+ * A bounded device-side wait that ran out is reported by yoco_kv_append_status. */
 int32_t yoco_gret_chunk(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay,
                         const yoco_norm_gate* norm, float* state, const int32_t* slot_in_host, const int32_t* slot_out_host,
                         const int32_t* len_host, void* O, void* workspace, size_t workspace_bytes, void* stream);
