@@ -78,7 +78,7 @@ struct GCfg {
     static constexpr int OFF_V = OFF_Q + QS * TILE_BYTES;
     static constexpr int OFF_KP = OFF_V + VS * KV_BYTES;
     static constexpr int OFF_S = OFF_KP + (STATES ? 0 : KP_WIDE * kTerms * TERM_BYTES);
-    static constexpr int OFF_DEC = OFF_S + (STATES ? 0 : D * D * 2);
+    static constexpr int OFF_DEC = OFF_S + (STATES ? D * 128 : D * D * 2);    // (the state-only pass: a way through for rows of the state)
     // Of a chunk: 2^(b_C - b_j); whole part and rest of b_C; and where there is output: whole parts and rests of -b_j; 2^(m - b_j).
     static constexpr int DEC_END = CT, DEC_WHOLE = CT + 4, DEC_REST = DEC_WHOLE + CT, DEC_U = DEC_REST + CT;
     static constexpr int DEC_FLOATS = STATES ? DEC_WHOLE : DEC_U + CT;
@@ -1067,11 +1067,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 dst = p.part + slot * (D * D);
             else if (whole_stream && tab.to[b] >= 0)
                 dst = p.base.state + ((int64_t)tab.to[b] * p.base.H + h) * (D * D);
-            if (STATES) {
-#pragma unroll
-                for (int j = 0; j < N; j += 4)
-                    *reinterpret_cast<float4*>(dst + row * D + col + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
-            } else if (dst) {
+            if (dst) {
                 through_rows([&](int j, int r, int ch, uint4* place) { *reinterpret_cast<uint4*>(dst + r * D + j + ch * 4) = *place; },
                              [&](int j, int ch, uint4* place) {
                                  *reinterpret_cast<float4*>(place) = make_float4(s[j + ch * 4], s[j + ch * 4 + 1], s[j + ch * 4 + 2], s[j + ch * 4 + 3]);
