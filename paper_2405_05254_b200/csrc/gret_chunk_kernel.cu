@@ -55,8 +55,9 @@ constexpr uint32_t COL_SC = 0, COL_O = 128, COL_DS = 384;     // two buffers of 
 // The state-only pass has the first 128 columns for a second buffer of DS, and the four pieces of K' where O is otherwise.
 constexpr uint32_t COL_KP = COL_O, KP_COLS = PIECE / 2;       // of each part
 // Registers per thread after the split; the CTA starts with 64 each.
-constexpr int kRegsIo = 56, kRegsP = 56, kRegsOut = 64, kRegsState = 88, kRegsKeys = 48;
+constexpr int kRegsIo = 56, kRegsP = 56, kRegsOut = 72, kRegsState = 88, kRegsKeys = 40;
 static_assert(kRegsIo + kRegsP + 2 * kRegsOut + 2 * kRegsState + 2 * kRegsKeys <= 8 * 64, "register pool of the CTA");
+static_assert(kRegsIo <= 64 && kRegsP <= 64 && kRegsKeys <= 64 && kRegsOut >= 64 && kRegsState >= 64, "which way the split goes");
 constexpr int kRegsAcross = 64, kRegsIdle = 24;               // the state-only pass: four warpgroups make K', one has nothing to do
 static_assert(kRegsIo + 4 * kRegsAcross + kRegsIdle + 2 * kRegsState <= 8 * 64, "register pool of the CTA");
 constexpr int kTerms = 3;                      // parts of K', where a state leaves; otherwise kTermsInside
@@ -816,7 +817,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
     } else if (warp < 12 || warp >= 20) {
         // ======================================= output ==========================================
-        setmaxnreg_dec<STATES ? kRegsIdle : kRegsOut>();
+        if constexpr (STATES) setmaxnreg_dec<kRegsIdle>(); else setmaxnreg_inc<kRegsOut>();
         const int quad = warp & 3;
         const uint32_t mine = warp < 12 ? 0u : 1u;             // chunks of this warpgroup: even, odd
         const uint32_t o = tmem_base + COL_O + mine * 128 + ((uint32_t)(quad * 32) << 16);
@@ -846,30 +847,27 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 if (nm.gate) ask(0);
                 if (!(ok = wait(&o_full[mine], (it >> 1) & 1u, kWaitTensor))) break;
                 tc_fence_after();
-                // 16 channels of the row: a * x + add
-                auto channels = [&](int j, float a, float add, uint64_t (&y)[8]) {
-                    float x[16];
-                    tmem_ld16(o + j, x);
+                // 16 channels of the row: a * x + add; the ones at `next` are on their way from then on
+                float x[16];
+                auto channels = [&](int next, float a, float add, uint64_t (&y)[8]) {
                     const uint64_t a2 = f2_pack(a, a), add2 = f2_pack(add, add);
                     tmem_wait_ld();
 #pragma unroll
                     for (int q = 0; q < 8; ++q) y[q] = f2_fma(a2, f2_pack(x[2 * q], x[2 * q + 1]), add2);
+                    if (next < D) tmem_ld16(o + next, x);
                 };
+                tmem_ld16(o, x);
                 float of = scale, add = 0.f;
                 if (nm.on) {
                     // sums of the differences from the row's first channel (rms: from zero) and of their squares: one of d values is at most
                     // sqrt(d) standard deviations from the mean, so the difference of the two loses at most d roundings
-                    float first = 0.f;
-                    if (!nm.rms) {
-                        tmem_ld1(o, first);
-                        tmem_wait_ld();
-                        first *= scale;
-                    }
+                    tmem_wait_ld();
+                    const float first = nm.rms ? 0.f : x[0] * scale;
                     uint64_t s1 = 0ull, s2 = 0ull;
 #pragma unroll 1
                     for (int j = 0; j < D; j += 16) {
                         uint64_t y[8];
-                        channels(j, scale, -first, y);
+                        channels((j + 16) % D, scale, -first, y);
 #pragma unroll
                         for (int q = 0; q < 8; ++q) {
                             s1 = f2_add(s1, y[q]);
@@ -887,7 +885,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll 1
                 for (int j = 0; j < D; j += 16) {
                     uint64_t y[8];
-                    channels(j, of, add, y);
+                    channels(j + 16, of, add, y);
                     if (j + 16 == D) {                     // all of it has been read
                         tc_fence_before();
                         __syncwarp();
