@@ -917,6 +917,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                             }
                         }
                     }
+                    if (nm.gate && j + 16 < D) ask(j + 16);
                     uint32_t w[8];
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {
@@ -925,7 +926,6 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         w[q] = pack_bf16x2(y0, y1);
                     }
                     if (live) store_row16(out + j, wide_out, w);
-                    if (nm.gate && j + 16 < D) ask(j + 16);
                 }
             }
         }
