@@ -767,8 +767,8 @@ int32_t check_slots(const yoco_gret_shape& s, const int32_t* in, const int32_t* 
 // 32 sequences 70 / 84, 64 in chunks.)
 constexpr int32_t kGretTokens = 18;
 // What a chunk costs in the state-only pass over split streams, and the extra launches, in chunks of the main pass.  (Measured, 32 heads of 128
-// on 148 SMs: whole streams 4.5 us a chunk, split 5.5 us a chunk for both passes, and 33 us more for the launches, their starts and ends.)
-constexpr double kGretStateCost = 0.25, kGretSplitCost = 7.0;
+// on 148 SMs: whole streams 4.3 us a chunk, split 5.6 us a chunk for both passes, and 30 us more for the launches, their starts and ends.)
+constexpr double kGretStateCost = 0.3, kGretSplitCost = 7.0;
 
 struct GretPlan {
     GretChunkTable tab;

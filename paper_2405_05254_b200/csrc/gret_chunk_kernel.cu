@@ -720,7 +720,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll 1
                 for (int e = 0; e < PIECES; ++e) {
                     if (TEAMS == 1 || (uint32_t)e == team) {
-                        if (!(ok = wait(&k_full[kat.at], kat.round, kWaitRingFull))) break;
+                        if ((TEAMS > 1 || !(e & 1)) && !(ok = wait(&k_full[kat.at], kat.round, kWaitRingFull))) break;
                         if (!(ok = wait(&kp_empty[pieces.at], pieces.parity(pieces.at) ^ 1u, kWaitTensor))) break;
                         if (STATES)
                             make_piece_across(kat.at, e, dec + buf * C::DEC_FLOATS, valid);
