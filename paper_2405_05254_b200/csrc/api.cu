@@ -766,9 +766,11 @@ int32_t check_slots(const yoco_gret_shape& s, const int32_t* in, const int32_t* 
 // (Measured, 32 heads of 128: one sequence of 18 / 24 tokens 12.7 / 14.7 us token by token, 13.5 in chunks; eight 19.9 / 24.9, 22.8 in chunks;
 // 32 sequences 70 / 84, 64 in chunks.)
 constexpr int32_t kGretTokens = 18;
-// What a chunk costs in the state-only pass over split streams, and the extra launches, in chunks of the main pass.  (Measured, 32 heads of 128
-// on 148 SMs: whole streams 4.3 us a chunk, split 5.6 us a chunk for both passes, and 30 us more for the launches, their starts and ends.)
-constexpr double kGretStateCost = 0.3, kGretSplitCost = 7.0;
+// Costs in chunks of a whole stream (32 heads of 128 on 148 SMs: 3.8 to 4.3 us, by how many SMs have one): a chunk in both passes over split
+// streams; the extra launches with their starts and ends; every further segment of a CTA, whose state comes and goes.  (Measured: one sequence of
+// 1,024 tokens, 8 / 16 / 32 heads, whole 36 / 36 / 38 us, split 23 / 26 / 34; 1,280 tokens, 32 heads 44, split 41; 896 tokens 33 whole; six
+// sequences of 37 to 1,501 tokens, 16 heads 52, split 70.)
+constexpr double kGretSplitChunk = 1.4, kGretSplitCost = 4.0, kGretSegmentCost = 1.0;
 
 struct GretPlan {
     GretChunkTable tab;
@@ -802,12 +804,15 @@ void plan_gret(const yoco_gret_shape& s, const int32_t* len_host, const GretTabl
     for (int32_t j = out->seqs; j < kAppendMaxSequences; ++j) out->tab.chunk0[j + 1] = out->tab.chunk0[out->seqs];
     out->total = (int64_t)out->tab.chunk0[out->seqs] * s.H;
     const int64_t streams = (int64_t)out->seqs * s.H;
-    // time of whole streams, dealt out longest first: no less than the longest one, and than an equal share in whole streams' steps
-    double whole = 0.0;
-    for (int64_t first = 0; first < streams; first += sm_count) whole += out->tab.chunk0[first / s.H + 1] - out->tab.chunk0[first / s.H];
+    // time of whole streams, dealt out longest first: the longest of every round
+    double whole = -kGretSegmentCost;
+    for (int64_t first = 0; first < streams; first += sm_count)
+        whole += out->tab.chunk0[first / s.H + 1] - out->tab.chunk0[first / s.H] + kGretSegmentCost;
+    // time of equal shares: the last one, of the shortest streams, has the most segments
     const int64_t cut = std::min<int64_t>(out->total, sm_count);
     const double share = cut > 0 ? (double)((out->total + cut - 1) / cut) : 0.0;
-    out->split = cut > 1 && share * (1.0 + kGretStateCost) + kGretSplitCost < whole;
+    const double segments = out->seqs > 0 ? share / (out->tab.chunk0[out->seqs] - out->tab.chunk0[out->seqs - 1]) : 0.0;
+    out->split = cut > 1 && share * kGretSplitChunk + kGretSplitCost + segments * kGretSegmentCost < whole;
     out->groups = (int32_t)(out->split ? cut : std::min<int64_t>(streams, sm_count));
     out->part_bytes = (size_t)3 * out->groups * s.d * s.d * sizeof(float);
 }
