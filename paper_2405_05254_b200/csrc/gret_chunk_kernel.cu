@@ -1105,7 +1105,7 @@ gret_merge_kernel(const GretChunkParams p, const __grid_constant__ Table tab) {
     if (tab.from[b] >= 0) s = *reinterpret_cast<const float4*>(p.base.state + ((int64_t)tab.from[b] * H + h) * (D * D) + at);
     // the parts are asked for kAhead at a time: one at a time, each behind the store of the one before, every CTA of the stream would cost a
     // way to memory and back
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 8;
     bool first = true;
     for (int g = g0;; g += kAhead) {
         float4 x[kAhead];
