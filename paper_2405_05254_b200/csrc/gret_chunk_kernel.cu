@@ -234,7 +234,10 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     float* dec = reinterpret_cast<float*>(smem + C::OFF_DEC);
 
-    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // (the same for all lanes, for the compiler to see)
+    // The same for all lanes, for the compiler to see, so that roles issue from uniform registers; but not where it measured worse.  (32 heads,
+    // one sequence.  d = 128, 16,384 tokens: main pass 188 K cycles without it, 175 K with it, state-only pass 109 K and 118 K.  d = 64,
+    // 4,096 tokens, both passes: state-only pass without / with it 53.6 / 52.1 us.)
+    const int warp = STATES && D == 128 ? (int)threadIdx.x >> 5 : __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const Abort ab{abort_flag, p.status, kWaitLimitNs};
     const bool aligned_ok = (smem_u32(smem) & 1023u) == 0;
 
