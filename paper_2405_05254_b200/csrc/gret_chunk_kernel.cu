@@ -20,12 +20,12 @@
 // With few streams a first pass over K and V (STATES) leaves the state of each CTA's range, a merge puts those in order, and the main
 // pass starts every range from its own: all SMs work, K and V are read twice.  In that first pass warpgroups 1, 2, 6 and 7 make K', a piece each, in
 // tensor memory.
-// What bounds it: not the bytes (measured: 45% and 51% of the memory's rate in the two passes), but what goes through the SM's shared
-// memory.  A chunk's matrix products read 320 KB of operands there, the copies write 96 KB, K' and S take another 130 KB: with the traffic of
-// tensor memory's loads and stores some 6,600 of the 6,900 cycles that a chunk takes.  What took load off it made it faster (output and gate
-// past it, K' of the first pass to tensor memory), what shortened the chain from Q K^T over P to P V did not.
-// Measured (bf16, d = 128, no gate): one sequence of 32,768 tokens, 32 heads 358 us (1.08 GB needed: 165 us at 6.56 TB/s); 4,096 tokens 72 us;
-// four of 4,096 tokens, 37 heads, whole streams 143 us (0.68 of that rate); one chunk 13 us.
+// What bounds it: not the bytes (measured: 46% and 55% of the memory's rate in the two passes) nor the tensor cores (39%, 41%), but the
+// roles' chain, through shared memory's data pipe: a chunk's matrix products read 320 KB of operands there, the copies write 96 KB, K' and S another
+// 130 KB (the pipe: 37% of the cycles the tensor cores' operands, 62% the threads' accesses, tensor memory's among them).  What took load off
+// it made it faster (output and gate past it, K' of the first pass to tensor memory), and so did fewer instructions on the chain (uniform registers).
+// Measured (d = 128, short bursts): one sequence of 32,768 tokens, 32 heads 355-364 us (1.08 GB needed: 165 us at 6.56 TB/s), with gate 415;
+// 4,096 tokens 69, with gate 78; four of 4,096 tokens, 37 heads, whole streams 141 (0.69 of that rate), with gate 175; one chunk 13.
 // Roundings: P and the copy of S that multiplies Q go to bf16 (half a step, 2^-9 of the value, like the output's own).  K' goes to
 // the tensor cores as a sum of bf16: where the sums leave the kernel as a state, of three (24 bits; with one it would be 1.7e-3 off (2-norm),
 // with two 2e-6), where they only multiply Q inside, of two.
