@@ -314,7 +314,9 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             at = at + 1 == count ? 0 : at + 1;
         }
     } pieces;
-    // the makers of K', before a segment's first piece: all places have been given back (they may lie differently from now on)
+    // The makers of K' in the main pass, before a segment's first piece: all places have been given back (they may lie differently from now
+    // on).  Not for the state-only pass: its places never move, and there a team fills one of them alone, so that the uses of the others may go on
+    // before a slower team has looked, which would then take the phase after the one it waits for, of the same parity, for that one not yet over.
     auto all_given_back = [&]() {
 #pragma unroll 1
         for (uint32_t i = 0; i < C::KP_STAGES; ++i)
@@ -695,8 +697,8 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
     } else if (warp >= 24 || (STATES && warp < 12)) {
         // ======================================= K' ==============================================
-        // 256 threads make a piece together; in the state-only pass four warpgroups make one of a chunk's pieces each (no more teams than
-        // places: a team that waits for a place has seen the use before the last one of it given back).
+        // 256 threads make a piece together; in the state-only pass four warpgroups make one of a chunk's pieces each, always in the same place, and
+        // wait for no other's: a team has seen the use before the last one of its place given back.
         setmaxnreg_dec<STATES ? kRegsAcross : kRegsKeys>();
         constexpr int TEAM = STATES ? 128 : 256;
         constexpr uint32_t TEAMS = STATES ? 4 : 1;
@@ -708,7 +710,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         bool ok = aligned_ok;
         while (ok && enter()) {
             const int len = tab.len[walk.b], terms = terms_of();
-            if (!(ok = all_given_back())) break;
+            if (!STATES && !(ok = all_given_back())) break;
             pieces.segment(terms);
 #pragma unroll 1
             for (int c = walk.c; c < walk.c_end; ++c, ++it) {
