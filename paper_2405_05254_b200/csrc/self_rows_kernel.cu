@@ -110,9 +110,10 @@ head_norm_kernel(const HeadNormParams p) {
     const int lane = threadIdx.x % W;
     const int64_t group = (int64_t)blockIdx.x * (kNormThreads / W) + threadIdx.x / W;
     const bool live = group < p.groups;
-    const int g = live ? (int)group : 0, tok = g / p.H, h = g - tok * p.H;
-    const __nv_bfloat16* src = p.x + (int64_t)tok * p.x_stride + h * p.d;
-    const __nv_bfloat16* gate = p.norm.gate ? p.norm.gate + (int64_t)tok * p.norm.gate_stride + h * p.d : nullptr;
+    const int g = live ? (int)group : 0, tok = g / p.H;
+    const int64_t col = (int64_t)(g - tok * p.H) * p.d;             // (rows may be longer than 2^31 channels)
+    const __nv_bfloat16* src = p.x + tok * p.x_stride + col;
+    const __nv_bfloat16* gate = p.norm.gate ? p.norm.gate + tok * p.norm.gate_stride + col : nullptr;
     uint4 xr[C], gr[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -148,7 +149,7 @@ head_norm_kernel(const HeadNormParams p) {
     for (int m = W / 2; m > 0; m >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, m);
     const float inv = 1.f / sqrtf(sq / (float)p.d + p.norm.eps);
     if (!live) return;
-    __nv_bfloat16* dst = p.y + (int64_t)tok * p.y_stride + h * p.d;
+    __nv_bfloat16* dst = p.y + tok * p.y_stride + col;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int at = (c * W + lane) * 8;
@@ -157,12 +158,12 @@ head_norm_kernel(const HeadNormParams p) {
         for (int j = 0; j < 8; ++j) x[c][j] *= inv;
         float w[8];
         if (p.norm.gain) {
-            unpack8(__ldg(reinterpret_cast<const uint4*>(p.norm.gain + h * p.d + at)), w);
+            unpack8(__ldg(reinterpret_cast<const uint4*>(p.norm.gain + col + at)), w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[c][j] *= w[j];
         }
         if (p.norm.bias) {
-            unpack8(__ldg(reinterpret_cast<const uint4*>(p.norm.bias + h * p.d + at)), w);
+            unpack8(__ldg(reinterpret_cast<const uint4*>(p.norm.bias + col + at)), w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[c][j] += w[j];
         }
