@@ -883,6 +883,8 @@ def prepare_tokens(fn_name, shape, *args, stream=None) -> PreparedTokensCall:
 def yoco_gret_workspace_size(shape: GretShape, lens=None, sm_count: int = 0) -> int:
     """Workspace bytes of yoco_gret_chunk for exactly these lengths (None: shape.T each); may be 0."""
     keep, p_len = _host_i32(lens)
+    if keep is not None and keep.size < shape.B:
+        raise ValueError(f"yoco_gret_workspace_size: {keep.size} lengths for {shape.B} sequences")
     out = ctypes.c_size_t(0)
     rc = lib().yoco_gret_workspace_size(ctypes.byref(shape), p_len, sm_count, ctypes.byref(out))
     if rc != OK:
