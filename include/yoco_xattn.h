@@ -502,7 +502,9 @@ int32_t yoco_gret_step(const yoco_gret_shape* shape, const void* Q, const void* 
                        const yoco_norm_gate* norm, float* state, const int32_t* slot_in_host, const int32_t* slot_out_host,
                        void* O, void* stream);
 /* Any number of tokens: len_host[i] (host [B], may be 0) or shape->T of sequence i.  The workspace (16-byte aligned) is sized by
- * yoco_gret_workspace_size, for these lengths exactly; where that is 0, it may be NULL.  Nothing in it outlives the call, but calls
+ * yoco_gret_workspace_size, for these lengths exactly (shorter ones, or fewer sequences, may take more: a few streams are cut where many
+ * are not); where that is 0, it may be NULL.  A workspace that serves calls of changing lengths is sized by yoco_gret_workspace_bound: enough for all
+ * lengths up to those given, 0 among them (shape the same), and never more than three states per SM.  Nothing in it outlives the call, but calls
  * (or recorded graphs) that may run at the same time need one each.  A call recorded into a CUDA graph keeps lengths and slots.
  * A bounded device-side wait that ran out is reported by yoco_kv_append_status. */
 int32_t yoco_gret_chunk(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay,
@@ -510,6 +512,7 @@ int32_t yoco_gret_chunk(const yoco_gret_shape* shape, const void* Q, const void*
                         const int32_t* len_host, void* O, void* workspace, size_t workspace_bytes, void* stream);
 /* sm_count <= 0: that of the current device. */
 int32_t yoco_gret_workspace_size(const yoco_gret_shape* shape, const int32_t* len_host, int32_t sm_count, size_t* bytes);
+int32_t yoco_gret_workspace_bound(const yoco_gret_shape* shape, const int32_t* len_host, int32_t sm_count, size_t* bytes);
 
 /* The normalisation and gate alone: X, Y [tokens, H * d] bf16.  Y may be X (with the same stride). */
 typedef struct yoco_head_norm_shape {

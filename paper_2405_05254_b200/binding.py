@@ -159,6 +159,7 @@ def lib() -> ctypes.CDLL:
         L.yoco_xattn_workspace_bound_paged.restype = i32
         for name, args in (("yoco_gret_step", [vp] * 11), ("yoco_gret_chunk", [vp] * 12 + [sz, vp]),
                            ("yoco_gret_workspace_size", [vp, vp, i32, ctypes.POINTER(sz)]),
+                           ("yoco_gret_workspace_bound", [vp, vp, i32, ctypes.POINTER(sz)]),
                            ("yoco_head_norm", [vp] * 5), ("yoco_rope", [vp] * 9)):
             getattr(L, name).argtypes = args
             getattr(L, name).restype = i32
@@ -880,16 +881,25 @@ def prepare_tokens(fn_name, shape, *args, stream=None) -> PreparedTokensCall:
     return PreparedTokensCall(fn_name, shape, *args, stream=stream)
 
 
-def yoco_gret_workspace_size(shape: GretShape, lens=None, sm_count: int = 0) -> int:
-    """Workspace bytes of yoco_gret_chunk for exactly these lengths (None: shape.T each); may be 0."""
+def _gret_workspace(fn_name, shape, lens, sm_count) -> int:
     keep, p_len = _host_i32(lens)
     if keep is not None and keep.size < shape.B:
-        raise ValueError(f"yoco_gret_workspace_size: {keep.size} lengths for {shape.B} sequences")
+        raise ValueError(f"{fn_name}: {keep.size} lengths for {shape.B} sequences")
     out = ctypes.c_size_t(0)
-    rc = lib().yoco_gret_workspace_size(ctypes.byref(shape), p_len, sm_count, ctypes.byref(out))
+    rc = getattr(lib(), fn_name)(ctypes.byref(shape), p_len, sm_count, ctypes.byref(out))
     if rc != OK:
-        raise YocoError(rc, "yoco_gret_workspace_size")
+        raise YocoError(rc, fn_name)
     return int(out.value)
+
+
+def yoco_gret_workspace_size(shape: GretShape, lens=None, sm_count: int = 0) -> int:
+    """Workspace bytes of yoco_gret_chunk for exactly these lengths (None: shape.T each); may be 0."""
+    return _gret_workspace("yoco_gret_workspace_size", shape, lens, sm_count)
+
+
+def yoco_gret_workspace_bound(shape: GretShape, lens=None, sm_count: int = 0) -> int:
+    """Workspace bytes that suffice for all lengths up to these: for a workspace kept while sequences come and go."""
+    return _gret_workspace("yoco_gret_workspace_bound", shape, lens, sm_count)
 
 
 def yoco_gret_chunk(shape: GretShape, Q, K, V, decay, norm, state, slot_in, slot_out, lens, O, workspace=None, stream=None) -> None:

@@ -778,6 +778,10 @@ struct GretPlan {
     int64_t total;              // chunks of all heads
     int32_t groups, split;
     size_t part_bytes;          // workspace: parts' states, then their decays
+    void set_groups(int32_t n, int32_t d) {
+        groups = n;
+        part_bytes = (size_t)3 * n * d * d * sizeof(float);
+    }
     size_t bytes() const { return split ? part_bytes + (size_t)3 * groups * sizeof(float) : 0; }
 };
 
@@ -813,8 +817,29 @@ void plan_gret(const yoco_gret_shape& s, const int32_t* len_host, const GretTabl
     const double share = cut > 0 ? (double)((out->total + cut - 1) / cut) : 0.0;
     const double segments = out->seqs > 0 ? share / (out->tab.chunk0[out->seqs] - out->tab.chunk0[out->seqs - 1]) : 0.0;
     out->split = cut > 1 && share * kGretSplitChunk + kGretSplitCost + segments * kGretSegmentCost < whole;
-    out->groups = (int32_t)(out->split ? cut : std::min<int64_t>(streams, sm_count));
-    out->part_bytes = (size_t)3 * out->groups * s.d * s.d * sizeof(float);
+    out->set_groups((int32_t)(out->split ? cut : std::min<int64_t>(streams, sm_count)), s.d);
+}
+
+// Workspace bytes of calls with these lengths, or with lengths up to these: none where all sequences are walked token by token.
+template <class F>
+int32_t gret_workspace(const yoco_gret_shape* shape, const int32_t* len_host, int32_t sm_count, size_t* bytes, F of_chunks) {
+    return no_throw([&]() -> int32_t {
+        if (!shape || !bytes) return YOCO_ERR_INVALID_ARG;
+        int64_t tokens = 0;
+        int32_t rc = check_gret_shape(*shape);
+        if (rc != YOCO_OK || (rc = check_lengths(shape->B, len_host, shape->T, &tokens)) != YOCO_OK) return rc;
+        int32_t longest = 0;
+        for (int32_t i = 0; i < shape->B; ++i) longest = std::max(longest, len_host ? len_host[i] : shape->T);
+        *bytes = 0;
+        if (longest <= kGretTokens) return YOCO_OK;
+        if (sm_count <= 0) {
+            DeviceState* dev = nullptr;
+            if ((rc = device_state(&dev)) != YOCO_OK) return rc;
+            sm_count = dev->sm_count;
+        }
+        *bytes = of_chunks(sm_count);
+        return YOCO_OK;
+    });
 }
 
 int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay, const yoco_norm_gate* norm,
@@ -1366,24 +1391,21 @@ int32_t yoco_gret_chunk(const yoco_gret_shape* shape, const void* Q, const void*
 }
 
 int32_t yoco_gret_workspace_size(const yoco_gret_shape* shape, const int32_t* len_host, int32_t sm_count, size_t* bytes) {
-    return no_throw([&]() -> int32_t {
-        if (!shape || !bytes) return YOCO_ERR_INVALID_ARG;
-        int64_t tokens = 0;
-        int32_t rc = check_gret_shape(*shape);
-        if (rc != YOCO_OK || (rc = check_lengths(shape->B, len_host, shape->T, &tokens)) != YOCO_OK) return rc;
-        int32_t longest = 0;
-        for (int32_t i = 0; i < shape->B; ++i) longest = std::max(longest, len_host ? len_host[i] : shape->T);
-        *bytes = 0;
-        if (longest <= kGretTokens) return YOCO_OK;
-        if (sm_count <= 0) {
-            DeviceState* dev = nullptr;
-            if ((rc = device_state(&dev)) != YOCO_OK) return rc;
-            sm_count = dev->sm_count;
-        }
+    return gret_workspace(shape, len_host, sm_count, bytes, [&](int32_t sms) {
         GretPlan plan;
-        plan_gret(*shape, len_host, nullptr, sm_count, &plan);
-        *bytes = plan.bytes();
-        return YOCO_OK;
+        plan_gret(*shape, len_host, nullptr, sms, &plan);
+        return plan.bytes();
+    });
+}
+
+int32_t yoco_gret_workspace_bound(const yoco_gret_shape* shape, const int32_t* len_host, int32_t sm_count, size_t* bytes) {
+    return gret_workspace(shape, len_host, sm_count, bytes, [&](int32_t sms) {
+        int64_t chunks = 0;
+        for (int32_t i = 0; i < shape->B; ++i) chunks += ((int64_t)(len_host ? len_host[i] : shape->T) + kGretChunk - 1) / kGretChunk;
+        GretPlan plan;                                     // streams cut over as many CTAs as there can be
+        plan.split = chunks * shape->H > 1;
+        plan.set_groups((int32_t)std::min<int64_t>(chunks * shape->H, sms), shape->d);
+        return plan.bytes();
     });
 }
 

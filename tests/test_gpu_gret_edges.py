@@ -22,3 +22,16 @@ def test_state_only_ranges_that_end_one_stream_and_begin_another(d):
         call.run()
         assert torch.equal(p.o, o) and torch.equal(p.state, state)
     assert p.yx.yoco_kv_append_status() == 0
+
+
+def test_one_workspace_while_sequences_leave_a_batch():
+    import torch
+    H, d, lens = 32, 64, [900] * 8
+    p = Problem(lens, H, d, seed=103, in_place=True)
+    ws = torch.empty(p.yx.yoco_gret_workspace_bound(p.shape, lens), dtype=torch.uint8, device="cuda")
+    for left in (8, 1):
+        q = Problem(lens[:left] + [0] * (8 - left), H, d, seed=104 + left, in_place=True)
+        q.yx.yoco_gret_chunk(q.shape, q.q, q.k, q.v, q.decay, None, q.state, q.slot_in, q.slot_out, q.lens, q.o, ws)
+        q.check()
+    assert p.yx.yoco_gret_workspace_size(p.shape, lens) < p.yx.yoco_gret_workspace_size(q.shape, q.lens) <= ws.numel()
+    assert p.yx.yoco_kv_append_status() == 0
