@@ -466,7 +466,8 @@ int32_t yoco_xattn_chunk_paged_q4(const yoco_xattn_shape* shape, const yoco_page
  * state in slot slot_in_host[i] (-1: from zero; the arrays are host [B], NULL = slot i) and leaves its state in slot
  * slot_out_host[i] (-1: nowhere).  A slot may be read by several sequences (a common prefix) and may be read and written by the same one; one
  * that is written by two sequences, or written by one and read by another, is refused.  Other slots are not touched.  A sequence
- * without tokens hands its state on. */
+ * without tokens hands its state on.  O must not overlap Q, K, V, the gate or the decays (refused; columns of one buffer beside theirs are
+ * fine), nor anything else that a call reads. */
 typedef struct yoco_gret_shape {
     int32_t B;               /* sequences (<= 512)                                        */
     int32_t H;               /* heads (<= 65535)                                          */
@@ -496,7 +497,7 @@ typedef struct yoco_norm_gate {
 } yoco_norm_gate;
 
 /* One token of every sequence: Q, K, V, O are rows [B, H * d], decay [B, H] (shape->T is not read).  norm may be NULL: O is o rounded
- * to bf16.  O must not overlap the inputs.  A call recorded into a CUDA graph keeps its slots; rows, decays and states are
+ * to bf16.  A call recorded into a CUDA graph keeps its slots; rows, decays and states are
  * read at every replay. */
 int32_t yoco_gret_step(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay,
                        const yoco_norm_gate* norm, float* state, const int32_t* slot_in_host, const int32_t* slot_out_host,

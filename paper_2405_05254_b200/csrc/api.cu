@@ -694,6 +694,25 @@ int32_t check_rows(const void* ptr, int64_t* stride, int64_t width) {
     return *stride % 8 == 0 ? YOCO_OK : YOCO_ERR_UNSUPPORTED;
 }
 
+// n rows of `bytes` bytes, `stride` bytes apart.
+struct Rows {
+    const void* ptr;
+    int64_t stride, bytes, n;
+    // whether any row touches the bytes [lo, hi)
+    bool touch(uintptr_t lo, uintptr_t hi) const {
+        const uintptr_t at = (uintptr_t)ptr;
+        const int64_t first = lo >= at + bytes ? (int64_t)((lo - at - bytes) / stride) + 1 : 0;      // that ends behind lo
+        return first < n && at + first * stride < hi;
+    }
+    uintptr_t begin() const { return (uintptr_t)ptr; }
+    uintptr_t end_of_first() const { return begin() + (stride == bytes ? n : 1) * bytes; }           // rows without gaps: of all
+};
+// Whether two sets of rows overlap; exact for rows of one distance (an overlap recurs from row to row) and where one set has no gaps.  Slices of one
+// buffer that lie beside one another do not.
+bool overlap(const Rows& a, const Rows& b) {
+    return a.ptr && b.ptr && a.n > 0 && b.n > 0 && (a.touch(b.begin(), b.end_of_first()) || b.touch(a.begin(), a.end_of_first()));
+}
+
 int32_t check_norm(const yoco_norm_gate* norm, int64_t width, NormGate* out) {
     *out = NormGate{};
     if (!norm) return YOCO_OK;
@@ -872,6 +891,12 @@ int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const v
         for (int32_t i = 0; i < s.B; ++i) tab.tok0[i + 1] = tab.tok0[i] + (len_host ? len_host[i] : step ? 1 : s.T);
         DeviceState* dev = nullptr;
         if ((rc = device_state(&dev)) != YOCO_OK) return rc;
+        const auto rows = [&](const void* ptr, int64_t stride) { return Rows{ptr, stride * 2, width * 2, tokens}; };
+        const Rows out = rows(O, p.o_stride);
+        const int64_t decay_bytes = s.decay_bf16 ? 2 : 4;
+        if (overlap(out, rows(Q, p.q_stride)) || overlap(out, rows(K, p.k_stride)) || overlap(out, rows(V, p.v_stride)) ||
+            overlap(out, rows(p.norm.gate, p.norm.gate_stride)) || overlap(out, Rows{decay, p.decay_stride * decay_bytes, s.H * decay_bytes, tokens}))
+            return YOCO_ERR_INVALID_ARG;
         p.q = static_cast<const __nv_bfloat16*>(Q);
         p.k = static_cast<const __nv_bfloat16*>(K);
         p.v = static_cast<const __nv_bfloat16*>(V);

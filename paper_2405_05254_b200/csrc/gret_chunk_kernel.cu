@@ -915,7 +915,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll
                                 for (int q = 0; q < 4; ++q) y[4 * e + q] = f2_add(y[4 * e + q], f[q]);
                             }
-                            if (nm.gate) {                     // (a thread's row of the gate gives way to its row of the output)
+                            if (nm.gate) {
                                 eight(make_uint4(g[4 * e], g[4 * e + 1], g[4 * e + 2], g[4 * e + 3]));
 #pragma unroll
                                 for (int q = 0; q < 4; ++q) y[4 * e + q] = f2_swish_mul(f[q], y[4 * e + q]);
