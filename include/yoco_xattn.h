@@ -543,7 +543,7 @@ int32_t yoco_rope(const yoco_rope_shape* shape, const void* Q, const void* K, co
                   const int32_t* pos_host, const int32_t* len_host, void* Q_rot, void* K_rot, void* stream);
 
 /* (No counterpart in the paper.)  Synchronises `stream`; returns YOCO_OK, or YOCO_ERR_TIMEOUT if an
- * append kernel on the current device gave up a wait (YOCO_ERR_BAD_PAGE: a paged append or gather met a bad page)
+ * append or chunkwise retention kernel on the current device gave up a wait (YOCO_ERR_BAD_PAGE: a paged append or gather met a bad page)
  * since the last call of this function (which clears the record).  The _detail form also reports which wait and which CTA (see below). */
 int32_t yoco_kv_append_status(void* stream);
 int32_t yoco_kv_append_status_detail(void* stream, int32_t* wait_class, int32_t* cta);
@@ -597,6 +597,15 @@ int32_t yoco_xattn_selftest_wait_expiry_paged(const yoco_xattn_shape* shape, con
                                               const void* V_scale, const int32_t* page_table, const int32_t* kv_len_host,
                                               void* O, void* workspace, size_t workspace_bytes, int32_t limit_ms,
                                               void* stream);
+
+/* The same for the chunkwise kernels of gated retention (arguments as for yoco_gret_chunk; no counterpart in the paper).  Every role of the
+ * kernel runs out at its first wait for a tile or a product: yoco_kv_append_status_detail reports YOCO_ERR_TIMEOUT with
+ * YOCO_WAIT_RING_FULL or YOCO_WAIT_TENSOR.  O and the slots that the call writes are left undefined.  Calls whose sequences are all so short that they are
+ * walked token by token have no waits: YOCO_ERR_UNSUPPORTED. */
+int32_t yoco_gret_selftest_wait_expiry(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay,
+                                       const yoco_norm_gate* norm, float* state, const int32_t* slot_in_host,
+                                       const int32_t* slot_out_host, const int32_t* len_host, void* O, void* workspace,
+                                       size_t workspace_bytes, int32_t limit_ms, void* stream);
 
 /* Measurement aid (no counterpart in the paper).  After yoco_xattn_profile_enable(n), each of
  * the next n decode/chunk calls records a CUDA event pair on its stream around the attention

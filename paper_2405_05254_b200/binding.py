@@ -160,6 +160,7 @@ def lib() -> ctypes.CDLL:
         for name, args in (("yoco_gret_step", [vp] * 11), ("yoco_gret_chunk", [vp] * 12 + [sz, vp]),
                            ("yoco_gret_workspace_size", [vp, vp, i32, ctypes.POINTER(sz)]),
                            ("yoco_gret_workspace_bound", [vp, vp, i32, ctypes.POINTER(sz)]),
+                           ("yoco_gret_selftest_wait_expiry", [vp] * 12 + [sz, i32, vp]),
                            ("yoco_head_norm", [vp] * 5), ("yoco_rope", [vp] * 9)):
             getattr(L, name).argtypes = args
             getattr(L, name).restype = i32
@@ -906,6 +907,16 @@ def yoco_gret_chunk(shape: GretShape, Q, K, V, decay, norm, state, slot_in, slot
     """Enqueue gated retention over whole prompts or chunks of them: ``lens`` [B] tokens (None: shape.T each), states from slots
     ``slot_in`` (-1: zero) into slots ``slot_out`` (-1: not kept; None: slot i of sequence i)."""
     prepare_tokens("yoco_gret_chunk", shape, Q, K, V, decay, norm, state, slot_in, slot_out, lens, O, workspace, stream=stream).run()
+
+
+def yoco_gret_selftest_wait_expiry(shape: GretShape, Q, K, V, decay, norm, state, slot_in, slot_out, lens, O, workspace, limit_ms: int,
+                                   stream=None) -> None:
+    """Self-test of the bounded waits (arguments as for yoco_gret_chunk): a producer that starts no copy and a limit of ``limit_ms``.  O and the
+    slots that the call writes are left undefined."""
+    call = prepare_tokens("yoco_gret_chunk", shape, Q, K, V, decay, norm, state, slot_in, slot_out, lens, O, workspace)
+    rc = lib().yoco_gret_selftest_wait_expiry(*call._args, int(limit_ms), _stream_ptr(stream))
+    if rc != OK:
+        raise YocoError(rc, "yoco_gret_selftest_wait_expiry")
 
 
 def yoco_gret_step(shape: GretShape, Q, K, V, decay, norm, state, slot_in, slot_out, O, stream=None) -> None:

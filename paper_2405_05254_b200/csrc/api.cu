@@ -863,7 +863,7 @@ int32_t gret_workspace(const yoco_gret_shape* shape, const int32_t* len_host, in
 
 int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay, const yoco_norm_gate* norm,
              float* state, const int32_t* slot_in_host, const int32_t* slot_out_host, const int32_t* len_host, bool step, void* O,
-             void* workspace, size_t workspace_bytes, void* stream) {
+             void* workspace, size_t workspace_bytes, void* stream, const SelfTest* selftest = nullptr) {
     return no_throw([&]() -> int32_t {
         if (!shape) return YOCO_ERR_INVALID_ARG;
         const yoco_gret_shape& s = *shape;
@@ -913,6 +913,7 @@ int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const v
         int32_t longest = 0;
         for (int32_t i = 0; i < s.B; ++i) longest = std::max(longest, tab.tok0[i + 1] - tab.tok0[i]);
         if (longest <= kGretTokens) {
+            if (selftest) return YOCO_ERR_UNSUPPORTED;     // (no waits there)
             YOCO_CUDA_TRY(launch_gret_tokens(p, tab, st));
             return YOCO_OK;
         }
@@ -941,6 +942,8 @@ int32_t gret(const yoco_gret_shape* shape, const void* Q, const void* K, const v
         cp.part = static_cast<float*>(workspace);
         cp.part_keep = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + plan.part_bytes);
         cp.status = dev->append_status;
+        cp.wait_limit_ns = selftest ? (int32_t)selftest->wait_limit_ns : 0;
+        cp.selftest_skip_loads = selftest ? 1 : 0;
         if (plan.seqs < s.B) {           // sequences without tokens hand their states on
             GretTable idle;
             std::memset(&idle, 0, sizeof idle);
@@ -1596,6 +1599,15 @@ int32_t yoco_xattn_selftest_wait_expiry_paged(const yoco_xattn_shape* shape, con
     const SelfTest st{(int64_t)limit_ms * 1000000ll};
     return attend_paged(YOCO_MODE_DECODE, shape, layout, Q, K, K_scale, V, V_scale, K_scale != nullptr, page_table,
                         kv_len_host, O, nullptr, workspace, workspace_bytes, stream, &st);
+}
+
+int32_t yoco_gret_selftest_wait_expiry(const yoco_gret_shape* shape, const void* Q, const void* K, const void* V, const void* decay,
+                                       const yoco_norm_gate* norm, float* state, const int32_t* slot_in_host,
+                                       const int32_t* slot_out_host, const int32_t* len_host, void* O, void* workspace,
+                                       size_t workspace_bytes, int32_t limit_ms, void* stream) {
+    if (limit_ms <= 0 || limit_ms > 1000) return YOCO_ERR_INVALID_ARG;
+    const SelfTest st{(int64_t)limit_ms * 1000000ll};
+    return gret(shape, Q, K, V, decay, norm, state, slot_in_host, slot_out_host, len_host, false, O, workspace, workspace_bytes, stream, &st);
 }
 
 int32_t yoco_xattn_profile_enable(int32_t max_records) {

@@ -94,6 +94,7 @@ struct GCfg {
 // loops together have to stay in the instruction cache of the SM, which is why they are rolled up wherever registers are not indexed by
 // them.  (With everything unrolled, 173 KB of code instead of 60, a chunk took twice as long.)
 struct Wait {
+    int32_t limit_ns;
     int32_t what = 0;
     __device__ __forceinline__ bool operator()(uint64_t* bar, uint32_t parity, int32_t wait_class) {
         uint32_t polls = 0, t0 = 0;
@@ -101,7 +102,7 @@ struct Wait {
             uint32_t t;
             asm volatile("mov.u32 %0, %globaltimer_lo;" : "=r"(t));
             if (polls == 0) t0 = t;
-            if (__any_sync(0xffffffffu, (int32_t)(t - t0) > (int32_t)kWaitLimitNs || ++polls >= kWaitMaxPolls)) {
+            if (__any_sync(0xffffffffu, (int32_t)(t - t0) > limit_ns || ++polls >= kWaitMaxPolls)) {
                 what = wait_class;
                 return false;
             }
@@ -291,7 +292,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     const uint32_t tmem_base = *tmem_slot;
     const uint32_t sbase = smem_u32(smem);
 
-    Wait wait;
+    Wait wait{p.wait_limit_ns > 0 ? p.wait_limit_ns : (int32_t)kWaitLimitNs};
     // every role walks the same segments: `enter` moves to the next one
     Walk<Table> walk(p, tab);
     auto enter = [&]() -> bool {
@@ -459,7 +460,7 @@ gret_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 Turn<C::KS> kat;
                 Turn<C::VS> vat;
                 uint32_t chunks = 0, k_armed = 0, v_armed = 0, q_armed = 0;
-                bool ok = true;
+                bool ok = !p.selftest_skip_loads;
                 while (ok && enter()) {
                     const int x = walk.h * D;
 #pragma unroll 1

@@ -329,6 +329,8 @@ struct GretChunkParams {
     float* part;                // split: 3 * groups states
     float* part_keep;           // split: decays over the segments that left them, 3 * groups
     int32_t* status;
+    int32_t wait_limit_ns;      // 0 = the default limit of a bounded wait
+    int32_t selftest_skip_loads;// self-test of the give-up path: the producer arms no copy, so the first waits run out with nothing in flight
 };
 // tmQ, tmK, tmV: bf16 maps over [tokens, H * d], box {64, kGretChunk} (K and V: kGretChunk / 2), 128-byte swizzle
 cudaError_t launch_gret_chunk(const GretChunkParams& p, const GretChunkTable& tab, const CUtensorMap& tmQ, const CUtensorMap& tmK,

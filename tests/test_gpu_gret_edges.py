@@ -1,4 +1,6 @@
 """Gated retention where its kernels meet their borders."""
+import time
+
 import numpy as np
 import pytest
 
@@ -85,3 +87,31 @@ def test_an_output_over_an_input_is_refused_and_one_beside_them_is_not(lens):
     assert torch.equal(x[:n, :4 * W], before[:n, :4 * W]) and torch.equal(x[n:], before[n:]) and bool((x[:, 5 * W:] == 0).all())
     p.o_buf[1:n + 1, :W] = o
     p.check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,H", [([300, 40, 129], 60), ([2600, 777], 3)], ids=["whole", "cut"])
+def test_an_expired_wait_is_reported_and_the_next_call_is_correct(lens, H, d):
+    """A producer that starts no copy: every role of the kernel gives up its first wait, with nothing in flight, the CTAs leave in the ordinary way, the
+    host reads which wait it was, and the next call on the same workspace and states is right."""
+    import torch
+    p = Problem(lens, H, d, seed=109, norm="group")
+    yx = p.yx
+    ws = torch.zeros(p.workspace()[1], dtype=torch.uint8, device="cuda")
+    assert (ws.numel() > 0) == (H == 3)
+    assert yx.yoco_kv_append_status() == 0
+    t0 = time.perf_counter()
+    yx.yoco_gret_selftest_wait_expiry(p.shape, p.q, p.k, p.v, p.decay, p.ng, p.state, p.slot_in, p.slot_out, p.lens, p.o, ws, limit_ms=20)
+    rc, wait_class, cta = yx.yoco_kv_append_status_detail()
+    dt = time.perf_counter() - t0
+    assert rc == yx.ERR_TIMEOUT and wait_class in (yx.WAIT_RING_FULL, yx.WAIT_TENSOR) and 0 <= cta < 148
+    assert 0.015 < dt < 2.0, dt                               # the limit was honoured, once per kernel
+    assert yx.yoco_kv_append_status() == 0                    # cleared
+    p.state.copy_(torch.from_numpy(p.state0))
+    yx.yoco_gret_chunk(p.shape, p.q, p.k, p.v, p.decay, p.ng, p.state, p.slot_in, p.slot_out, p.lens, p.o, ws)
+    assert yx.yoco_kv_append_status() == 0
+    p.check()
+    short = yx.make_gret_shape(len(lens), H, d, T=5, num_slots=p.n_slots, tau=p.tau, q_stride=4 * H * d, k_stride=4 * H * d, v_stride=4 * H * d)
+    with pytest.raises(yx.YocoError) as e:                    # token by token: no waits
+        yx.yoco_gret_selftest_wait_expiry(short, p.q, p.k, p.v, p.decay, None, p.state, p.slot_in, p.slot_out, None, torch.empty_like(p.o), ws, limit_ms=20)
+    assert e.value.code == yx.ERR_UNSUPPORTED

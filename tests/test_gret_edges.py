@@ -1,4 +1,6 @@
 """Host side of gated retention: what the calls refuse beside their own arguments' ranges."""
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -36,3 +38,16 @@ def test_a_workspace_for_lengths_up_to_those_given(H, d):
     for bad in (bd.make_gret_shape(1, 32, 100), bd.make_gret_shape(1, 32, 128, T=-1)):
         with pytest.raises(bd.YocoError):
             bd.yoco_gret_workspace_bound(bad, None, 148)
+
+
+def test_the_self_test_of_the_waits_checks_its_arguments():
+    A = ctypes.c_void_p(4096)
+    L = bd.lib()
+    shape = bd.make_gret_shape(1, 2, 128, T=300)
+
+    def call(limit_ms, Q=A):
+        return L.yoco_gret_selftest_wait_expiry(ctypes.addressof(shape), Q, A, A, A, None, A, None, None, None, A, None, 0, limit_ms, None)
+
+    for ms in (0, -1, 1001):
+        assert call(ms) == bd.ERR_INVALID_ARG
+    assert call(20, Q=None) == bd.ERR_INVALID_ARG and call(20) not in (bd.OK, bd.ERR_INVALID_ARG, bd.ERR_UNSUPPORTED)
