@@ -456,7 +456,9 @@ int32_t yoco_xattn_chunk_paged_q4(const yoco_xattn_shape* shape, const yoco_page
 /* ---- Self-decoder with gated retention (Section 3.1) --------------------------------------------------
  * Per head, with rows q_t, k_t, v_t of d channels and a decay g_t, a state S (d x d) runs along a sequence:
  *     S_t = g_t S_(t-1) + k_t^T v_t,    o_t = scale * q_t S_t
- * (the recurrent form; for whole prompts the calls evaluate the chunkwise form, which is the same sums in another order).
+ * (the recurrent form; for whole prompts the calls evaluate the chunkwise form, which is the same sums in another order, with the scores and the state
+ * that a chunk's queries meet rounded to bf16: an output is off by about 2^-9 of the root of its terms' squares, beside its own rounding.  A norm
+ * that takes out a mean far above the row's deviation leaves that error as it is.  The step, and calls of a few tokens a sequence, round the output alone).
  * Rows are token-major, as a projection leaves them: the tokens of all sequences one after the other (no padding between
  * sequences), heads consecutive inside a token, `stride` elements from token to token; Q, K, V (and the gate) may be slices of one
  * fused projection.  They start on 16-byte boundaries, strides are multiples of 8 elements (0 -> H * d).  Rows should be finite: a value that is

@@ -782,13 +782,18 @@ int32_t check_slots(const yoco_gret_shape& s, const int32_t* in, const int32_t* 
 }
 
 // Calls whose sequences all have no more tokens than this walk them one by one (one CTA per head, state in registers); longer ones in chunks.
-// (Measured, 32 heads of 128: one sequence of 18 / 24 tokens 12.7 / 14.7 us token by token, 13.5 in chunks; eight 19.9 / 24.9, 22.8 in chunks;
-// 32 sequences 70 / 84, 64 in chunks.)
+// (Measured in recorded graphs, 32 heads, us token by token / in chunks.  Heads of 128, where the border was set: one sequence of 16, 18, 20 tokens
+// 9.8 / 11.1, 11.3 / 11.1, 11.9 / 11.1; eight 16.2 / 20.1, 18.0 / 20.0, 19.0 / 20.1; 32 sequences of 12, 16, 18 tokens 48 / 60, 59 / 61, 68 / 61.  Heads of 64
+// would have it higher: one sequence of 20, 24, 32 tokens 6.9 / 8.2, 7.4 / 8.2, 9.3 / 8.1; eight 8.6 / 13.5, 9.1 / 13.6, 11.5 / 13.5; 32
+// sequences 20 / 35, 22 / 35, 29 / 35.)
 constexpr int32_t kGretTokens = 18;
-// Costs in chunks of a whole stream (32 heads of 128 on 148 SMs: 3.8 to 4.3 us, by how many SMs have one): a chunk in both passes over split
-// streams; the extra launches with their starts and ends; every further segment of a CTA, whose state comes and goes.  (Measured: one sequence of
-// 1,024 tokens, 8 / 16 / 32 heads, whole 36 / 36 / 38 us, split 23 / 26 / 34; 1,280 tokens, 32 heads 44, split 41; 896 tokens 33 whole; six
-// sequences of 37 to 1,501 tokens, 16 heads 52, split 70.)
+// Costs in chunks of a whole stream (heads of 128: 3.3 us; of 64: 2.8): a chunk in both passes over split streams; the extra launches with their starts
+// and ends; every further segment of a CTA, whose state comes and goes.  Set by heads of 128 and used for both.  (Measured in recorded graphs, us whole / split,
+// one sequence.  Heads of 128: 512 tokens, 8 / 16 / 32 heads 20.4 / 18.6, 20.8 / 18.9, 21.1 / 23.1, all taken whole; 768: 27.1 / 19.1, 27.3 / 20.6
+// split, 27.6 / 28.2 whole; 896, 32 heads 31.0 / 32.9 whole; 1,024: 33.7 / 19.5, 33.8 / 22.9, 34.5 / 29.6 split.  Six sequences of 37 to 1,501 tokens, 16 heads
+// 49.9 / 64.5 whole.  Heads of 64: 512 tokens 16.0 / 12.6, 16.1 / 13.6, 16.3 / 17.4 whole; 768 21.5 / 13.3, 21.6 / 14.9 split, 21.8 / 21.0 whole; 896, 32 heads
+// 24.7 / 22.5 whole; 1,024 split, 26.9 / 13.7, 27.2 / 16.4, 27.5 / 22.8; the six sequences 38.3 / 42.9 whole.  So the rule keeps a few short
+// streams whole where a split would take 1 to 3.5 us off: 512 tokens of 8 and 16 heads, and of 32 heads of 64 768 and 896 tokens.)
 constexpr double kGretSplitChunk = 1.4, kGretSplitCost = 4.0, kGretSegmentCost = 1.0;
 
 struct GretPlan {

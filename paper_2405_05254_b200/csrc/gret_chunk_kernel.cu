@@ -20,13 +20,16 @@
 // With few streams a first pass over K and V (STATES) leaves the state of each CTA's range, a merge puts those in order, and the main
 // pass starts every range from its own: all SMs work, K and V are read twice.  In that first pass warpgroups 1, 2, 6 and 7 make K', a piece each, in
 // tensor memory.
-// What bounds it: not the bytes (measured: 46% and 55% of the memory's rate in the two passes) nor the tensor cores (39%, 41%), but the
+// What bounds it: not the bytes (measured: 47% and 55% of the memory's rate in the two passes) nor the tensor cores (39%, 40%), but the
 // roles' chain, through shared memory's data pipe: a chunk's matrix products read 320 KB of operands there, the copies write 96 KB, K' and S another
-// 130 KB (the pipe: 37% of the cycles the tensor cores' operands, 62% the threads' accesses, tensor memory's among them).  What took load off
+// 130 KB (the pipe: 37% of the cycles the tensor cores' operands, 61% the threads' accesses, tensor memory's among them).  What took load off
 // it made it faster (output and gate past it, K' of the first pass to tensor memory), and so did fewer instructions on the chain (uniform registers).
-// Measured (d = 128, short bursts): one sequence of 32,768 tokens, 32 heads 355-364 us (1.08 GB needed: 165 us at 6.56 TB/s), with gate 415;
-// 4,096 tokens 69, with gate 78; four of 4,096 tokens, 37 heads, whole streams 141 (0.69 of that rate), with gate 175; one chunk 13.
-// Roundings: P and the copy of S that multiplies Q go to bf16 (half a step, 2^-9 of the value, like the output's own).  K' goes to
+// Measured (d = 128): one sequence of 32,719 tokens, 32 heads 430-434 us in a long row of calls (1.08 GB needed: 164 us at 6.56 TB/s), in which the SM
+// clock falls, 347-366 in short bursts, with gate 410; 4,096 tokens 68 in bursts, with gate 78, 82-83 in a long row; four of 4,096 tokens, 37 heads, whole
+// streams, in bursts 136-141 (0.69-0.72 of that rate), with gate 172-180; one chunk 13.
+// Roundings: P and the copy of S that multiplies Q go to bf16 (half a step, up to 2^-8 of the value, like the output's own): products of
+// bf16 keep fp32's range at the tensor cores' full rate.  Outputs are 2.3e-3 off (2-norm), 1.7e-3 with their own rounding alone.  A group norm that takes a common offset of V out
+// leaves these roundings: 2.7e-3 with an offset of 3 deviations, 5.2e-3 to 5.6e-3 with 10.  K' goes to
 // the tensor cores as a sum of bf16: where the sums leave the kernel as a state, of three (24 bits; with one it would be 1.7e-3 off (2-norm),
 // with two 2e-6), where they only multiply Q inside, of two.
 #include <type_traits>
@@ -92,7 +95,7 @@ struct GCfg {
 
 // The bounded wait of this kernel: one answer for the warp, in few instructions; what ran out is reported at the role's end.  The roles'
 // loops together have to stay in the instruction cache of the SM, which is why they are rolled up wherever registers are not indexed by
-// them.  (With everything unrolled, 173 KB of code instead of 60, a chunk took twice as long.)
+// them.  (With everything unrolled, more than twice the code, one sequence of 32,768 tokens took 583 us, as it was then, instead of 400.)
 struct Wait {
     int32_t limit_ns;
     int32_t what = 0;

@@ -7,8 +7,8 @@
 //
 // Bound: a step reads and writes 8 d^2 bytes of state per head and little else, so the loads of the state are all issued before
 // anything is waited for (64 KB in flight per CTA at d = 128, two CTAs per SM).
-// Measured: one token of 64 sequences, 32 heads of 128, with gate 49.1 us (0.84 of the copy rate of 6.56 TB/s), of 128 sequences without 86 us (0.95); of 37
-// sequences, 24 heads of 64, 8.2 us; of one sequence 3.8 us in a recorded graph, 6.1 us a call (the host's part).
+// Measured: one token of 64 sequences, 32 heads of 128, with gate 49.2-49.5 us (0.84 of the copy rate of 6.56 TB/s), of 128 sequences without 86 us (0.95); of 37
+// sequences, 24 heads of 64, 8.2 us; of one sequence 4.3 us in a recorded graph, 6.1 us a call (the host's part).
 #include "gret.cuh"
 #include "kernels.h"
 #include "ptx.cuh"

@@ -16,8 +16,8 @@ namespace {
 // into shared memory.  The angle is a product in 64 bits, reduced to a fraction of a turn in 64 bits, and only that is rounded to
 // fp32: at position 10^6 an fp32 angle would be off by 0.06.  Then a thread takes units of 16 channels of a (token, head) row: eight pairs
 // (halves: channels 8 u .. and rot / 2 + 8 u ..; neighbours: 16 u ..), or 16 channels that are copied.
-// Bound: bytes.  Measured: 32,768 tokens, 32 + 32 heads of 128, 171 us (0.96 of the copy rate); five sequences, 10,800 tokens, 16 + 16 heads,
-// half of each head turned, 33.7 us (0.80: two and a third rounds of blocks); one token of 64 sequences 2.4 us in a recorded graph.
+// Bound: bytes.  Measured: 32,768 tokens, 32 + 32 heads of 128, 174-176 us (0.94 of the copy rate; 169-171 in short bursts); five sequences, 10,800 tokens, 16 + 16 heads,
+// half of each head turned, 33.7 us (0.80: two and a third rounds of blocks); one token of 64 sequences 2.6 us in a recorded graph.
 constexpr int kRopeThreads = 256;
 constexpr int kRopeRows = 2;            // rows that a thread has in flight
 
